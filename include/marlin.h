@@ -338,6 +338,151 @@ marlin_status_t marlin_quantize(const uint16_t *W, int64_t K, int64_t N, int64_t
                                 const float *ratios, int n_ratios, uint8_t *q, uint16_t *s,
                                 hipStream_t stream);
 
+/*
+ * ---- Paged key-value cache: what runs between a layer's projections ----
+ *
+ * A cache is two arrays of pages, k_cache and v_cache, 16-bit elements
+ * [pages][kv_heads][page_size][head_dim]: the keys a kv head keeps in one page are
+ * contiguous.  A sequence's token at position j lies in slot j % page_size of
+ * page table[b][j / page_size].  Entries past a sequence's last page are not
+ * read; an entry outside 0 .. pages - 1 names no page: nothing is written
+ * there, and its positions count as masked when read.  No two sequences of a
+ * call may share a page that the call writes.
+ *
+ * lengths[b] is the number of tokens of sequence b, the ones a step adds
+ * included, so one array serves the append and the attention of every layer
+ * of a step.  It stays on the device: no entry point needs it on the host, so
+ * all of them can be captured into a HIP graph and replayed as sequences grow.
+ * A length below 0 counts as 0, one beyond width * page_size as that.
+ *
+ * Shapes: head_dim 64, 96, 128 or 256; page_size a power of two, 16 .. 1024;
+ * heads a multiple of kv_heads, the query heads h * heads / kv_heads .. sharing
+ * kv head h; B <= 2^16, pages >= 1, 1 <= width, width * page_size <= 2^30,
+ * kv_heads <= heads <= 1024.  Rows of q, k and v may be strided (slices of one
+ * projection's output): strides are in elements, multiples of 8, and the
+ * channels of a head are contiguous.  Outputs are dense.
+ * Alignment: 16 bytes, except int32 and float arrays (4; cos_sin 16).
+ */
+typedef enum {
+    MARLIN_F16 = 0,
+    MARLIN_BF16 = 1
+} marlin_dtype_t;
+
+/* Every field is 8 bytes, so an array of 64-bit words is the struct. */
+typedef struct {
+    const void *q, *k, *v;     /* new tokens, [tokens][heads | kv_heads][head_dim]          */
+    int64_t q_row, q_head;     /* strides from token to token and from head to head         */
+    int64_t k_row, k_head;
+    int64_t v_row, v_head;
+    void *q_out;               /* [tokens][heads][head_dim], written: rotated queries; may be q where q is dense */
+    void *k_cache, *v_cache;   /* new tokens' slots written                                 */
+    void *bounds;              /* [pages][kv_heads][2][head_dim] or NULL, see below         */
+    const float *cos_sin;      /* [positions][rot]: rot / 2 cosines, then rot / 2 sines     */
+    int64_t positions;         /* rows of cos_sin                                           */
+    int64_t rot;               /* rotated channels, the head's first: a multiple of 16, 0 .. head_dim */
+    int64_t interleaved;       /* 0: channel c pairs with c + rot / 2; 1: 2c with 2c + 1    */
+    const int32_t *table;      /* [B][width]                                                */
+    int64_t table_row;         /* stride from sequence to sequence                          */
+    const int32_t *lengths;    /* [B], new tokens included                                  */
+    const int32_t *starts;     /* [B + 1]: sequence b's new tokens are rows starts[b] .. starts[b + 1] - 1, from 0 to
+                                  tokens without a gap; NULL: one each (tokens = B)         */
+    int64_t tokens;            /* rows of q, k, v, at most 2^24                             */
+    int64_t B, heads, kv_heads, head_dim, pages, page_size, width;
+    int64_t dtype;             /* marlin_dtype_t of q, k, v, q_out and the cache            */
+} marlin_kv_append_args;
+
+/*
+ * marlin_kv_append - new tokens into the cache, rotated by their positions.
+ *
+ * The i-th of sequence b's n new tokens has position j = lengths[b] - n + i.
+ * Queries and keys are rotated, pair (x, y) of angle row j to
+ * (x cos - y sin, y cos + x sin), in fp32, rounded once; channels from rot on,
+ * and values, are copied.  A token whose position is below 0 (an unused row of a
+ * padded batch has length 0), at or past positions (rot > 0) or past the
+ * table, or whose table entry names no page, is not appended and its q_out row is zero.
+ *
+ * bounds keeps, per page, kv head and channel, the smallest and the largest key of the
+ * page (two rows of head_dim), in the order -NaN < -inf < ... < -0 < 0 < ... <
+ * inf < NaN.  A page's first slot starts its bounds anew, later tokens widen them.
+ * Errors: NULL_POINTER, INVALID_SHAPE, MISALIGNED, INVALID_ARGUMENT (rot,
+ * interleaved or dtype), HIP.
+ */
+marlin_status_t marlin_kv_append(const marlin_kv_append_args *args, hipStream_t stream);
+
+typedef struct {
+    const void *q;               /* [B][heads][head_dim], one token per sequence            */
+    int64_t q_row, q_head;
+    const void *k_cache, *v_cache;
+    const int32_t *table;        /* [B][width] or, with table_head, [B][kv_heads][width]    */
+    int64_t table_row;
+    int64_t table_head;          /* 0: the heads share a row                                */
+    const int32_t *lengths;      /* [B]                                                     */
+    void *out;                   /* [B][heads][head_dim], written                           */
+    float *lse;                  /* [B][heads], written, or NULL                            */
+    void *workspace;             /* as for marlin_gemm (one buffer serves both)             */
+    uint64_t workspace_bytes;
+    int64_t B, heads, kv_heads, head_dim, pages, page_size, width;
+    double scale;                /* finite; 1 / sqrt(head_dim) as a rule                    */
+    int64_t dtype;
+} marlin_paged_attention_args;
+
+/* Bytes of workspace marlin_paged_attention needs (0 for a head_dim it does not take). */
+size_t marlin_paged_attention_workspace_bytes(int64_t head_dim);
+
+/*
+ * marlin_paged_attention - attention of one token per sequence over the cache.
+ *
+ *   out = sum_j p_j v_j,  p_j = exp(scale q . k_j) / sum_i exp(scale q . k_i)
+ *   lse = log sum_j exp(scale q . k_j)
+ *
+ * over the positions j < lengths[b] whose table entries name pages.  Without any (or
+ * with every score -inf) out is 0 and lse -inf.  What other slots hold does
+ * not matter, NaN included.  Scores, sums and partial results are fp32; the
+ * weights are rounded to the cache's type for the second product, and out
+ * once at the end.  Bitwise reproducible for a given device and input.
+ * Errors: NULL_POINTER, INVALID_SHAPE (also B * rows of heads * the table's
+ * 32-key steps beyond 2^31), MISALIGNED, INVALID_ARGUMENT (scale, dtype),
+ * WORKSPACE_TOO_SMALL, HIP.
+ */
+marlin_status_t marlin_paged_attention(const marlin_paged_attention_args *args, hipStream_t stream);
+
+typedef struct {
+    const void *q;               /* [B][heads][head_dim]                                    */
+    int64_t q_row, q_head;
+    const void *bounds;          /* [pages][kv_heads][2][head_dim], marlin_kv_append's      */
+    const int32_t *table;        /* [B][width]                                              */
+    int64_t table_row;
+    const int32_t *lengths;      /* [B]                                                     */
+    int32_t *chosen;             /* [B][kv_heads][select], written: pages                   */
+    int32_t *chosen_lengths;     /* [B], written: tokens in them                            */
+    void *workspace;             /* as for marlin_gemm (one buffer serves both)             */
+    uint64_t workspace_bytes;
+    int64_t B, heads, kv_heads, head_dim, pages, page_size, width;
+    int64_t select;              /* pages to choose, 1 .. 2^20                              */
+    int64_t dtype;
+} marlin_select_pages_args;
+
+/* Bytes of workspace marlin_select_pages needs (0 for sizes it does not take). */
+size_t marlin_select_pages_workspace_bytes(int64_t B, int64_t kv_heads, int64_t width);
+
+/*
+ * marlin_select_pages - the pages each kv head's new token attends to.
+ *
+ * A page's score for kv head h is the largest product that its bounds allow
+ * with any of the head's queries, in fp32:
+ *   max over the heads of sum_c (q_c > 0 ? q_c * largest_c : q_c * smallest_c)
+ * A score that is not a number ranks first, a table entry that names no page
+ * last, the lower position first among equals.  The sequence's last page is always chosen, and
+ * the select - 1 best of the others.  chosen lists the entries of table in
+ * the order of their positions, -1 after the last, and chosen_lengths the tokens in them:
+ * marlin_paged_attention takes both in the place of table (table_row kv_heads * select,
+ * table_head select, width select) and lengths.
+ * A sequence of at most `select` pages keeps them all.
+ * Errors: as marlin_paged_attention, INVALID_ARGUMENT also for select, and
+ * INVALID_SHAPE where B * kv_heads * width, width rounded up to 64, exceeds 2^29.
+ */
+marlin_status_t marlin_select_pages(const marlin_select_pages_args *args, hipStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

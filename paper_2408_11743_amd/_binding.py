@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libmarlin_mi355x.so")
@@ -47,6 +48,11 @@ SIGNATURES = {
     "marlin_describe_sparse": (ctypes.c_int, [_i64, _i64, _i64, _i64, ctypes.c_char_p, _sz]),
     "marlin_quantize": (ctypes.c_int, [_vp, _i64, _i64, _i64, ctypes.POINTER(ctypes.c_float), ctypes.c_int,
                                        _vp, _vp, _vp]),
+    "marlin_kv_append": (ctypes.c_int, [_vp, _vp]),
+    "marlin_paged_attention_workspace_bytes": (_sz, [_i64]),
+    "marlin_paged_attention": (ctypes.c_int, [_vp, _vp]),
+    "marlin_select_pages_workspace_bytes": (_sz, [_i64, _i64, _i64]),
+    "marlin_select_pages": (ctypes.c_int, [_vp, _vp]),
     # marlin_quantize and marlin_pack_weights in one launch for a linear
     # layer's weight [N, K] (internal: not declared in marlin.h)
     "marlin_quantize_linear": (ctypes.c_int, [_vp, _i64, _i64, _i64, ctypes.POINTER(ctypes.c_float), ctypes.c_int,
@@ -198,3 +204,52 @@ def marlin_quantize_linear(W, K, N, group, ratios, w_packed, s_packed, stream=No
     arr, n = _ratio_array(ratios)
     _check("marlin_quantize", lib().marlin_quantize_linear(_ptr(W), K, N, group, arr, n, _ptr(w_packed),
                                                            _ptr(s_packed), _stream(stream)))
+
+
+# ---- paged key-value cache ----
+# The argument structs of marlin.h, whose fields are all 8 bytes: one struct.pack
+# costs a third of filling a ctypes.Structure.
+DTYPES = {"float16": 0, "bfloat16": 1}
+KV_APPEND_FIELDS = ("q k v q_row q_head k_row k_head v_row v_head q_out k_cache v_cache bounds cos_sin positions rot "
+                    "interleaved table table_row lengths starts tokens B heads kv_heads head_dim pages page_size width "
+                    "dtype").split()
+PAGED_ATTENTION_FIELDS = ("q q_row q_head k_cache v_cache table table_row table_head lengths out lse workspace "
+                          "workspace_bytes B heads kv_heads head_dim pages page_size width scale dtype").split()
+SELECT_PAGES_FIELDS = ("q q_row q_head bounds table table_row lengths chosen chosen_lengths workspace workspace_bytes B "
+                       "heads kv_heads head_dim pages page_size width select dtype").split()
+pack_kv_append = struct.Struct("%dq" % len(KV_APPEND_FIELDS)).pack
+pack_paged_attention = struct.Struct("20qdq").pack
+pack_select_pages = struct.Struct("%dq" % len(SELECT_PAGES_FIELDS)).pack
+
+
+def _fields(func: str, names, args: dict):
+    """Tensors as addresses (None: NULL), everything else as it is; every field is named."""
+    if set(args) != set(names):
+        raise TypeError("%s: fields %s" % (func, ", ".join(sorted(set(args) ^ set(names)))))
+    return [_ptr(args[n]) or 0 if args[n] is None or hasattr(args[n], "data_ptr") else args[n] for n in names]
+
+
+def marlin_kv_append(stream=None, **args) -> None:
+    """args: the fields of marlin_kv_append_args by name."""
+    _check("marlin_kv_append", lib().marlin_kv_append(
+        pack_kv_append(*_fields("marlin_kv_append", KV_APPEND_FIELDS, args)), _stream(stream)))
+
+
+def marlin_paged_attention_workspace_bytes(head_dim: int) -> int:
+    return lib().marlin_paged_attention_workspace_bytes(head_dim)
+
+
+def marlin_paged_attention(stream=None, **args) -> None:
+    """args: the fields of marlin_paged_attention_args by name."""
+    _check("marlin_paged_attention", lib().marlin_paged_attention(
+        pack_paged_attention(*_fields("marlin_paged_attention", PAGED_ATTENTION_FIELDS, args)), _stream(stream)))
+
+
+def marlin_select_pages_workspace_bytes(B: int, kv_heads: int, width: int) -> int:
+    return lib().marlin_select_pages_workspace_bytes(B, kv_heads, width)
+
+
+def marlin_select_pages(stream=None, **args) -> None:
+    """args: the fields of marlin_select_pages_args by name."""
+    _check("marlin_select_pages", lib().marlin_select_pages(
+        pack_select_pages(*_fields("marlin_select_pages", SELECT_PAGES_FIELDS, args)), _stream(stream)))

@@ -1,0 +1,347 @@
+// New tokens into the paged key-value cache: queries and keys rotated by their
+// positions, (x, y) -> (x cos a - y sin a, y cos a + x sin a) in fp32 with one
+// rounding, keys and values written to their pages, and the pages' bounds (the
+// smallest and largest key per channel) widened.
+//
+// A head is D / 16 threads, each with the two 16-byte pieces that hold its
+// eight pairs.  Nothing is read twice but the angles; the kernels are bound by
+// memory, and by launch latency where there is one token per sequence.
+#include <hip/hip_runtime.h>
+
+#include "kv.h"
+#include "kv_device.h"
+
+namespace marlin {
+namespace {
+
+using namespace dev;
+
+typedef int16_t short2_t __attribute__((ext_vector_type(2)));
+
+// 16-bit floats, two to a dword, to integers in the same order (and back): the
+// magnitude bits of negative ones are inverted.
+__device__ __forceinline__ uint32_t ordered(uint32_t x) { return x ^ ((x >> 15) & 0x00010001u) * 0x7FFFu; }
+
+__device__ __forceinline__ uint32_t min2(uint32_t a, uint32_t b)
+{
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_min(__builtin_bit_cast(short2_t, a), __builtin_bit_cast(short2_t, b)));
+}
+__device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b)
+{
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(short2_t, a), __builtin_bit_cast(short2_t, b)));
+}
+
+struct Pieces {
+    uint32_t w[8];  // two 16-byte pieces
+};
+
+// Elements where thread `pair` of a head's D / 16 has its two pieces: the
+// halves of eight pairs, or (interleaved, or past the rotated channels)
+// sixteen adjacent channels.
+struct Where {
+    int first, second;
+};
+__device__ __forceinline__ Where where(const AppendProblem &p, int pair)
+{
+    if (!p.interleaved && pair < p.rot / 16) return {8 * pair, 8 * pair + p.rot / 2};
+    return {16 * pair, 16 * pair + 8};
+}
+
+template <typename T>
+__device__ __forceinline__ Pieces load_pieces(const T *row, Where at)
+{
+    Pieces x;
+    __builtin_memcpy(x.w, __builtin_assume_aligned(row + at.first, 16), 16);
+    __builtin_memcpy(x.w + 4, __builtin_assume_aligned(row + at.second, 16), 16);
+    return x;
+}
+
+template <typename T>
+__device__ __forceinline__ void store_pieces(T *row, Where at, const Pieces &x)
+{
+    __builtin_memcpy(__builtin_assume_aligned(row + at.first, 16), x.w, 16);
+    __builtin_memcpy(__builtin_assume_aligned(row + at.second, 16), x.w + 4, 16);
+}
+
+// Eight pairs' cosines and sines.
+struct Angles {
+    float4_t c[2], s[2];
+};
+__device__ __forceinline__ Angles load_angles(const AppendProblem &p, int pos, int pair)
+{
+    Angles a{};
+    if (pair < p.rot / 16) {
+        const float *row = p.cos_sin + (int64_t)pos * p.rot + 8 * pair;
+        a.c[0] = *(const float4_t *)row;
+        a.c[1] = *(const float4_t *)(row + 4);
+        a.s[0] = *(const float4_t *)(row + p.rot / 2);
+        a.s[1] = *(const float4_t *)(row + p.rot / 2 + 4);
+    }
+    return a;
+}
+
+template <typename T>
+__device__ __forceinline__ Pieces rotate(const AppendProblem &p, const Pieces &x, const Angles &a, int pair)
+{
+    if (pair >= p.rot / 16) return x;
+    typedef T vec16 __attribute__((ext_vector_type(16)));
+    const vec16 e = __builtin_bit_cast(vec16, x);
+    vec16 y;
+    if (p.interleaved) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float c = a.c[i >> 2][i & 3], s = a.s[i >> 2][i & 3], u = (float)e[2 * i], v = (float)e[2 * i + 1];
+            y[2 * i] = (T)(u * c - v * s);
+            y[2 * i + 1] = (T)(v * c + u * s);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float c = a.c[i >> 2][i & 3], s = a.s[i >> 2][i & 3], u = (float)e[i], v = (float)e[i + 8];
+            y[i] = (T)(u * c - v * s);
+            y[i + 8] = (T)(v * c + u * s);
+        }
+    }
+    return __builtin_bit_cast(Pieces, y);
+}
+
+__device__ __forceinline__ int clamped(int n) { return n < 0 ? 0 : n < (1 << 30) ? n : (1 << 30); }
+
+// Slot (in rows of D of the cache, kv head 0) of sequence b's position, or -1:
+// the token is not appended.
+__device__ __forceinline__ int64_t slot_of(const AppendProblem &p, int b, int pos)
+{
+    if (pos < 0 || pos >= (p.width << p.page_shift) || (p.rot > 0 && pos >= p.positions)) return -1;
+    const int page = p.table[b * p.table_row + (pos >> p.page_shift)];
+    if ((uint32_t)page >= (uint32_t)p.pages) return -1;
+    return ((int64_t)page * p.kv_heads << p.page_shift) + (pos & ((1 << p.page_shift) - 1));
+}
+
+// ---- one token per sequence ----
+template <typename T, int D>
+__global__ void __launch_bounds__(256) append_token_kernel(const AppendProblem p)
+{
+    constexpr int kPairs = D / 16, kHeads = 256 / kPairs;
+    const int pair = threadIdx.x % kPairs, slabs = (p.heads + 2 * p.kv_heads + kHeads - 1) / kHeads;
+    const int b = blockIdx.x / slabs, h = blockIdx.x % slabs * kHeads + threadIdx.x / kPairs;
+    if (threadIdx.x >= kHeads * kPairs || h >= p.heads + 2 * p.kv_heads) return;
+    const int pos = clamped(p.lengths[b]) - 1;
+    const int64_t slot = slot_of(p, b, pos);
+    const Where at = where(p, pair);
+    if (h < p.heads) {
+        Pieces x{};
+        if (slot >= 0)
+            x = rotate<T>(p, load_pieces((const T *)p.q + b * p.q_row + h * p.q_head, at), load_angles(p, pos, pair), pair);
+        store_pieces((T *)p.q_out + ((int64_t)b * p.heads + h) * D, at, x);
+        return;
+    }
+    if (slot < 0) return;
+    const int kh = h - p.heads < p.kv_heads ? h - p.heads : h - p.heads - p.kv_heads;
+    const int64_t to = (slot + ((int64_t)kh << p.page_shift)) * D;
+    if (h >= p.heads + p.kv_heads) {
+        store_pieces((T *)p.v_cache + to, at, load_pieces((const T *)p.v + b * p.v_row + kh * p.v_head, at));
+        return;
+    }
+    Pieces x = rotate<T>(p, load_pieces((const T *)p.k + b * p.k_row + kh * p.k_head, at), load_angles(p, pos, pair), pair);
+    store_pieces((T *)p.k_cache + to, at, x);
+    if (p.bounds) {
+        T *lo = (T *)p.bounds + ((slot >> p.page_shift) + kh) * 2 * D, *hi = lo + D;
+        Pieces y = x;
+        if (slot & ((1 << p.page_shift) - 1)) {
+            const Pieces old_lo = load_pieces(lo, at), old_hi = load_pieces(hi, at);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const uint32_t o = ordered(x.w[i]);
+                x.w[i] = ordered(min2(ordered(old_lo.w[i]), o));
+                y.w[i] = ordered(max2(ordered(old_hi.w[i]), o));
+            }
+        }
+        store_pieces(lo, at, x);
+        store_pieces(hi, at, y);
+    }
+}
+
+// ---- any number of tokens per sequence ----
+// A work-group takes the new tokens of one page of one sequence and four heads
+// of q, of k or of v, so that a page's bounds are one work-group's: its tokens'
+// smallest and largest keys are kept in registers and joined at the end.
+constexpr int kSlab = 4;
+
+template <typename T, int D>
+__global__ void __launch_bounds__(256) append_prompt_kernel(const AppendProblem p)
+{
+    constexpr int kPairs = D / 16;
+    constexpr int kTokens = D == 64 ? 16 : D == 256 ? 4 : 8;  // of a wave at a time
+    __shared__ uint32_t lds[4][kPairs][kSlab][16];
+
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int pair = lane % kPairs, slot = lane / kPairs;
+
+    // the page: sequence b's blockIdx.x - before
+    int b = -1, first = 0, from = 0, n = 0, len = 0, before = 0;
+    for (int b0 = 0; b0 < p.B; b0 += 64) {
+        int pages = 0, begin = 0, count = 0, total = 0;
+        if (b0 + lane < p.B) {
+            begin = p.starts[b0 + lane];
+            int end = p.starts[b0 + lane + 1];
+            begin = begin < 0 ? 0 : begin < p.tokens ? begin : p.tokens;
+            end = end < begin ? begin : end < p.tokens ? end : p.tokens;
+            count = end - begin;
+            total = clamped(p.lengths[b0 + lane]);
+            pages = count > 0 ? ((total - 1) >> p.page_shift) - ((total - count) >> p.page_shift) + 1 : 0;
+        }
+        const int incl = before + wave_scan(pages, lane);
+        const uint64_t past = __ballot(incl > (int)blockIdx.x);
+        if (past) {
+            const int at = __builtin_ctzll(past);
+            b = b0 + at;
+            from = __shfl(begin, at);
+            n = __shfl(count, at);
+            len = __shfl(total, at);
+            first = (int)blockIdx.x - (__shfl(incl, at) - __shfl(pages, at));
+            break;
+        }
+        before = __shfl(incl, 63);
+    }
+    if (b < 0) return;
+    const int start = len - n;  // position of the first new token; below 0 where there are more than the length says
+    const int page0 = ((start >> p.page_shift) + first) * (1 << p.page_shift);
+    const int lo_pos = page0 > start ? page0 : start;
+    const int hi_pos = page0 + (1 << p.page_shift) < len ? page0 + (1 << p.page_shift) : len;
+
+    const int q_slabs = (p.heads + kSlab - 1) / kSlab, kv_slabs = (p.kv_heads + kSlab - 1) / kSlab;
+    const int y = blockIdx.y;
+    const int kind = y < q_slabs ? 0 : y < q_slabs + kv_slabs ? 1 : 2;
+    const int h0 = (kind == 0 ? y : kind == 1 ? y - q_slabs : y - q_slabs - kv_slabs) * kSlab;
+    const int nh = (kind == 0 ? p.heads : p.kv_heads) - h0 < kSlab ? (kind == 0 ? p.heads : p.kv_heads) - h0 : kSlab;
+    const T *src = (const T *)(kind == 0 ? p.q : kind == 1 ? p.k : p.v);
+    const int64_t row = kind == 0 ? p.q_row : kind == 1 ? p.k_row : p.v_row;
+    const int64_t head = kind == 0 ? p.q_head : kind == 1 ? p.k_head : p.v_head;
+    const Where at = where(p, pair);
+    const bool keep = kind == 1 && p.bounds;
+
+    uint32_t lo[kSlab][8], hi[kSlab][8];
+#pragma unroll
+    for (int j = 0; j < kSlab; ++j)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            lo[j][i] = 0x7FFF7FFFu;
+            hi[j][i] = 0x80008000u;
+        }
+    int kept = 0;
+    if (slot < kTokens) {
+        for (int pos = lo_pos + wave * kTokens + slot; pos < hi_pos; pos += 4 * kTokens) {
+            const int64_t t = from + (pos - start);
+            const int64_t to = slot_of(p, b, pos);
+            Angles a{};
+            if (kind < 2 && to >= 0) a = load_angles(p, pos, pair);
+#pragma unroll
+            for (int j = 0; j < kSlab; ++j) {
+                if (j >= nh) break;
+                Pieces x{};
+                if (to >= 0) x = load_pieces(src + t * row + (h0 + j) * head, at);
+                if (kind < 2 && to >= 0) x = rotate<T>(p, x, a, pair);
+                if (kind == 0) {
+                    store_pieces((T *)p.q_out + (t * p.heads + h0 + j) * D, at, x);
+                } else if (to >= 0) {
+                    store_pieces((T *)(kind == 1 ? p.k_cache : p.v_cache) + (to + ((int64_t)(h0 + j) << p.page_shift)) * D, at, x);
+                    if (keep) {
+                        kept = 1;
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const uint32_t o = ordered(x.w[i]);
+                            lo[j][i] = min2(lo[j][i], o);
+                            hi[j][i] = max2(hi[j][i], o);
+                        }
+                    }
+                }
+            }
+        }
+    }
+    if (!keep) return;  // uniform
+    // over the wave's tokens, then over the waves
+#pragma unroll
+    for (int d = kTokens / 2; d > 0; d >>= 1)
+#pragma unroll
+        for (int j = 0; j < kSlab; ++j)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                lo[j][i] = min2(lo[j][i], __shfl(lo[j][i], (lane + kPairs * d) & 63));
+                hi[j][i] = max2(hi[j][i], __shfl(hi[j][i], (lane + kPairs * d) & 63));
+            }
+    if (slot == 0)
+#pragma unroll
+        for (int j = 0; j < kSlab; ++j)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                lds[wave][pair][j][i] = lo[j][i];
+                lds[wave][pair][j][8 + i] = hi[j][i];
+            }
+    const int any = __syncthreads_or(kept);
+    if (!any) return;
+    if (threadIdx.x < kPairs * kSlab) {
+        const int j = threadIdx.x / kPairs, pr = threadIdx.x % kPairs;
+        if (j >= nh) return;
+        const Where w = where(p, pr);
+        Pieces x, z;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            x.w[i] = min2(min2(lds[0][pr][j][i], lds[1][pr][j][i]), min2(lds[2][pr][j][i], lds[3][pr][j][i]));
+            z.w[i] = max2(max2(lds[0][pr][j][8 + i], lds[1][pr][j][8 + i]), max2(lds[2][pr][j][8 + i], lds[3][pr][j][8 + i]));
+        }
+        const int page = p.table[b * p.table_row + (page0 >> p.page_shift)];
+        T *to_lo = (T *)p.bounds + ((int64_t)page * p.kv_heads + h0 + j) * 2 * D, *to_hi = to_lo + D;
+        if (lo_pos > page0) {
+            const Pieces old_lo = load_pieces(to_lo, w), old_hi = load_pieces(to_hi, w);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                x.w[i] = min2(x.w[i], ordered(old_lo.w[i]));
+                z.w[i] = max2(z.w[i], ordered(old_hi.w[i]));
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            x.w[i] = ordered(x.w[i]);
+            z.w[i] = ordered(z.w[i]);
+        }
+        store_pieces(to_lo, w, x);
+        store_pieces(to_hi, w, z);
+    }
+}
+
+template <typename T, int D>
+hipError_t launch_one(const AppendProblem &p, hipStream_t stream)
+{
+    if (!p.starts) {
+        constexpr int kHeads = 256 / (D / 16);
+        const int slabs = (p.heads + 2 * p.kv_heads + kHeads - 1) / kHeads;
+        hipLaunchKernelGGL((append_token_kernel<T, D>), dim3((uint32_t)p.B * slabs), dim3(256), 0, stream, p);
+    } else {
+        // a sequence of n tokens touches at most n / page size + 2 pages
+        const int pages = (p.tokens >> p.page_shift) + 2 * (p.B < p.tokens ? p.B : p.tokens);
+        const int slabs = (p.heads + kSlab - 1) / kSlab + 2 * ((p.kv_heads + kSlab - 1) / kSlab);
+        hipLaunchKernelGGL((append_prompt_kernel<T, D>), dim3(pages, slabs), dim3(256), 0, stream, p);
+    }
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch_typed(const AppendProblem &p, int head_dim, hipStream_t stream)
+{
+    switch (head_dim) {
+    case 64: return launch_one<T, 64>(p, stream);
+    case 96: return launch_one<T, 96>(p, stream);
+    case 128: return launch_one<T, 128>(p, stream);
+    case 256: return launch_one<T, 256>(p, stream);
+    }
+    return hipErrorInvalidValue;
+}
+
+}  // namespace
+
+hipError_t launch_append(const AppendProblem &p, int head_dim, marlin_dtype_t dtype, hipStream_t stream)
+{
+    return dtype == MARLIN_BF16 ? launch_typed<__bf16>(p, head_dim, stream) : launch_typed<_Float16>(p, head_dim, stream);
+}
+
+}  // namespace marlin

@@ -1,0 +1,97 @@
+// Device helpers of the key-value cache operators.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include "device.h"
+
+namespace marlin {
+namespace dev {
+
+template <typename T>
+struct Elem;
+
+template <>
+struct Elem<_Float16> {
+    typedef _Float16 vec8 __attribute__((ext_vector_type(8)));
+    static __device__ __forceinline__ float4_t mfma(vec8 a, vec8 b, float4_t c)
+    {
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+    }
+};
+
+template <>
+struct Elem<__bf16> {
+    typedef __bf16 vec8 __attribute__((ext_vector_type(8)));
+    static __device__ __forceinline__ float4_t mfma(vec8 a, vec8 b, float4_t c)
+    {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+    }
+};
+
+// N adjacent dwords, aligned to their size (three: to one).
+template <int N>
+__device__ __forceinline__ void load_dwords(uint32_t (&to)[N], const void *from)
+{
+    __builtin_memcpy(to, __builtin_assume_aligned(from, N == 3 ? 4 : 4 * N), 4 * N);
+}
+
+// x of lane l and of lane l ^ D, D = 32 or 16, in the same order in both: an
+// exchange of the wave's halves (of its odd and even 16-lane rows) between two
+// registers that both hold x.
+struct Pair {
+    float a, b;
+};
+template <int D>
+__device__ __forceinline__ Pair exchange(float x)
+{
+    const uint32_t w = __builtin_bit_cast(uint32_t, x);
+    const auto s = D == 32 ? __builtin_amdgcn_permlane32_swap(w, w, false, false) : __builtin_amdgcn_permlane16_swap(w, w, false, false);
+    const uint32_t a = s[0], b = s[1];  // named: a bit cast of a vector's element s[1] yields s[0]
+    return {__builtin_bit_cast(float, a), __builtin_bit_cast(float, b)};
+}
+
+// Over lanes l, l ^ 16, l ^ 32, l ^ 48 (the four groups of 16).
+__device__ __forceinline__ float max_over_groups(float x)
+{
+    const Pair p = exchange<32>(x);
+    const Pair q = exchange<16>(fmaxf(p.a, p.b));
+    return fmaxf(q.a, q.b);
+}
+
+__device__ __forceinline__ float sum_over_groups(float x)
+{
+    x += __shfl_xor(x, 32);
+    return x + __shfl_xor(x, 16);
+}
+
+__device__ __forceinline__ int wave_sum(int x)
+{
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) x += __shfl_xor(x, d);
+    return x;
+}
+
+// Inclusive sums over the lanes.
+__device__ __forceinline__ int wave_scan(int x, int lane)
+{
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int y = __shfl_up(x, d);
+        x += lane >= d ? y : 0;
+    }
+    return x;
+}
+
+// One float of a partial result, past the L2s that are not coherent.
+__device__ __forceinline__ void store_float(float *to, float x)
+{
+    __hip_atomic_store(to, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float load_float(const float *from)
+{
+    return __hip_atomic_load(from, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+}  // namespace dev
+}  // namespace marlin
