@@ -3,7 +3,7 @@
 //   o_h = sum_j p_hj v_j,  p_hj = exp(scale q_h . k_j) / sum_i exp(scale q_h . k_i)
 //
 // One row of work is a (sequence, kv head, tile of up to 16 query heads that
-// share it).  A wave takes 32 keys at a time and both products are MFMAs whose
+// share it).  A wave takes 32 keys of a row at a time, and both products are MFMAs whose
 // columns are the 16 heads, so nothing passes between lanes but the maximum:
 //
 //   S^T [16 keys x 16 heads] = K [16 x D] Q^T: lane (r = l % 16, g = l / 16)
@@ -16,10 +16,11 @@
 //     keys' elements with v_perm, which is the whole transpose.
 //
 // The work is split evenly however ragged the lengths are: the rows' 32-key
-// steps are numbered through and every work-group takes an equal range of
-// them, found from the lengths on the device.  A work-group's eight waves split
-// a row's steps and join in LDS; rows cut by range borders leave fp32 partial
-// results in the workspace, and whoever arrives last joins them in order.
+// steps are numbered through and every wave takes an equal range of them,
+// found from the lengths on the device.  Rows that lie within one wave's range go from
+// its registers to the output.  Pieces of rows cut between the waves of a
+// work-group are joined in LDS; what a work-group has of rows cut at its borders it leaves
+// in the workspace, and whoever arrives last there joins them, in order.
 #include <hip/hip_runtime.h>
 
 #include "device.h"
@@ -31,169 +32,264 @@ namespace {
 
 using namespace dev;
 
-// Rows shorter than twice this many steps are never cut, and no work-group
-// takes less: a cut costs a round trip through the workspace, about what a
-// work-group needs for as many steps.
-constexpr int kMinSteps = kAttendWaves;
+// No row is cut closer to its ends than this many steps, and no wave's range
+// is planned shorter.
+constexpr int kMinSteps = 2;
 
-// Where a unit (step) of the numbering lies.
-struct Place {
-    int row;    // (sequence, kv head, head tile)
-    int step;   // within the row
-    int start;  // unit of the row's first step
-};
-
-// Steps of sequence b; a sequence without keys still has one, in which its
-// outputs are written.
-__device__ __forceinline__ int tokens_of(const AttendProblem &p, int b)
+__device__ __forceinline__ int cap_tokens(const AttendProblem &p, int n)
 {
-    const int n = p.lengths[b], cap = p.width << p.page_shift;
+    const int cap = p.width << p.page_shift;
     return n < 0 ? 0 : n < cap ? n : cap;
 }
+// A sequence without keys still has a step, in which its outputs are written.
 __device__ __forceinline__ int steps_of(int tokens) { return tokens > 0 ? (tokens + kStepKeys - 1) / kStepKeys : 1; }
 
-// Row and step of unit u.  Borders near a row's ends move there.
-__device__ __forceinline__ Place place_of(const AttendProblem &p, int u, int lane)
-{
-    const int rows = p.kv_heads * p.head_tiles;  // of a sequence
-    const int x = u / rows;
-    int before = 0;
-    for (int b0 = 0; b0 < p.B; b0 += 64) {
-        const int c = b0 + lane < p.B ? steps_of(tokens_of(p, b0 + lane)) : 0;
-        const int incl = before + wave_scan(c, lane);
-        const uint64_t past = __ballot(b0 + lane < p.B && incl > x);
-        if (past) {
-            const int at = __builtin_ctzll(past);
-            const int cb = __shfl(c, at), first = (__shfl(incl, at) - cb) * rows;
-            const int r = (u - first) / cb, step = u - first - r * cb;
-            const int row = (b0 + at) * rows + r, start = u - step;
-            if (step < kMinSteps) return {row, 0, start};
-            if (cb - step < kMinSteps) return {row + 1, 0, start + cb};
-            return {row, step, start};
-        }
-        before = __shfl(incl, 63);
-    }
-    return {p.B * rows, 0, u};
-}
+// Where a step of the numbering lies: row 0 of sequence b, and so on.
+struct Place {
+    int b, row;  // row of the sequence: kv head and head tile
+    int step;    // within the row
+    int start;   // number of the row's first step
+};
 
-// Smallest w with range start w * q + min(w, r) >= x.
+// Smallest worker whose range's start w * q + min(w, r) is >= x, largest <= x.
 __device__ __forceinline__ int first_at(int x, int q, int r)
 {
     return x <= r * (q + 1) ? (x + q) / (q + 1) : r + (x - r * (q + 1) + q - 1) / q;
 }
-// Largest w with range start <= x.
 __device__ __forceinline__ int last_at(int x, int q, int r)
 {
     return x <= r * (q + 1) ? x / (q + 1) : r + (x - r * (q + 1)) / q;
 }
+
+// A step of 32 keys: its row, and the table's entries for its two 16-key tiles.
+struct Step {
+    int b, row, tokens, s;
+    int e0, e1;
+};
 
 template <typename T, int D, int NW>
 __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendProblem p)
 {
     typedef Elem<T> E;
     typedef typename E::vec8 vec8;
-    constexpr int kQ = D / 32;                 // 16-byte pieces of a row per lane, keys
-    constexpr int kHalves = D > 128 ? 2 : 1;   // 16-byte pieces of a row per lane, values
-    constexpr int kCh = D / 16 / kHalves;      // channels in each
+    constexpr int kQ = D / 32;                // 16-byte pieces of a key's row per lane
+    constexpr int kHalves = D > 128 ? 2 : 1;  // pieces of a value's row per lane
+    constexpr int kCh = D / 16 / kHalves;     // channels in each
     constexpr int kDw = kCh / 2;
-    constexpr int kPad = D + 4;                // LDS row: 16 heads' float4 reach all banks
-    constexpr int kItems = (kHeadTile * D / 4 + 64 * NW - 1) / (64 * NW);
+    constexpr int kAcc = D / 16;
+    constexpr int kSlotFloats = kHeadTile * D + 2 * kHeadTile;
 
-    __shared__ float lds_o[NW][kHeadTile][kPad];
+    __shared__ float4_t lds_acc[NW][kAcc][64];
     __shared__ float lds_m[NW][kHeadTile], lds_l[NW][kHeadTile];
-    __shared__ int lds_flag;
+    __shared__ int lds_within[NW], lds_from[4], lds_to[4], lds_flags[2];
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int r = lane & 15, g = lane >> 4;
+    const int rows = p.kv_heads * p.head_tiles;  // of a sequence
 
-    // this work-group's range of steps
-    const int rows = p.kv_heads * p.head_tiles;
-    int units = 0;
-    for (int b0 = 0; b0 < p.B; b0 += 64) units += b0 + lane < p.B ? steps_of(tokens_of(p, b0 + lane)) : 0;
-    units = __builtin_amdgcn_readfirstlane(wave_sum(units)) * rows;
-    int wgs = units / kMinSteps;
+    // ---- this wave's range of steps ----
+    int count = 0, incl = 0, total = 0;  // of the first 64 sequences, lane by lane
+    for (int b0 = 0; b0 < p.B; b0 += 64) {
+        const int c = b0 + lane < p.B ? steps_of(cap_tokens(p, p.lengths[b0 + lane])) : 0;
+        const int i = wave_scan(c, lane);
+        if (b0 == 0) {
+            count = c;
+            incl = i;
+        }
+        total += __builtin_amdgcn_readlane(i, 63);
+    }
+    const int units = total * rows;
+    int wgs = units / (NW * kMinSteps);
     wgs = wgs < 1 ? 1 : wgs < (int)gridDim.x ? wgs : (int)gridDim.x;
     const int wg = blockIdx.x;
     if (wg >= wgs) return;
-    const int per = units / wgs, extra = units % wgs;
-    auto start_of = [&](int w) { return w * per + (w < extra ? w : extra); };
-    Place from = place_of(p, start_of(wg), lane), to = place_of(p, start_of(wg + 1), lane);
-    from.row = __builtin_amdgcn_readfirstlane(from.row);
-    from.step = __builtin_amdgcn_readfirstlane(from.step);
-    from.start = __builtin_amdgcn_readfirstlane(from.start);
-    to.row = __builtin_amdgcn_readfirstlane(to.row);
-    to.step = __builtin_amdgcn_readfirstlane(to.step);
-    to.start = __builtin_amdgcn_readfirstlane(to.start);
-
-    const int slot_floats = kHeadTile * D + 2 * kHeadTile;
-    const int last_row = to.step > 0 ? to.row : to.row - 1;
-    for (int row = from.row; row <= last_row; ++row) {
-        const int b = row / rows, in_b = row - b * rows;
-        const int kvh = in_b / p.head_tiles, ht = in_b - kvh * p.head_tiles;
-        const int heads = p.group - ht * kHeadTile < kHeadTile ? p.group - ht * kHeadTile : kHeadTile;
-        const int head0 = kvh * p.group + ht * kHeadTile;
-        const int tokens = tokens_of(p, b), steps = steps_of(tokens);
-        const int begin = row == from.row ? from.step : 0, end = row == to.row ? to.step : steps;
-
-        // the heads' queries: head r's channels 32t + 8g .. + 7
-        vec8 qf[kQ];
-        const T *q = (const T *)p.q + b * p.q_row + (head0 + r) * p.q_head + 8 * g;
-#pragma unroll
-        for (int t = 0; t < kQ; ++t) qf[t] = r < heads ? *(const vec8 *)(q + 32 * t) : vec8{};
-
-        float4_t acc[kHalves * kCh];
-#pragma unroll
-        for (int j = 0; j < kHalves * kCh; ++j) acc[j] = float4_t{0.f, 0.f, 0.f, 0.f};
-        float m = -INFINITY, l = 0.f;
-
-        const int32_t *table = p.table + b * p.table_row + kvh * p.table_head;
-        const int n = end - begin;
-        const int s1 = begin + n * (wave + 1) / NW;
-        for (int s = begin + n * wave / NW; s < s1 && s * kStepKeys < tokens; ++s) {
-            // the step's two 16-key tiles: pages (one outside the cache counts as masked) and valid keys
-            vec8 kf[2][kQ];
-            uint32_t vr[2][4][kHalves][kDw];
-            int valid[2];
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const int pos = s * kStepKeys + 16 * u;
-                const int left = tokens - pos;
-                const int page = left > 0 ? table[pos >> p.page_shift] : 0;
-                const bool inside = (uint32_t)page < (uint32_t)p.pages;
-                valid[u] = !inside || left < 0 ? 0 : left < 16 ? left : 16;
-                const int64_t at = (((int64_t)(inside ? page : 0) * p.kv_heads + kvh) << p.page_shift) +
-                                   (pos & ((1 << p.page_shift) - 1));
-                const T *k = (const T *)p.k + at * D, *v = (const T *)p.v + at * D;
-#pragma unroll
-                for (int t = 0; t < kQ; ++t) kf[u][t] = *(const vec8 *)(k + (r * D + 8 * g) + 32 * t);
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-#pragma unroll
-                    for (int hf = 0; hf < kHalves; ++hf)
-                        load_dwords<kDw>(vr[u][i][hf], v + (4 * g * D + kCh * r) + i * D + 128 * hf);
+    const int per = units / (wgs * NW), extra = units - per * wgs * NW;
+    auto place_of = [&](int worker) -> Place {
+        const int u = worker * per + (worker < extra ? worker : extra);
+        int before = 0;
+        for (int b0 = 0; b0 < p.B; b0 += 64) {
+            int c = count, i = incl;
+            if (b0 > 0) {
+                c = b0 + lane < p.B ? steps_of(cap_tokens(p, p.lengths[b0 + lane])) : 0;
+                i = wave_scan(c, lane);
             }
+            const uint64_t past = __ballot((before + i) * rows > u);
+            if (past) {
+                const int at = __builtin_ctzll(past);
+                const int cb = __builtin_amdgcn_readlane(c, at);
+                const int first = (before + __builtin_amdgcn_readlane(i, at) - cb) * rows;
+                const int row = (u - first) / cb, step = u - first - row * cb, start = u - step;
+                // borders near a row's ends move there
+                if (step < kMinSteps) return {b0 + at, row, 0, start};
+                if (cb - step >= kMinSteps) return {b0 + at, row, step, start};
+                return row + 1 < rows ? Place{b0 + at, row + 1, 0, start + cb} : Place{b0 + at + 1, 0, 0, start + cb};
+            }
+            before += __builtin_amdgcn_readlane(i, 63);
+        }
+        return {p.B, 0, 0, units};
+    };
+    const Place from = place_of(wg * NW + wave), to = place_of(wg * NW + wave + 1);
+    int left = to.start + to.step - from.start - from.step;  // steps of this wave
+
+    // ---- the steps ----
+    auto table_of = [&](const Step &x) {
+        const int kvh = p.head_tiles == 1 ? x.row : x.row / p.head_tiles;
+        return p.table + x.b * p.table_row + kvh * p.table_head;
+    };
+    // the entries' loads (scalar) are issued a step before they are needed; past the row's tokens nothing is read
+    auto entries = [&](Step &x) {
+        const int32_t *table = table_of(x);
+        const int pos = x.s * kStepKeys;
+        x.e0 = x.e1 = -1;
+        if (pos < x.tokens) x.e0 = scalar_load(table + (pos >> p.page_shift));
+        if (pos + 16 < x.tokens) x.e1 = scalar_load(table + ((pos + 16) >> p.page_shift));
+    };
+    auto advance = [&](Step x) -> Step {
+        if (x.s + 1 < steps_of(x.tokens)) {
+            ++x.s;
+        } else {
+            x.s = 0;
+            if (++x.row == rows) {
+                x.row = 0;
+                ++x.b;
+                x.tokens = cap_tokens(p, scalar_load(p.lengths + x.b));
+            }
+        }
+        entries(x);
+        return x;
+    };
+    vec8 qf[kQ], kf[2][kQ];
+    uint32_t vr[2][4][kHalves][kDw];
+    auto load_queries = [&](const Step &x) {
+        const int kvh = p.head_tiles == 1 ? x.row : x.row / p.head_tiles;
+        const int h0 = (x.row - kvh * p.head_tiles) * kHeadTile;
+        const T *q = (const T *)p.q + x.b * p.q_row + (kvh * p.group + h0 + r) * p.q_head + 8 * g;
+#pragma unroll
+        for (int t = 0; t < kQ; ++t) qf[t] = h0 + r < p.group ? *(const vec8 *)(q + 32 * t) : vec8{};
+    };
+    // a tile's first element in the caches; an entry that names no page is read as page 0 and masked
+    auto tile_at = [&](const Step &x, int u) -> int64_t {
+        const int e = u ? x.e1 : x.e0, kvh = p.head_tiles == 1 ? x.row : x.row / p.head_tiles;
+        const int slot = (x.s * kStepKeys + 16 * u) & ((1 << p.page_shift) - 1);
+        return ((((int64_t)((uint32_t)e < (uint32_t)p.pages ? e : 0) * p.kv_heads + kvh) << p.page_shift) + slot) * D;
+    };
+    auto load_keys = [&](const Step &x) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const T *k = (const T *)p.k + tile_at(x, u);
+#pragma unroll
+            for (int t = 0; t < kQ; ++t) kf[u][t] = *(const vec8 *)(k + (r * D + 8 * g) + 32 * t);
+        }
+    };
+    auto load_values = [&](const Step &x) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const T *v = (const T *)p.v + tile_at(x, u);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int hf = 0; hf < kHalves; ++hf)
+                    load_dwords<kDw>(vr[u][i][hf], v + (4 * g * D + kCh * r) + i * D + 128 * hf);
+        }
+    };
+    float4_t acc[kAcc];
+    float m, l;
+    auto clear = [&] {
+#pragma unroll
+        for (int j = 0; j < kAcc; ++j) acc[j] = float4_t{0.f, 0.f, 0.f, 0.f};
+        m = -INFINITY;
+        l = 0.f;
+    };
+    // Joins another piece of the row: its maximum, its sum (each lane that of head r), its accumulators.
+    auto join = [&](float m2, float l2, const float4_t(&acc2)[kAcc]) {
+        const float top = fmaxf(m, m2), ref = top == -INFINITY ? 0.f : top;
+        const float f = __builtin_amdgcn_exp2f(m - ref), f2 = __builtin_amdgcn_exp2f(m2 - ref);
+        m = top;
+        l = l * f + l2 * f2;
+#pragma unroll
+        for (int j = 0; j < kAcc; ++j) acc[j] = acc[j] * f + acc2[j] * f2;
+    };
+    auto put_piece = [&](int slot) {
+#pragma unroll
+        for (int j = 0; j < kAcc; ++j) lds_acc[slot][j][lane] = acc[j];
+        if (g == 0) {
+            lds_m[slot][r] = m;
+            lds_l[slot][r] = l;
+        }
+    };
+    auto join_piece = [&](int slot) {
+        float4_t acc2[kAcc];
+#pragma unroll
+        for (int j = 0; j < kAcc; ++j) acc2[j] = lds_acc[slot][j][lane];
+        join(lds_m[slot][r], lds_l[slot][r], acc2);
+    };
+    // The finished row: lane (r, g) holds head r's channels kCh (4g + i) + j.
+    auto write_row = [&](int b, int row) {
+        const int kvh = p.head_tiles == 1 ? row : row / p.head_tiles, h0 = (row - kvh * p.head_tiles) * kHeadTile;
+        if (h0 + r >= p.group) return;
+        const int64_t at = (int64_t)b * p.heads + kvh * p.group + h0 + r;
+        const float inv = l == 0.f ? 0.f : 1.f / l;  // no key: zero
+#pragma unroll
+        for (int hf = 0; hf < kHalves; ++hf)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                T y[kCh];
+#pragma unroll
+                for (int j = 0; j < kCh; ++j) y[j] = (T)(acc[hf * kCh + j][i] * inv);
+                uint32_t w[kDw];
+                __builtin_memcpy(w, y, sizeof(y));
+                store_dwords<kDw>((T *)p.out + at * D + 128 * hf + kCh * (4 * g + i), w);
+            }
+        if (p.lse && g == 0) p.lse[at] = (m + __builtin_amdgcn_logf(l)) * 0.693147180559945f;
+    };
+
+    bool begun_before = from.step > 0;  // the row at hand began in another wave
+    if (left > 0) {
+        Step cur{from.b, from.row, cap_tokens(p, scalar_load(p.lengths + from.b)), from.step, -1, -1}, next;
+        entries(cur);
+        load_queries(cur);
+        load_keys(cur);
+        load_values(cur);
+        if (left > 1) next = advance(cur);
+        clear();
+        while (true) {
             float4_t sc[2];
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
                 sc[u] = float4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int t = 0; t < kQ; ++t) sc[u] = E::mfma(kf[u][t], qf[t], sc[u]);
+            }
+            // The next step's keys are under way while this one's scores and values are dealt with,
+            // its values while the next scores are.
+            const bool row_ends = cur.s + 1 == steps_of(cur.tokens);
+            Step ahead;
+            issue_order_point();
+            if (left > 1) {
+                if (row_ends) load_queries(next);
+                load_keys(next);
+                if (left > 2) ahead = advance(next);
+            }
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) sc[u][i] *= p.scale_log2;
-            }
-            if (valid[0] < 16 || valid[1] < 16) {
+            const int pos = cur.s * kStepKeys;
+            if (pos + 32 > cur.tokens || (uint32_t)cur.e0 >= (uint32_t)p.pages || (uint32_t)cur.e1 >= (uint32_t)p.pages) {
                 // whatever a masked slot holds (an infinity, not a number) stays out of both products
 #pragma unroll
-                for (int u = 0; u < 2; ++u)
+                for (int u = 0; u < 2; ++u) {
+                    const int valid = (uint32_t)(u ? cur.e1 : cur.e0) < (uint32_t)p.pages ? cur.tokens - pos - 16 * u : 0;
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
-                        if (4 * g + i >= valid[u]) {
+                        if (4 * g + i >= valid) {
                             sc[u][i] = -INFINITY;
 #pragma unroll
                             for (int hf = 0; hf < kHalves; ++hf)
 #pragma unroll
                                 for (int w = 0; w < kDw; ++w) vr[u][i][hf][w] = 0;
                         }
+                }
             }
             float top = m;
 #pragma unroll
@@ -202,19 +298,24 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
                 for (int i = 0; i < 4; ++i) top = fmaxf(top, sc[u][i]);
             top = max_over_groups(top);
             const float ref = top == -INFINITY ? 0.f : top;  // nothing but -inf so far: weights 0
-            const float keep = __builtin_amdgcn_exp2f(m - ref);
+            if (__any(top > m)) {
+                const float keep = __builtin_amdgcn_exp2f(m - ref);
+                l *= keep;
+#pragma unroll
+                for (int j = 0; j < kAcc; ++j) acc[j] *= keep;
+            }
             m = top;
             float pr[2][4];
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) pr[u][i] = __builtin_amdgcn_exp2f(sc[u][i] - ref);
-            l = l * keep + ((pr[0][0] + pr[0][1]) + (pr[0][2] + pr[0][3])) + ((pr[1][0] + pr[1][1]) + (pr[1][2] + pr[1][3]));
+            l += ((pr[0][0] + pr[0][1]) + (pr[0][2] + pr[0][3])) + ((pr[1][0] + pr[1][1]) + (pr[1][2] + pr[1][3]));
+            // The weights go to the second product in the cache's type, as its MFMAs want them: half an ulp each, the size of
+            // the output's own rounding, with the sum l kept of the unrounded ones.
             vec8 pf;
 #pragma unroll
             for (int e = 0; e < 8; ++e) pf[e] = (T)pr[e >> 2][e & 3];
-#pragma unroll
-            for (int j = 0; j < kHalves * kCh; ++j) acc[j] *= keep;
 #pragma unroll
             for (int hf = 0; hf < kHalves; ++hf)
 #pragma unroll
@@ -226,106 +327,119 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
                                                      (j & 1) ? 0x07060302u : 0x05040100u);
                     acc[hf * kCh + j] = E::mfma(__builtin_bit_cast(vec8, u32x4_t{w[0], w[1], w[2], w[3]}), pf, acc[hf * kCh + j]);
                 }
+            issue_order_point();
+            if (left > 1) load_values(next);
+            if (row_ends || left == 1) l = sum_over_groups(l);
+            if (row_ends) {
+                if (begun_before)
+                    put_piece(wave);
+                else
+                    write_row(cur.b, cur.row);
+                begun_before = false;
+                if (left > 1) clear();
+            }
+            if (--left == 0) break;
+            cur = next;
+            next = ahead;
         }
-        l = sum_over_groups(l);
+    }
 
-        // the waves' results: lane (r, g) holds head r's channels kCh (4g + i) + j
+    // ---- rows cut between waves ----
+    const bool open = to.step > 0;            // the last row continues in the next wave; its piece is in the registers
+    const bool within = open && begun_before;  // and began in an earlier one: nothing but a piece of it here
+    if (within) put_piece(wave);
+    if (lane == 0) {
+        lds_within[wave] = within;
+        if (wave == 0) {
+            lds_from[0] = from.b;
+            lds_from[1] = from.row;
+            lds_from[2] = from.step;
+            lds_from[3] = from.start;
+        }
+        if (wave == NW - 1) {
+            lds_to[0] = to.b;
+            lds_to[1] = to.row;
+            lds_to[2] = to.step;
+            lds_to[3] = to.start;
+        }
+    }
+    __syncthreads();
+    const bool wg_head = lds_from[2] > 0, wg_tail = lds_to[2] > 0;
+    const bool one_row = wg_head && wg_tail && lds_from[3] == lds_to[3];  // the whole range lies in one row
+    // the pieces of waves w, w + 1, .. up to the row's end; true if it goes on in the next work-group
+    auto gather = [&](int w) -> bool {
+#pragma unroll 1
+        for (; w < NW; ++w) {
+            join_piece(w);
+            if (!lds_within[w]) return false;
+        }
+        return true;
+    };
+    auto put_partial = [&](float *slot) {
 #pragma unroll
-        for (int hf = 0; hf < kHalves; ++hf)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < kCh; ++j) lds_o[wave][r][128 * hf + kCh * (4 * g + i) + j] = acc[hf * kCh + j][i];
+        for (int j = 0; j < kAcc; ++j) store_partial16(slot, j, lane, acc[j]);
         if (g == 0) {
-            lds_m[wave][r] = m;
-            lds_l[wave][r] = l;
+            store_float(slot + kHeadTile * D + r, m);
+            store_float(slot + kHeadTile * D + kHeadTile + r, l);
+        }
+        wait_vmcnt<0>();
+    };
+    float *const slots = p.partials + (int64_t)wg * 2 * kSlotFloats;
+    if (open && !within) {
+        if (gather(wave + 1))
+            put_partial(slots + kSlotFloats);
+        else
+            write_row(to.b, to.row);
+    }
+    if (wave == 0 && wg_head) {
+        clear();
+        gather(0);
+        put_partial(slots);
+    }
+    if (!wg_head && !wg_tail) return;
+
+    // ---- rows cut between work-groups: 0: the first row, 1: the last ----
+    const int n_head = wg_head ? steps_of(cap_tokens(p, scalar_load(p.lengths + lds_from[0]))) : 0;
+    const int n_tail = wg_tail && !one_row ? steps_of(cap_tokens(p, scalar_load(p.lengths + lds_to[0]))) : 0;
+    // contributors: the work-group that holds the row's start and those whose ranges start within it
+    auto first_of = [&](int start) { return (first_at(start + kMinSteps, per, extra) + NW - 1) / NW - 1; };
+    auto last_of = [&](int start, int n) { return last_at(start + n - kMinSteps, per, extra) / NW; };
+    __syncthreads();
+    if (tid < 2) {
+        int flag = 0;
+        const int n = tid == 0 ? n_head : n_tail, start = tid == 0 ? lds_from[3] : lds_to[3];
+        if (n > 0) {
+            const int first = first_of(start), others = last_of(start, n) - first;
+            uint32_t *const ctr = p.counters + kCounterStride * first;
+            flag = __hip_atomic_fetch_add(ctr, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)others;
+            if (flag) __hip_atomic_store(ctr, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+        lds_flags[tid] = flag;
+    }
+    __syncthreads();
+#pragma unroll 1
+    for (int which = 0; which < 2; ++which) {
+        if (!lds_flags[which]) continue;
+        const int start = which == 0 ? lds_from[3] : lds_to[3], n = which == 0 ? n_head : n_tail;
+        const int first = first_of(start), last = last_of(start, n);
+        // every wave joins some of the contributors, in order, then wave 0 the waves': the same bits every time
+        clear();
+#pragma unroll 1
+        for (int w = first + wave; w <= last; w += NW) {
+            const float *slot = p.partials + ((int64_t)w * 2 + (w == first ? 1 : 0)) * kSlotFloats;
+            float4_t acc2[kAcc];
+#pragma unroll
+            for (int j = 0; j < kAcc; ++j) acc2[j] = load_partial16(slot, j, lane);
+            join(load_float(slot + kHeadTile * D + r), load_float(slot + kHeadTile * D + kHeadTile + r), acc2);
+        }
+        put_piece(wave);
+        __syncthreads();
+        if (wave == 0) {
+#pragma unroll 1
+            for (int w = 1; w < NW; ++w) join_piece(w);
+            write_row(which == 0 ? lds_from[0] : lds_to[0], which == 0 ? lds_from[1] : lds_to[1]);
         }
         __syncthreads();
-        const bool whole = begin == 0 && end == steps;
-        // contributors of a row that is cut: those whose ranges start within it, and the one before
-        int w_first = 0, others = 0;
-        if (!whole) {
-            const int start = row == from.row ? from.start : to.start;
-            w_first = first_at(start + kMinSteps, per, extra) - 1;
-            others = last_at(start + steps - kMinSteps, per, extra) - w_first;
-        }
-        float *const slot = p.partials + ((int64_t)wg * 2 + (begin > 0 ? 0 : 1)) * slot_floats;
-        float4_t res[kItems];
-        float top[kItems], sum[kItems];
-#pragma unroll
-        for (int k = 0; k < kItems; ++k) {
-            const int it = tid + k * 64 * NW, h = it / (D / 4), d = it % (D / 4) * 4;
-            if (h >= heads) continue;
-            float t = -INFINITY, s = 0.f;
-            float4_t o{0.f, 0.f, 0.f, 0.f};
-            for (int w = 0; w < NW; ++w) t = fmaxf(t, lds_m[w][h]);
-            const float ref = t == -INFINITY ? 0.f : t;
-            for (int w = 0; w < NW; ++w) {
-                const float f = __builtin_amdgcn_exp2f(lds_m[w][h] - ref);
-                s += f * lds_l[w][h];
-                o += f * *(const float4_t *)&lds_o[w][h][d];
-            }
-            res[k] = o;
-            top[k] = t;
-            sum[k] = s;
-            if (!whole) {
-                store_partial16(slot, wave + k * NW, lane, o);
-                if (d == 0) {
-                    store_float(slot + kHeadTile * D + h, t);
-                    store_float(slot + kHeadTile * D + kHeadTile + h, s);
-                }
-            }
-        }
-        if (!whole) {
-            wait_vmcnt<0>();
-            __syncthreads();
-            if (tid == 0) {
-                uint32_t *const ctr = p.counters + kCounterStride * w_first;
-                const bool last = __hip_atomic_fetch_add(ctr, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)others;
-                if (last) __hip_atomic_store(ctr, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                lds_flag = last;
-            }
-            __syncthreads();
-            if (lds_flag) {
-                // in the order of the ranges, so the same inputs give the same bits
-#pragma unroll
-                for (int k = 0; k < kItems; ++k) {
-                    const int it = tid + k * 64 * NW, h = it / (D / 4);
-                    if (h >= heads) continue;
-                    float t = -INFINITY, s = 0.f;
-                    float4_t o{0.f, 0.f, 0.f, 0.f};
-                    for (int w = w_first; w <= w_first + others; ++w) {
-                        const float *from_w = p.partials + ((int64_t)w * 2 + (w == w_first ? 1 : 0)) * slot_floats;
-                        const float mw = load_float(from_w + kHeadTile * D + h), lw = load_float(from_w + kHeadTile * D + kHeadTile + h);
-                        const float4_t ow = load_partial16(from_w, wave + k * NW, lane);
-                        const float nt = fmaxf(t, mw), ref = nt == -INFINITY ? 0.f : nt;
-                        const float fo = __builtin_amdgcn_exp2f(t - ref), fw = __builtin_amdgcn_exp2f(mw - ref);
-                        s = s * fo + lw * fw;
-                        o = o * fo + ow * fw;
-                        t = nt;
-                    }
-                    res[k] = o;
-                    top[k] = t;
-                    sum[k] = s;
-                }
-            }
-        }
-        if (whole || lds_flag) {
-#pragma unroll
-            for (int k = 0; k < kItems; ++k) {
-                const int it = tid + k * 64 * NW, h = it / (D / 4), d = it % (D / 4) * 4;
-                if (h >= heads) continue;
-                const int64_t at = (int64_t)b * p.heads + head0 + h;
-                const float inv = sum[k] == 0.f ? 0.f : 1.f / sum[k];  // no key: zero
-                typedef T vec4 __attribute__((ext_vector_type(4)));
-                vec4 y;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) y[i] = (T)(res[k][i] * inv);
-                *(vec4 *)((T *)p.out + at * D + d) = y;
-                if (p.lse && d == 0) p.lse[at] = (top[k] + __builtin_amdgcn_logf(sum[k])) * 0.693147180559945f;
-            }
-        }
-        __syncthreads();  // before the next row's results go to LDS
     }
 }
 

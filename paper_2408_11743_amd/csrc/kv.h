@@ -15,7 +15,7 @@ constexpr int kKvMaxCus = 256;        // compute units a workspace is sized for
 constexpr int kStepKeys = 32;         // keys a wave takes at a time
 constexpr int kHeadTile = 16;         // query heads of one kv head that share a pass over its keys
 constexpr int kAttendWaves = 8;       // waves per work-group
-constexpr int kAttendGroupsPerCu = 2; // work-groups per compute unit
+constexpr int kAttendGroupsPerCu = 1; // work-groups per compute unit
 
 // Floats of one partial result: fp32 sums of up to kHeadTile heads, then each
 // head's maximum and sum.

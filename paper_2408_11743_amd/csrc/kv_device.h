@@ -36,6 +36,19 @@ __device__ __forceinline__ void load_dwords(uint32_t (&to)[N], const void *from)
     __builtin_memcpy(to, __builtin_assume_aligned(from, N == 3 ? 4 : 4 * N), 4 * N);
 }
 
+template <int N>
+__device__ __forceinline__ void store_dwords(void *to, const uint32_t (&from)[N])
+{
+    __builtin_memcpy(__builtin_assume_aligned(to, N == 3 ? 4 : 4 * N), from, 4 * N);
+}
+
+// A word at an address that is the same in every lane and that nothing writes during the
+// kernel: by the scalar cache, whose loads the vector ones do not wait for.
+__device__ __forceinline__ int scalar_load(const int32_t *p)
+{
+    return *(const __attribute__((address_space(4))) int32_t *)(uintptr_t)p;
+}
+
 // x of lane l and of lane l ^ D, D = 32 or 16, in the same order in both: an
 // exchange of the wave's halves (of its odd and even 16-lane rows) between two
 // registers that both hold x.
