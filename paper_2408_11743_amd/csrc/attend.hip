@@ -178,7 +178,7 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
         for (int u = 0; u < 2; ++u) {
             const T *k = (const T *)p.k + tile_at(x, u);
 #pragma unroll
-            for (int t = 0; t < kQ; ++t) kf[u][t] = *(const vec8 *)(k + (r * D + 8 * g) + 32 * t);
+            for (int t = 0; t < kQ; ++t) kf[u][t] = __builtin_nontemporal_load((const vec8 *)(k + (r * D + 8 * g) + 32 * t));
         }
     };
     auto load_values = [&](const Step &x) {
@@ -189,7 +189,7 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
             for (int i = 0; i < 4; ++i)
 #pragma unroll
                 for (int hf = 0; hf < kHalves; ++hf)
-                    load_dwords<kDw>(vr[u][i][hf], v + (4 * g * D + kCh * r) + i * D + 128 * hf);
+                    load_dwords_once<kDw>(vr[u][i][hf], v + (4 * g * D + kCh * r) + i * D + 128 * hf);
         }
     };
     float4_t acc[kAcc];

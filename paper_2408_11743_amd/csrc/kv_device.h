@@ -36,6 +36,23 @@ __device__ __forceinline__ void load_dwords(uint32_t (&to)[N], const void *from)
     __builtin_memcpy(to, __builtin_assume_aligned(from, N == 3 ? 4 : 4 * N), 4 * N);
 }
 
+// The same of what is read once (see attend.hip).
+template <int N>
+__device__ __forceinline__ void load_dwords_once(uint32_t (&to)[N], const void *from)
+{
+    if constexpr (N == 3) {  // aligned to a dword only
+        typedef uint32_t dword3 __attribute__((ext_vector_type(3), aligned(4)));
+        const dword3 x = __builtin_nontemporal_load((const dword3 *)from);
+#pragma unroll
+        for (int i = 0; i < 3; ++i) to[i] = x[i];
+    } else {
+        typedef uint32_t dwordn __attribute__((ext_vector_type(N)));
+        const dwordn x = __builtin_nontemporal_load((const dwordn *)from);
+#pragma unroll
+        for (int i = 0; i < N; ++i) to[i] = x[i];
+    }
+}
+
 template <int N>
 __device__ __forceinline__ void store_dwords(void *to, const uint32_t (&from)[N])
 {
