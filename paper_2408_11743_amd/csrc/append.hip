@@ -190,7 +190,7 @@ __global__ void __launch_bounds__(256) append_prompt_kernel(const AppendProblem 
             total = clamped(p.lengths[b0 + lane]);
             pages = count > 0 ? ((total - 1) >> p.page_shift) - ((total - count) >> p.page_shift) + 1 : 0;
         }
-        const int incl = before + wave_scan(pages, lane);
+        const int incl = before + wave_scan(pages);
         const uint64_t past = __ballot(incl > (int)blockIdx.x);
         if (past) {
             const int at = __builtin_ctzll(past);

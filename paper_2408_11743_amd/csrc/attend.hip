@@ -32,8 +32,13 @@ namespace {
 
 using namespace dev;
 
-// No row is cut closer to its ends than this many steps, and no wave's range
-// is planned shorter.
+// A work-group border does not cut a row closer to its ends than this many
+// steps (it moves to the end): a cut costs a round trip through the workspace,
+// as long as a work-group takes for about as many steps.
+constexpr int kMinCut = kAttendWaves;
+// What a row costs beyond its steps (queries, output), in steps.
+constexpr int kRowCost = 1;
+// Steps a wave gets at least where there are few.
 constexpr int kMinSteps = 2;
 
 __device__ __forceinline__ int cap_tokens(const AttendProblem &p, int n)
@@ -44,14 +49,16 @@ __device__ __forceinline__ int cap_tokens(const AttendProblem &p, int n)
 // A sequence without keys still has a step, in which its outputs are written.
 __device__ __forceinline__ int steps_of(int tokens) { return tokens > 0 ? (tokens + kStepKeys - 1) / kStepKeys : 1; }
 
-// Where a step of the numbering lies: row 0 of sequence b, and so on.
+// Where a range begins or ends: a step of a row.
 struct Place {
-    int b, row;  // row of the sequence: kv head and head tile
-    int step;    // within the row
-    int start;   // number of the row's first step
+    int b, row;  // sequence, and its row: kv head and head tile
+    int step;    // of the row
+    int before;  // steps of all rows before it
+    int steps;   // the row's (where step > 0)
+    int tokens;  // the sequence's (-1: still to be read)
 };
 
-// Smallest worker whose range's start w * q + min(w, r) is >= x, largest <= x.
+// Smallest w whose range's start w * q + min(w, r) is >= x, largest whose is <= x.
 __device__ __forceinline__ int first_at(int x, int q, int r)
 {
     return x <= r * (q + 1) ? (x + q) / (q + 1) : r + (x - r * (q + 1) + q - 1) / q;
@@ -81,55 +88,104 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
 
     __shared__ float4_t lds_acc[NW][kAcc][64];
     __shared__ float lds_m[NW][kHeadTile], lds_l[NW][kHeadTile];
-    __shared__ int lds_within[NW], lds_from[4], lds_to[4], lds_flags[2];
+    __shared__ int lds_within[NW], lds_flags[2];
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int r = lane & 15, g = lane >> 4;
     const int rows = p.kv_heads * p.head_tiles;  // of a sequence
 
-    // ---- this wave's range of steps ----
-    int count = 0, incl = 0, total = 0;  // of the first 64 sequences, lane by lane
+    // ---- this work-group's range of steps, and this wave's share of it ----
+    // Everything until the first loads of keys is latency: no divisions, and the first 64 sequences' lengths stay in
+    // the lanes.
+    int length0 = 0, count0 = 0, incl0 = 0, total = 0;  // tokens, steps, and steps up to and with the lane's sequence
     for (int b0 = 0; b0 < p.B; b0 += 64) {
-        const int c = b0 + lane < p.B ? steps_of(cap_tokens(p, p.lengths[b0 + lane])) : 0;
-        const int i = wave_scan(c, lane);
+        const int n = b0 + lane < p.B ? cap_tokens(p, p.lengths[b0 + lane]) : 0;
+        const int c = b0 + lane < p.B ? steps_of(n) : 0, i = wave_scan(c);
         if (b0 == 0) {
-            count = c;
-            incl = i;
+            length0 = n;
+            count0 = c;
+            incl0 = i;
         }
         total += __builtin_amdgcn_readlane(i, 63);
     }
-    const int units = total * rows;
-    int wgs = units / (NW * kMinSteps);
-    wgs = wgs < 1 ? 1 : wgs < (int)gridDim.x ? wgs : (int)gridDim.x;
-    const int wg = blockIdx.x;
+    const int units = (total + kRowCost * p.B) * rows;
+    // Range w starts at unit w * per + min(w, extra).
+    const int grid = gridDim.x, wg = blockIdx.x;
+    int wgs = grid, per, extra;
+    if (units < grid * NW * kMinSteps) {
+        wgs = (uint32_t)(units + NW * kMinSteps - 1) / (NW * kMinSteps);
+        per = NW * kMinSteps;
+        extra = 0;
+    } else {
+        per = (int)__umulhi((uint32_t)units, p.grid_reciprocal);
+        extra = units - per * grid;
+        if (extra >= grid) {
+            ++per;
+            extra -= grid;
+        }
+    }
     if (wg >= wgs) return;
-    const int per = units / (wgs * NW), extra = units - per * wgs * NW;
-    auto place_of = [&](int worker) -> Place {
-        const int u = worker * per + (worker < extra ? worker : extra);
-        int before = 0;
-        for (int b0 = 0; b0 < p.B; b0 += 64) {
-            int c = count, i = incl;
-            if (b0 > 0) {
-                c = b0 + lane < p.B ? steps_of(cap_tokens(p, p.lengths[b0 + lane])) : 0;
-                i = wave_scan(c, lane);
-            }
-            const uint64_t past = __ballot((before + i) * rows > u);
-            if (past) {
-                const int at = __builtin_ctzll(past);
-                const int cb = __builtin_amdgcn_readlane(c, at);
-                const int first = (before + __builtin_amdgcn_readlane(i, at) - cb) * rows;
-                const int row = (u - first) / cb, step = u - first - row * cb, start = u - step;
-                // borders near a row's ends move there
-                if (step < kMinSteps) return {b0 + at, row, 0, start};
-                if (cb - step >= kMinSteps) return {b0 + at, row, step, start};
-                return row + 1 < rows ? Place{b0 + at, row + 1, 0, start + cb} : Place{b0 + at + 1, 0, 0, start + cb};
-            }
+    auto start_of = [&](int w) {
+        const int u = w * per + (w < extra ? w : extra);
+        return u < units ? u : units;
+    };
+    // the row that holds unit u of the numbering in which a row counts its steps and `cost` more, where it is one of
+    // the 64 sequences from b0 on; n, c, i as above, `before` the steps of the sequences before b0
+    auto place_among = [&](int u, int cost, int b0, int before, int n, int c, int i, Place &x) -> bool {
+        const int ends = b0 + lane < p.B ? (before + i + cost * (b0 + lane + 1)) * rows : 0;
+        const uint64_t past = __builtin_amdgcn_ballot_w64(ends > u);
+        if (past == 0) return false;
+        const int at = __builtin_ctzll(past);
+        const int cb = __builtin_amdgcn_readlane(c, at);
+        const int off = u - __builtin_amdgcn_readlane(ends, at) + (cb + cost) * rows;
+        // off / (cb + cost): the lanes count the rows that end by then
+        const int row = rows == 1 ? 0
+                        : rows <= 64 ? __popcll(__builtin_amdgcn_ballot_w64((lane + 1) * (cb + cost) <= off))
+                                     : (uint32_t)off / (uint32_t)(cb + cost);
+        const int step = off - row * (cb + cost) - cost;
+        x = {b0 + at, row, step < 0 ? 0 : step, u - off - cost * (b0 + at) * rows + row * cb, cb, __builtin_amdgcn_readlane(n, at)};
+        return true;
+    };
+    auto place_of = [&](int u, int cost) -> Place {
+        Place x{p.B, 0, 0, total * rows, 1, 0};
+        if (place_among(u, cost, 0, 0, length0, count0, incl0, x) || p.B <= 64) return x;
+        int before = __builtin_amdgcn_readlane(incl0, 63);
+#pragma unroll 1
+        for (int b0 = 64; b0 < p.B; b0 += 64) {
+            const int n = b0 + lane < p.B ? cap_tokens(p, p.lengths[b0 + lane]) : 0;
+            const int c = b0 + lane < p.B ? steps_of(n) : 0, i = wave_scan(c);
+            if (place_among(u, cost, b0, before, n, c, i, x)) break;
             before += __builtin_amdgcn_readlane(i, 63);
         }
-        return {p.B, 0, 0, units};
+        return x;
     };
-    const Place from = place_of(wg * NW + wave), to = place_of(wg * NW + wave + 1);
-    int left = to.start + to.step - from.start - from.step;  // steps of this wave
+    auto border = [&](int w) -> Place {
+        Place x = place_of(start_of(w), kRowCost);
+        if (x.step < kMinCut) {
+            x.step = 0;
+        } else if (x.steps - x.step < kMinCut) {
+            x.step = 0;
+            x.before += x.steps;
+            if (++x.row == rows) {
+                x.row = 0;
+                ++x.b;
+                x.tokens = -1;
+            }
+        }
+        return x;
+    };
+    const Place wg_from = border(wg), wg_to = border(wg + 1);
+    const int begin = wg_from.before + wg_from.step, steps = wg_to.before + wg_to.step - begin;
+    const int mine = (int)((int64_t)steps * wave / NW);
+    int left = (int)((int64_t)steps * (wave + 1) / NW) - mine;  // steps of this wave
+    Place from = wg_from, to = wg_to;
+    if (wg_from.before == wg_to.before) {  // all in one row
+        from.step += mine;
+        to.step = from.step + left;
+    } else {
+        if (wave > 0) from = place_of(begin + mine, 0);
+        if (wave < NW - 1) to = place_of(begin + mine + left, 0);
+    }
 
     // ---- the steps ----
     auto table_of = [&](const Step &x) {
@@ -244,14 +300,14 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
     };
 
     bool begun_before = from.step > 0;  // the row at hand began in another wave
+    clear();  // a wave without steps between two that share a row adds nothing to it
     if (left > 0) {
-        Step cur{from.b, from.row, cap_tokens(p, scalar_load(p.lengths + from.b)), from.step, -1, -1}, next;
+        Step cur{from.b, from.row, from.tokens >= 0 ? from.tokens : cap_tokens(p, scalar_load(p.lengths + from.b)), from.step, -1, -1}, next;
         entries(cur);
         load_queries(cur);
         load_keys(cur);
         load_values(cur);
         if (left > 1) next = advance(cur);
-        clear();
         while (true) {
             float4_t sc[2];
 #pragma unroll
@@ -348,24 +404,10 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
     const bool open = to.step > 0;            // the last row continues in the next wave; its piece is in the registers
     const bool within = open && begun_before;  // and began in an earlier one: nothing but a piece of it here
     if (within) put_piece(wave);
-    if (lane == 0) {
-        lds_within[wave] = within;
-        if (wave == 0) {
-            lds_from[0] = from.b;
-            lds_from[1] = from.row;
-            lds_from[2] = from.step;
-            lds_from[3] = from.start;
-        }
-        if (wave == NW - 1) {
-            lds_to[0] = to.b;
-            lds_to[1] = to.row;
-            lds_to[2] = to.step;
-            lds_to[3] = to.start;
-        }
-    }
+    if (lane == 0) lds_within[wave] = within;
     __syncthreads();
-    const bool wg_head = lds_from[2] > 0, wg_tail = lds_to[2] > 0;
-    const bool one_row = wg_head && wg_tail && lds_from[3] == lds_to[3];  // the whole range lies in one row
+    const bool wg_head = wg_from.step > 0, wg_tail = wg_to.step > 0;
+    const bool one_row = wg_head && wg_from.before == wg_to.before;  // the whole range lies in one row
     // the pieces of waves w, w + 1, .. up to the row's end; true if it goes on in the next work-group
     auto gather = [&](int w) -> bool {
 #pragma unroll 1
@@ -399,17 +441,15 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
     if (!wg_head && !wg_tail) return;
 
     // ---- rows cut between work-groups: 0: the first row, 1: the last ----
-    const int n_head = wg_head ? steps_of(cap_tokens(p, scalar_load(p.lengths + lds_from[0]))) : 0;
-    const int n_tail = wg_tail && !one_row ? steps_of(cap_tokens(p, scalar_load(p.lengths + lds_to[0]))) : 0;
-    // contributors: the work-group that holds the row's start and those whose ranges start within it
-    auto first_of = [&](int start) { return (first_at(start + kMinSteps, per, extra) + NW - 1) / NW - 1; };
-    auto last_of = [&](int start, int n) { return last_at(start + n - kMinSteps, per, extra) / NW; };
+    // Contributors: the work-group that holds the row's start, and those whose ranges start within it.
+    auto unit_of = [&](const Place &x) { return x.before + kRowCost * (x.b * rows + x.row + 1); };  // of its first step
     __syncthreads();
     if (tid < 2) {
         int flag = 0;
-        const int n = tid == 0 ? n_head : n_tail, start = tid == 0 ? lds_from[3] : lds_to[3];
-        if (n > 0) {
-            const int first = first_of(start), others = last_of(start, n) - first;
+        const Place &x = tid == 0 ? wg_from : wg_to;
+        if (tid == 0 ? wg_head : wg_tail && !one_row) {
+            const int first = first_at(unit_of(x) + kMinCut, per, extra) - 1;
+            const int others = last_at(unit_of(x) + x.steps - kMinCut, per, extra) - first;
             uint32_t *const ctr = p.counters + kCounterStride * first;
             flag = __hip_atomic_fetch_add(ctr, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)others;
             if (flag) __hip_atomic_store(ctr, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -420,24 +460,39 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
 #pragma unroll 1
     for (int which = 0; which < 2; ++which) {
         if (!lds_flags[which]) continue;
-        const int start = which == 0 ? lds_from[3] : lds_to[3], n = which == 0 ? n_head : n_tail;
-        const int first = first_of(start), last = last_of(start, n);
-        // every wave joins some of the contributors, in order, then wave 0 the waves': the same bits every time
+        const Place x = which == 0 ? wg_from : wg_to;
+        const int first = first_at(unit_of(x) + kMinCut, per, extra) - 1;
+        const int last = last_at(unit_of(x) + x.steps - kMinCut, per, extra);
+        // Every wave joins some of the contributors, in order, then the first wave the waves': the same bits every time.
+        const __amdgpu_buffer_rsrc_t partials =
+            __builtin_amdgcn_make_buffer_rsrc((void *)p.partials, (short)0, 0x7fffffffu, kBufferFlags);
         clear();
-#pragma unroll 1
-        for (int w = first + wave; w <= last; w += NW) {
-            const float *slot = p.partials + ((int64_t)w * 2 + (w == first ? 1 : 0)) * kSlotFloats;
-            float4_t acc2[kAcc];
+        struct Piece {
+            float m, l;
+            float4_t acc[kAcc];
+        };
+        auto load_piece = [&](int w, Piece &x) {
+            const int slot = __builtin_amdgcn_readfirstlane((w * 2 + (w == first ? 1 : 0)) * kSlotFloats * 4);
 #pragma unroll
-            for (int j = 0; j < kAcc; ++j) acc2[j] = load_partial16(slot, j, lane);
-            join(load_float(slot + kHeadTile * D + r), load_float(slot + kHeadTile * D + kHeadTile + r), acc2);
+            for (int j = 0; j < kAcc; ++j) x.acc[j] = load_slot16(partials, slot, j * 1024 + lane * 16);
+            x.m = load_slot4(partials, slot, kHeadTile * D * 4 + r * 4);
+            x.l = load_slot4(partials, slot, kHeadTile * D * 4 + kHeadTile * 4 + r * 4);
+        };
+#pragma unroll 1
+        for (int w = first + wave; w <= last; w += 2 * NW) {  // two at a time: a round trip is 2 us
+            Piece x, y;
+            load_piece(w, x);
+            const bool two = w + NW <= last;
+            if (two) load_piece(w + NW, y);
+            join(x.m, x.l, x.acc);
+            if (two) join(y.m, y.l, y.acc);
         }
         put_piece(wave);
         __syncthreads();
         if (wave == 0) {
 #pragma unroll 1
-            for (int w = 1; w < NW; ++w) join_piece(w);
-            write_row(which == 0 ? lds_from[0] : lds_to[0], which == 0 ? lds_from[1] : lds_to[1]);
+            for (int w = 1; w < NW && w <= last - first; ++w) join_piece(w);
+            write_row(x.b, x.row);
         }
         __syncthreads();
     }
@@ -447,7 +502,9 @@ template <typename T, int D>
 hipError_t launch_one(const AttendProblem &p, int cus, hipStream_t stream)
 {
     const int grid = (cus < kKvMaxCus ? cus : kKvMaxCus) * kAttendGroupsPerCu;
-    hipLaunchKernelGGL((paged_attention_kernel<T, D, kAttendWaves>), dim3(grid), dim3(64 * kAttendWaves), 0, stream, p);
+    AttendProblem q = p;
+    q.grid_reciprocal = grid > 1 ? (uint32_t)(((uint64_t)1 << 32) / (uint64_t)grid) : 0xFFFFFFFFu;
+    hipLaunchKernelGGL((paged_attention_kernel<T, D, kAttendWaves>), dim3(grid), dim3(64 * kAttendWaves), 0, stream, q);
     return hipGetLastError();
 }
 

@@ -95,21 +95,15 @@ __device__ __forceinline__ float sum_over_groups(float x)
     return x + __shfl_xor(x, 16);
 }
 
-__device__ __forceinline__ int wave_sum(int x)
+// Inclusive sums over the lanes, by row shifts and broadcasts of a row's last lane.
+__device__ __forceinline__ int wave_scan(int x)
 {
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) x += __shfl_xor(x, d);
-    return x;
-}
-
-// Inclusive sums over the lanes.
-__device__ __forceinline__ int wave_scan(int x, int lane)
-{
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const int y = __shfl_up(x, d);
-        x += lane >= d ? y : 0;
-    }
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);  // row_shr:1
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, true);  // row_bcast:15 into rows 1 and 3
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, true);  // row_bcast:31 into rows 2 and 3
     return x;
 }
 
@@ -118,9 +112,15 @@ __device__ __forceinline__ void store_float(float *to, float x)
 {
     __hip_atomic_store(to, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
-__device__ __forceinline__ float load_float(const float *from)
+// A float4 or a float of the partial results, `slot` bytes into them (the same in
+// every lane) and `at` bytes further.
+__device__ __forceinline__ float4_t load_slot16(__amdgpu_buffer_rsrc_t partials, int slot, int at)
 {
-    return __hip_atomic_load(from, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    return __builtin_bit_cast(float4_t, __builtin_amdgcn_raw_buffer_load_b128(partials, at, slot, kAuxDeviceCoherent));
+}
+__device__ __forceinline__ float load_slot4(__amdgpu_buffer_rsrc_t partials, int slot, int at)
+{
+    return __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(partials, at, slot, kAuxDeviceCoherent));
 }
 
 }  // namespace dev

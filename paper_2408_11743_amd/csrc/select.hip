@@ -126,7 +126,7 @@ __global__ void __launch_bounds__(kPickThreads) page_pick_kernel(const SelectPro
             // lane l: bytes 255 - 4l .. 252 - 4l, from the top
             int c[4], sum = 0;
             for (int k = 0; k < 4; ++k) sum += c[k] = count[255 - 4 * lane - k];
-            int upto = wave_scan(sum, lane) - sum;
+            int upto = wave_scan(sum) - sum;
             for (int k = 0; k < 4; ++k) {
                 if (upto < want && want <= upto + c[k]) {
                     bucket = 255 - 4 * lane - k;
