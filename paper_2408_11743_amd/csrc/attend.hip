@@ -35,11 +35,11 @@ using namespace dev;
 // A work-group border does not cut a row closer to its ends than this many
 // steps (it moves to the end): a cut costs a round trip through the workspace,
 // as long as a work-group takes for about as many steps.
-constexpr int kMinCut = kAttendWaves;
+constexpr int kMinCut = 3;
 // What a row costs beyond its steps (queries, output), in steps.
 constexpr int kRowCost = 1;
-// Steps a wave gets at least where there are few.
-constexpr int kMinSteps = 2;
+// Steps a work-group gets at least where there are few.
+constexpr int kMinSteps = 4;
 
 __device__ __forceinline__ int cap_tokens(const AttendProblem &p, int n)
 {
@@ -86,9 +86,10 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
     constexpr int kAcc = D / 16;
     constexpr int kSlotFloats = kHeadTile * D + 2 * kHeadTile;
 
-    __shared__ float4_t lds_acc[NW][kAcc][64];
-    __shared__ float lds_m[NW][kHeadTile], lds_l[NW][kHeadTile];
-    __shared__ int lds_within[NW], lds_flags[2];
+    // one piece of a row per wave, and that of the row the range ends in
+    __shared__ float4_t lds_acc[NW + 1][kAcc][64];
+    __shared__ float lds_m[NW + 1][kHeadTile], lds_l[NW + 1][kHeadTile];
+    __shared__ int lds_within[NW], lds_flags[2], lds_first[2], lds_last[2];
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int r = lane & 15, g = lane >> 4;
@@ -112,9 +113,9 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
     // Range w starts at unit w * per + min(w, extra).
     const int grid = gridDim.x, wg = blockIdx.x;
     int wgs = grid, per, extra;
-    if (units < grid * NW * kMinSteps) {
-        wgs = (uint32_t)(units + NW * kMinSteps - 1) / (NW * kMinSteps);
-        per = NW * kMinSteps;
+    if (units < grid * kMinSteps) {
+        wgs = (uint32_t)(units + kMinSteps - 1) / (kMinSteps);
+        per = kMinSteps;
         extra = 0;
     } else {
         per = (int)__umulhi((uint32_t)units, p.grid_reciprocal);
@@ -188,9 +189,18 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
     }
 
     // ---- the steps ----
+    // a row's kv head, its first query head and how many it has
+    auto kv_head_of = [&](int row) { return p.head_tiles == 1 ? row : row / p.head_tiles; };
+    auto head0_of = [&](int row) {
+        const int kvh = kv_head_of(row);
+        return kvh * p.group + (row - kvh * p.head_tiles) * kHeadTile;
+    };
+    auto heads_of = [&](int row) {
+        const int n = p.head_tiles == 1 ? p.group : p.group - row % p.head_tiles * kHeadTile;
+        return n < kHeadTile ? n : kHeadTile;
+    };
     auto table_of = [&](const Step &x) {
-        const int kvh = p.head_tiles == 1 ? x.row : x.row / p.head_tiles;
-        return p.table + x.b * p.table_row + kvh * p.table_head;
+        return p.table + x.b * p.table_row + kv_head_of(x.row) * p.table_head;
     };
     // the entries' loads (scalar) are issued a step before they are needed; past the row's tokens nothing is read
     auto entries = [&](Step &x) {
@@ -217,15 +227,14 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
     vec8 qf[kQ], kf[2][kQ];
     uint32_t vr[2][4][kHalves][kDw];
     auto load_queries = [&](const Step &x) {
-        const int kvh = p.head_tiles == 1 ? x.row : x.row / p.head_tiles;
-        const int h0 = (x.row - kvh * p.head_tiles) * kHeadTile;
-        const T *q = (const T *)p.q + x.b * p.q_row + (kvh * p.group + h0 + r) * p.q_head + 8 * g;
+        const T *q = (const T *)p.q + x.b * p.q_row + (head0_of(x.row) + r) * p.q_head + 8 * g;
+        const bool have = r < heads_of(x.row);
 #pragma unroll
-        for (int t = 0; t < kQ; ++t) qf[t] = h0 + r < p.group ? *(const vec8 *)(q + 32 * t) : vec8{};
+        for (int t = 0; t < kQ; ++t) qf[t] = have ? *(const vec8 *)(q + 32 * t) : vec8{};
     };
     // a tile's first element in the caches; an entry that names no page is read as page 0 and masked
     auto tile_at = [&](const Step &x, int u) -> int64_t {
-        const int e = u ? x.e1 : x.e0, kvh = p.head_tiles == 1 ? x.row : x.row / p.head_tiles;
+        const int e = u ? x.e1 : x.e0, kvh = kv_head_of(x.row);
         const int slot = (x.s * kStepKeys + 16 * u) & ((1 << p.page_shift) - 1);
         return ((((int64_t)((uint32_t)e < (uint32_t)p.pages ? e : 0) * p.kv_heads + kvh) << p.page_shift) + slot) * D;
     };
@@ -281,9 +290,8 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
     };
     // The finished row: lane (r, g) holds head r's channels kCh (4g + i) + j.
     auto write_row = [&](int b, int row) {
-        const int kvh = p.head_tiles == 1 ? row : row / p.head_tiles, h0 = (row - kvh * p.head_tiles) * kHeadTile;
-        if (h0 + r >= p.group) return;
-        const int64_t at = (int64_t)b * p.heads + kvh * p.group + h0 + r;
+        if (r >= heads_of(row)) return;
+        const int64_t at = (int64_t)b * p.heads + head0_of(row) + r;
         const float inv = l == 0.f ? 0.f : 1.f / l;  // no key: zero
 #pragma unroll
         for (int hf = 0; hf < kHalves; ++hf)
@@ -401,55 +409,92 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
     }
 
     // ---- rows cut between waves ----
-    const bool open = to.step > 0;            // the last row continues in the next wave; its piece is in the registers
+    const bool wg_head = wg_from.step > 0, wg_tail = wg_to.step > 0;  // the first row began before, the last goes on after
+    const bool one_row = wg_head && wg_from.before == wg_to.before;   // the whole range lies in one row
+    const bool open = to.step > 0;             // this wave's last row goes on in the next one; its piece is in the registers
     const bool within = open && begun_before;  // and began in an earlier one: nothing but a piece of it here
+    const bool ends_range = open && !within && wg_tail && to.before == wg_to.before;
     if (within) put_piece(wave);
+    if (ends_range) put_piece(NW);
     if (lane == 0) lds_within[wave] = within;
-    __syncthreads();
-    const bool wg_head = wg_from.step > 0, wg_tail = wg_to.step > 0;
-    const bool one_row = wg_head && wg_from.before == wg_to.before;  // the whole range lies in one row
-    // the pieces of waves w, w + 1, .. up to the row's end; true if it goes on in the next work-group
-    auto gather = [&](int w) -> bool {
-#pragma unroll 1
-        for (; w < NW; ++w) {
-            join_piece(w);
-            if (!lds_within[w]) return false;
+    // Contributors to the rows cut at the range's borders (0: the first row, 1: the last): the work-group that holds
+    // the row's start, and those whose ranges start within it.  The first wave, which is done early, sees to it.
+    if (wave == 0 && (wg_head || wg_tail)) {
+        const Place x = lane == 0 ? wg_from : wg_to;
+        const int unit = x.before + kRowCost * (x.b * rows + x.row + 1);  // of the row's first step
+        const int first = first_at(unit + kMinCut, per, extra) - 1, last = last_at(unit + x.steps - kMinCut, per, extra);
+        if (lane < 2) {
+            lds_first[lane] = first;
+            lds_last[lane] = last;
         }
-        return true;
-    };
-    auto put_partial = [&](float *slot) {
-#pragma unroll
-        for (int j = 0; j < kAcc; ++j) store_partial16(slot, j, lane, acc[j]);
-        if (g == 0) {
-            store_float(slot + kHeadTile * D + r, m);
-            store_float(slot + kHeadTile * D + kHeadTile + r, l);
-        }
-        wait_vmcnt<0>();
-    };
-    float *const slots = p.partials + (int64_t)wg * 2 * kSlotFloats;
-    if (open && !within) {
-        if (gather(wave + 1))
-            put_partial(slots + kSlotFloats);
-        else
-            write_row(to.b, to.row);
     }
-    if (wave == 0 && wg_head) {
-        clear();
-        gather(0);
-        put_partial(slots);
+    __syncthreads();
+    if (open && !within && !ends_range) {  // a row that ends in a later wave of this work-group
+        bool more = true;
+#pragma unroll 1
+        for (int w = wave + 1; more; ++w) {
+            join_piece(w);
+            more = lds_within[w];
+        }
+        write_row(to.b, to.row);
     }
     if (!wg_head && !wg_tail) return;
 
-    // ---- rows cut between work-groups: 0: the first row, 1: the last ----
-    // Contributors: the work-group that holds the row's start, and those whose ranges start within it.
-    auto unit_of = [&](const Place &x) { return x.before + kRowCost * (x.b * rows + x.row + 1); };  // of its first step
+    // ---- rows cut between work-groups ----
+    // Their pieces (bits of `slots`) are joined by all waves, each some of the channels.
+    auto join_slots = [&](uint32_t slots, auto &&put) {
+        float mk[NW + 1], lk[NW + 1], top = -INFINITY, sum = 0.f;
+#pragma unroll
+        for (int k = 0; k <= NW; ++k)
+            if (slots >> k & 1) {
+                mk[k] = lds_m[k][r];
+                lk[k] = lds_l[k][r];
+            }
+#pragma unroll
+        for (int k = 0; k <= NW; ++k)
+            if (slots >> k & 1) top = fmaxf(top, mk[k]);
+        const float ref = top == -INFINITY ? 0.f : top;
+#pragma unroll
+        for (int k = 0; k <= NW; ++k)
+            if (slots >> k & 1) {
+                mk[k] = __builtin_amdgcn_exp2f(mk[k] - ref);
+                sum += lk[k] * mk[k];
+            }
+#pragma unroll 1
+        for (int j = wave; j < kAcc; j += NW) {
+            float4_t o{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int k = 0; k <= NW; ++k)
+                if (slots >> k & 1) o += lds_acc[k][j][lane] * mk[k];
+            put(j, o, top, sum);
+        }
+    };
+    const uint32_t all = (1u << NW) - 1;
+    const uint32_t inner = (uint32_t)__builtin_amdgcn_ballot_w64(lane < NW && lds_within[lane < NW ? lane : 0]);
+#pragma unroll 1
+    for (int which = 0; which < 2; ++which) {
+        if (which == 0 ? !wg_head : !wg_tail || one_row) continue;
+        // the first row: the waves within it from the first on and the one that ends it; the last: its first piece
+        // and the waves after that one
+        const uint32_t slots = which == 0 ? (inner == all ? all : ((~inner & (inner + 1)) << 1) - 1)
+                                          : (all & ~((2u << (31 - __builtin_clz(~inner & all))) - 1)) | 1u << NW;
+        float *const slot = p.partials + ((int64_t)wg * 2 + which) * kSlotFloats;
+        const int nh = heads_of(which == 0 ? wg_from.row : wg_to.row);
+        join_slots(slots, [&](int j, float4_t o, float top, float sum) {
+            if (r >= nh) return;
+            store_partial16(slot, j, lane, o);
+            if (j == 0 && g == 0) {
+                store_float(slot + kHeadTile * D + r, top);
+                store_float(slot + kHeadTile * D + kHeadTile + r, sum);
+            }
+        });
+    }
+    wait_vmcnt<0>();
     __syncthreads();
     if (tid < 2) {
         int flag = 0;
-        const Place &x = tid == 0 ? wg_from : wg_to;
         if (tid == 0 ? wg_head : wg_tail && !one_row) {
-            const int first = first_at(unit_of(x) + kMinCut, per, extra) - 1;
-            const int others = last_at(unit_of(x) + x.steps - kMinCut, per, extra) - first;
+            const int first = lds_first[tid], others = lds_last[tid] - first;
             uint32_t *const ctr = p.counters + kCounterStride * first;
             flag = __hip_atomic_fetch_add(ctr, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)others;
             if (flag) __hip_atomic_store(ctr, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -459,41 +504,48 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
     __syncthreads();
 #pragma unroll 1
     for (int which = 0; which < 2; ++which) {
-        if (!lds_flags[which]) continue;
-        const Place x = which == 0 ? wg_from : wg_to;
-        const int first = first_at(unit_of(x) + kMinCut, per, extra) - 1;
-        const int last = last_at(unit_of(x) + x.steps - kMinCut, per, extra);
-        // Every wave joins some of the contributors, in order, then the first wave the waves': the same bits every time.
+        if (!__builtin_amdgcn_readfirstlane(lds_flags[which])) continue;
+        const int first = __builtin_amdgcn_readfirstlane(lds_first[which]), last = __builtin_amdgcn_readfirstlane(lds_last[which]);
+        // Every wave joins some of the contributors, in order, then all of them the waves': the same bits every time.
         const __amdgpu_buffer_rsrc_t partials =
             __builtin_amdgcn_make_buffer_rsrc((void *)p.partials, (short)0, 0x7fffffffu, kBufferFlags);
+        const int b = which == 0 ? wg_from.b : wg_to.b, row = which == 0 ? wg_from.row : wg_to.row, nh = heads_of(row);
         clear();
-        struct Piece {
-            float m, l;
-            float4_t acc[kAcc];
-        };
-        auto load_piece = [&](int w, Piece &x) {
-            const int slot = __builtin_amdgcn_readfirstlane((w * 2 + (w == first ? 1 : 0)) * kSlotFloats * 4);
+        if (r < nh) {
+            struct Piece {
+                float m, l;
+                float4_t acc[kAcc];
+            };
+            auto load_piece = [&](int w, Piece &x) {
+                const int slot = (w * 2 + (w == first ? 1 : 0)) * (kSlotFloats * 4);
 #pragma unroll
-            for (int j = 0; j < kAcc; ++j) x.acc[j] = load_slot16(partials, slot, j * 1024 + lane * 16);
-            x.m = load_slot4(partials, slot, kHeadTile * D * 4 + r * 4);
-            x.l = load_slot4(partials, slot, kHeadTile * D * 4 + kHeadTile * 4 + r * 4);
-        };
+                for (int j = 0; j < kAcc; ++j) x.acc[j] = load_slot16(partials, slot, j * 1024 + lane * 16);
+                x.m = load_slot4(partials, slot, kHeadTile * D * 4 + r * 4);
+                x.l = load_slot4(partials, slot, kHeadTile * D * 4 + kHeadTile * 4 + r * 4);
+            };
+            constexpr int kAhead = 2;  // under way together
 #pragma unroll 1
-        for (int w = first + wave; w <= last; w += 2 * NW) {  // two at a time: a round trip is 2 us
-            Piece x, y;
-            load_piece(w, x);
-            const bool two = w + NW <= last;
-            if (two) load_piece(w + NW, y);
-            join(x.m, x.l, x.acc);
-            if (two) join(y.m, y.l, y.acc);
+            for (int w = first + wave; w <= last; w += kAhead * NW) {
+                Piece x[kAhead];
+#pragma unroll
+                for (int k = 0; k < kAhead; ++k)
+                    if (w + k * NW <= last) load_piece(w + k * NW, x[k]);
+#pragma unroll
+                for (int k = 0; k < kAhead; ++k)
+                    if (w + k * NW <= last) join(x[k].m, x[k].l, x[k].acc);
+            }
         }
         put_piece(wave);
         __syncthreads();
-        if (wave == 0) {
-#pragma unroll 1
-            for (int w = 1; w < NW && w <= last - first; ++w) join_piece(w);
-            write_row(x.b, x.row);
-        }
+        join_slots(last - first >= NW - 1 ? all : (2u << (last - first)) - 1, [&](int j, float4_t o, float top, float sum) {
+            if (r >= nh) return;
+            const int64_t at = (int64_t)b * p.heads + head0_of(row) + r;
+            const float inv = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                ((T *)p.out)[at * D + 128 * (j / kCh) + kCh * (4 * g + i) + j % kCh] = (T)(o[i] * inv);
+            if (p.lse && g == 0 && j == 0) p.lse[at] = (top + __builtin_amdgcn_logf(sum)) * 0.693147180559945f;
+        });
         __syncthreads();
     }
 }
