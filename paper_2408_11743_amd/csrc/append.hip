@@ -3,8 +3,7 @@
 // rounding, keys and values written to their pages, and the pages' bounds (the
 // smallest and largest key per channel) widened.
 //
-// A head is D / 16 threads, each with the two 16-byte pieces that hold its
-// eight pairs.  Nothing is read twice but the angles; the kernels are bound by
+// A head is D / 16 threads, each with two 16-byte pieces that hold eight pairs.  Nothing is read twice but the angles; the kernels are bound by
 // memory, and by launch latency where there is one token per sequence.
 #include <hip/hip_runtime.h>
 
@@ -35,16 +34,17 @@ struct Pieces {
     uint32_t w[8];  // two 16-byte pieces
 };
 
-// Elements where thread `pair` of a head's D / 16 has its two pieces: the
-// halves of eight pairs, or (interleaved, or past the rotated channels)
-// sixteen adjacent channels.
+// Channels where thread `pair` of a head's D / 16 has its two pieces: where halves
+// are paired, both of eight pairs; else the pieces that make neighbouring threads' accesses adjacent.
 struct Where {
     int first, second;
 };
-__device__ __forceinline__ Where where(const AppendProblem &p, int pair)
+__device__ __forceinline__ Where where(const AppendProblem &p, int D, int pair)
 {
-    if (!p.interleaved && pair < p.rot / 16) return {8 * pair, 8 * pair + p.rot / 2};
-    return {16 * pair, 16 * pair + 8};
+    if (p.interleaved) return {8 * pair, 8 * pair + D / 2};
+    if (pair < p.rot / 16) return {8 * pair, 8 * pair + p.rot / 2};
+    const int first = 8 * pair + p.rot / 2;  // past the rotated ones
+    return {first, first + (D - p.rot) / 2};
 }
 
 template <typename T>
@@ -63,38 +63,42 @@ __device__ __forceinline__ void store_pieces(T *row, Where at, const Pieces &x)
     __builtin_memcpy(__builtin_assume_aligned(row + at.second, 16), x.w + 4, 16);
 }
 
-// Eight pairs' cosines and sines.
+// Cosines and sines of the pieces' pairs: of eight (c[0], c[1]), or interleaved
+// of the first piece's four and the second's.
 struct Angles {
     float4_t c[2], s[2];
 };
-__device__ __forceinline__ Angles load_angles(const AppendProblem &p, int pos, int pair)
+__device__ __forceinline__ Angles load_angles(const AppendProblem &p, Where at, int pos)
 {
     Angles a{};
-    if (pair < p.rot / 16) {
-        const float *row = p.cos_sin + (int64_t)pos * p.rot + 8 * pair;
-        a.c[0] = *(const float4_t *)row;
-        a.c[1] = *(const float4_t *)(row + 4);
-        a.s[0] = *(const float4_t *)(row + p.rot / 2);
-        a.s[1] = *(const float4_t *)(row + p.rot / 2 + 4);
+    const float *row = p.cos_sin + (int64_t)pos * p.rot;
+    const int i0 = p.interleaved ? at.first / 2 : at.first, i1 = p.interleaved ? at.second / 2 : at.first + 4;
+    if (at.first < p.rot) {
+        a.c[0] = *(const float4_t *)(row + i0);
+        a.s[0] = *(const float4_t *)(row + p.rot / 2 + i0);
+    }
+    if (at.second < p.rot) {
+        a.c[1] = *(const float4_t *)(row + i1);
+        a.s[1] = *(const float4_t *)(row + p.rot / 2 + i1);
     }
     return a;
 }
 
 template <typename T>
-__device__ __forceinline__ Pieces rotate(const AppendProblem &p, const Pieces &x, const Angles &a, int pair)
+__device__ __forceinline__ Pieces rotate(const AppendProblem &p, const Pieces &x, const Angles &a, Where at)
 {
-    if (pair >= p.rot / 16) return x;
     typedef T vec16 __attribute__((ext_vector_type(16)));
     const vec16 e = __builtin_bit_cast(vec16, x);
-    vec16 y;
+    vec16 y = e;
     if (p.interleaved) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
+            if ((i < 4 ? at.first : at.second) >= p.rot) continue;  // copied
             const float c = a.c[i >> 2][i & 3], s = a.s[i >> 2][i & 3], u = (float)e[2 * i], v = (float)e[2 * i + 1];
             y[2 * i] = (T)(u * c - v * s);
             y[2 * i + 1] = (T)(v * c + u * s);
         }
-    } else {
+    } else if (at.second < p.rot) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const float c = a.c[i >> 2][i & 3], s = a.s[i >> 2][i & 3], u = (float)e[i], v = (float)e[i + 8];
@@ -127,11 +131,11 @@ __global__ void __launch_bounds__(256) append_token_kernel(const AppendProblem p
     if (threadIdx.x >= kHeads * kPairs || h >= p.heads + 2 * p.kv_heads) return;
     const int pos = clamped(p.lengths[b]) - 1;
     const int64_t slot = slot_of(p, b, pos);
-    const Where at = where(p, pair);
+    const Where at = where(p, D, pair);
     if (h < p.heads) {
         Pieces x{};
         if (slot >= 0)
-            x = rotate<T>(p, load_pieces((const T *)p.q + b * p.q_row + h * p.q_head, at), load_angles(p, pos, pair), pair);
+            x = rotate<T>(p, load_pieces((const T *)p.q + b * p.q_row + h * p.q_head, at), load_angles(p, at, pos), at);
         store_pieces((T *)p.q_out + ((int64_t)b * p.heads + h) * D, at, x);
         return;
     }
@@ -142,7 +146,7 @@ __global__ void __launch_bounds__(256) append_token_kernel(const AppendProblem p
         store_pieces((T *)p.v_cache + to, at, load_pieces((const T *)p.v + b * p.v_row + kh * p.v_head, at));
         return;
     }
-    Pieces x = rotate<T>(p, load_pieces((const T *)p.k + b * p.k_row + kh * p.k_head, at), load_angles(p, pos, pair), pair);
+    Pieces x = rotate<T>(p, load_pieces((const T *)p.k + b * p.k_row + kh * p.k_head, at), load_angles(p, at, pos), at);
     store_pieces((T *)p.k_cache + to, at, x);
     if (p.bounds) {
         T *lo = (T *)p.bounds + ((slot >> p.page_shift) + kh) * 2 * D, *hi = lo + D;
@@ -217,7 +221,7 @@ __global__ void __launch_bounds__(256) append_prompt_kernel(const AppendProblem 
     const T *src = (const T *)(kind == 0 ? p.q : kind == 1 ? p.k : p.v);
     const int64_t row = kind == 0 ? p.q_row : kind == 1 ? p.k_row : p.v_row;
     const int64_t head = kind == 0 ? p.q_head : kind == 1 ? p.k_head : p.v_head;
-    const Where at = where(p, pair);
+    const Where at = where(p, D, pair);
     const bool keep = kind == 1 && p.bounds;
 
     uint32_t lo[kSlab][8], hi[kSlab][8];
@@ -234,13 +238,13 @@ __global__ void __launch_bounds__(256) append_prompt_kernel(const AppendProblem 
             const int64_t t = from + (pos - start);
             const int64_t to = slot_of(p, b, pos);
             Angles a{};
-            if (kind < 2 && to >= 0) a = load_angles(p, pos, pair);
+            if (kind < 2 && to >= 0) a = load_angles(p, at, pos);
 #pragma unroll
             for (int j = 0; j < kSlab; ++j) {
                 if (j >= nh) break;
                 Pieces x{};
                 if (to >= 0) x = load_pieces(src + t * row + (h0 + j) * head, at);
-                if (kind < 2 && to >= 0) x = rotate<T>(p, x, a, pair);
+                if (kind < 2 && to >= 0) x = rotate<T>(p, x, a, at);
                 if (kind == 0) {
                     store_pieces((T *)p.q_out + (t * p.heads + h0 + j) * D, at, x);
                 } else if (to >= 0) {
@@ -282,7 +286,7 @@ __global__ void __launch_bounds__(256) append_prompt_kernel(const AppendProblem 
     if (threadIdx.x < kPairs * kSlab) {
         const int j = threadIdx.x / kPairs, pr = threadIdx.x % kPairs;
         if (j >= nh) return;
-        const Where w = where(p, pr);
+        const Where w = where(p, D, pr);
         Pieces x, z;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
