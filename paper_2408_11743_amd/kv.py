@@ -63,13 +63,19 @@ def _need(ok: bool, func: str, what: str) -> None:
         raise ValueError("%s: %s" % (func, what))
 
 
-def _rows(func: str, name: str, x: torch.Tensor, dtype) -> torch.Tensor:
+# A decode step waits for the host between these small launches, so every call
+# first asks, in one expression of the cheapest questions, whether its arguments
+# are as they nearly always are; the checks below, which name what is wrong
+# (or copy a view that the kernels cannot read), run only if not.  Single token, 32 + 16
+# heads: 11.4 us a call with the checks alone.
+
+def _rows(func: str, name: str, x: torch.Tensor, dtype, device) -> torch.Tensor:
     """x [rows, heads, head dim] as the kernels read it: channels contiguous, rows
     and heads at multiples of 16 bytes (any other view is copied)."""
     if x.dtype != dtype or not x.is_cuda:
         raise TypeError("%s: %s must be a device tensor of the cache's dtype" % (func, name))
-    if x.dim() != 3:
-        raise ValueError("%s: %s must be [tokens, heads, head_dim]" % (func, name))
+    _need(x.dim() == 3, func, "%s must be [tokens, heads, head_dim]" % name)
+    _need(x.device == device, func, "all tensors must be on one device")
     if x.is_neg():
         x = x.resolve_neg()
     s = x.stride()
@@ -80,30 +86,40 @@ def _rows(func: str, name: str, x: torch.Tensor, dtype) -> torch.Tensor:
     return x
 
 
-def _caches(func: str, k_cache: torch.Tensor, v_cache: torch.Tensor) -> tuple:
-    dtype = k_cache.dtype
-    if dtype not in _DTYPE or v_cache.dtype != dtype or not k_cache.is_cuda:
+def _check_caches(func: str, k_cache: torch.Tensor, v_cache: torch.Tensor) -> None:
+    if k_cache.dtype not in _DTYPE or v_cache.dtype != k_cache.dtype or not k_cache.is_cuda:
         raise TypeError("%s: the caches must be float16 or bfloat16 device tensors of one dtype" % func)
-    shape = k_cache.shape
-    if len(shape) != 4 or v_cache.shape != shape or not k_cache.is_contiguous() or not v_cache.is_contiguous():
-        raise ValueError("%s: the caches must be contiguous [pages, kv_heads, page_size, head_dim]" % func)
-    if k_cache.is_neg() or v_cache.is_neg():
-        raise ValueError("%s: the caches must not be lazily negated views" % func)
-    return shape
+    _need(k_cache.dim() == 4 and v_cache.shape == k_cache.shape and k_cache.is_contiguous() and v_cache.is_contiguous(),
+          func, "the caches must be contiguous [pages, kv_heads, page_size, head_dim]")
+    _need(v_cache.device == k_cache.device, func, "all tensors must be on one device")
+    _need(not (k_cache.is_neg() or v_cache.is_neg()), func, "the caches must not be lazily negated views")
 
 
-def _ints(func: str, name: str, x: torch.Tensor, dims: int) -> None:
+def _check_ints(func: str, name: str, x: torch.Tensor, dims: int, device) -> None:
     if x.dtype != torch.int32 or not x.is_cuda:
         raise TypeError("%s: %s must be an int32 device tensor" % (func, name))
-    if x.dim() != dims or (x.stride(-1) != 1 and x.shape[-1] > 1):
-        raise ValueError("%s: %s must have %d dimensions, the last one contiguous" % (func, name, dims))
+    _need(x.dim() == dims and (x.stride(-1) == 1 or x.shape[-1] <= 1), func,
+          "%s must have %d dimensions, the last one contiguous" % (name, dims))
+    _need(x.device == device, func, "all tensors must be on one device")
 
 
-def _workspace(index: int, device, stream: int, workspace, nbytes: int):
+def _check_out(func: str, out: torch.Tensor, shape, dtype, device) -> None:
+    _need(out.shape == shape and out.dtype == dtype and out.device == device and out.is_contiguous()
+          and not out.is_neg(), func, "out must be a contiguous tensor of q's shape, dtype and device")
+
+
+_i32 = torch.int32
+
+
+_empty_like, _contiguous = torch.empty_like, torch.contiguous_format
+
+
+def _workspace(index: int, stream: int, workspace, nbytes: int) -> torch.Tensor:
+    """The caller's workspace, or the one ``ops.gemm`` uses on this device and stream, of nbytes at least."""
     if workspace is None:
         workspace = ops._default_ws.get((index, stream))
         if workspace is None:
-            workspace = ops._default_ws.setdefault((index, stream), ops.Workspace(device))
+            workspace = ops._default_ws.setdefault((index, stream), ops.Workspace("cuda:%d" % index))
     buf = workspace.buf
     return buf if buf.numel() >= nbytes else workspace.ensure(nbytes)
 
@@ -122,48 +138,60 @@ def kv_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_cache: torch.
     [positions, rot] (``rotation_table``) rotates the first rot channels, in
     halves or ``interleaved`` pairs; None rotates nothing.  ``bounds``: the pages' bounds,
     kept up to date."""
-    f = "kv_append"
-    pages, kv_heads, page_size, D = _caches(f, k_cache, v_cache)
-    dtype, device = k_cache.dtype, k_cache.device
-    q, k, v = _rows(f, "q", q, dtype), _rows(f, "k", k, dtype), _rows(f, "v", v, dtype)
-    _ints(f, "table", table, 2)
-    _ints(f, "lengths", lengths, 1)
-    n, width = table.shape
-    tokens, heads = q.shape[0], q.shape[1]
-    _need(q.shape[2] == D and k.shape == (tokens, kv_heads, D) and v.shape == k.shape, f,
-          "q, k and v must be [tokens, heads or kv_heads, %d]" % D)
-    _need(lengths.shape[0] == n, f, "lengths must have one entry per row of table")
-    _need(q.device == device and k.device == device and v.device == device and table.device == device
-          and lengths.device == device and v_cache.device == device, f, "all tensors must be on one device")
+    dtype, dev = k_cache.dtype, k_cache.get_device()
+    qs, ks, vs, cs, ts = q.shape, k.shape, v.shape, k_cache.shape, table.shape
+    qt, kt, vt, tt = q.stride(), k.stride(), v.stride(), table.stride()
+    qp, kp, vp = q.data_ptr(), k.data_ptr(), v.data_ptr()
+    if not (dtype in _DTYPE and v_cache.dtype is dtype and q.dtype is dtype and k.dtype is dtype and v.dtype is dtype
+            and table.dtype is _i32 and lengths.dtype is _i32 and dev >= 0 and v_cache.get_device() == dev
+            and q.get_device() == dev and k.get_device() == dev and v.get_device() == dev
+            and table.get_device() == dev and lengths.get_device() == dev
+            and len(cs) == 4 and v_cache.shape == cs and k_cache.is_contiguous() and v_cache.is_contiguous()
+            and len(qs) == 3 and len(ks) == 3 and ks == vs and qs[0] == ks[0] and qs[2] == ks[2] == cs[3]
+            and ks[1] == cs[1] and len(ts) == 2 and lengths.shape == ts[:1] and tt[1] == 1 and lengths.is_contiguous()
+            and qt[2] == kt[2] == vt[2] == 1 and not (qt[0] | qt[1] | kt[0] | kt[1] | vt[0] | vt[1]) & 7
+            and not (qp | kp | vp) & 15 and not (q.is_neg() or k.is_neg() or v.is_neg())
+            and not (k_cache.is_neg() or v_cache.is_neg())):
+        f, device = "kv_append", k_cache.device
+        _check_caches(f, k_cache, v_cache)
+        q, k, v = (_rows(f, n, x, dtype, device) for n, x in (("q", q), ("k", k), ("v", v)))
+        _check_ints(f, "table", table, 2, device)
+        _check_ints(f, "lengths", lengths, 1, device)
+        qs, ks, vs = q.shape, k.shape, v.shape
+        _need(qs[2] == cs[3] and ks == (qs[0], cs[1], cs[3]) and vs == ks, f,
+              "q, k and v must be [tokens, heads or kv_heads, %d]" % cs[3])
+        _need(lengths.shape[0] == ts[0], f, "lengths must have one entry per row of table")
+        qt, kt, vt = q.stride(), k.stride(), v.stride()
+        qp, kp, vp = q.data_ptr(), k.data_ptr(), v.data_ptr()
+    pages, kv_heads, page_size, D = cs
+    tokens, heads, _ = qs
+    n, width = ts
     if starts is not None:
-        _ints(f, "starts", starts, 1)
-        _need(starts.shape[0] == n + 1 and starts.device == device, f,
-              "starts must have one entry more than table has rows, on its device")
-    else:
-        _need(tokens == n, f, "without starts there is one token per row of table")
-    rot = positions = 0
+        _check_ints("kv_append", "starts", starts, 1, k_cache.device)
+        _need(starts.shape[0] == n + 1, "kv_append", "starts must have one entry more than table has rows")
+    elif tokens != n:
+        raise ValueError("kv_append: without starts there is one token per row of table")
+    positions = rot = 0
     if cos_sin is not None:
-        if cos_sin.dtype != torch.float32:
+        if cos_sin.dtype is not torch.float32:
             raise TypeError("kv_append: cos_sin must be float32")
-        _need(cos_sin.dim() == 2 and cos_sin.is_contiguous() and cos_sin.device == device and not cos_sin.is_neg(), f,
-              "cos_sin must be a contiguous [positions, rot] tensor on the cache's device")
-        positions, rot = cos_sin.shape
+        shape = cos_sin.shape
+        _need(len(shape) == 2 and cos_sin.is_contiguous() and cos_sin.get_device() == dev and not cos_sin.is_neg(),
+              "kv_append", "cos_sin must be a contiguous [positions, rot] tensor on the cache's device")
+        positions, rot = shape
     if bounds is not None:
-        _need(bounds.dtype == dtype and bounds.shape == (pages, kv_heads, 2, D) and bounds.is_contiguous()
-              and bounds.device == device and not bounds.is_neg(), f,
+        _need(bounds.dtype is dtype and bounds.shape == (pages, kv_heads, 2, D) and bounds.is_contiguous()
+              and bounds.get_device() == dev and not bounds.is_neg(), "kv_append",
               "bounds must be a contiguous [pages, kv_heads, 2, head_dim] tensor of the cache's dtype and device")
     if out is None:
-        out = torch.empty((tokens, heads, D), dtype=dtype, device=device)
+        out = _empty_like(q, memory_format=_contiguous)
     else:
-        _need(out.shape == (tokens, heads, D) and out.dtype == dtype and out.device == device and out.is_contiguous()
-              and not out.is_neg(), f, "out must be a contiguous tensor of q's shape, dtype and device")
-    qs, ks, vs = q.stride(), k.stride(), v.stride()
+        _check_out("kv_append", out, (tokens, heads, D), dtype, k_cache.device)
     status = B.lib().marlin_kv_append(B.pack_kv_append(
-        q.data_ptr(), k.data_ptr(), v.data_ptr(), qs[0], qs[1], ks[0], ks[1], vs[0], vs[1], out.data_ptr(),
-        k_cache.data_ptr(), v_cache.data_ptr(), 0 if bounds is None else bounds.data_ptr(),
-        0 if rot == 0 else cos_sin.data_ptr(), positions, rot, 1 if interleaved else 0, table.data_ptr(),
-        table.stride(0), lengths.data_ptr(), 0 if starts is None else starts.data_ptr(), tokens, n, heads, kv_heads, D,
-        pages, page_size, width, _DTYPE[dtype]), _raw_stream(device.index))
+        qp, kp, vp, qt[0], qt[1], kt[0], kt[1], vt[0], vt[1], out.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(),
+        0 if bounds is None else bounds.data_ptr(), cos_sin.data_ptr() if rot else 0, positions, rot,
+        1 if interleaved else 0, table.data_ptr(), tt[0], lengths.data_ptr(), 0 if starts is None else starts.data_ptr(),
+        tokens, n, heads, kv_heads, D, pages, page_size, width, _DTYPE[dtype]), _raw_stream(dev))
     if status:
         raise B.MarlinError("marlin_kv_append", status)
     return out
@@ -179,34 +207,46 @@ def paged_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tenso
     ``table`` [sequences, width], or [sequences, kv heads, width] where each kv
     head has pages of its own (``select_pages``); ``scale`` defaults to
     1 / sqrt(head dim).  A sequence without tokens gives 0 and -inf."""
-    f = "paged_attention"
-    pages, kv_heads, page_size, D = _caches(f, k_cache, v_cache)
-    dtype, device = k_cache.dtype, k_cache.device
-    q = _rows(f, "q", q, dtype)
-    per_head = table.dim() == 3
-    _ints(f, "table", table, 3 if per_head else 2)
-    _ints(f, "lengths", lengths, 1)
-    n, heads, d = q.shape
-    _need(d == D, f, "q must be [sequences, heads, %d]" % D)
-    _need(table.shape[0] == n and lengths.shape[0] == n and (not per_head or table.shape[1] == kv_heads), f,
-          "table must be [sequences, width] or [sequences, kv_heads, width] and lengths [sequences]")
-    _need(q.device == device and v_cache.device == device and table.device == device and lengths.device == device, f,
-          "all tensors must be on one device")
+    dtype, dev = k_cache.dtype, k_cache.get_device()
+    qs, cs, ts = q.shape, k_cache.shape, table.shape
+    qt, tt, qp = q.stride(), table.stride(), q.data_ptr()
+    per_head = len(ts) == 3
+    if not (dtype in _DTYPE and v_cache.dtype is dtype and q.dtype is dtype and table.dtype is _i32
+            and lengths.dtype is _i32 and dev >= 0 and v_cache.get_device() == dev and q.get_device() == dev
+            and table.get_device() == dev and lengths.get_device() == dev
+            and len(cs) == 4 and v_cache.shape == cs and k_cache.is_contiguous() and v_cache.is_contiguous()
+            and len(qs) == 3 and qs[2] == cs[3] and (per_head or len(ts) == 2) and qs[0] == ts[0]
+            and lengths.shape == ts[:1] and (not per_head or ts[1] == cs[1]) and tt[-1] == 1 and lengths.is_contiguous()
+            and qt[2] == 1 and not (qt[0] | qt[1]) & 7 and not qp & 15 and not q.is_neg()
+            and not (k_cache.is_neg() or v_cache.is_neg())):
+        f, device = "paged_attention", k_cache.device
+        _check_caches(f, k_cache, v_cache)
+        q = _rows(f, "q", q, dtype, device)
+        _check_ints(f, "table", table, 3 if per_head else 2, device)
+        _check_ints(f, "lengths", lengths, 1, device)
+        qs = q.shape
+        _need(qs[2] == cs[3], f, "q must be [sequences, heads, %d]" % cs[3])
+        _need(ts[0] == qs[0] and lengths.shape[0] == qs[0] and (not per_head or ts[1] == cs[1]), f,
+              "table must be [sequences, width] or [sequences, kv_heads, width] and lengths [sequences]")
+        qt, qp = q.stride(), q.data_ptr()
+    pages, kv_heads, page_size, D = cs
+    n, heads, _ = qs
     if out is None:
-        out = torch.empty((n, heads, D), dtype=dtype, device=device)
+        out = _empty_like(q, memory_format=_contiguous)
     else:
-        _need(out.shape == (n, heads, D) and out.dtype == dtype and out.device == device and out.is_contiguous()
-              and not out.is_neg(), f, "out must be a contiguous tensor of q's shape, dtype and device")
-    lse = torch.empty((n, heads), dtype=torch.float32, device=device) if return_lse else None
-    index = device.index
-    stream = _raw_stream(index)
-    buf = _workspace(index, device, stream, workspace, B.marlin_paged_attention_workspace_bytes(D))
-    qs, ts = q.stride(), table.stride()
-    status = B.lib().marlin_paged_attention(B.pack_paged_attention(
-        q.data_ptr(), qs[0], qs[1], k_cache.data_ptr(), v_cache.data_ptr(), table.data_ptr(), ts[0],
-        ts[1] if per_head else 0, lengths.data_ptr(), out.data_ptr(), 0 if lse is None else lse.data_ptr(),
-        buf.data_ptr(), buf.numel(), n, heads, kv_heads, D, pages, page_size, table.shape[-1],
-        1.0 / math.sqrt(D) if scale is None else scale, _DTYPE[dtype]), stream)
+        _check_out("paged_attention", out, (n, heads, D), dtype, k_cache.device)
+    lse = torch.empty((n, heads), dtype=torch.float32, device=k_cache.device) if return_lse else None
+    stream = _raw_stream(dev)
+    buf = _workspace(dev, stream, workspace, 0)
+    ptrs = (qp, qt[0], qt[1], k_cache.data_ptr(), v_cache.data_ptr(), table.data_ptr(), tt[0],
+            tt[1] if per_head else 0, lengths.data_ptr(), out.data_ptr(), 0 if lse is None else lse.data_ptr())
+    sizes = (n, heads, kv_heads, D, pages, page_size, ts[-1], 1.0 / math.sqrt(D) if scale is None else scale,
+             _DTYPE[dtype])
+    status = B.lib().marlin_paged_attention(B.pack_paged_attention(*ptrs, buf.data_ptr(), buf.numel(), *sizes), stream)
+    if status == 5:  # WORKSPACE_TOO_SMALL: nothing was enqueued
+        buf = _workspace(dev, stream, workspace, B.marlin_paged_attention_workspace_bytes(D))
+        status = B.lib().marlin_paged_attention(B.pack_paged_attention(*ptrs, buf.data_ptr(), buf.numel(), *sizes),
+                                                stream)
     if status:
         raise B.MarlinError("marlin_paged_attention", status)
     return (out, lse) if return_lse else out
@@ -218,34 +258,42 @@ def select_pages(q: torch.Tensor, bounds: torch.Tensor, table: torch.Tensor, len
     the keys nearest the queries, the last page always among them
     (``marlin_select_pages``): (pages int32 [sequences, kv heads, select] in the
     order of their positions, tokens int32 [sequences]) for ``paged_attention``."""
-    f = "select_pages"
-    dtype, device = bounds.dtype, bounds.device
-    if dtype not in _DTYPE or not bounds.is_cuda:
-        raise TypeError("select_pages: bounds must be a float16 or bfloat16 device tensor")
-    _need(bounds.dim() == 4 and bounds.shape[2] == 2 and bounds.is_contiguous() and not bounds.is_neg(), f,
-          "bounds must be a contiguous [pages, kv_heads, 2, head_dim] tensor")
-    pages, kv_heads, _, D = bounds.shape
-    q = _rows(f, "q", q, dtype)
-    _ints(f, "table", table, 2)
-    _ints(f, "lengths", lengths, 1)
-    n, heads, d = q.shape
-    _need(d == D, f, "q must be [sequences, heads, %d]" % D)
-    _need(table.shape[0] == n and lengths.shape[0] == n, f, "table and lengths must have one row per sequence")
-    _need(q.device == device and table.device == device and lengths.device == device, f,
-          "all tensors must be on one device")
+    dtype, dev = bounds.dtype, bounds.get_device()
+    qs, bs, ts = q.shape, bounds.shape, table.shape
+    qt, tt, qp = q.stride(), table.stride(), q.data_ptr()
+    if not (dtype in _DTYPE and q.dtype is dtype and table.dtype is _i32 and lengths.dtype is _i32 and dev >= 0
+            and q.get_device() == dev and table.get_device() == dev and lengths.get_device() == dev
+            and len(bs) == 4 and bs[2] == 2 and bounds.is_contiguous() and len(qs) == 3 and qs[2] == bs[3]
+            and len(ts) == 2 and qs[0] == ts[0] and lengths.shape == ts[:1] and tt[1] == 1 and lengths.is_contiguous()
+            and qt[2] == 1 and not (qt[0] | qt[1]) & 7 and not qp & 15 and not (q.is_neg() or bounds.is_neg())):
+        f, device = "select_pages", bounds.device
+        if dtype not in _DTYPE or not bounds.is_cuda:
+            raise TypeError("select_pages: bounds must be a float16 or bfloat16 device tensor")
+        _need(len(bs) == 4 and bs[2] == 2 and bounds.is_contiguous() and not bounds.is_neg(), f,
+              "bounds must be a contiguous [pages, kv_heads, 2, head_dim] tensor")
+        q = _rows(f, "q", q, dtype, device)
+        _check_ints(f, "table", table, 2, device)
+        _check_ints(f, "lengths", lengths, 1, device)
+        qs = q.shape
+        _need(qs[2] == bs[3], f, "q must be [sequences, heads, %d]" % bs[3])
+        _need(ts[0] == qs[0] and lengths.shape[0] == qs[0], f, "table and lengths must have one row per sequence")
+        qt, qp = q.stride(), q.data_ptr()
+    pages, kv_heads, _, D = bs
+    n, heads, _ = qs
+    width = ts[1]
     if not 1 <= select <= 1 << 20:
         raise B.MarlinError("marlin_select_pages", 8)
-    chosen = torch.empty((n, kv_heads, select), dtype=torch.int32, device=device)
-    tokens = torch.empty(n, dtype=torch.int32, device=device)
-    index = device.index
-    stream = _raw_stream(index)
-    width = table.shape[1]
-    buf = _workspace(index, device, stream, workspace, B.marlin_select_pages_workspace_bytes(n, kv_heads, width))
-    qs = q.stride()
-    status = B.lib().marlin_select_pages(B.pack_select_pages(
-        q.data_ptr(), qs[0], qs[1], bounds.data_ptr(), table.data_ptr(), table.stride(0), lengths.data_ptr(),
-        chosen.data_ptr(), tokens.data_ptr(), buf.data_ptr(), buf.numel(), n, heads, kv_heads, D, pages, page_size,
-        width, select, _DTYPE[dtype]), stream)
+    chosen = torch.empty((n, kv_heads, select), dtype=_i32, device=table.device)
+    tokens = torch.empty_like(lengths, memory_format=_contiguous)
+    stream = _raw_stream(dev)
+    buf = _workspace(dev, stream, workspace, 0)
+    args = (qp, qt[0], qt[1], bounds.data_ptr(), table.data_ptr(), tt[0], lengths.data_ptr(), chosen.data_ptr(),
+            tokens.data_ptr())
+    sizes = (n, heads, kv_heads, D, pages, page_size, width, select, _DTYPE[dtype])
+    status = B.lib().marlin_select_pages(B.pack_select_pages(*args, buf.data_ptr(), buf.numel(), *sizes), stream)
+    if status == 5:  # WORKSPACE_TOO_SMALL: nothing was enqueued
+        buf = _workspace(dev, stream, workspace, B.marlin_select_pages_workspace_bytes(n, kv_heads, width))
+        status = B.lib().marlin_select_pages(B.pack_select_pages(*args, buf.data_ptr(), buf.numel(), *sizes), stream)
     if status:
         raise B.MarlinError("marlin_select_pages", status)
     return chosen, tokens
