@@ -177,37 +177,54 @@ __global__ void __launch_bounds__(256) append_prompt_kernel(const AppendProblem 
     constexpr int kPairs = D / 16;
     constexpr int kTokens = D == 64 ? 16 : D == 256 ? 4 : 8;  // of a wave at a time
     __shared__ uint32_t lds[4][kPairs][kSlab][16];
+    __shared__ int lds_chunks[kKvMaxBatch / 64];
 
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int pair = lane % kPairs, slot = lane / kPairs;
 
-    // the page: sequence b's blockIdx.x - before
-    int b = -1, first = 0, from = 0, n = 0, len = 0, before = 0;
-    for (int b0 = 0; b0 < p.B; b0 += 64) {
-        int pages = 0, begin = 0, count = 0, total = 0;
-        if (b0 + lane < p.B) {
-            begin = p.starts[b0 + lane];
-            int end = p.starts[b0 + lane + 1];
+    // the page: the blockIdx.x-th that the sequences touch, found among the sums of 64 sequences' pages, then among theirs
+    const int chunks = (p.B + 63) / 64;
+    int begin = 0, count = 0, total = 0, pages = 0, incl = 0;  // of the lane's sequence: tokens, length, pages, pages up to it
+    auto hold = [&](int chunk) {
+        const int b = chunk * 64 + lane;
+        begin = count = total = pages = 0;
+        if (b < p.B) {
+            begin = p.starts[b];
+            int end = p.starts[b + 1];
             begin = begin < 0 ? 0 : begin < p.tokens ? begin : p.tokens;
             end = end < begin ? begin : end < p.tokens ? end : p.tokens;
             count = end - begin;
-            total = clamped(p.lengths[b0 + lane]);
+            total = clamped(p.lengths[b]);
             pages = count > 0 ? ((total - 1) >> p.page_shift) - ((total - count) >> p.page_shift) + 1 : 0;
         }
-        const int incl = before + wave_scan(pages);
-        const uint64_t past = __ballot(incl > (int)blockIdx.x);
-        if (past) {
-            const int at = __builtin_ctzll(past);
-            b = b0 + at;
-            from = __shfl(begin, at);
-            n = __shfl(count, at);
-            len = __shfl(total, at);
-            first = (int)blockIdx.x - (__shfl(incl, at) - __shfl(pages, at));
-            break;
+        incl = wave_scan(pages);
+    };
+    int chunk = 0, before = 0;
+    const int mine = blockIdx.x;
+    if (chunks == 1) {
+        hold(0);
+    } else {
+        for (int c = wave; c < chunks; c += 4) {
+            hold(c);
+            if (lane == 63) lds_chunks[c] = incl;
         }
-        before = __shfl(incl, 63);
+        __syncthreads();
+        chunk = -1;
+        for (int c0 = 0; c0 < chunks && chunk < 0; c0 += 64) {
+            const int c = c0 + lane < chunks ? lds_chunks[c0 + lane] : 0, i = wave_scan(c);
+            const uint64_t past = __builtin_amdgcn_ballot_w64(before + i > mine);
+            const int at = past ? __builtin_ctzll(past) : 63;
+            if (past) chunk = c0 + at;
+            before += __shfl(i, at) - (past ? __shfl(c, at) : 0);
+        }
+        if (chunk < 0) return;
+        hold(chunk);
     }
-    if (b < 0) return;
+    const uint64_t past = __builtin_amdgcn_ballot_w64(before + incl > mine);
+    if (!past) return;
+    const int lane_of = __builtin_ctzll(past), b = chunk * 64 + lane_of;
+    const int from = __shfl(begin, lane_of), n = __shfl(count, lane_of), len = __shfl(total, lane_of);
+    const int first = mine - before - (__shfl(incl, lane_of) - __shfl(pages, lane_of));  // of the sequence's touched pages
     const int start = len - n;  // position of the first new token; below 0 where there are more than the length says
     const int page0 = ((start >> p.page_shift) + first) * (1 << p.page_shift);
     const int lo_pos = page0 > start ? page0 : start;

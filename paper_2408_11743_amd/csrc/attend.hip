@@ -92,24 +92,36 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
     __shared__ float4_t lds_acc[NW + 1][kAcc][64];
     __shared__ float lds_m[NW + 1][kHeadTile], lds_l[NW + 1][kHeadTile];
     __shared__ int lds_within[NW], lds_flags[2], lds_first[2], lds_last[2];
+    __shared__ int lds_chunks[kKvMaxBatch / 64];
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int r = lane & 15, g = lane >> 4;
     const int rows = p.kv_heads * p.head_tiles;  // of a sequence
 
     // ---- this work-group's range of steps, and this wave's share of it ----
-    // Everything until the first loads of keys is latency: no divisions, and the first 64 sequences' lengths stay in
-    // the lanes.
-    int length0 = 0, count0 = 0, incl0 = 0, total = 0;  // tokens, steps, and steps up to and with the lane's sequence
-    for (int b0 = 0; b0 < p.B; b0 += 64) {
-        const int n = b0 + lane < p.B ? cap_tokens(p, p.lengths[b0 + lane]) : 0;
-        const int c = b0 + lane < p.B ? steps_of(n) : 0, i = wave_scan(c);
-        if (b0 == 0) {
-            length0 = n;
-            count0 = c;
-            incl0 = i;
+    // Everything until the first loads of keys is latency: no divisions, the lengths of 64 sequences stay in the lanes,
+    // and of more only sums of 64 are kept.
+    const int chunks = (p.B + 63) / 64;
+    int held = -1, length = 0, count = 0, incl = 0;  // chunk in the lanes: tokens, steps, steps up to and with the lane's
+    auto hold = [&](int chunk) {
+        held = chunk;
+        const int b = chunk * 64 + lane;
+        length = b < p.B ? cap_tokens(p, p.lengths[b]) : 0;
+        count = b < p.B ? steps_of(length) : 0;
+        incl = wave_scan(count);
+    };
+    int total = 0;
+    if (chunks == 1) {
+        hold(0);
+        total = __builtin_amdgcn_readlane(incl, 63);
+    } else {
+        for (int chunk = wave; chunk < chunks; chunk += NW) {
+            hold(chunk);
+            if (lane == 63) lds_chunks[chunk] = incl;
         }
-        total += __builtin_amdgcn_readlane(i, 63);
+        __syncthreads();
+        for (int c0 = 0; c0 < chunks; c0 += 64)
+            total += __builtin_amdgcn_readlane(wave_scan(c0 + lane < chunks ? lds_chunks[c0 + lane] : 0), 63);
     }
     const int units = (total + kRowCost * p.B) * rows;
     // Range w starts at unit w * per + min(w, extra).
@@ -133,35 +145,39 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
         const int u = w * per + (w < extra ? w : extra);
         return u < units ? u : units;
     };
-    // the row that holds unit u of the numbering in which a row counts its steps and `cost` more, where it is one of
-    // the 64 sequences from b0 on; n, c, i as above, `before` the steps of the sequences before b0
-    auto place_among = [&](int u, int cost, int b0, int before, int n, int c, int i, Place &x) -> bool {
-        const int ends = b0 + lane < p.B ? (before + i + cost * (b0 + lane + 1)) * rows : 0;
+    // the row that holds unit u of the numbering in which a row counts its steps and `cost` more
+    auto place_of = [&](int u, int cost) -> Place {
+        int before = 0;  // steps of the sequences before the chunk
+        if (chunks > 1) {
+            int chunk = chunks;
+            for (int c0 = 0; c0 < chunks; c0 += 64) {
+                const int c = c0 + lane < chunks ? lds_chunks[c0 + lane] : 0, i = wave_scan(c);
+                const int last = (c0 + lane + 1) * 64;
+                const int ends = c0 + lane < chunks ? (before + i + cost * (last < p.B ? last : p.B)) * rows : 0;
+                const uint64_t past = __builtin_amdgcn_ballot_w64(ends > u);
+                if (past) {
+                    const int at = __builtin_ctzll(past);
+                    chunk = c0 + at;
+                    before += __builtin_amdgcn_readlane(i, at) - __builtin_amdgcn_readlane(c, at);
+                    break;
+                }
+                before += __builtin_amdgcn_readlane(i, 63);
+            }
+            if (chunk < chunks && chunk != held) hold(chunk);
+        }
+        const int b0 = held * 64;
+        const int ends = b0 + lane < p.B ? (before + incl + cost * (b0 + lane + 1)) * rows : 0;
         const uint64_t past = __builtin_amdgcn_ballot_w64(ends > u);
-        if (past == 0) return false;
+        if (u >= units - (kRowCost - cost) * p.B * rows) return {p.B, 0, 0, total * rows, 1, 0};
         const int at = __builtin_ctzll(past);
-        const int cb = __builtin_amdgcn_readlane(c, at);
+        const int cb = __builtin_amdgcn_readlane(count, at);
         const int off = u - __builtin_amdgcn_readlane(ends, at) + (cb + cost) * rows;
         // off / (cb + cost): the lanes count the rows that end by then
         const int row = rows == 1 ? 0
                         : rows <= 64 ? __popcll(__builtin_amdgcn_ballot_w64((lane + 1) * (cb + cost) <= off))
                                      : (uint32_t)off / (uint32_t)(cb + cost);
         const int step = off - row * (cb + cost) - cost;
-        x = {b0 + at, row, step < 0 ? 0 : step, u - off - cost * (b0 + at) * rows + row * cb, cb, __builtin_amdgcn_readlane(n, at)};
-        return true;
-    };
-    auto place_of = [&](int u, int cost) -> Place {
-        Place x{p.B, 0, 0, total * rows, 1, 0};
-        if (place_among(u, cost, 0, 0, length0, count0, incl0, x) || p.B <= 64) return x;
-        int before = __builtin_amdgcn_readlane(incl0, 63);
-#pragma unroll 1
-        for (int b0 = 64; b0 < p.B; b0 += 64) {
-            const int n = b0 + lane < p.B ? cap_tokens(p, p.lengths[b0 + lane]) : 0;
-            const int c = b0 + lane < p.B ? steps_of(n) : 0, i = wave_scan(c);
-            if (place_among(u, cost, b0, before, n, c, i, x)) break;
-            before += __builtin_amdgcn_readlane(i, 63);
-        }
-        return x;
+        return {b0 + at, row, step < 0 ? 0 : step, u - off - cost * (b0 + at) * rows + row * cb, cb, __builtin_amdgcn_readlane(length, at)};
     };
     auto border = [&](int w) -> Place {
         Place x = place_of(start_of(w), kRowCost);

@@ -28,7 +28,7 @@ bool dtype_ok(int64_t d) { return d == MARLIN_F16 || d == MARLIN_BF16; }
 bool shape_ok(int64_t B, int64_t heads, int64_t kv_heads, int64_t head_dim, int64_t pages, int64_t page_size,
               int64_t width)
 {
-    if (B < 0 || B > (1 << 16)) return false;
+    if (B < 0 || B > kKvMaxBatch) return false;
     if (kv_heads < 1 || heads < kv_heads || heads > 1024 || heads % kv_heads != 0) return false;
     if (head_dim != 64 && head_dim != 96 && head_dim != 128 && head_dim != 256) return false;
     if (page_size < 16 || page_size > 1024 || (page_size & (page_size - 1)) != 0) return false;
@@ -158,7 +158,7 @@ marlin_status_t marlin_paged_attention(const marlin_paged_attention_args *a, hip
 
 size_t marlin_select_pages_workspace_bytes(int64_t B, int64_t kv_heads, int64_t width)
 {
-    if (B < 0 || B > (1 << 16) || kv_heads < 1 || kv_heads > 1024 || width < 1 || !scores_ok(B, kv_heads, width)) return 0;
+    if (B < 0 || B > kKvMaxBatch || kv_heads < 1 || kv_heads > 1024 || width < 1 || !scores_ok(B, kv_heads, width)) return 0;
     return kCounterRegionBytes + (size_t)B * (size_t)kv_heads * (size_t)width * sizeof(uint32_t);
 }
 

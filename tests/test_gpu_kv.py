@@ -106,6 +106,12 @@ def test_attention_splits(mk, lengths, hq, hkv, dtype):
     check_attention(mk, *make(len(lengths), lengths, hq, hkv, 64, 16, dtype))
 
 
+@pytest.mark.parametrize("n", [64, 65, 128, 500, 4096, 4200])
+def test_attention_many_sequences(mk, n):
+    lengths = [(i * 37) % 23 if i % 50 else 200 + i % 7 for i in range(n)]
+    check_attention(mk, *make(n, lengths, 1, 1, 64, 16, BF16))
+
+
 def test_attention_long(mk):
     check_attention(mk, *make(5, [40001, 17, 9000], 2, 1, 64, 64, F16))
 
@@ -348,8 +354,9 @@ def test_append_prompts_page_sizes(mk, ps, hq, hkv):
     check_append(mk, *args, starts=starts, bounds=bounds)
 
 
-def test_append_prompts_many_sequences(mk):
-    new = [(i * 7) % 5 for i in range(150)]
+@pytest.mark.parametrize("n", [64, 65, 150, 4200])
+def test_append_prompts_many_sequences(mk, n):
+    new = [(i * 7) % 5 for i in range(n)]
     lengths = [n + (i * 11) % 40 for i, n in enumerate(new)]
     args, starts, bounds = append_inputs(3, lengths, new, 2, 1, 64, 16, BF16, 64)
     check_append(mk, *args, starts=starts, bounds=bounds)
@@ -413,6 +420,12 @@ def test_append_in_place_and_strided(mk):
     assert got.data_ptr() == q.data_ptr() and torch.equal(got, want)
     turned = [x.transpose(0, 1).contiguous().transpose(0, 1) for x in dev[:3]]
     assert torch.equal(mk.kv_append(*turned, *dev[3:], starts=starts.cuda()), want)
+
+
+def test_append_one_token_many_sequences(mk):
+    lengths = [(i * 11) % 40 for i in range(1000)]
+    args, _, bounds = append_inputs(4, lengths, [1] * 1000, 2, 1, 64, 16, F16, 64)
+    check_append(mk, *args, bounds=bounds)
 
 
 def test_append_no_tokens(mk):
