@@ -56,6 +56,21 @@ __device__ __forceinline__ Pieces load_pieces(const T *row, Where at)
     return x;
 }
 
+// The same of new tokens, of which nothing is read again: non-temporal (once) where they and what becomes of them are more than the last-level cache
+// holds, as what a projection has just written may still lie there, and where a piece's row of threads takes
+// whole lines of 128 bytes.  300 MB of prompts, heads of 128: 137 -> 128 us; 26 MB: 10.7 -> 13.8; heads of 64: 233 -> 256.
+template <typename T>
+__device__ __forceinline__ Pieces load_new(const T *row, Where at, bool once)
+{
+    if (!once) return load_pieces(row, at);
+    const u32x4_t a = __builtin_nontemporal_load((const u32x4_t *)(row + at.first));
+    const u32x4_t b = __builtin_nontemporal_load((const u32x4_t *)(row + at.second));
+    Pieces x;
+    __builtin_memcpy(x.w, &a, 16);
+    __builtin_memcpy(x.w + 4, &b, 16);
+    return x;
+}
+
 template <typename T>
 __device__ __forceinline__ void store_pieces(T *row, Where at, const Pieces &x)
 {
@@ -169,10 +184,12 @@ __global__ void __launch_bounds__(256) append_token_kernel(const AppendProblem p
 // A work-group takes the new tokens of one page of one sequence and four heads
 // of q, of k or of v, so that a page's bounds are one work-group's: its tokens'
 // smallest and largest keys are kept in registers and joined at the end.
+// Neighbouring work-groups take the heads of one page, which lie side by side in the
+// tokens' rows (143 us; neighbouring pages instead: 156), four waves per SIMD (137).
 constexpr int kSlab = 4;
 
 template <typename T, int D>
-__global__ void __launch_bounds__(256) append_prompt_kernel(const AppendProblem p)
+__global__ void __launch_bounds__(256, 4) append_prompt_kernel(const AppendProblem p, bool once)
 {
     constexpr int kPairs = D / 16;
     constexpr int kTokens = D == 64 ? 16 : D == 256 ? 4 : 8;  // of a wave at a time
@@ -200,7 +217,8 @@ __global__ void __launch_bounds__(256) append_prompt_kernel(const AppendProblem 
         incl = wave_scan(pages);
     };
     int chunk = 0, before = 0;
-    const int mine = blockIdx.x;
+    const int q_slabs = (p.heads + kSlab - 1) / kSlab, kv_slabs = (p.kv_heads + kSlab - 1) / kSlab;
+    const int mine = blockIdx.x / (q_slabs + 2 * kv_slabs), y = blockIdx.x - mine * (q_slabs + 2 * kv_slabs);
     if (chunks == 1) {
         hold(0);
     } else {
@@ -230,8 +248,6 @@ __global__ void __launch_bounds__(256) append_prompt_kernel(const AppendProblem 
     const int lo_pos = page0 > start ? page0 : start;
     const int hi_pos = page0 + (1 << p.page_shift) < len ? page0 + (1 << p.page_shift) : len;
 
-    const int q_slabs = (p.heads + kSlab - 1) / kSlab, kv_slabs = (p.kv_heads + kSlab - 1) / kSlab;
-    const int y = blockIdx.y;
     const int kind = y < q_slabs ? 0 : y < q_slabs + kv_slabs ? 1 : 2;
     const int h0 = (kind == 0 ? y : kind == 1 ? y - q_slabs : y - q_slabs - kv_slabs) * kSlab;
     const int nh = (kind == 0 ? p.heads : p.kv_heads) - h0 < kSlab ? (kind == 0 ? p.heads : p.kv_heads) - h0 : kSlab;
@@ -260,7 +276,7 @@ __global__ void __launch_bounds__(256) append_prompt_kernel(const AppendProblem 
             for (int j = 0; j < kSlab; ++j) {
                 if (j >= nh) break;
                 Pieces x{};
-                if (to >= 0) x = load_pieces(src + t * row + (h0 + j) * head, at);
+                if (to >= 0) x = load_new(src + t * row + (h0 + j) * head, at, once);
                 if (kind < 2 && to >= 0) x = rotate<T>(p, x, a, at);
                 if (kind == 0) {
                     store_pieces((T *)p.q_out + (t * p.heads + h0 + j) * D, at, x);
@@ -341,7 +357,8 @@ hipError_t launch_one(const AppendProblem &p, hipStream_t stream)
         // a sequence of n tokens touches at most n / page size + 2 pages
         const int pages = (p.tokens >> p.page_shift) + 2 * (p.B < p.tokens ? p.B : p.tokens);
         const int slabs = (p.heads + kSlab - 1) / kSlab + 2 * ((p.kv_heads + kSlab - 1) / kSlab);
-        hipLaunchKernelGGL((append_prompt_kernel<T, D>), dim3(pages, slabs), dim3(256), 0, stream, p);
+        const bool once = D % 128 == 0 && (int64_t)p.tokens * (p.heads + 2 * p.kv_heads) * D * 2 > ((int64_t)128 << 20);
+        hipLaunchKernelGGL((append_prompt_kernel<T, D>), dim3((uint32_t)pages * slabs), dim3(256), 0, stream, p, once);
     }
     return hipGetLastError();
 }
