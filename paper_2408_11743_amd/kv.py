@@ -23,6 +23,7 @@ makes the workspace).  There is no autograd formula (inference only).
 """
 from __future__ import annotations
 
+import ctypes
 import math
 
 import torch
@@ -63,11 +64,28 @@ def _need(ok: bool, func: str, what: str) -> None:
         raise ValueError("%s: %s" % (func, what))
 
 
-# A decode step waits for the host between these small launches, so every call
-# first asks, in one expression of the cheapest questions, whether its arguments
-# are as they nearly always are; the checks below, which name what is wrong
-# (or copy a view that the kernels cannot read), run only if not.  Single token, 32 + 16
-# heads: 11.4 us a call with the checks alone.
+# A decode step waits for the host between these small launches, so a call is
+# first handed to a native module (csrc/fast.cpp), which does it where the tensors are as
+# they nearly always are.  Anything else comes back as None, with nothing done,
+# to the checks below, which name what is wrong or copy a view that the kernels
+# cannot read.  A token of 32 + 16 heads appended: 11.4 us a call in Python.
+_native = None
+
+
+def _connect():
+    """The native module, connected to the library's entry points; raises if either has not been built."""
+    global _native
+    handle = B.lib()
+    try:
+        from . import _fast
+    except ImportError as e:
+        raise RuntimeError("the native call module is missing: build it with `python -m paper_2408_11743_amd.build`") from e
+    address = lambda f: ctypes.cast(f, ctypes.c_void_p).value  # noqa: E731
+    _fast.connect(address(handle.marlin_kv_append), address(handle.marlin_paged_attention),
+                  address(handle.marlin_select_pages), _raw_stream, ops._default_ws)
+    _native = _fast
+    return _fast
+
 
 def _rows(func: str, name: str, x: torch.Tensor, dtype, device) -> torch.Tensor:
     """x [rows, heads, head dim] as the kernels read it: channels contiguous, rows
@@ -108,9 +126,6 @@ def _check_out(func: str, out: torch.Tensor, shape, dtype, device) -> None:
           and not out.is_neg(), func, "out must be a contiguous tensor of q's shape, dtype and device")
 
 
-_i32 = torch.int32
-
-
 _empty_like, _contiguous = torch.empty_like, torch.contiguous_format
 
 
@@ -138,36 +153,24 @@ def kv_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_cache: torch.
     [positions, rot] (``rotation_table``) rotates the first rot channels, in
     halves or ``interleaved`` pairs; None rotates nothing.  ``bounds``: the pages' bounds,
     kept up to date."""
-    dtype, dev = k_cache.dtype, k_cache.get_device()
-    qs, ks, vs, cs, ts = q.shape, k.shape, v.shape, k_cache.shape, table.shape
-    qt, kt, vt, tt = q.stride(), k.stride(), v.stride(), table.stride()
-    qp, kp, vp = q.data_ptr(), k.data_ptr(), v.data_ptr()
-    if not (dtype in _DTYPE and v_cache.dtype is dtype and q.dtype is dtype and k.dtype is dtype and v.dtype is dtype
-            and table.dtype is _i32 and lengths.dtype is _i32 and dev >= 0 and v_cache.get_device() == dev
-            and q.get_device() == dev and k.get_device() == dev and v.get_device() == dev
-            and table.get_device() == dev and lengths.get_device() == dev
-            and len(cs) == 4 and v_cache.shape == cs and k_cache.is_contiguous() and v_cache.is_contiguous()
-            and len(qs) == 3 and len(ks) == 3 and ks == vs and qs[0] == ks[0] and qs[2] == ks[2] == cs[3]
-            and ks[1] == cs[1] and len(ts) == 2 and lengths.shape == ts[:1] and tt[1] == 1 and lengths.is_contiguous()
-            and qt[2] == kt[2] == vt[2] == 1 and not (qt[0] | qt[1] | kt[0] | kt[1] | vt[0] | vt[1]) & 7
-            and not (qp | kp | vp) & 15 and not (q.is_neg() or k.is_neg() or v.is_neg())
-            and not (k_cache.is_neg() or v_cache.is_neg())):
-        f, device = "kv_append", k_cache.device
-        _check_caches(f, k_cache, v_cache)
-        q, k, v = (_rows(f, n, x, dtype, device) for n, x in (("q", q), ("k", k), ("v", v)))
-        _check_ints(f, "table", table, 2, device)
-        _check_ints(f, "lengths", lengths, 1, device)
-        qs, ks, vs = q.shape, k.shape, v.shape
-        _need(qs[2] == cs[3] and ks == (qs[0], cs[1], cs[3]) and vs == ks, f,
-              "q, k and v must be [tokens, heads or kv_heads, %d]" % cs[3])
-        _need(lengths.shape[0] == ts[0], f, "lengths must have one entry per row of table")
-        qt, kt, vt = q.stride(), k.stride(), v.stride()
-        qp, kp, vp = q.data_ptr(), k.data_ptr(), v.data_ptr()
+    done = (_native or _connect()).kv_append(q, k, v, k_cache, v_cache, table, lengths, cos_sin, starts, interleaved,
+                                             bounds, out)
+    if done is not None:
+        return done
+    f, dtype, device = "kv_append", k_cache.dtype, k_cache.device
+    _check_caches(f, k_cache, v_cache)
+    q, k, v = (_rows(f, name, x, dtype, device) for name, x in (("q", q), ("k", k), ("v", v)))
+    _check_ints(f, "table", table, 2, device)
+    _check_ints(f, "lengths", lengths, 1, device)
+    dev, qs, cs, ts = device.index, q.shape, k_cache.shape, table.shape
+    _need(qs[2] == cs[3] and k.shape == (qs[0], cs[1], cs[3]) and v.shape == k.shape, f,
+          "q, k and v must be [tokens, heads or kv_heads, %d]" % cs[3])
+    _need(lengths.shape[0] == ts[0], f, "lengths must have one entry per row of table")
     pages, kv_heads, page_size, D = cs
     tokens, heads, _ = qs
     n, width = ts
     if starts is not None:
-        _check_ints("kv_append", "starts", starts, 1, k_cache.device)
+        _check_ints(f, "starts", starts, 1, device)
         _need(starts.shape[0] == n + 1, "kv_append", "starts must have one entry more than table has rows")
     elif tokens != n:
         raise ValueError("kv_append: without starts there is one token per row of table")
@@ -176,22 +179,25 @@ def kv_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_cache: torch.
         if cos_sin.dtype is not torch.float32:
             raise TypeError("kv_append: cos_sin must be float32")
         shape = cos_sin.shape
-        _need(len(shape) == 2 and cos_sin.is_contiguous() and cos_sin.get_device() == dev and not cos_sin.is_neg(),
+        _need(len(shape) == 2 and cos_sin.is_contiguous() and cos_sin.device == device and not cos_sin.is_neg(),
               "kv_append", "cos_sin must be a contiguous [positions, rot] tensor on the cache's device")
         positions, rot = shape
     if bounds is not None:
         _need(bounds.dtype is dtype and bounds.shape == (pages, kv_heads, 2, D) and bounds.is_contiguous()
-              and bounds.get_device() == dev and not bounds.is_neg(), "kv_append",
+              and bounds.device == device and not bounds.is_neg(), "kv_append",
               "bounds must be a contiguous [pages, kv_heads, 2, head_dim] tensor of the cache's dtype and device")
     if out is None:
         out = _empty_like(q, memory_format=_contiguous)
     else:
         _check_out("kv_append", out, (tokens, heads, D), dtype, k_cache.device)
-    status = B.lib().marlin_kv_append(B.pack_kv_append(
-        qp, kp, vp, qt[0], qt[1], kt[0], kt[1], vt[0], vt[1], out.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(),
-        0 if bounds is None else bounds.data_ptr(), cos_sin.data_ptr() if rot else 0, positions, rot,
-        1 if interleaved else 0, table.data_ptr(), tt[0], lengths.data_ptr(), 0 if starts is None else starts.data_ptr(),
-        tokens, n, heads, kv_heads, D, pages, page_size, width, _DTYPE[dtype]), _raw_stream(dev))
+    qt, kt, vt, tt = q.stride(), k.stride(), v.stride(), table.stride()
+    with torch.cuda.device(dev):
+        status = B.lib().marlin_kv_append(B.pack_kv_append(
+            q.data_ptr(), k.data_ptr(), v.data_ptr(), qt[0], qt[1], kt[0], kt[1], vt[0], vt[1], out.data_ptr(),
+            k_cache.data_ptr(), v_cache.data_ptr(), 0 if bounds is None else bounds.data_ptr(),
+            cos_sin.data_ptr() if rot else 0, positions, rot, 1 if interleaved else 0, table.data_ptr(), tt[0],
+            lengths.data_ptr(), 0 if starts is None else starts.data_ptr(), tokens, n, heads, kv_heads, D, pages,
+            page_size, width, _DTYPE[dtype]), _raw_stream(dev))
     if status:
         raise B.MarlinError("marlin_kv_append", status)
     return out
@@ -207,28 +213,19 @@ def paged_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tenso
     ``table`` [sequences, width], or [sequences, kv heads, width] where each kv
     head has pages of its own (``select_pages``); ``scale`` defaults to
     1 / sqrt(head dim).  A sequence without tokens gives 0 and -inf."""
-    dtype, dev = k_cache.dtype, k_cache.get_device()
-    qs, cs, ts = q.shape, k_cache.shape, table.shape
-    qt, tt, qp = q.stride(), table.stride(), q.data_ptr()
-    per_head = len(ts) == 3
-    if not (dtype in _DTYPE and v_cache.dtype is dtype and q.dtype is dtype and table.dtype is _i32
-            and lengths.dtype is _i32 and dev >= 0 and v_cache.get_device() == dev and q.get_device() == dev
-            and table.get_device() == dev and lengths.get_device() == dev
-            and len(cs) == 4 and v_cache.shape == cs and k_cache.is_contiguous() and v_cache.is_contiguous()
-            and len(qs) == 3 and qs[2] == cs[3] and (per_head or len(ts) == 2) and qs[0] == ts[0]
-            and lengths.shape == ts[:1] and (not per_head or ts[1] == cs[1]) and tt[-1] == 1 and lengths.is_contiguous()
-            and qt[2] == 1 and not (qt[0] | qt[1]) & 7 and not qp & 15 and not q.is_neg()
-            and not (k_cache.is_neg() or v_cache.is_neg())):
-        f, device = "paged_attention", k_cache.device
-        _check_caches(f, k_cache, v_cache)
-        q = _rows(f, "q", q, dtype, device)
-        _check_ints(f, "table", table, 3 if per_head else 2, device)
-        _check_ints(f, "lengths", lengths, 1, device)
-        qs = q.shape
-        _need(qs[2] == cs[3], f, "q must be [sequences, heads, %d]" % cs[3])
-        _need(ts[0] == qs[0] and lengths.shape[0] == qs[0] and (not per_head or ts[1] == cs[1]), f,
-              "table must be [sequences, width] or [sequences, kv_heads, width] and lengths [sequences]")
-        qt, qp = q.stride(), q.data_ptr()
+    done = (_native or _connect()).paged_attention(q, k_cache, v_cache, table, lengths, scale, return_lse, out, workspace)
+    if done is not None:
+        return done
+    f, dtype, device = "paged_attention", k_cache.dtype, k_cache.device
+    _check_caches(f, k_cache, v_cache)
+    q = _rows(f, "q", q, dtype, device)
+    per_head = table.dim() == 3
+    _check_ints(f, "table", table, 3 if per_head else 2, device)
+    _check_ints(f, "lengths", lengths, 1, device)
+    dev, qs, cs, ts = device.index, q.shape, k_cache.shape, table.shape
+    _need(qs[2] == cs[3], f, "q must be [sequences, heads, %d]" % cs[3])
+    _need(ts[0] == qs[0] and lengths.shape[0] == qs[0] and (not per_head or ts[1] == cs[1]), f,
+          "table must be [sequences, width] or [sequences, kv_heads, width] and lengths [sequences]")
     pages, kv_heads, page_size, D = cs
     n, heads, _ = qs
     if out is None:
@@ -237,16 +234,18 @@ def paged_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tenso
         _check_out("paged_attention", out, (n, heads, D), dtype, k_cache.device)
     lse = torch.empty((n, heads), dtype=torch.float32, device=k_cache.device) if return_lse else None
     stream = _raw_stream(dev)
-    buf = _workspace(dev, stream, workspace, 0)
-    ptrs = (qp, qt[0], qt[1], k_cache.data_ptr(), v_cache.data_ptr(), table.data_ptr(), tt[0],
+    qt, tt = q.stride(), table.stride()
+    ptrs = (q.data_ptr(), qt[0], qt[1], k_cache.data_ptr(), v_cache.data_ptr(), table.data_ptr(), tt[0],
             tt[1] if per_head else 0, lengths.data_ptr(), out.data_ptr(), 0 if lse is None else lse.data_ptr())
     sizes = (n, heads, kv_heads, D, pages, page_size, ts[-1], 1.0 / math.sqrt(D) if scale is None else scale,
              _DTYPE[dtype])
-    status = B.lib().marlin_paged_attention(B.pack_paged_attention(*ptrs, buf.data_ptr(), buf.numel(), *sizes), stream)
-    if status == 5:  # WORKSPACE_TOO_SMALL: nothing was enqueued
-        buf = _workspace(dev, stream, workspace, B.marlin_paged_attention_workspace_bytes(D))
-        status = B.lib().marlin_paged_attention(B.pack_paged_attention(*ptrs, buf.data_ptr(), buf.numel(), *sizes),
-                                                stream)
+    for nbytes in (0, B.marlin_paged_attention_workspace_bytes(D)):  # grown if the call says WORKSPACE_TOO_SMALL
+        buf = _workspace(dev, stream, workspace, nbytes)
+        with torch.cuda.device(dev):
+            status = B.lib().marlin_paged_attention(
+                B.pack_paged_attention(*ptrs, buf.data_ptr(), buf.numel(), *sizes), stream)
+        if status != 5:
+            break
     if status:
         raise B.MarlinError("marlin_paged_attention", status)
     return (out, lse) if return_lse else out
@@ -258,42 +257,38 @@ def select_pages(q: torch.Tensor, bounds: torch.Tensor, table: torch.Tensor, len
     the keys nearest the queries, the last page always among them
     (``marlin_select_pages``): (pages int32 [sequences, kv heads, select] in the
     order of their positions, tokens int32 [sequences]) for ``paged_attention``."""
-    dtype, dev = bounds.dtype, bounds.get_device()
-    qs, bs, ts = q.shape, bounds.shape, table.shape
-    qt, tt, qp = q.stride(), table.stride(), q.data_ptr()
-    if not (dtype in _DTYPE and q.dtype is dtype and table.dtype is _i32 and lengths.dtype is _i32 and dev >= 0
-            and q.get_device() == dev and table.get_device() == dev and lengths.get_device() == dev
-            and len(bs) == 4 and bs[2] == 2 and bounds.is_contiguous() and len(qs) == 3 and qs[2] == bs[3]
-            and len(ts) == 2 and qs[0] == ts[0] and lengths.shape == ts[:1] and tt[1] == 1 and lengths.is_contiguous()
-            and qt[2] == 1 and not (qt[0] | qt[1]) & 7 and not qp & 15 and not (q.is_neg() or bounds.is_neg())):
-        f, device = "select_pages", bounds.device
-        if dtype not in _DTYPE or not bounds.is_cuda:
-            raise TypeError("select_pages: bounds must be a float16 or bfloat16 device tensor")
-        _need(len(bs) == 4 and bs[2] == 2 and bounds.is_contiguous() and not bounds.is_neg(), f,
-              "bounds must be a contiguous [pages, kv_heads, 2, head_dim] tensor")
-        q = _rows(f, "q", q, dtype, device)
-        _check_ints(f, "table", table, 2, device)
-        _check_ints(f, "lengths", lengths, 1, device)
-        qs = q.shape
-        _need(qs[2] == bs[3], f, "q must be [sequences, heads, %d]" % bs[3])
-        _need(ts[0] == qs[0] and lengths.shape[0] == qs[0], f, "table and lengths must have one row per sequence")
-        qt, qp = q.stride(), q.data_ptr()
+    done = (_native or _connect()).select_pages(q, bounds, table, lengths, page_size, select, workspace)
+    if done is not None:
+        return done
+    f, dtype, device = "select_pages", bounds.dtype, bounds.device
+    if dtype not in _DTYPE or not bounds.is_cuda:
+        raise TypeError("select_pages: bounds must be a float16 or bfloat16 device tensor")
+    _need(bounds.dim() == 4 and bounds.shape[2] == 2 and bounds.is_contiguous() and not bounds.is_neg(), f,
+          "bounds must be a contiguous [pages, kv_heads, 2, head_dim] tensor")
+    q = _rows(f, "q", q, dtype, device)
+    _check_ints(f, "table", table, 2, device)
+    _check_ints(f, "lengths", lengths, 1, device)
+    dev, qs, bs, ts = device.index, q.shape, bounds.shape, table.shape
+    _need(qs[2] == bs[3], f, "q must be [sequences, heads, %d]" % bs[3])
+    _need(ts[0] == qs[0] and lengths.shape[0] == qs[0], f, "table and lengths must have one row per sequence")
     pages, kv_heads, _, D = bs
     n, heads, _ = qs
     width = ts[1]
     if not 1 <= select <= 1 << 20:
         raise B.MarlinError("marlin_select_pages", 8)
-    chosen = torch.empty((n, kv_heads, select), dtype=_i32, device=table.device)
+    chosen = torch.empty((n, kv_heads, select), dtype=torch.int32, device=table.device)
     tokens = torch.empty_like(lengths, memory_format=_contiguous)
     stream = _raw_stream(dev)
-    buf = _workspace(dev, stream, workspace, 0)
-    args = (qp, qt[0], qt[1], bounds.data_ptr(), table.data_ptr(), tt[0], lengths.data_ptr(), chosen.data_ptr(),
+    qt, tt = q.stride(), table.stride()
+    args = (q.data_ptr(), qt[0], qt[1], bounds.data_ptr(), table.data_ptr(), tt[0], lengths.data_ptr(), chosen.data_ptr(),
             tokens.data_ptr())
     sizes = (n, heads, kv_heads, D, pages, page_size, width, select, _DTYPE[dtype])
-    status = B.lib().marlin_select_pages(B.pack_select_pages(*args, buf.data_ptr(), buf.numel(), *sizes), stream)
-    if status == 5:  # WORKSPACE_TOO_SMALL: nothing was enqueued
-        buf = _workspace(dev, stream, workspace, B.marlin_select_pages_workspace_bytes(n, kv_heads, width))
-        status = B.lib().marlin_select_pages(B.pack_select_pages(*args, buf.data_ptr(), buf.numel(), *sizes), stream)
+    for nbytes in (0, B.marlin_select_pages_workspace_bytes(n, kv_heads, width)):
+        buf = _workspace(dev, stream, workspace, nbytes)
+        with torch.cuda.device(dev):
+            status = B.lib().marlin_select_pages(B.pack_select_pages(*args, buf.data_ptr(), buf.numel(), *sizes), stream)
+        if status != 5:
+            break
     if status:
         raise B.MarlinError("marlin_select_pages", status)
     return chosen, tokens
