@@ -15,6 +15,11 @@ the last dimension of its input, y = x W (no bias).  ``from_float`` takes an
 ``nn.Linear``-style fp16 weight [out_features, in_features] and quantises and
 packs it on the GPU, in one launch where it is contiguous (``ops.quantize_linear``).
 
+``kv_append``, ``paged_attention`` and ``select_pages`` of ``kv`` are registered
+the same way under ``torch.ops.marlin_mi355x`` (``kv_append`` declares the caches and
+the bounds it writes), for code that is traced or compiled; eager callers save the
+dispatch by calling ``kv``'s functions.
+
 HIP graphs: the operator enqueues kernels only, so it can be captured.  Its
 workspace is the per-(device, stream) one of ``ops.gemm``, allocated on first
 use; call the layer once eagerly on the capturing stream before capturing so
@@ -22,9 +27,11 @@ that no allocation happens inside the capture.
 """
 from __future__ import annotations
 
+from typing import Optional, Tuple
+
 import torch
 
-from . import ops
+from . import kv, ops
 
 _NS = "marlin_mi355x"
 
@@ -42,6 +49,48 @@ def _gemm_fake(A, w_packed, s_packed, K, N, group, sparse=False):
     if A.dtype != torch.float16:
         raise TypeError("marlin_mi355x::gemm: A must be float16")
     return A.new_empty((A.shape[0], N))
+
+
+@torch.library.custom_op(_NS + "::kv_append", mutates_args=("k_cache", "v_cache", "bounds"))
+def kv_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor,
+              bounds: Optional[torch.Tensor], table: torch.Tensor, lengths: torch.Tensor,
+              cos_sin: Optional[torch.Tensor] = None, starts: Optional[torch.Tensor] = None,
+              interleaved: bool = False) -> torch.Tensor:
+    return kv.kv_append(q, k, v, k_cache, v_cache, table, lengths, cos_sin, starts, interleaved, bounds)
+
+
+@kv_append.register_fake
+def _kv_append_fake(q, k, v, k_cache, v_cache, bounds, table, lengths, cos_sin=None, starts=None, interleaved=False):
+    if q.dim() != 3 or q.dtype not in (torch.float16, torch.bfloat16) or q.dtype != k_cache.dtype:
+        raise TypeError("marlin_mi355x::kv_append: q must be [tokens, heads, head_dim] of the cache's float16 or bfloat16")
+    return q.new_empty(q.shape)
+
+
+@torch.library.custom_op(_NS + "::paged_attention", mutates_args=())
+def paged_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, table: torch.Tensor,
+                    lengths: torch.Tensor, scale: Optional[float] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """(out, lse)"""
+    return kv.paged_attention(q, k_cache, v_cache, table, lengths, scale, return_lse=True)
+
+
+@paged_attention.register_fake
+def _paged_attention_fake(q, k_cache, v_cache, table, lengths, scale=None):
+    if q.dim() != 3 or q.dtype not in (torch.float16, torch.bfloat16) or q.dtype != k_cache.dtype:
+        raise TypeError("marlin_mi355x::paged_attention: q must be [sequences, heads, head_dim] of the cache's float16 or bfloat16")
+    return q.new_empty(q.shape), q.new_empty(q.shape[:2], dtype=torch.float32)
+
+
+@torch.library.custom_op(_NS + "::select_pages", mutates_args=())
+def select_pages(q: torch.Tensor, bounds: torch.Tensor, table: torch.Tensor, lengths: torch.Tensor, page_size: int,
+                 select: int) -> Tuple[torch.Tensor, torch.Tensor]:
+    return kv.select_pages(q, bounds, table, lengths, page_size, select)
+
+
+@select_pages.register_fake
+def _select_pages_fake(q, bounds, table, lengths, page_size, select):
+    if q.dim() != 3 or bounds.dim() != 4:
+        raise ValueError("marlin_mi355x::select_pages: q must be [sequences, heads, head_dim], bounds [pages, kv_heads, 2, head_dim]")
+    return (table.new_empty((q.shape[0], bounds.shape[1], select)), lengths.new_empty(lengths.shape))
 
 
 # What the check below asks of torch, bound once: looking the names up took as

@@ -549,6 +549,35 @@ def test_captured_step_follows_the_lengths(mk):
             assert torch.equal(a, b), i
 
 
+def test_registered_operators_are_the_functions(mk):
+    ns = torch.ops.marlin_mi355x
+    args, starts, bounds = append_inputs(42, [40, 17], [40, 3], 4, 2, 64, 16, F16, 64)
+    dev = [x.cuda() for x in args]
+    b1, b2 = bounds.cuda(), bounds.cuda()
+    other = [dev[3].clone(), dev[4].clone()]
+    a = mk.kv_append(*dev, starts=starts.cuda(), bounds=b1)
+    b = ns.kv_append(*dev[:3], *other, b2, *dev[5:], starts.cuda())
+    assert torch.equal(a, b) and torch.equal(dev[3], other[0]) and torch.equal(dev[4], other[1]) and torch.equal(b1, b2)
+    one = [dev[5], dev[6]]
+    x, lse = mk.paged_attention(a[[39, 42]], *other, *one, scale=0.2, return_lse=True)
+    y, lse2 = ns.paged_attention(a[[39, 42]], *other, *one, 0.2)
+    assert torch.equal(x, y) and torch.equal(lse, lse2)
+    for u, w in zip(mk.select_pages(a[[39, 42]], b1, *one, 16, 2), ns.select_pages(a[[39, 42]], b1, *one, 16, 2)):
+        assert torch.equal(u, w)
+
+
+@pytest.mark.parametrize("select", [0, 3])
+def test_example_layer(mk, select):
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "decode_layer.py")
+    spec = importlib.util.spec_from_file_location("decode_layer", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    assert example.main(["--hidden", "512", "--heads", "8", "--kv-heads", "2", "--head-dim", "64", "--sequences", "5",
+                         "--prompt", "90", "--steps", "9", "--select", str(select)])
+
+
 # ---- refusals ----
 
 def test_refusals(mk):
