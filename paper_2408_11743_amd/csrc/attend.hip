@@ -128,7 +128,7 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
     const int grid = gridDim.x, wg = blockIdx.x;
     int wgs = grid, per, extra;
     if (units < grid * kMinSteps) {
-        wgs = (uint32_t)(units + kMinSteps - 1) / (kMinSteps);
+        wgs = (uint32_t)(units + kMinSteps - 1) / kMinSteps;
         per = kMinSteps;
         extra = 0;
     } else {
@@ -174,7 +174,7 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
         const int off = u - __builtin_amdgcn_readlane(ends, at) + (cb + cost) * rows;
         // off / (cb + cost): the lanes count the rows that end by then
         const int row = rows == 1 ? 0
-                        : rows <= 64 ? __popcll(__builtin_amdgcn_ballot_w64((lane + 1) * (cb + cost) <= off))
+                        : rows <= 64 ? __popcll(__builtin_amdgcn_ballot_w64((uint32_t)(lane + 1) * (uint32_t)(cb + cost) <= (uint32_t)off))
                                      : (uint32_t)off / (uint32_t)(cb + cost);
         const int step = off - row * (cb + cost) - cost;
         return {b0 + at, row, step < 0 ? 0 : step, u - off - cost * (b0 + at) * rows + row * cb, cb, __builtin_amdgcn_readlane(length, at)};
@@ -243,8 +243,8 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
         entries(x);
         return x;
     };
-    vec8 qf[kQ], kf[2][kQ];
-    uint32_t vr[2][4][kHalves][kDw];
+    vec8 qf[kQ], kf[2][kQ] = {};
+    uint32_t vr[2][4][kHalves][kDw] = {};
     auto load_queries = [&](const Step &x) {
         const T *q = (const T *)p.q + x.b * p.q_row + (head0_of(x.row) + r) * p.q_head + 8 * g;
         const bool have = r < heads_of(x.row);
@@ -266,6 +266,7 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
     auto load_keys = [&](const Step &x) {
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
+            if (u == 1 && x.s * kStepKeys + 16 >= x.tokens) break;  // masked, whatever the registers hold
             const T *k = (const T *)p.k + tile_at(x, u);
 #pragma unroll
             for (int t = 0; t < kQ; ++t) {
@@ -277,6 +278,7 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
     auto load_values = [&](const Step &x) {
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
+            if (u == 1 && x.s * kStepKeys + 16 >= x.tokens) break;
             const T *v = (const T *)p.v + tile_at(x, u);
 #pragma unroll
             for (int i = 0; i < 4; ++i)
