@@ -441,7 +441,7 @@ size_t marlin_paged_attention_workspace_bytes(int64_t head_dim);
  * weights are rounded to the cache's type for the second product, and out
  * once at the end.  Bitwise reproducible for a given device and input.
  * Errors: NULL_POINTER, INVALID_SHAPE (also B * rows of heads * the table's
- * 32-key steps beyond 2^31), MISALIGNED, INVALID_ARGUMENT (scale, dtype),
+ * 16-key tiles beyond 2^31), MISALIGNED, INVALID_ARGUMENT (scale, dtype),
  * WORKSPACE_TOO_SMALL, HIP.
  */
 marlin_status_t marlin_paged_attention(const marlin_paged_attention_args *args, hipStream_t stream);

@@ -3,8 +3,9 @@
 //   o_h = sum_j p_hj v_j,  p_hj = exp(scale q_h . k_j) / sum_i exp(scale q_h . k_i)
 //
 // One row of work is a (sequence, kv head, tile of up to 16 query heads that
-// share it).  A wave takes 32 keys of a row at a time, and both products are MFMAs whose
-// columns are the 16 heads, so nothing passes between lanes but the maximum:
+// share it).  A wave takes a step of 32 keys of a row at a time (16 of wide heads), and
+// both products are MFMAs whose columns are the 16 heads, so nothing passes
+// between lanes but the maximum:
 //
 //   S^T [16 keys x 16 heads] = K [16 x D] Q^T: lane (r = l % 16, g = l / 16)
 //     loads 16-byte pieces of key r, and gets the scores of head r for keys
@@ -15,7 +16,7 @@
 //     channels of them (a 16-lane row reads a whole key's row) and pairs two
 //     keys' elements with v_perm, which is the whole transpose.
 //
-// The work is split evenly however ragged the lengths are: the rows' 32-key
+// The work is split evenly however ragged the lengths are: the rows'
 // steps are numbered through and every wave takes an equal range of them,
 // found from the lengths on the device.  Rows that lie within one wave's range go from
 // its registers to the output.  Pieces of rows cut between the waves of a
@@ -32,24 +33,23 @@ namespace {
 
 using namespace dev;
 
-// A work-group border does not cut a row closer to its ends than min_cut steps
+// Constants of the split, in 16-key tiles.
+// A work-group border does not cut a row closer to its ends than min_cut
 // (it moves to the end): a cut costs a round trip through the workspace.
-// min_cut is a quarter of a range's steps, so that no range grows much, between these: with 3
-// throughout, 256 sequences of 1 .. 1000 tokens take 43.7 us and not 42, with 8
+// min_cut is a quarter of a range, so that no range grows much, between these: with 6
+// throughout, 256 sequences of 1 .. 1000 tokens take 43.7 us and not 42, with 16
 // throughout, one of 2000 takes 14.7 and not 12.7.
-constexpr int kMinCut = 3, kMaxCut = 8;
-// What a row costs beyond its steps (queries, output), in steps.
-constexpr int kRowCost = 1;
-// Steps a work-group gets at least where there are few.
-constexpr int kMinSteps = 4;
+constexpr int kMinCut = 6, kMaxCut = 16;
+// What a row costs beyond its steps (queries, output).
+constexpr int kRowTiles = 2;
+// What a work-group gets at least where there is little.
+constexpr int kMinTiles = 8;
 
 __device__ __forceinline__ int cap_tokens(const AttendProblem &p, int n)
 {
     const int cap = p.width << p.page_shift;
     return n < 0 ? 0 : n < cap ? n : cap;
 }
-// A sequence without keys still has a step, in which its outputs are written.
-__device__ __forceinline__ int steps_of(int tokens) { return tokens > 0 ? (tokens + kStepKeys - 1) / kStepKeys : 1; }
 
 // Where a range begins or ends: a step of a row.
 struct Place {
@@ -60,27 +60,21 @@ struct Place {
     int tokens;  // the sequence's (-1: still to be read)
 };
 
-// Smallest w whose range's start w * q + min(w, r) is >= x, largest whose is <= x.
-__device__ __forceinline__ int first_at(int x, int q, int r)
-{
-    return x <= r * (q + 1) ? (x + q) / (q + 1) : r + (x - r * (q + 1) + q - 1) / q;
-}
-__device__ __forceinline__ int last_at(int x, int q, int r)
-{
-    return x <= r * (q + 1) ? x / (q + 1) : r + (x - r * (q + 1)) / q;
-}
-
-// A step of 32 keys: its row, and the table's entries for its two 16-key tiles.
+// A step: its row, and the table's entries for its 16-key tiles.
+template <int KT>
 struct Step {
     int b, row, tokens, s;
-    int e0, e1;
+    int e[KT];
 };
 
-template <typename T, int D, int NW>
+// KT: 16-key tiles of a step
+template <typename T, int D, int NW, int KT>
 __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendProblem p)
 {
     typedef Elem<T> E;
     typedef typename E::vec8 vec8;
+    typedef T weights_t __attribute__((ext_vector_type(4 * KT)));
+    typedef Step<KT> Step;
     constexpr int kQ = D / 32;                // 16-byte pieces of a key's row per lane
     constexpr int kHalves = D > 128 ? 2 : 1;  // pieces of a value's row per lane
     constexpr int kCh = D / 16 / kHalves;     // channels in each
@@ -97,6 +91,9 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int r = lane & 15, g = lane >> 4;
     const int rows = p.kv_heads * p.head_tiles;  // of a sequence
+    constexpr int kStepKeys = kTileKeys * KT, kRowCost = kRowTiles / KT, kMinSteps = kMinTiles / KT;
+    // a sequence without keys still has a step, in which its outputs are written
+    auto steps_of = [](int tokens) { return tokens > 0 ? (tokens + kStepKeys - 1) / kStepKeys : 1; };
 
     // ---- this work-group's range of steps, and this wave's share of it ----
     // Everything until the first loads of keys is latency: no divisions, the lengths of 64 sequences stay in the lanes,
@@ -124,14 +121,12 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
             total += __builtin_amdgcn_readlane(wave_scan(c0 + lane < chunks ? lds_chunks[c0 + lane] : 0), 63);
     }
     const int units = (total + kRowCost * p.B) * rows;
-    // Range w starts at unit w * per + min(w, extra).
+    // Range w starts at unit w * units / grid, rounded down, which puts borders between rows of one length; or, where
+    // there are few, at w * kMinSteps.
     const int grid = gridDim.x, wg = blockIdx.x;
-    int wgs = grid, per, extra;
-    if (units < grid * kMinSteps) {
-        wgs = (uint32_t)(units + kMinSteps - 1) / kMinSteps;
-        per = kMinSteps;
-        extra = 0;
-    } else {
+    const bool few = units < grid * kMinSteps;
+    int per = kMinSteps, extra = 0;
+    if (!few) {
         per = (int)__umulhi((uint32_t)units, p.grid_reciprocal);
         extra = units - per * grid;
         if (extra >= grid) {
@@ -139,11 +134,19 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
             extra -= grid;
         }
     }
-    if (wg >= wgs) return;
-    const int min_cut = per / 4 < kMinCut ? kMinCut : per / 4 < kMaxCut ? per / 4 : kMaxCut;
+    if (few && wg * kMinSteps >= units) return;
+    const int min_cut = (per / 4 * KT < kMinCut ? kMinCut : per / 4 * KT < kMaxCut ? per / 4 * KT : kMaxCut) / KT;
     auto start_of = [&](int w) {
-        const int u = w * per + (w < extra ? w : extra);
+        // w * extra / grid: exact, as both are below 2^9 and the reciprocal, rounded up, is less than 1 too large
+        const int u = w * per + (int)__umulhi((uint32_t)(w * extra), p.grid_reciprocal + 1);
         return u < units ? u : units;
+    };
+    // smallest w whose range starts at x or later; largest whose starts at x or before
+    auto first_at = [&](int x) {
+        return few ? (x + kMinSteps - 1) / kMinSteps : (int)(((double)x * grid + (units - 1)) / (double)units);
+    };
+    auto last_at = [&](int x) {
+        return few ? x / kMinSteps : (int)(((double)(x + 1) * grid - 1) / (double)units);
     };
     // the row that holds unit u of the numbering in which a row counts its steps and `cost` more
     auto place_of = [&](int u, int cost) -> Place {
@@ -225,9 +228,11 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
     auto entries = [&](Step &x) {
         const int32_t *table = table_of(x);
         const int pos = x.s * kStepKeys;
-        x.e0 = x.e1 = -1;
-        if (pos < x.tokens) x.e0 = scalar_load(table + (pos >> p.page_shift));
-        if (pos + 16 < x.tokens) x.e1 = scalar_load(table + ((pos + 16) >> p.page_shift));
+#pragma unroll
+        for (int u = 0; u < KT; ++u) {
+            x.e[u] = -1;
+            if (pos + kTileKeys * u < x.tokens) x.e[u] = scalar_load(table + ((pos + kTileKeys * u) >> p.page_shift));
+        }
     };
     auto advance = [&](Step x) -> Step {
         if (x.s + 1 < steps_of(x.tokens)) {
@@ -243,8 +248,8 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
         entries(x);
         return x;
     };
-    vec8 qf[kQ], kf[2][kQ] = {};
-    uint32_t vr[2][4][kHalves][kDw] = {};
+    vec8 qf[kQ], kf[KT][kQ] = {};
+    uint32_t vr[KT][4][kHalves][kDw] = {};
     auto load_queries = [&](const Step &x) {
         const T *q = (const T *)p.q + x.b * p.q_row + (head0_of(x.row) + r) * p.q_head + 8 * g;
         const bool have = r < heads_of(x.row);
@@ -253,8 +258,8 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
     };
     // a tile's first element in the caches; an entry that names no page is read as page 0 and masked
     auto tile_at = [&](const Step &x, int u) -> int64_t {
-        const int e = u ? x.e1 : x.e0, kvh = kv_head_of(x.row);
-        const int slot = (x.s * kStepKeys + 16 * u) & ((1 << p.page_shift) - 1);
+        const int e = x.e[u], kvh = kv_head_of(x.row);
+        const int slot = (x.s * kStepKeys + kTileKeys * u) & ((1 << p.page_shift) - 1);
         return ((((int64_t)((uint32_t)e < (uint32_t)p.pages ? e : 0) * p.kv_heads + kvh) << p.page_shift) + slot) * D;
     };
     // Values are read once, whole rows at a time: non-temporal.  A load of keys takes 64 bytes of a row, the
@@ -265,8 +270,8 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
     const bool stream_keys = D != 96 && p.head_tiles == 1 && total * rows > ((256 << 20) / (kStepKeys * 4 * D));
     auto load_keys = [&](const Step &x) {
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            if (u == 1 && x.s * kStepKeys + 16 >= x.tokens) break;  // masked, whatever the registers hold
+        for (int u = 0; u < KT; ++u) {
+            if (u > 0 && x.s * kStepKeys + kTileKeys * u >= x.tokens) break;  // masked, whatever the registers hold
             const T *k = (const T *)p.k + tile_at(x, u);
 #pragma unroll
             for (int t = 0; t < kQ; ++t) {
@@ -277,8 +282,8 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
     };
     auto load_values = [&](const Step &x) {
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            if (u == 1 && x.s * kStepKeys + 16 >= x.tokens) break;
+        for (int u = 0; u < KT; ++u) {
+            if (u > 0 && x.s * kStepKeys + kTileKeys * u >= x.tokens) break;
             const T *v = (const T *)p.v + tile_at(x, u);
 #pragma unroll
             for (int i = 0; i < 4; ++i)
@@ -340,16 +345,16 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
     bool begun_before = from.step > 0;  // the row at hand began in another wave
     clear();  // a wave without steps between two that share a row adds nothing to it
     if (left > 0) {
-        Step cur{from.b, from.row, from.tokens >= 0 ? from.tokens : cap_tokens(p, scalar_load(p.lengths + from.b)), from.step, -1, -1}, next;
+        Step cur{from.b, from.row, from.tokens >= 0 ? from.tokens : cap_tokens(p, scalar_load(p.lengths + from.b)), from.step, {}}, next;
         entries(cur);
         load_queries(cur);
         load_keys(cur);
         load_values(cur);
         if (left > 1) next = advance(cur);
         while (true) {
-            float4_t sc[2];
+            float4_t sc[KT];
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
+            for (int u = 0; u < KT; ++u) {
                 sc[u] = float4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int t = 0; t < kQ; ++t) sc[u] = E::mfma(kf[u][t], qf[t], sc[u]);
@@ -365,15 +370,15 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
                 if (left > 2) ahead = advance(next);
             }
 #pragma unroll
-            for (int u = 0; u < 2; ++u)
+            for (int u = 0; u < KT; ++u)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) sc[u][i] *= p.scale_log2;
             const int pos = cur.s * kStepKeys;
-            if (pos + 32 > cur.tokens || (uint32_t)cur.e0 >= (uint32_t)p.pages || (uint32_t)cur.e1 >= (uint32_t)p.pages) {
+            if (pos + kStepKeys > cur.tokens || (uint32_t)cur.e[0] >= (uint32_t)p.pages || (uint32_t)cur.e[KT - 1] >= (uint32_t)p.pages) {
                 // whatever a masked slot holds (an infinity, not a number) stays out of both products
 #pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    const int valid = (uint32_t)(u ? cur.e1 : cur.e0) < (uint32_t)p.pages ? cur.tokens - pos - 16 * u : 0;
+                for (int u = 0; u < KT; ++u) {
+                    const int valid = (uint32_t)cur.e[u] < (uint32_t)p.pages ? cur.tokens - pos - kTileKeys * u : 0;
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
                         if (4 * g + i >= valid) {
@@ -387,7 +392,7 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
             }
             float top = m;
 #pragma unroll
-            for (int u = 0; u < 2; ++u)
+            for (int u = 0; u < KT; ++u)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) top = fmaxf(top, sc[u][i]);
             top = max_over_groups(top);
@@ -399,27 +404,28 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
                 for (int j = 0; j < kAcc; ++j) acc[j] *= keep;
             }
             m = top;
-            float pr[2][4];
+            float pr[KT][4];
 #pragma unroll
-            for (int u = 0; u < 2; ++u)
+            for (int u = 0; u < KT; ++u)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) pr[u][i] = __builtin_amdgcn_exp2f(sc[u][i] - ref);
-            l += ((pr[0][0] + pr[0][1]) + (pr[0][2] + pr[0][3])) + ((pr[1][0] + pr[1][1]) + (pr[1][2] + pr[1][3]));
+#pragma unroll
+            for (int u = 0; u < KT; ++u) l += (pr[u][0] + pr[u][1]) + (pr[u][2] + pr[u][3]);
             // The weights go to the second product in the cache's type, as its MFMAs want them: half an ulp each, the size of
             // the output's own rounding, with the sum l kept of the unrounded ones.
-            vec8 pf;
+            weights_t pf;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) pf[e] = (T)pr[e >> 2][e & 3];
+            for (int e = 0; e < 4 * KT; ++e) pf[e] = (T)pr[e >> 2][e & 3];
 #pragma unroll
             for (int hf = 0; hf < kHalves; ++hf)
 #pragma unroll
                 for (int j = 0; j < kCh; ++j) {
-                    uint32_t w[4];
+                    uint32_t w[2 * KT];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
+                    for (int e = 0; e < 2 * KT; ++e)
                         w[e] = __builtin_amdgcn_perm(vr[e >> 1][2 * (e & 1) + 1][hf][j >> 1], vr[e >> 1][2 * (e & 1)][hf][j >> 1],
                                                      (j & 1) ? 0x07060302u : 0x05040100u);
-                    acc[hf * kCh + j] = E::mfma(__builtin_bit_cast(vec8, u32x4_t{w[0], w[1], w[2], w[3]}), pf, acc[hf * kCh + j]);
+                    acc[hf * kCh + j] = E::mfma(__builtin_bit_cast(weights_t, w), pf, acc[hf * kCh + j]);
                 }
             issue_order_point();
             if (left > 1) load_values(next);
@@ -452,7 +458,7 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
     if (wave == 0 && (wg_head || wg_tail)) {
         const Place x = lane == 0 ? wg_from : wg_to;
         const int unit = x.before + kRowCost * (x.b * rows + x.row + 1);  // of the row's first step
-        const int first = first_at(unit + min_cut, per, extra) - 1, last = last_at(unit + x.steps - min_cut, per, extra);
+        const int first = first_at(unit + min_cut) - 1, last = last_at(unit + x.steps - min_cut);
         if (lane < 2) {
             lds_first[lane] = first;
             lds_last[lane] = last;
@@ -584,9 +590,13 @@ template <typename T, int D>
 hipError_t launch_one(const AttendProblem &p, int cus, hipStream_t stream)
 {
     const int grid = (cus < kKvMaxCus ? cus : kKvMaxCus) * kAttendGroupsPerCu;
+    // Wide heads: one tile a step, which keeps the registers and divides short ranges finer (heads of 256, 20 sequences of up
+    // to 9001 tokens 27.8 us, two tiles 30.6; 16 of 30000: 158, 168).  Narrower ones: two, fewer round trips in short
+    // ranges (one sequence of 2000, heads of 128: 10.4 us, one tile 11.1).
+    constexpr int kTiles = D > 128 ? 1 : 2;
     AttendProblem q = p;
     q.grid_reciprocal = grid > 1 ? (uint32_t)(((uint64_t)1 << 32) / (uint64_t)grid) : 0xFFFFFFFFu;
-    hipLaunchKernelGGL((paged_attention_kernel<T, D, kAttendWaves>), dim3(grid), dim3(64 * kAttendWaves), 0, stream, q);
+    hipLaunchKernelGGL((paged_attention_kernel<T, D, kAttendWaves, kTiles>), dim3(grid), dim3(64 * kAttendWaves), 0, stream, q);
     return hipGetLastError();
 }
 

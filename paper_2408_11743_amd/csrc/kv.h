@@ -13,7 +13,7 @@ namespace marlin {
 
 constexpr int kKvMaxCus = 256;        // compute units a workspace is sized for
 constexpr int kKvMaxBatch = 1 << 16;  // sequences of a call
-constexpr int kStepKeys = 32;         // keys a wave takes at a time
+constexpr int kTileKeys = 16;         // keys of a tile
 constexpr int kHeadTile = 16;         // query heads of one kv head that share a pass over its keys
 constexpr int kAttendWaves = 8;       // waves per work-group
 constexpr int kAttendGroupsPerCu = 1; // work-groups per compute unit

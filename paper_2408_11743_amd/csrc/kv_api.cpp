@@ -114,8 +114,8 @@ marlin_status_t marlin_paged_attention(const marlin_paged_attention_args *a, hip
     if (!shape_ok(a->B, a->heads, a->kv_heads, a->head_dim, a->pages, a->page_size, a->width)) return MARLIN_ERR_INVALID_SHAPE;
     if (!strides_ok(a->q_row, a->q_head) || a->table_row < 0 || a->table_head < 0) return MARLIN_ERR_INVALID_SHAPE;
     const int64_t group = a->heads / a->kv_heads, head_tiles = (group + kHeadTile - 1) / kHeadTile;
-    const int64_t steps = (a->width * a->page_size + kStepKeys - 1) / kStepKeys;
-    if (a->B > 0 && steps + 1 > INT32_MAX / (a->B * a->kv_heads * head_tiles)) return MARLIN_ERR_INVALID_SHAPE;
+    const int64_t tiles = a->width * a->page_size / kTileKeys;
+    if (a->B > 0 && tiles + 2 > INT32_MAX / (a->B * a->kv_heads * head_tiles)) return MARLIN_ERR_INVALID_SHAPE;
     if (!dtype_ok(a->dtype) || !std::isfinite(a->scale) || !std::isfinite((float)(a->scale * 1.4426950408889634)))
         return MARLIN_ERR_INVALID_ARGUMENT;
     if (a->B == 0) return MARLIN_OK;

@@ -14,18 +14,29 @@ struct Elem;
 template <>
 struct Elem<_Float16> {
     typedef _Float16 vec8 __attribute__((ext_vector_type(8)));
+    typedef _Float16 vec4 __attribute__((ext_vector_type(4)));
     static __device__ __forceinline__ float4_t mfma(vec8 a, vec8 b, float4_t c)
     {
         return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+    }
+    static __device__ __forceinline__ float4_t mfma(vec4 a, vec4 b, float4_t c)
+    {
+        return __builtin_amdgcn_mfma_f32_16x16x16f16(a, b, c, 0, 0, 0);
     }
 };
 
 template <>
 struct Elem<__bf16> {
     typedef __bf16 vec8 __attribute__((ext_vector_type(8)));
+    typedef __bf16 vec4 __attribute__((ext_vector_type(4)));
     static __device__ __forceinline__ float4_t mfma(vec8 a, vec8 b, float4_t c)
     {
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+    }
+    static __device__ __forceinline__ float4_t mfma(vec4 a, vec4 b, float4_t c)
+    {
+        typedef short short4_t __attribute__((ext_vector_type(4)));
+        return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(short4_t, a), __builtin_bit_cast(short4_t, b), c, 0, 0, 0);
     }
 };
 
