@@ -3,8 +3,11 @@
 // rounding, keys and values written to their pages, and the pages' bounds (the
 // smallest and largest key per channel) widened.
 //
-// A head is D / 16 threads, each with two 16-byte pieces that hold eight pairs.  Nothing is read twice but the angles; the kernels are bound by
-// memory, and by launch latency where there is one token per sequence.
+// A head is D / 16 threads, each with two 16-byte pieces that hold eight pairs.
+// Nothing is read twice but the angles.  Prompts are bound by memory (24
+// prompts of up to 4096 tokens, 64 + 16 heads of 128 with bounds, 605 MB read and written:
+// 128 us, 4.7 TB/s, what a large copy reaches), a token per sequence by launch
+// latency (32 + 16 heads: 2.7 us; 128 sequences of 64 + 16 heads with bounds: 3.7).
 #include <hip/hip_runtime.h>
 
 #include "kv.h"
