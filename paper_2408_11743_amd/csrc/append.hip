@@ -6,7 +6,7 @@
 // A head is D / 16 threads, each with two 16-byte pieces that hold eight pairs.
 // Nothing is read twice but the angles.  Prompts are bound by memory (24
 // prompts of up to 4096 tokens, 64 + 16 heads of 128 with bounds, 605 MB read and written:
-// 128 us, 4.7 TB/s, what a large copy reaches), a token per sequence by launch
+// 111 us, 5.4 TB/s; a large copy reaches 4.8), a token per sequence by launch
 // latency (32 + 16 heads: 2.7 us; 128 sequences of 64 + 16 heads with bounds: 3.7).
 #include <hip/hip_runtime.h>
 
@@ -61,7 +61,7 @@ __device__ __forceinline__ Pieces load_pieces(const T *row, Where at)
 
 // The same of new tokens, of which nothing is read again: non-temporal (once) where they and what becomes of them are more than the last-level cache
 // holds, as what a projection has just written may still lie there, and where a piece's row of threads takes
-// whole lines of 128 bytes.  300 MB of prompts, heads of 128: 137 -> 128 us; 26 MB: 10.7 -> 13.8; heads of 64: 233 -> 256.
+// whole lines of 128 bytes.  300 MB of prompts, heads of 128: 126 -> 111 us; 26 MB: 11.9 -> 15.5; heads of 64: 223 -> 242.
 template <typename T>
 __device__ __forceinline__ Pieces load_new(const T *row, Where at, bool once)
 {
@@ -185,10 +185,13 @@ __global__ void __launch_bounds__(256) append_token_kernel(const AppendProblem p
 
 // ---- any number of tokens per sequence ----
 // A work-group takes the new tokens of one page of one sequence and four heads
-// of q, of k or of v, so that a page's bounds are one work-group's: its tokens'
-// smallest and largest keys are kept in registers and joined at the end.
-// Neighbouring work-groups take the heads of one page, which lie side by side in the
-// tokens' rows (143 us; neighbouring pages instead: 156), four waves per SIMD (137).
+// of q, of k or of v: each wave some tokens, whose four heads it reads before
+// it writes any.  Keys with bounds are a head a wave instead, so that a page's
+// bounds are one wave's: kept in its registers and joined across its lanes (all
+// four heads' in every wave, joined in LDS: 64 registers, which spilled, 130 us for the
+// prompts above).  Neighbouring work-groups take the heads of one page, which lie side by side in
+// the tokens' rows (neighbouring pages instead: 9 % more).
+// Slabs of two heads: 24 % more, of eight 5 % more.
 constexpr int kSlab = 4;
 
 template <typename T, int D>
@@ -196,7 +199,6 @@ __global__ void __launch_bounds__(256, 4) append_prompt_kernel(const AppendProbl
 {
     constexpr int kPairs = D / 16;
     constexpr int kTokens = D == 64 ? 16 : D == 256 ? 4 : 8;  // of a wave at a time
-    __shared__ uint32_t lds[4][kPairs][kSlab][16];
     __shared__ int lds_chunks[kKvMaxBatch / 64];
 
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -258,95 +260,94 @@ __global__ void __launch_bounds__(256, 4) append_prompt_kernel(const AppendProbl
     const int64_t row = kind == 0 ? p.q_row : kind == 1 ? p.k_row : p.v_row;
     const int64_t head = kind == 0 ? p.q_head : kind == 1 ? p.k_head : p.v_head;
     const Where at = where(p, D, pair);
-    const bool keep = kind == 1 && p.bounds;
 
-    uint32_t lo[kSlab][8], hi[kSlab][8];
-#pragma unroll
-    for (int j = 0; j < kSlab; ++j)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            lo[j][i] = 0x7FFF7FFFu;
-            hi[j][i] = 0x80008000u;
-        }
-    int kept = 0;
-    if (slot < kTokens) {
+    if (!(kind == 1 && p.bounds)) {
+        if (slot >= kTokens) return;
         for (int pos = lo_pos + wave * kTokens + slot; pos < hi_pos; pos += 4 * kTokens) {
             const int64_t t = from + (pos - start);
             const int64_t to = slot_of(p, b, pos);
-            Angles a{};
-            if (kind < 2 && to >= 0) a = load_angles(p, at, pos);
+            if (to < 0) {
+                if (kind == 0)
+                    for (int j = 0; j < nh; ++j) store_pieces((T *)p.q_out + (t * p.heads + h0 + j) * D, at, Pieces{});
+                continue;
+            }
+            Pieces x[kSlab];
 #pragma unroll
-            for (int j = 0; j < kSlab; ++j) {
-                if (j >= nh) break;
-                Pieces x{};
-                if (to >= 0) x = load_new(src + t * row + (h0 + j) * head, at, once);
-                if (kind < 2 && to >= 0) x = rotate<T>(p, x, a, at);
-                if (kind == 0) {
-                    store_pieces((T *)p.q_out + (t * p.heads + h0 + j) * D, at, x);
-                } else if (to >= 0) {
-                    store_pieces((T *)(kind == 1 ? p.k_cache : p.v_cache) + (to + ((int64_t)(h0 + j) << p.page_shift)) * D, at, x);
-                    if (keep) {
-                        kept = 1;
+            for (int j = 0; j < kSlab; ++j)
+                if (j < nh) x[j] = load_new(src + t * row + (h0 + j) * head, at, once);
+            if (kind == 0) {
+                const Angles a = load_angles(p, at, pos);
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            const uint32_t o = ordered(x.w[i]);
-                            lo[j][i] = min2(lo[j][i], o);
-                            hi[j][i] = max2(hi[j][i], o);
-                        }
-                    }
-                }
+                for (int j = 0; j < kSlab; ++j)
+                    if (j < nh) store_pieces((T *)p.q_out + (t * p.heads + h0 + j) * D, at, rotate<T>(p, x[j], a, at));
+                continue;
+            }
+            if (kind == 1) {
+                const Angles a = load_angles(p, at, pos);
+#pragma unroll
+                for (int j = 0; j < kSlab; ++j) x[j] = rotate<T>(p, x[j], a, at);
+            }
+            T *cache = (T *)(kind == 1 ? p.k_cache : p.v_cache) + to * D;
+#pragma unroll
+            for (int j = 0; j < kSlab; ++j)
+                if (j < nh) store_pieces(cache + ((int64_t)(h0 + j) << p.page_shift) * D, at, x[j]);
+        }
+        return;
+    }
+
+    // keys with bounds: a head is one wave's
+    if (wave >= nh) return;
+    const int h = h0 + wave;
+    uint32_t lo[8], hi[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        lo[i] = 0x7FFF7FFFu;
+        hi[i] = 0x80008000u;
+    }
+    bool kept = false;
+    if (slot < kTokens) {
+        for (int pos = lo_pos + slot; pos < hi_pos; pos += kTokens) {
+            const int64_t to = slot_of(p, b, pos);
+            if (to < 0) continue;
+            const Pieces x = load_new(src + (int64_t)(from + (pos - start)) * row + h * head, at, once);
+            const Pieces y = rotate<T>(p, x, load_angles(p, at, pos), at);
+            store_pieces((T *)p.k_cache + (to + ((int64_t)h << p.page_shift)) * D, at, y);
+            kept = true;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const uint32_t o = ordered(y.w[i]);
+                lo[i] = min2(lo[i], o);
+                hi[i] = max2(hi[i], o);
             }
         }
     }
-    if (!keep) return;  // uniform
-    // over the wave's tokens, then over the waves
+    if (!__any(kept)) return;
 #pragma unroll
     for (int d = kTokens / 2; d > 0; d >>= 1)
 #pragma unroll
-        for (int j = 0; j < kSlab; ++j)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                lo[j][i] = min2(lo[j][i], __shfl(lo[j][i], (lane + kPairs * d) & 63));
-                hi[j][i] = max2(hi[j][i], __shfl(hi[j][i], (lane + kPairs * d) & 63));
-            }
-    if (slot == 0)
-#pragma unroll
-        for (int j = 0; j < kSlab; ++j)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                lds[wave][pair][j][i] = lo[j][i];
-                lds[wave][pair][j][8 + i] = hi[j][i];
-            }
-    const int any = __syncthreads_or(kept);
-    if (!any) return;
-    if (threadIdx.x < kPairs * kSlab) {
-        const int j = threadIdx.x / kPairs, pr = threadIdx.x % kPairs;
-        if (j >= nh) return;
-        const Where w = where(p, D, pr);
-        Pieces x, z;
+        for (int i = 0; i < 8; ++i) {
+            lo[i] = min2(lo[i], __shfl(lo[i], (lane + kPairs * d) & 63));
+            hi[i] = max2(hi[i], __shfl(hi[i], (lane + kPairs * d) & 63));
+        }
+    if (slot > 0) return;
+    const int page = p.table[b * p.table_row + (page0 >> p.page_shift)];
+    T *to_lo = (T *)p.bounds + ((int64_t)page * p.kv_heads + h) * 2 * D, *to_hi = to_lo + D;
+    Pieces x, z;
+    if (lo_pos > page0) {
+        const Pieces old_lo = load_pieces(to_lo, at), old_hi = load_pieces(to_hi, at);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            x.w[i] = min2(min2(lds[0][pr][j][i], lds[1][pr][j][i]), min2(lds[2][pr][j][i], lds[3][pr][j][i]));
-            z.w[i] = max2(max2(lds[0][pr][j][8 + i], lds[1][pr][j][8 + i]), max2(lds[2][pr][j][8 + i], lds[3][pr][j][8 + i]));
+            lo[i] = min2(lo[i], ordered(old_lo.w[i]));
+            hi[i] = max2(hi[i], ordered(old_hi.w[i]));
         }
-        const int page = p.table[b * p.table_row + (page0 >> p.page_shift)];
-        T *to_lo = (T *)p.bounds + ((int64_t)page * p.kv_heads + h0 + j) * 2 * D, *to_hi = to_lo + D;
-        if (lo_pos > page0) {
-            const Pieces old_lo = load_pieces(to_lo, w), old_hi = load_pieces(to_hi, w);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                x.w[i] = min2(x.w[i], ordered(old_lo.w[i]));
-                z.w[i] = max2(z.w[i], ordered(old_hi.w[i]));
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            x.w[i] = ordered(x.w[i]);
-            z.w[i] = ordered(z.w[i]);
-        }
-        store_pieces(to_lo, w, x);
-        store_pieces(to_hi, w, z);
     }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        x.w[i] = ordered(lo[i]);
+        z.w[i] = ordered(hi[i]);
+    }
+    store_pieces(to_lo, at, x);
+    store_pieces(to_hi, at, z);
 }
 
 template <typename T, int D>
