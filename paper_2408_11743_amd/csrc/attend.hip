@@ -27,10 +27,10 @@
 // Bound by memory: a step's 16 KB (d = 128) take a compute unit 0.6 us of its
 // share of the bandwidth and 0.1 us of MFMA and vector work.  64 sequences of
 // 32768 tokens, 64 heads over 8 (8.6 GB): 1.26 ms, 6.8 TB/s, where a kernel that
-// only reads reaches 7.1; one of 131071 tokens: 90 us, 6.0.  Short
+// only reads reaches 7.1; one of 131071 tokens: 89 us, 6.0.  Short
 // calls are latency: 2 us to the first load of keys, a round trip a step, 4 to
-// 6 us where rows are cut between work-groups (77 tokens of 32 heads: 5.9 us,
-// one sequence of 8000 tokens over 8 kv heads, 33 MB: 14.5).  Four waves a work-group,
+// 6 us where rows are cut between work-groups (77 tokens of 32 heads: 5.2 us,
+// one sequence of 8000 tokens over 8 kv heads, 33 MB: 14.0).  Four waves a work-group,
 // two work-groups a compute unit: 98 us for the 131071 tokens; eight and two: 100.
 #include <hip/hip_runtime.h>
 
@@ -209,8 +209,11 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
     };
     const Place wg_from = border(wg), wg_to = border(wg + 1);
     const int begin = wg_from.before + wg_from.step, steps = wg_to.before + wg_to.step - begin;
-    const int mine = (int)((int64_t)steps * wave / NW);
-    int left = (int)((int64_t)steps * (wave + 1) / NW) - mine;  // steps of this wave
+    // Uneven shares: more to the first waves, whose loads are served first (77 tokens of 32 heads: 5.2 us, to the last
+    // waves 5.9; 20 sequences, heads of 256: 26.9, 28.4).
+    const int share = steps / NW, odd = steps % NW;
+    const int mine = share * wave + (wave < odd ? wave : odd);
+    int left = share + (wave < odd ? 1 : 0);  // steps of this wave
     Place from = wg_from, to = wg_to;
     if (wg_from.before == wg_to.before) {  // all in one row
         from.step += mine;
@@ -526,14 +529,20 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
                                           : (all & ~((2u << (31 - __builtin_clz(~inner & all))) - 1)) | 1u << NW;
         float *const slot = p.partials + ((int64_t)wg * 2 + which) * kSlotFloats;
         const int nh = heads_of(which == 0 ? wg_from.row : wg_to.row);
-        join_slots(slots, [&](int j, float4_t o, float top, float sum) {
+        auto put = [&](int j, float4_t o, float top, float sum) {
             if (r >= nh) return;
             store_partial16(slot, j, lane, o);
             if (j == 0 && g == 0) {
                 store_float(slot + kHeadTile * D + r, top);
                 store_float(slot + kHeadTile * D + kHeadTile + r, sum);
             }
-        });
+        };
+        // a row through the whole range, without branches: one sequence of 8000 tokens 13.9 us, 14.4 (ragged ones of
+        // heads of 256: 27 us, 25.5)
+        if (D <= 128 && slots == all)
+            join_slots(all, put);
+        else
+            join_slots(slots, put);
     }
     wait_vmcnt<0>();
     __syncthreads();
@@ -552,10 +561,50 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
     for (int which = 0; which < 2; ++which) {
         if (!__builtin_amdgcn_readfirstlane(lds_flags[which])) continue;
         const int first = __builtin_amdgcn_readfirstlane(lds_first[which]), last = __builtin_amdgcn_readfirstlane(lds_last[which]);
-        // Every wave joins some of the contributors, in order, then all of them the waves': the same bits every time.
         const __amdgpu_buffer_rsrc_t partials =
             __builtin_amdgcn_make_buffer_rsrc((void *)p.partials, (short)0, 0x7fffffffu, kBufferFlags);
         const int b = which == 0 ? wg_from.b : wg_to.b, row = which == 0 ? wg_from.row : wg_to.row, nh = heads_of(row);
+        auto write = [&](int j, float4_t o, float top, float sum) {
+            if (r >= nh) return;
+            const int64_t at = (int64_t)b * p.heads + head0_of(row) + r;
+            const float inv = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                ((T *)p.out)[at * D + 128 * (j / kCh) + kCh * (4 * g + i) + j % kCh] = (T)(o[i] * inv);
+            if (p.lse && g == 0 && j == 0) p.lse[at] = (top + __builtin_amdgcn_logf(sum)) * 0.693147180559945f;
+        };
+        // Contributors are joined in order, so that the bits are the same every time.  Of a few, a wave takes its channels at once
+        // (16 sequences of up to 4001 tokens: 25.1 us, by LDS as below 26.4; the registers of both do not go together where heads are wide).
+        constexpr int kFew = 8;
+        if (D <= 128 && last - first < kFew) {
+            if (wave < kAcc && r < nh) {
+                const int j = wave;
+                float mk[kFew], lk[kFew], top = -INFINITY, sum = 0.f;
+                float4_t a[kFew], o{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int k = 0; k < kFew; ++k)
+                    if (first + k <= last) {
+                        const int slot = ((first + k) * 2 + (k == 0 ? 1 : 0)) * (kSlotFloats * 4);
+                        mk[k] = load_slot4(partials, slot, kHeadTile * D * 4 + r * 4);
+                        lk[k] = load_slot4(partials, slot, kHeadTile * D * 4 + kHeadTile * 4 + r * 4);
+                        a[k] = load_slot16(partials, slot, j * 1024 + lane * 16);
+                    }
+#pragma unroll
+                for (int k = 0; k < kFew; ++k)
+                    if (first + k <= last) top = fmaxf(top, mk[k]);
+                const float ref = top == -INFINITY ? 0.f : top;
+#pragma unroll
+                for (int k = 0; k < kFew; ++k)
+                    if (first + k <= last) {
+                        const float f = __builtin_amdgcn_exp2f(mk[k] - ref);
+                        sum += lk[k] * f;
+                        o += a[k] * f;
+                    }
+                write(j, o, top, sum);
+            }
+            continue;
+        }
+        // Of more, a wave takes some of the contributors, then all take the waves'.
         clear();
         if (r < nh) {
             struct Piece {
@@ -583,15 +632,7 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
         }
         put_piece(wave);
         __syncthreads();
-        join_slots(last - first >= NW - 1 ? all : (2u << (last - first)) - 1, [&](int j, float4_t o, float top, float sum) {
-            if (r >= nh) return;
-            const int64_t at = (int64_t)b * p.heads + head0_of(row) + r;
-            const float inv = sum == 0.f ? 0.f : 1.f / sum;
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                ((T *)p.out)[at * D + 128 * (j / kCh) + kCh * (4 * g + i) + j % kCh] = (T)(o[i] * inv);
-            if (p.lse && g == 0 && j == 0) p.lse[at] = (top + __builtin_amdgcn_logf(sum)) * 0.693147180559945f;
-        });
+        join_slots(all, write);
         __syncthreads();
     }
 }
