@@ -8,8 +8,8 @@
 // a product over 2 D channels for the MFMAs, and the best `select` are kept in the
 // order of their positions.
 //
-// Latency bounds both kernels: 8 rows of 4063 pages are scored in 6 us (16.6
-// MB) and picked from in 10, 256 rows of 10 .. 1875 in 14 (48.7 MB) and 9.
+// Latency bounds both kernels: 8 rows of 4063 pages are scored in 5.7 us (16.6
+// MB) and picked from in 9, 256 rows of 10 .. 1875 in 14.8 (48.7 MB) and 6.4.
 #include <hip/hip_runtime.h>
 
 #include "kv.h"
@@ -20,7 +20,9 @@ namespace {
 
 using namespace dev;
 
-constexpr int kScoreWaves = 4, kFewBlocks = 2048;
+// Waves are independent: small work-groups come and go faster (32 sequences of up to 60000 tokens selected and attended
+// in 63.5 us with two, 64.7 four, 65.9 eight, 83 sixteen).
+constexpr int kScoreWaves = 2, kFewBlocks = 4096;
 
 __device__ __forceinline__ int pages_of(const SelectProblem &p, int b)
 {
@@ -103,40 +105,73 @@ __global__ void __launch_bounds__(64 * kScoreWaves) page_score_kernel(const Sele
     if (g == 0 && at < pages) p.scores[(int64_t)row * p.width + at] = !inside ? kNoPage : any ? kNan : score_key(best);
 }
 
-// Sums over the work-group's lanes before this one, and (total) all of them.
 constexpr int kPickThreads = 512, kPickWaves = kPickThreads / 64;
-__device__ __forceinline__ int group_scan(int x, int *waves, int &total)
+
+struct Counts {
+    int a, b;
+};
+// Sums over the work-group's lanes before this one.
+__device__ __forceinline__ Counts group_scan(Counts x, Counts *waves)
 {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = wave_scan(x);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const Counts i{wave_scan(x.a), wave_scan(x.b)};
     if (lane == 63) waves[wave] = i;
     __syncthreads();
-    int before = 0;
-    total = 0;
+    Counts before{i.a - x.a, i.b - x.b};
 #pragma unroll
     for (int w = 0; w < kPickWaves; ++w) {
-        before += w < wave ? waves[w] : 0;
-        total += waves[w];
+        before.a += w < wave ? waves[w].a : 0;
+        before.b += w < wave ? waves[w].b : 0;
     }
-    __syncthreads();
-    return before + i - x;
+    return before;
+}
+
+// The wave's smallest (largest) value, in lane 63.
+template <bool MIN>
+__device__ __forceinline__ uint32_t wave_end(uint32_t x)
+{
+    auto with = [&](uint32_t y) { x = MIN ? (y < x ? y : x) : (y > x ? y : x); };
+    with((uint32_t)__builtin_amdgcn_update_dpp((int)x, (int)x, 0x111, 0xf, 0xf, false));
+    with((uint32_t)__builtin_amdgcn_update_dpp((int)x, (int)x, 0x112, 0xf, 0xf, false));
+    with((uint32_t)__builtin_amdgcn_update_dpp((int)x, (int)x, 0x114, 0xf, 0xf, false));
+    with((uint32_t)__builtin_amdgcn_update_dpp((int)x, (int)x, 0x118, 0xf, 0xf, false));
+    with((uint32_t)__builtin_amdgcn_update_dpp((int)x, (int)x, 0x142, 0xa, 0xf, false));
+    with((uint32_t)__builtin_amdgcn_update_dpp((int)x, (int)x, 0x143, 0xc, 0xf, false));
+    return x;
 }
 
 // One work-group per (sequence, kv head) finds the score that the select - 1 best
 // pages but the last reach: counts of the scores in 2048 equal parts
 // of their range, then of the part that holds it, until the part is one score or wanted whole
 // (the parts follow the range, so that few scores meet in one counter); then every page above it and the first ones equal to
-// it, in order.  Scores are read once; up to kPickCached stay in LDS.
-constexpr int kPickBins = 2048, kPickCached = 16384;
+// it, in order.  A thread's pages are adjacent; up to kHeld of them, it reads their scores and entries
+// while the length is under way and keeps them in registers (HELD).  Of more, scores are read once
+// where kPickCached stay in LDS, as do the places of the chosen (4062 pages so: 26.9 us with scores and attention, HELD 24.5).
+constexpr int kPickBins = 2048, kPickCached = 16384, kHeld = 8;
 
+template <bool HELD>
 __global__ void __launch_bounds__(kPickThreads) page_pick_kernel(const SelectProblem p)
 {
-    __shared__ uint32_t cached[kPickCached];
-    __shared__ int bins[kPickBins], waves[kPickWaves], found[3];
+    __shared__ uint32_t cached[HELD ? 1 : kPickCached];
+    __shared__ int bins[kPickBins], found[3];
+    __shared__ Counts waves[2][kPickWaves];
     __shared__ uint32_t ends[2][kPickWaves];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int b = blockIdx.x / p.kv_heads, kvh = blockIdx.x % p.kv_heads;
-    const int pages = pages_of(p, b);
     const int32_t *table = p.table + b * p.table_row;
+    const uint32_t *scores = p.scores + (int64_t)blockIdx.x * p.width;
+    uint32_t held[kHeld];
+    int32_t entry[kHeld];
+    const int spread = (p.width + kPickThreads - 1) / kPickThreads;
+    if (HELD)
+#pragma unroll
+        for (int k = 0; k < kHeld; ++k) {
+            if (k >= spread) break;
+            const int i = spread * tid + k < p.width ? spread * tid + k : 0;
+            held[k] = scores[i];
+            entry[k] = table[i];
+        }
+    const int pages = pages_of(p, b);
     int32_t *out = p.chosen + (int64_t)blockIdx.x * p.select;
     if (kvh == 0 && tid == 0) {
         const int n = p.lengths[b], cap = p.width << p.page_shift, len = n < 0 ? 0 : n < cap ? n : cap;
@@ -146,50 +181,66 @@ __global__ void __launch_bounds__(kPickThreads) page_pick_kernel(const SelectPro
         for (int i = tid; i < p.select; i += kPickThreads) out[i] = i < pages ? table[i] : -1;
         return;
     }
-    const uint32_t *scores = p.scores + (int64_t)blockIdx.x * p.width;
     const int n = pages - 1;  // the last page is chosen anyway
-    int want = p.select - 1;  // of the pages with scores from lo to hi; those above hi are chosen
+    const int per = HELD ? spread : (n + kPickThreads - 1) / kPickThreads, i0 = tid * per < n ? tid * per : n, i1 = i0 + per < n ? i0 + per : n;
     const bool in_lds = n <= kPickCached;
+    auto score = [&](int i) { return in_lds ? cached[i] : scores[i]; };
+    // the scores, a thread's in order (any: in whatever order)
+    auto each = [&](bool any, auto &&f) {
+        if (HELD) {
+#pragma unroll
+            for (int k = 0; k < kHeld; ++k)
+                if (i0 + k < i1) f(k, held[k]);
+        } else if (any) {
+            for (int i = tid; i < n; i += kPickThreads) f(i, score(i));
+        } else {
+            for (int i = i0; i < i1; ++i) f(i, score(i));
+        }
+    };
+    int want = p.select - 1;  // of the pages with scores from lo to hi; those above hi are chosen
     uint32_t lo = 0xFFFFFFFFu, hi = 0;
-#pragma unroll 8
-    for (int i = tid; i < n; i += kPickThreads) {
-        const uint32_t s = scores[i];
-        if (in_lds) cached[i] = s;
+    auto widen = [&](uint32_t s) {
         lo = s < lo ? s : lo;
         hi = s > hi ? s : hi;
+    };
+    if (HELD) {
+        each(true, [&](int, uint32_t s) { widen(s); });
+    } else {
+#pragma unroll 8
+        for (int i = tid; i < n; i += kPickThreads) {
+            const uint32_t s = scores[i];
+            if (in_lds) cached[i] = s;
+            widen(s);
+        }
     }
     for (int i = tid; i < kPickBins; i += kPickThreads) bins[i] = 0;
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) {
-        const uint32_t l2 = __shfl_xor(lo, d), h2 = __shfl_xor(hi, d);
-        lo = l2 < lo ? l2 : lo;
-        hi = h2 > hi ? h2 : hi;
-    }
-    if (lane == 0) {
+    lo = wave_end<true>(lo);
+    hi = wave_end<false>(hi);
+    if (lane == 63) {
         ends[0][wave] = lo;
         ends[1][wave] = hi;
     }
     __syncthreads();
+    lo = ends[0][0];
+    hi = ends[1][0];
 #pragma unroll
-    for (int w = 0; w < kPickWaves; ++w) {
+    for (int w = 1; w < kPickWaves; ++w) {
         lo = ends[0][w] < lo ? ends[0][w] : lo;
         hi = ends[1][w] > hi ? ends[1][w] : hi;
     }
-    auto score = [&](int i) { return in_lds ? cached[i] : scores[i]; };
     uint32_t bar = 0xFFFFFFFFu;  // chosen: scores above it, and the first `want` equal to it
     while (want > 0) {
         const int bits = 32 - __clz(hi - lo | 1u), shift = bits > 11 ? bits - 11 : 0;
-        for (int i = tid; i < n; i += kPickThreads) {
-            const uint32_t s = score(i);
+        each(true, [&](int, uint32_t s) {
             if (s >= lo && s <= hi) atomicAdd(&bins[(s - lo) >> shift], 1);
-        }
+        });
         __syncthreads();
         // thread t: bins 4 (511 - t) .. + 3, from the top
         constexpr int kPer = kPickBins / kPickThreads;
-        int c[kPer], sum = 0, all;
+        int c[kPer], sum = 0;
 #pragma unroll
         for (int k = 0; k < kPer; ++k) sum += c[k] = bins[kPickBins - 1 - kPer * tid - k];
-        int upto = group_scan(sum, waves, all);
+        int upto = group_scan({sum, 0}, waves[0]).a;
 #pragma unroll
         for (int k = 0; k < kPer; ++k) {
             const int bin = kPickBins - 1 - kPer * tid - k;
@@ -205,7 +256,6 @@ __global__ void __launch_bounds__(kPickThreads) page_pick_kernel(const SelectPro
         const uint32_t first = lo + ((uint32_t)found[0] << shift);
         want -= found[1];
         const bool whole = want == found[2];
-        __syncthreads();
         if (shift == 0 || whole) {
             bar = first;
             if (whole) want = n;  // all from `first` on
@@ -213,30 +263,29 @@ __global__ void __launch_bounds__(kPickThreads) page_pick_kernel(const SelectPro
         }
         lo = first;
         hi = hi - first < 1u << shift ? hi : first + ((1u << shift) - 1);
-    }
-    // in order: a thread's pages are adjacent
-    const int per = (n + kPickThreads - 1) / kPickThreads, i0 = tid * per < n ? tid * per : n, i1 = i0 + per < n ? i0 + per : n;
-    int above = 0, equal = 0, all;
-    for (int i = i0; i < i1; ++i) {
-        const uint32_t s = score(i);
-        above += s > bar;
-        equal += s == bar;
+        __syncthreads();
     }
     if (bar != 0xFFFFFFFFu) {
-        const int equal_before = group_scan(equal, waves, all);
-        int to = group_scan(above, waves, all) + (equal_before < want ? equal_before : want), e = equal_before;
-        const bool listed = p.select <= kPickBins;  // then the table is read for all of them together
-        for (int i = i0; i < i1; ++i) {
-            const uint32_t s = score(i);
+        Counts mine{0, 0};
+        each(false, [&](int, uint32_t s) {
+            mine.a += s > bar;
+            mine.b += s == bar;
+        });
+        const Counts before = group_scan(mine, waves[1]);
+        int e = before.b, to = before.a + (e < want ? e : want);
+        const bool listed = !HELD && p.select <= kPickBins;  // then the table is read for all of them together
+        each(false, [&](int i, uint32_t s) {
             if (s > bar || (s == bar && e < want)) {
-                if (listed)
+                if (HELD)
+                    out[to] = entry[i];
+                else if (listed)
                     bins[to] = i;
                 else
                     out[to] = table[i];
                 ++to;
             }
             e += s == bar;
-        }
+        });
         if (listed) {
             __syncthreads();
             for (int k = tid; k < p.select - 1; k += kPickThreads) out[k] = table[bins[k]];
@@ -251,7 +300,10 @@ hipError_t launch_one(const SelectProblem &p, hipStream_t stream)
     constexpr int kPer = 16 * kScoreWaves;
     const int blocks = (p.width + kPer - 1) / kPer;
     hipLaunchKernelGGL((page_score_kernel<T, D>), dim3(blocks * p.B * p.kv_heads), dim3(64 * kScoreWaves), 0, stream, p, blocks);
-    hipLaunchKernelGGL(page_pick_kernel, dim3(p.B * p.kv_heads), dim3(kPickThreads), 0, stream, p);
+    if (p.width <= kPickThreads * kHeld)
+        hipLaunchKernelGGL(page_pick_kernel<true>, dim3(p.B * p.kv_heads), dim3(kPickThreads), 0, stream, p);
+    else
+        hipLaunchKernelGGL(page_pick_kernel<false>, dim3(p.B * p.kv_heads), dim3(kPickThreads), 0, stream, p);
     return hipGetLastError();
 }
 
