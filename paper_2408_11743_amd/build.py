@@ -61,7 +61,7 @@ def _fast_command(out: str) -> list[str]:
               os.path.join(os.environ.get("ROCM_PATH", "/opt/rocm"), "include")):
         cmd += ["-isystem", d]
     return cmd + ["-I", INCLUDE, "-o", out, os.path.join(CSRC, "fast.cpp"), "-L" + os.path.join(home, "lib"), "-lc10",
-                  "-ltorch_cpu", "-ltorch", "-ltorch_python"]
+                  "-ltorch_cpu", "-ltorch_hip", "-ltorch", "-ltorch_python"]
 
 
 def build(verbose: bool = False, out: str = LIB, extra: list[str] | None = None) -> str:

@@ -8,7 +8,7 @@
 
 #include <torch/csrc/autograd/python_variable.h>
 
-#include <ATen/ops/empty.h>
+#include <ATen/hip/EmptyTensor.h>
 #include <c10/core/DeviceGuard.h>
 
 #include <cmath>
@@ -63,7 +63,7 @@ bool caches_ok(const at::Tensor &k, const at::Tensor &v)
 
 at::Tensor dense(const at::Tensor &like, at::IntArrayRef sizes, at::ScalarType dtype)
 {
-    return at::empty(sizes, at::TensorOptions().dtype(dtype).device(like.device()));
+    return at::Tensor(at::detail::empty_cuda(sizes, dtype, like.device(), std::nullopt));
 }
 
 bool out_ok(PyObject *o, const at::Tensor &q, const Place &at, at::Tensor &out)
