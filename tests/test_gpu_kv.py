@@ -116,6 +116,45 @@ def test_attention_long(mk):
     check_attention(mk, *make(5, [40001, 17, 9000], 2, 1, 64, 64, F16))
 
 
+@pytest.mark.parametrize("D", [64, 96, 128, 256])
+@pytest.mark.parametrize("n,hq", [(270, 16), (700, 5), (1100, 16), (2600, 3), (9001, 16)])
+def test_attention_joins_of_few_and_many_pieces(mk, D, n, hq):
+    """One row in two pieces to more than a work-group has waves, alone and between short rows."""
+    check_attention(mk, *make(n + D, [n], hq, 1, D, 16, F16))
+    check_attention(mk, *make(n + D, [40, n, 0, 40], hq, 1, D, 32, BF16))
+
+
+@pytest.mark.parametrize("D", [128, 256])
+def test_attention_uneven_shares(mk, D):
+    """Ranges of every number of steps modulo the waves, rows that end within a range."""
+    for n in (130, 290, 450, 610, 770):
+        check_attention(mk, *make(n + D, [n, n // 3, n], 4, 4, D, 16, BF16))
+
+
+@pytest.mark.parametrize("D,hq", [(64, 16), (96, 16), (128, 16), (128, 136), (256, 16)])
+def test_attention_larger_than_the_last_level_cache(mk, D, hq):
+    """More keys and values than the caches hold are read another way; two of the sequences are looked at."""
+    g = torch.Generator(device="cuda").manual_seed(D + hq)
+    hkv, ps, lengths = 8, 64, [9000 * 128 // D - 100 * i for i in range(12)]
+    used = [-(-n // ps) for n in lengths]
+    k, v = (torch.randn(sum(used), hkv, ps, D, dtype=BF16, device="cuda", generator=g) for _ in range(2))
+    assert k.numel() * 4 > 256 << 20
+    q = torch.randn(12, hq, D, dtype=BF16, device="cuda", generator=g)
+    table = torch.zeros(12, max(used), dtype=torch.int32, device="cuda")
+    perm = torch.randperm(sum(used), device="cuda", generator=g).int()
+    for b, n in enumerate(used):
+        table[b, :n] = perm[sum(used[:b]):sum(used[:b]) + n]
+    got, lse = mk.paged_attention(q, k, v, table, torch.tensor(lengths, dtype=torch.int32, device="cuda"), return_lse=True)
+    for b, heads in ((0, slice(0, hq // hkv)), (11, slice(hq - hq // hkv, hq))):
+        kvh = heads.start // (hq // hkv)
+        pages = table[b, :used[b]].long()
+        mine = torch.arange(used[b], dtype=torch.int32)[None]
+        want, want_lse, tol, tol_lse = ref.attention(q[b:b + 1, heads].cpu(), k[pages, kvh:kvh + 1].cpu(), v[pages, kvh:kvh + 1].cpu(),
+                                                     mine, torch.tensor([lengths[b]]))
+        assert ((got[b:b + 1, heads].cpu().double() - want).abs() <= tol).all()
+        assert ((lse[b:b + 1, heads].cpu().double() - want_lse).abs() <= tol_lse).all()
+
+
 def test_attention_no_sequence_has_tokens(mk):
     check_attention(mk, *make(6, [0, 0, 0], 4, 2, 128, 16, F16))
 
@@ -376,6 +415,39 @@ def test_append_tokens_that_have_no_place(mk, prompts):
     check_append(mk, *args, starts=starts if prompts else None, bounds=bounds)
 
 
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_append_prompts_large(mk, interleaved):
+    """Prompts larger than the last-level cache are read another way: the same bits as one sequence at a time."""
+    g = torch.Generator(device="cuda").manual_seed(25)
+    hq, hkv, D, ps, new = 24, 4, 128, 32, [9001, 7013, 8191]
+    lengths = torch.tensor([9001, 7013 + 45, 8191 + 7], dtype=torch.int32, device="cuda")
+    used = [-(-n // ps) for n in lengths.tolist()]
+    qkv = torch.randn(sum(new), hq + 2 * hkv, D, dtype=F16, device="cuda", generator=g)
+    assert qkv.numel() * 2 > 128 << 20
+    q, k, v = qkv.split([hq, hkv, hkv], 1)
+    table = torch.full((3, max(used)), -1, dtype=torch.int32, device="cuda")
+    perm = torch.randperm(sum(used) + 1, device="cuda", generator=g).int()
+    for b, n in enumerate(used):
+        table[b, :n] = perm[sum(used[:b]):sum(used[:b]) + n]
+    angles = mk.rotation_table(9001, D)
+    sides = []
+    for whole in (True, False):
+        kc, vc, bounds = mk.kv_cache(sum(used) + 1, hkv, ps, D, F16, bounds=True)
+        starts = torch.tensor([0] + list(torch.tensor(new).cumsum(0)), dtype=torch.int32, device="cuda")
+        if whole:
+            out = mk.kv_append(q, k, v, kc, vc, table, lengths, angles, starts, interleaved, bounds)
+        else:
+            outs = []
+            for b, n in enumerate(new):
+                at = slice(sum(new[:b]), sum(new[:b]) + n)
+                outs.append(mk.kv_append(q[at], k[at], v[at], kc, vc, table[b:b + 1], lengths[b:b + 1], angles,
+                                         starts[b:b + 2] - starts[b], interleaved, bounds))
+            out = torch.cat(outs)
+        sides.append((out, kc, vc, bounds))
+    for a, b in zip(*sides):
+        assert torch.equal(a, b)
+
+
 def test_append_past_the_angles(mk):
     args, starts, bounds = append_inputs(22, [90, 100], [30, 40], 4, 2, 64, 16, F16, 32)
     args = list(args)
@@ -479,6 +551,16 @@ def test_select_head_groups(mk, hq, hkv):
 @pytest.mark.parametrize("pages,count", [(2100, 64), (2100, 2099), (2100, 2100), (2100, 2500), (513, 512), (9000, 1000)])
 def test_select_many_pages(mk, pages, count):
     check_select(mk, *select_inputs(pages, [16 * pages - 3], 2, 1, 64, 16, BF16), 16, count)
+
+
+@pytest.mark.parametrize("pages,count", [(4095, 30), (4096, 4000), (4097, 4000), (4097, 1), (16385, 64), (16386, 3000)])
+def test_select_registers_lds_and_memory(mk, pages, count):
+    check_select(mk, *select_inputs(pages, [16 * pages - 5, 16 * (pages // 2), 16], 2, 1, 64, 16, F16), 16, count)
+
+
+def test_select_many_rows(mk):
+    lengths = [(i * 997) % 9000 + 1 if i % 9 else 0 for i in range(40)]
+    check_select(mk, *select_inputs(77, lengths, 8, 8, 64, 16, BF16), 16, 12)
 
 
 def test_select_equal_scores(mk):
