@@ -6,8 +6,9 @@
 // A head is D / 16 threads, each with two 16-byte pieces that hold eight pairs.
 // Nothing is read twice but the angles.  Prompts are bound by memory (24
 // prompts of up to 4096 tokens, 64 + 16 heads of 128 with bounds, 605 MB read and written:
-// 111 us, 5.4 TB/s; a large copy reaches 4.8), a token per sequence by launch
-// latency (32 + 16 heads: 2.7 us; 128 sequences of 64 + 16 heads with bounds: 3.7).
+// 123 us, 4.9 TB/s, and 111 where the queries' last-level lines are written again; a large copy
+// reaches 4.8), a token per sequence by launch latency (32 + 16 heads: 2.7 us; 128
+// sequences of 64 + 16 heads with bounds: 3.7).
 #include <hip/hip_runtime.h>
 
 #include "kv.h"
