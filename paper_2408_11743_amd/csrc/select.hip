@@ -9,7 +9,7 @@
 // order of their positions.
 //
 // Latency bounds both kernels: 8 rows of 4063 pages are scored in 5.7 us (16.6
-// MB) and picked from in 9, 256 rows of 10 .. 1875 in 14.8 (48.7 MB) and 6.4.
+// MB) and picked from in 7, 256 rows of 10 .. 1875 in 14.8 (48.7 MB) and 6.4.
 #include <hip/hip_runtime.h>
 
 #include "kv.h"
@@ -144,15 +144,28 @@ __device__ __forceinline__ uint32_t wave_end(uint32_t x)
 // pages but the last reach: counts of the scores in 2048 equal parts
 // of their range, then of the part that holds it, until the part is one score or wanted whole
 // (the parts follow the range, so that few scores meet in one counter); then every page above it and the first ones equal to
-// it, in order.  A thread's pages are adjacent; up to kHeld of them, it reads their scores and entries
-// while the length is under way and keeps them in registers (HELD).  Of more, scores are read once
-// where kPickCached stay in LDS, as do the places of the chosen (4062 pages so: 26.9 us with scores and attention, HELD 24.5).
-constexpr int kPickBins = 2048, kPickCached = 16384, kHeld = 8;
+// it, in order.  A thread's pages are adjacent; HELD of them, it reads their scores and entries
+// while the length is under way, in vectors, and keeps them in registers.  Of more (HELD 0), scores are read in each
+// pass, and the entries of the chosen in the end (8125 pages so: 37.6 us with scores and attention, HELD 26.3).
+constexpr int kPickBins = 2048;
 
-template <bool HELD>
+// N adjacent words, in vectors aligned to a word.
+template <int N, typename T>
+__device__ __forceinline__ void load_unaligned(T (&to)[N], const T *from)
+{
+    constexpr int kVec = N < 4 ? N : 4;
+    typedef T vec __attribute__((ext_vector_type(kVec), aligned(4)));
+#pragma unroll
+    for (int i = 0; i < N; i += kVec) {
+        const vec x = *(const vec *)(from + i);
+#pragma unroll
+        for (int k = 0; k < kVec; ++k) to[i + k] = x[k];
+    }
+}
+
+template <int HELD>
 __global__ void __launch_bounds__(kPickThreads) page_pick_kernel(const SelectProblem p)
 {
-    __shared__ uint32_t cached[HELD ? 1 : kPickCached];
     __shared__ int bins[kPickBins], found[3];
     __shared__ Counts waves[2][kPickWaves];
     __shared__ uint32_t ends[2][kPickWaves];
@@ -160,17 +173,22 @@ __global__ void __launch_bounds__(kPickThreads) page_pick_kernel(const SelectPro
     const int b = blockIdx.x / p.kv_heads, kvh = blockIdx.x % p.kv_heads;
     const int32_t *table = p.table + b * p.table_row;
     const uint32_t *scores = p.scores + (int64_t)blockIdx.x * p.width;
-    uint32_t held[kHeld];
-    int32_t entry[kHeld];
-    const int spread = (p.width + kPickThreads - 1) / kPickThreads;
-    if (HELD)
+    uint32_t held[HELD ? HELD : 1];
+    int32_t entry[HELD ? HELD : 1];
+    if constexpr (HELD > 0) {
+        const int first = HELD * tid;
+        if (first + HELD <= p.width) {
+            load_unaligned(held, scores + first);
+            load_unaligned(entry, table + first);
+        } else {
 #pragma unroll
-        for (int k = 0; k < kHeld; ++k) {
-            if (k >= spread) break;
-            const int i = spread * tid + k < p.width ? spread * tid + k : 0;
-            held[k] = scores[i];
-            entry[k] = table[i];
+            for (int k = 0; k < HELD; ++k)
+                if (first + k < p.width) {
+                    held[k] = scores[first + k];
+                    entry[k] = table[first + k];
+                }
         }
+    }
     const int pages = pages_of(p, b);
     int32_t *out = p.chosen + (int64_t)blockIdx.x * p.select;
     if (kvh == 0 && tid == 0) {
@@ -182,19 +200,19 @@ __global__ void __launch_bounds__(kPickThreads) page_pick_kernel(const SelectPro
         return;
     }
     const int n = pages - 1;  // the last page is chosen anyway
-    const int per = HELD ? spread : (n + kPickThreads - 1) / kPickThreads, i0 = tid * per < n ? tid * per : n, i1 = i0 + per < n ? i0 + per : n;
-    const bool in_lds = n <= kPickCached;
-    auto score = [&](int i) { return in_lds ? cached[i] : scores[i]; };
+    const int per = HELD ? HELD : (n + kPickThreads - 1) / kPickThreads, i0 = tid * per < n ? tid * per : n, i1 = i0 + per < n ? i0 + per : n;
     // the scores, a thread's in order (any: in whatever order)
     auto each = [&](bool any, auto &&f) {
-        if (HELD) {
+        if constexpr (HELD > 0) {
 #pragma unroll
-            for (int k = 0; k < kHeld; ++k)
+            for (int k = 0; k < HELD; ++k)
                 if (i0 + k < i1) f(k, held[k]);
         } else if (any) {
-            for (int i = tid; i < n; i += kPickThreads) f(i, score(i));
+#pragma unroll 8
+            for (int i = tid; i < n; i += kPickThreads) f(i, scores[i]);
         } else {
-            for (int i = i0; i < i1; ++i) f(i, score(i));
+#pragma unroll 4
+            for (int i = i0; i < i1; ++i) f(i, scores[i]);
         }
     };
     int want = p.select - 1;  // of the pages with scores from lo to hi; those above hi are chosen
@@ -203,16 +221,7 @@ __global__ void __launch_bounds__(kPickThreads) page_pick_kernel(const SelectPro
         lo = s < lo ? s : lo;
         hi = s > hi ? s : hi;
     };
-    if (HELD) {
-        each(true, [&](int, uint32_t s) { widen(s); });
-    } else {
-#pragma unroll 8
-        for (int i = tid; i < n; i += kPickThreads) {
-            const uint32_t s = scores[i];
-            if (in_lds) cached[i] = s;
-            widen(s);
-        }
-    }
+    each(true, [&](int, uint32_t s) { widen(s); });
     for (int i = tid; i < kPickBins; i += kPickThreads) bins[i] = 0;
     lo = wave_end<true>(lo);
     hi = wave_end<false>(hi);
@@ -300,10 +309,21 @@ hipError_t launch_one(const SelectProblem &p, hipStream_t stream)
     constexpr int kPer = 16 * kScoreWaves;
     const int blocks = (p.width + kPer - 1) / kPer;
     hipLaunchKernelGGL((page_score_kernel<T, D>), dim3(blocks * p.B * p.kv_heads), dim3(64 * kScoreWaves), 0, stream, p, blocks);
-    if (p.width <= kPickThreads * kHeld)
-        hipLaunchKernelGGL(page_pick_kernel<true>, dim3(p.B * p.kv_heads), dim3(kPickThreads), 0, stream, p);
+    const dim3 rows(p.B * p.kv_heads), threads(kPickThreads);
+    if (p.width <= kPickThreads)
+        hipLaunchKernelGGL(page_pick_kernel<1>, rows, threads, 0, stream, p);
+    else if (p.width <= 2 * kPickThreads)
+        hipLaunchKernelGGL(page_pick_kernel<2>, rows, threads, 0, stream, p);
+    else if (p.width <= 4 * kPickThreads)
+        hipLaunchKernelGGL(page_pick_kernel<4>, rows, threads, 0, stream, p);
+    else if (p.width <= 8 * kPickThreads)
+        hipLaunchKernelGGL(page_pick_kernel<8>, rows, threads, 0, stream, p);
+    else if (p.width <= 16 * kPickThreads)
+        hipLaunchKernelGGL(page_pick_kernel<16>, rows, threads, 0, stream, p);
+    else if (p.width <= 32 * kPickThreads)
+        hipLaunchKernelGGL(page_pick_kernel<32>, rows, threads, 0, stream, p);
     else
-        hipLaunchKernelGGL(page_pick_kernel<false>, dim3(p.B * p.kv_heads), dim3(kPickThreads), 0, stream, p);
+        hipLaunchKernelGGL(page_pick_kernel<0>, rows, threads, 0, stream, p);
     return hipGetLastError();
 }
 
