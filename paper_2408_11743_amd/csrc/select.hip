@@ -8,8 +8,8 @@
 // a product over 2 D channels for the MFMAs, and the best `select` are kept in the
 // order of their positions.
 //
-// Latency bounds both kernels: 8 rows of 4063 pages are scored in 5.7 us (16.6
-// MB) and picked from in 7, 256 rows of 10 .. 1875 in 14.8 (48.7 MB) and 6.4.
+// Latency bounds both kernels: 8 rows of 4063 pages are scored in 5.6 us (16.6
+// MB) and picked from in 5.9, 256 rows of 10 .. 1875 in 14.8 (48.7 MB) and 5.9.
 #include <hip/hip_runtime.h>
 
 #include "kv.h"
