@@ -54,6 +54,8 @@ constexpr int kMinCut = 6, kMaxCut = 16;
 constexpr int kRowTiles = 2;
 // What a work-group gets at least where there is little.
 constexpr int kMinTiles = 8;
+// Floats of all contributors to a row from which on they are joined in teams.
+constexpr int kTeamFloats = 80 << 10;
 
 __device__ __forceinline__ int cap_tokens(const AttendProblem &p, int n)
 {
@@ -95,7 +97,7 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
     // one piece of a row per wave, and that of the row the range ends in
     __shared__ float4_t lds_acc[NW + 1][kAcc][64];
     __shared__ float lds_m[NW + 1][kHeadTile], lds_l[NW + 1][kHeadTile];
-    __shared__ int lds_within[NW], lds_flags[2], lds_first[2], lds_last[2];
+    __shared__ int lds_within[NW], lds_flags[3], lds_first[2], lds_last[2];
     __shared__ int lds_chunks[kKvMaxBatch / 64];
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -547,13 +549,21 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
         else
             join_slots(slots, put);
     }
+    // Many contributors are joined in teams (beside each other, the last to arrive joins the team's pieces into its first
+    // one's slot, and the last of those the teams'), as one compute unit reads 57 KB a us at most (one sequence of
+    // 102932 tokens, 5 heads of 256 over 1: 30.6 us, all by one work-group 54; 60000, 32 heads of 128 over 1: 21.1, 26.3; joins of 9 to
+    // 30 contributors, which take this path in one step, cost 0.2 us more for it).
+    constexpr int kTeam = 2 * NW;
+    auto in_teams = [&](int n, int row) { return n * heads_of(row) * D > kTeamFloats; };
     wait_vmcnt<0>();
     __syncthreads();
     if (tid < 2) {
         int flag = 0;
         if (tid == 0 ? wg_head : wg_tail && !one_row) {
-            const int first = lds_first[tid], others = lds_last[tid] - first;
-            uint32_t *const ctr = p.counters + kCounterStride * first;
+            const int first = lds_first[tid], n = lds_last[tid] - first + 1;
+            const int team = in_teams(n, tid == 0 ? wg_from.row : wg_to.row) ? first + (wg - first) / kTeam * kTeam : -1;
+            uint32_t *const ctr = p.counters + kCounterStride * (team < 0 ? first : team) + (team < 0 ? 0 : team == first ? 2 : 1);
+            const int others = (team < 0 ? n : first + n - team < kTeam ? first + n - team : kTeam) - 1;
             flag = __hip_atomic_fetch_add(ctr, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)others;
             if (flag) __hip_atomic_store(ctr, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         }
@@ -608,34 +618,61 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
             continue;
         }
         // Of more, a wave takes some of the contributors, then all take the waves'.
-        clear();
-        if (r < nh) {
-            struct Piece {
-                float m, l;
-                float4_t acc[kAcc];
-            };
-            auto load_piece = [&](int w, Piece &x) {
-                const int slot = (w * 2 + (w == first ? 1 : 0)) * (kSlotFloats * 4);
-#pragma unroll
-                for (int j = 0; j < kAcc; ++j) x.acc[j] = load_slot16(partials, slot, j * 1024 + lane * 16);
-                x.m = load_slot4(partials, slot, kHeadTile * D * 4 + r * 4);
-                x.l = load_slot4(partials, slot, kHeadTile * D * 4 + kHeadTile * 4 + r * 4);
-            };
-            constexpr int kAhead = 2;  // under way together
+        const bool teams = in_teams(last - first + 1, which == 0 ? wg_from.row : wg_to.row);
+        const int team = first + (wg - first) / kTeam * kTeam;
 #pragma unroll 1
-            for (int w = first + wave; w <= last; w += kAhead * NW) {
-                Piece x[kAhead];
+        for (int level = teams ? 0 : 1; level < 2; ++level) {
+            const int begin_w = level == 0 ? team : first, step_w = level == 1 && teams ? kTeam : 1;
+            const int end_w = level == 0 && team + kTeam - 1 < last ? team + kTeam - 1 : last;
+            clear();
+            if (r < nh) {
+                struct Piece {
+                    float m, l;
+                    float4_t acc[kAcc];
+                };
+                auto load_piece = [&](int w, Piece &x) {
+                    const int slot = (w * 2 + (w == first ? 1 : 0)) * (kSlotFloats * 4);
 #pragma unroll
-                for (int k = 0; k < kAhead; ++k)
-                    if (w + k * NW <= last) load_piece(w + k * NW, x[k]);
+                    for (int j = 0; j < kAcc; ++j) x.acc[j] = load_slot16(partials, slot, j * 1024 + lane * 16);
+                    x.m = load_slot4(partials, slot, kHeadTile * D * 4 + r * 4);
+                    x.l = load_slot4(partials, slot, kHeadTile * D * 4 + kHeadTile * 4 + r * 4);
+                };
+                constexpr int kAhead = 2;  // under way together
+#pragma unroll 1
+                for (int w = begin_w + wave * step_w; w <= end_w; w += kAhead * NW * step_w) {
+                    Piece x[kAhead];
 #pragma unroll
-                for (int k = 0; k < kAhead; ++k)
-                    if (w + k * NW <= last) join(x[k].m, x[k].l, x[k].acc);
+                    for (int k = 0; k < kAhead; ++k)
+                        if (w + k * NW * step_w <= end_w) load_piece(w + k * NW * step_w, x[k]);
+#pragma unroll
+                    for (int k = 0; k < kAhead; ++k)
+                        if (w + k * NW * step_w <= end_w) join(x[k].m, x[k].l, x[k].acc);
+                }
             }
+            put_piece(wave);
+            __syncthreads();
+            float *const slot = p.partials + ((int64_t)team * 2 + (team == first ? 1 : 0)) * kSlotFloats;
+            join_slots(all, [&](int j, float4_t o, float top, float sum) {
+                if (level == 1) return write(j, o, top, sum);
+                if (r >= nh) return;
+                store_partial16(slot, j, lane, o);
+                if (j == 0 && g == 0) {
+                    store_float(slot + kHeadTile * D + r, top);
+                    store_float(slot + kHeadTile * D + kHeadTile + r, sum);
+                }
+            });
+            if (level == 1) break;
+            wait_vmcnt<0>();
+            __syncthreads();
+            if (tid == 0) {
+                uint32_t *const ctr = p.counters + kCounterStride * first;
+                const bool done = __hip_atomic_fetch_add(ctr, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)((last - first) / kTeam);
+                if (done) __hip_atomic_store(ctr, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                lds_flags[2] = done;
+            }
+            __syncthreads();
+            if (!__builtin_amdgcn_readfirstlane(lds_flags[2])) break;
         }
-        put_piece(wave);
-        __syncthreads();
-        join_slots(all, write);
         __syncthreads();
     }
 }

@@ -269,6 +269,21 @@ def test_attention_repeats_bit_for_bit_and_leaves_its_counters(mk):
         assert torch.equal(mk.paged_attention(q, k, v, table, lengths, workspace=ws), first)
 
 
+@pytest.mark.parametrize("D,hq,lengths", [
+    (128, 16, [6001, 7000, 8100, 33]), (256, 16, [5000, 9000]), (256, 5, [21000]), (64, 16, [9001]), (128, 7, [16001, 16]),
+    (96, 32, [12000])])
+def test_attention_joins_in_teams(mk, D, hq, lengths):
+    """Rows of so many pieces that teams of work-groups join them: right, the same bits each time, counters left at zero."""
+    args = make(D + hq, lengths, hq, 1, D, 64, BF16)
+    check_attention(mk, *args)
+    args = [x.cuda() for x in args]
+    ws = mk.Workspace("cuda")
+    first = mk.paged_attention(*args, workspace=ws)
+    for _ in range(4):
+        assert torch.equal(mk.paged_attention(*args, workspace=ws), first)
+    assert int(ws.buf[:1 << 20].count_nonzero()) == 0
+
+
 def test_attention_on_another_stream(mk):
     q, k, v, table, lengths = make(17, [3000, 40, 900], 8, 2, 128, 16, F16)
     side = torch.cuda.Stream()
