@@ -102,7 +102,7 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int r = lane & 15, g = lane >> 4;
-    const int rows = p.kv_heads * p.head_tiles;  // of a sequence
+    const int rows = p.kv_heads;  // of a sequence
     constexpr int kStepKeys = kTileKeys * KT, kRowCost = kRowTiles / KT, kMinSteps = kMinTiles / KT;
     // a sequence without keys still has a step, in which its outputs are written
     auto steps_of = [](int tokens) { return tokens > 0 ? (tokens + kStepKeys - 1) / kStepKeys : 1; };
@@ -135,10 +135,13 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
     const int units = (total + kRowCost * p.B) * rows;
     // Range w starts at unit w * units / grid, rounded down, which puts borders between rows of one length; or, where
     // there are few, at w * kMinSteps.
-    // Ranges of a larger group's tiles, which read the same keys, lie side by side and go to one XCD's L2 (16 sequences of up to 30000
-    // tokens, 64 heads over 2: 103 us, in the order of the work-groups 145; one of 60000, 32 over 1: 26.4, 25.3). Other rows share
-    // nothing, and large caches go faster spread over the XCDs (64 sequences of 32768 tokens: 1.25 ms, 1.27).
-    const int grid = gridDim.x, wg = p.head_tiles > 1 ? xcd_local_wg(blockIdx.x, grid) : (int)blockIdx.x;
+    // A larger group's head tiles read the same keys: the work-groups of a range, one a tile, are neighbours on one XCD, whose L2
+    // they share (173 sequences of 4859 tokens, 32 heads over 1: 96 us; tiles one after the other as rows 120, and these spread over the XCDs
+    // 146 where they take 103 for 16 of up to 30000, 64 over 2). Other ranges share nothing, and large caches go faster spread over the XCDs (64
+    // sequences of 32768 tokens: 1.25 ms, 1.27).
+    const int tiles = p.head_tiles, grid = tiles == 1 ? gridDim.x : gridDim.x / tiles;
+    const int place = tiles == 1 ? blockIdx.x : xcd_local_wg(blockIdx.x, gridDim.x);
+    const int wg = tiles == 1 ? place : place / tiles, tile = place - wg * tiles;
     const bool few = units < grid * kMinSteps;
     int per = kMinSteps, extra = 0;
     if (!few) {
@@ -229,18 +232,11 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
     }
 
     // ---- the steps ----
-    // a row's kv head, its first query head and how many it has
-    auto kv_head_of = [&](int row) { return p.head_tiles == 1 ? row : row / p.head_tiles; };
-    auto head0_of = [&](int row) {
-        const int kvh = kv_head_of(row);
-        return kvh * p.group + (row - kvh * p.head_tiles) * kHeadTile;
-    };
-    auto heads_of = [&](int row) {
-        const int n = p.head_tiles == 1 ? p.group : p.group - row % p.head_tiles * kHeadTile;
-        return n < kHeadTile ? n : kHeadTile;
-    };
+    // a row's first query head of this work-group's, and how many they are
+    auto head0_of = [&](int row) { return row * p.group + tile * kHeadTile; };
+    const int nh = p.group - tile * kHeadTile < kHeadTile ? p.group - tile * kHeadTile : kHeadTile;
     auto table_of = [&](const Step &x) {
-        return p.table + x.b * p.table_row + kv_head_of(x.row) * p.table_head;
+        return p.table + x.b * p.table_row + x.row * p.table_head;
     };
     // the entries' loads (scalar) are issued a step before they are needed; past the row's tokens nothing is read
     auto entries = [&](Step &x) {
@@ -270,13 +266,13 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
     uint32_t vr[KT][4][kHalves][kDw] = {};
     auto load_queries = [&](const Step &x) {
         const T *q = (const T *)p.q + x.b * p.q_row + (head0_of(x.row) + r) * p.q_head + 8 * g;
-        const bool have = r < heads_of(x.row);
+        const bool have = r < nh;
 #pragma unroll
         for (int t = 0; t < kQ; ++t) qf[t] = have ? *(const vec8 *)(q + 32 * t) : vec8{};
     };
     // a tile's first element in the caches; an entry that names no page is read as page 0 and masked
     auto tile_at = [&](const Step &x, int u) -> int64_t {
-        const int e = x.e[u], kvh = kv_head_of(x.row);
+        const int e = x.e[u], kvh = x.row;
         const int slot = (x.s * kStepKeys + kTileKeys * u) & ((1 << p.page_shift) - 1);
         return ((((int64_t)((uint32_t)e < (uint32_t)p.pages ? e : 0) * p.kv_heads + kvh) << p.page_shift) + slot) * D;
     };
@@ -285,7 +281,7 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
     // of up to 9001 tokens, heads of 256, 30.3 us, values alone 29.1, neither 28.8), until
     // the keys and values are more than the last-level cache holds (131071 tokens, 537 MB: 88, 90, 99 us).
     // Rows of 192 bytes straddle lines (d = 96, 3 GB: 487, 462, 517 us), and the tiles of a larger group read the keys again.
-    const bool stream_keys = D != 96 && p.head_tiles == 1 && total * rows > ((256 << 20) / (kStepKeys * 4 * D));
+    const bool stream_keys = D != 96 && tiles == 1 && total * rows > ((256 << 20) / (kStepKeys * 4 * D));
     auto load_keys = [&](const Step &x) {
 #pragma unroll
         for (int u = 0; u < KT; ++u) {
@@ -312,6 +308,8 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
     };
     float4_t acc[kAcc];
     float m, l;
+    // slots and counters of this tile's work-group of range w
+    auto group_of = [&](int w) { return w * tiles + tile; };
     auto clear = [&] {
 #pragma unroll
         for (int j = 0; j < kAcc; ++j) acc[j] = float4_t{0.f, 0.f, 0.f, 0.f};
@@ -343,7 +341,7 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
     };
     // The finished row: lane (r, g) holds head r's channels kCh (4g + i) + j.
     auto write_row = [&](int b, int row) {
-        if (r >= heads_of(row)) return;
+        if (r >= nh) return;
         const int64_t at = (int64_t)b * p.heads + head0_of(row) + r;
         const float inv = l == 0.f ? 0.f : 1.f / l;  // no key: zero
 #pragma unroll
@@ -532,8 +530,7 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
         // and the waves after that one
         const uint32_t slots = which == 0 ? (inner == all ? all : ((~inner & (inner + 1)) << 1) - 1)
                                           : (all & ~((2u << (31 - __builtin_clz(~inner & all))) - 1)) | 1u << NW;
-        float *const slot = p.partials + ((int64_t)wg * 2 + which) * kSlotFloats;
-        const int nh = heads_of(which == 0 ? wg_from.row : wg_to.row);
+        float *const slot = p.partials + ((int64_t)group_of(wg) * 2 + which) * kSlotFloats;
         auto put = [&](int j, float4_t o, float top, float sum) {
             if (r >= nh) return;
             store_partial16(slot, j, lane, o);
@@ -554,15 +551,15 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
     // 102932 tokens, 5 heads of 256 over 1: 30.6 us, all by one work-group 54; 60000, 32 heads of 128 over 1: 21.1, 26.3; joins of 9 to
     // 30 contributors, which take this path in one step, cost 0.2 us more for it).
     constexpr int kTeam = 2 * NW;
-    auto in_teams = [&](int n, int row) { return n * heads_of(row) * D > kTeamFloats; };
+    auto in_teams = [&](int n) { return n * nh * D > kTeamFloats; };
     wait_vmcnt<0>();
     __syncthreads();
     if (tid < 2) {
         int flag = 0;
         if (tid == 0 ? wg_head : wg_tail && !one_row) {
             const int first = lds_first[tid], n = lds_last[tid] - first + 1;
-            const int team = in_teams(n, tid == 0 ? wg_from.row : wg_to.row) ? first + (wg - first) / kTeam * kTeam : -1;
-            uint32_t *const ctr = p.counters + kCounterStride * (team < 0 ? first : team) + (team < 0 ? 0 : team == first ? 2 : 1);
+            const int team = in_teams(n) ? first + (wg - first) / kTeam * kTeam : -1;
+            uint32_t *const ctr = p.counters + kCounterStride * group_of(team < 0 ? first : team) + (team < 0 ? 0 : team == first ? 2 : 1);
             const int others = (team < 0 ? n : first + n - team < kTeam ? first + n - team : kTeam) - 1;
             flag = __hip_atomic_fetch_add(ctr, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)others;
             if (flag) __hip_atomic_store(ctr, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -576,7 +573,7 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
         const int first = __builtin_amdgcn_readfirstlane(lds_first[which]), last = __builtin_amdgcn_readfirstlane(lds_last[which]);
         const __amdgpu_buffer_rsrc_t partials =
             __builtin_amdgcn_make_buffer_rsrc((void *)p.partials, (short)0, 0x7fffffffu, kBufferFlags);
-        const int b = which == 0 ? wg_from.b : wg_to.b, row = which == 0 ? wg_from.row : wg_to.row, nh = heads_of(row);
+        const int b = which == 0 ? wg_from.b : wg_to.b, row = which == 0 ? wg_from.row : wg_to.row;
         auto write = [&](int j, float4_t o, float top, float sum) {
             if (r >= nh) return;
             const int64_t at = (int64_t)b * p.heads + head0_of(row) + r;
@@ -597,7 +594,7 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
 #pragma unroll
                 for (int k = 0; k < kFew; ++k)
                     if (first + k <= last) {
-                        const int slot = ((first + k) * 2 + (k == 0 ? 1 : 0)) * (kSlotFloats * 4);
+                        const int slot = (group_of(first + k) * 2 + (k == 0 ? 1 : 0)) * (kSlotFloats * 4);
                         mk[k] = load_slot4(partials, slot, kHeadTile * D * 4 + r * 4);
                         lk[k] = load_slot4(partials, slot, kHeadTile * D * 4 + kHeadTile * 4 + r * 4);
                         a[k] = load_slot16(partials, slot, j * 1024 + lane * 16);
@@ -618,7 +615,7 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
             continue;
         }
         // Of more, a wave takes some of the contributors, then all take the waves'.
-        const bool teams = in_teams(last - first + 1, which == 0 ? wg_from.row : wg_to.row);
+        const bool teams = in_teams(last - first + 1);
         const int team = first + (wg - first) / kTeam * kTeam;
 #pragma unroll 1
         for (int level = teams ? 0 : 1; level < 2; ++level) {
@@ -631,7 +628,7 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
                     float4_t acc[kAcc];
                 };
                 auto load_piece = [&](int w, Piece &x) {
-                    const int slot = (w * 2 + (w == first ? 1 : 0)) * (kSlotFloats * 4);
+                    const int slot = (group_of(w) * 2 + (w == first ? 1 : 0)) * (kSlotFloats * 4);
 #pragma unroll
                     for (int j = 0; j < kAcc; ++j) x.acc[j] = load_slot16(partials, slot, j * 1024 + lane * 16);
                     x.m = load_slot4(partials, slot, kHeadTile * D * 4 + r * 4);
@@ -651,7 +648,7 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
             }
             put_piece(wave);
             __syncthreads();
-            float *const slot = p.partials + ((int64_t)team * 2 + (team == first ? 1 : 0)) * kSlotFloats;
+            float *const slot = p.partials + ((int64_t)group_of(team) * 2 + (team == first ? 1 : 0)) * kSlotFloats;
             join_slots(all, [&](int j, float4_t o, float top, float sum) {
                 if (level == 1) return write(j, o, top, sum);
                 if (r >= nh) return;
@@ -665,7 +662,7 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
             wait_vmcnt<0>();
             __syncthreads();
             if (tid == 0) {
-                uint32_t *const ctr = p.counters + kCounterStride * first;
+                uint32_t *const ctr = p.counters + kCounterStride * group_of(first);
                 const bool done = __hip_atomic_fetch_add(ctr, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)((last - first) / kTeam);
                 if (done) __hip_atomic_store(ctr, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
                 lds_flags[2] = done;
@@ -680,14 +677,15 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
 template <typename T, int D>
 hipError_t launch_one(const AttendProblem &p, int cus, hipStream_t stream)
 {
-    const int grid = (cus < kKvMaxCus ? cus : kKvMaxCus) * kAttendGroupsPerCu;
+    const int groups = (cus < kKvMaxCus ? cus : kKvMaxCus) * kAttendGroupsPerCu;
+    const int ranges = groups > p.head_tiles ? groups / p.head_tiles : 1;  // at most 64 tiles
     // Wide heads: one tile a step, which keeps the registers and divides short ranges finer (heads of 256, 20 sequences of up
     // to 9001 tokens 27.8 us, two tiles 30.6; 16 of 30000: 158, 168).  Narrower ones: two, fewer round trips in short
     // ranges (one sequence of 2000, heads of 128: 10.4 us, one tile 11.1).
     constexpr int kTiles = D > 128 ? 1 : 2;
     AttendProblem q = p;
-    q.grid_reciprocal = grid > 1 ? (uint32_t)(((uint64_t)1 << 32) / (uint64_t)grid) : 0xFFFFFFFFu;
-    hipLaunchKernelGGL((paged_attention_kernel<T, D, kAttendWaves, kTiles>), dim3(grid), dim3(64 * kAttendWaves), 0, stream, q);
+    q.grid_reciprocal = ranges > 1 ? (uint32_t)(((uint64_t)1 << 32) / (uint64_t)ranges) : 0xFFFFFFFFu;
+    hipLaunchKernelGGL((paged_attention_kernel<T, D, kAttendWaves, kTiles>), dim3(ranges * p.head_tiles), dim3(64 * kAttendWaves), 0, stream, q);
     return hipGetLastError();
 }
 

@@ -36,7 +36,7 @@ struct AttendProblem {
     int B, heads, kv_heads, group, head_tiles;
     int page_shift, width, pages;
     float scale_log2;  // scale * log2(e)
-    uint32_t grid_reciprocal;  // floor(2^32 / work-groups)
+    uint32_t grid_reciprocal;  // floor(2^32 / ranges)
 };
 
 hipError_t launch_attend(const AttendProblem &p, int head_dim, marlin_dtype_t dtype, int cus, hipStream_t stream);
