@@ -17,8 +17,8 @@
 //     keys' elements with v_perm, which is the whole transpose.
 //
 // The work is split evenly however ragged the lengths are: the rows'
-// steps are numbered through, every work-group (one a compute unit) takes an
-// equal range of them, found from the lengths on the device, and its eight
+// steps are numbered through, every work-group (one a compute unit; where a kv head has
+// more than 16 query heads, one a range and tile) takes an equal range of them, found from the lengths on the device, and its eight
 // waves share it.  Rows that lie within one wave's share go from its registers
 // to the output.  Pieces of rows cut between the waves are joined in LDS; what a
 // work-group has of rows cut at its borders it leaves in the workspace, and whoever
@@ -65,7 +65,7 @@ __device__ __forceinline__ int cap_tokens(const AttendProblem &p, int n)
 
 // Where a range begins or ends: a step of a row.
 struct Place {
-    int b, row;  // sequence, and its row: kv head and head tile
+    int b, row;  // sequence, and its row: kv head
     int step;    // of the row
     int before;  // steps of all rows before it
     int steps;   // the row's (where step > 0)
