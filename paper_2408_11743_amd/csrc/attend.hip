@@ -343,7 +343,7 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
     auto write_row = [&](int b, int row) {
         if (r >= nh) return;
         const int64_t at = (int64_t)b * p.heads + head0_of(row) + r;
-        const float inv = l == 0.f ? 0.f : 1.f / l;  // no key: zero
+        const float inv = l == 0.f ? 0.f : 1.f / (l * E::kWeightUnit);  // no key: zero
 #pragma unroll
         for (int hf = 0; hf < kHalves; ++hf)
 #pragma unroll
@@ -427,11 +427,39 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
                 for (int i = 0; i < 4; ++i) pr[u][i] = __builtin_amdgcn_exp2f(sc[u][i] - ref);
 #pragma unroll
             for (int u = 0; u < KT; ++u) l += (pr[u][0] + pr[u][1]) + (pr[u][2] + pr[u][3]);
-            // The weights go to the second product in the cache's type, as its MFMAs want them: half an ulp each, the size of
-            // the output's own rounding, with the sum l kept of the unrounded ones.
-            weights_t pf;
+            // The second product takes the weights in the cache's type, as its MFMAs want them, in two parts: rounded, and what
+            // that left out, rounded.  Together they hold 22 bits of a float16 cache's weights and 16 of a bfloat16 one's,
+            // float16's times 2^15, so that those far below the maximum are no subnormals (an absolute 2^-40 of it is all that is lost).
+            weights_t pf, rest;
 #pragma unroll
-            for (int e = 0; e < 4 * KT; ++e) pf[e] = (T)pr[e >> 2][e & 3];
+            for (int e = 0; e < 4 * KT; ++e) {
+                const float x = pr[e >> 2][e & 3] * E::kWeightUnit;
+                pf[e] = (T)x;
+                rest[e] = (T)(x - (float)pf[e]);
+            }
+            float odd = 0.f;
+#pragma unroll
+            for (int u = 0; u < KT; ++u)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int hf = 0; hf < kHalves; ++hf)
+#pragma unroll
+                        for (int w = 0; w < kDw; ++w) odd = E::times_zero(vr[u][i][hf][w], odd);
+            if (__any(odd != 0.f)) {  // with an infinite value, both parts of a weight above zero have to be above zero
+#pragma unroll
+                for (int e = 0; e < 4 * KT; ++e) {
+                    const float x = pr[e >> 2][e & 3] * E::kWeightUnit;
+                    if (!(x > 0.f)) continue;
+                    T part = pf[e];  // named: a bit cast of a vector's element yields the first one
+                    uint16_t bits = __builtin_bit_cast(uint16_t, part);
+                    if ((float)part > x) --bits;  // towards zero
+                    part = __builtin_bit_cast(T, bits < E::kSmallest ? E::kSmallest : bits);
+                    const T left_out = (T)(x - (float)part);
+                    pf[e] = part;
+                    rest[e] = (float)left_out > 0.f ? left_out : __builtin_bit_cast(T, E::kSmallest);
+                }
+            }
 #pragma unroll
             for (int hf = 0; hf < kHalves; ++hf)
 #pragma unroll
@@ -441,7 +469,9 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
                     for (int e = 0; e < 2 * KT; ++e)
                         w[e] = __builtin_amdgcn_perm(vr[e >> 1][2 * (e & 1) + 1][hf][j >> 1], vr[e >> 1][2 * (e & 1)][hf][j >> 1],
                                                      (j & 1) ? 0x07060302u : 0x05040100u);
-                    acc[hf * kCh + j] = E::mfma(__builtin_bit_cast(weights_t, w), pf, acc[hf * kCh + j]);
+                    const weights_t x = __builtin_bit_cast(weights_t, w);
+                    acc[hf * kCh + j] = E::mfma(x, pf, acc[hf * kCh + j]);
+                    acc[hf * kCh + j] = E::mfma(x, rest, acc[hf * kCh + j]);
                 }
             issue_order_point();
             if (left > 1) load_values(next);
@@ -577,7 +607,7 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
         auto write = [&](int j, float4_t o, float top, float sum) {
             if (r >= nh) return;
             const int64_t at = (int64_t)b * p.heads + head0_of(row) + r;
-            const float inv = sum == 0.f ? 0.f : 1.f / sum;
+            const float inv = sum == 0.f ? 0.f : 1.f / (sum * E::kWeightUnit);
 #pragma unroll
             for (int i = 0; i < 4; ++i)
                 ((T *)p.out)[at * D + 128 * (j / kCh) + kCh * (4 * g + i) + j % kCh] = (T)(o[i] * inv);

@@ -15,6 +15,13 @@ template <>
 struct Elem<_Float16> {
     typedef _Float16 vec8 __attribute__((ext_vector_type(8)));
     typedef _Float16 vec4 __attribute__((ext_vector_type(4)));
+    static constexpr float kWeightUnit = 32768.f;  // what a softmax weight of one is in the second product (see attend.hip)
+    static constexpr uint16_t kSmallest = 0x0001;  // the bits of 2^-24
+    // c, or not a number if one of the two elements is no finite one
+    static __device__ __forceinline__ float times_zero(uint32_t x, float c)
+    {
+        return __builtin_amdgcn_fdot2(__builtin_bit_cast(half2_t, x), half2_t{}, c, false);
+    }
     static __device__ __forceinline__ float4_t mfma(vec8 a, vec8 b, float4_t c)
     {
         return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
@@ -29,6 +36,13 @@ template <>
 struct Elem<__bf16> {
     typedef __bf16 vec8 __attribute__((ext_vector_type(8)));
     typedef __bf16 vec4 __attribute__((ext_vector_type(4)));
+    static constexpr float kWeightUnit = 1.f;
+    static constexpr uint16_t kSmallest = 0x0080;  // 2^-126
+    static __device__ __forceinline__ float times_zero(uint32_t x, float c)
+    {
+        typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+        return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, x), bf16x2_t{}, c, false);
+    }
     static __device__ __forceinline__ float4_t mfma(vec8 a, vec8 b, float4_t c)
     {
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);

@@ -1,0 +1,132 @@
+"""The paged key-value cache operators where a result can go wrong without a
+crash: weights far below a row's maximum, infinite values, and the limits of
+sizes and lengths.  References are 64-bit forms written here or in kv_reference.py.
+"""
+import math
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+import kv_reference as ref  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+
+F16, BF16 = torch.float16, torch.bfloat16
+WEIGHT = {F16: 2.0 ** -22, BF16: 2.0 ** -17}   # a softmax weight's relative error in the second product
+LOST = {F16: 2.0 ** -40, BF16: 2.0 ** -126}    # and its absolute one, of the row's maximum
+
+
+@pytest.fixture(scope="module")
+def mk():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    import paper_2408_11743_amd as mk
+    mk.lib()
+    return mk
+
+
+def gen(seed):
+    return torch.Generator().manual_seed(seed)
+
+
+def paged(x, ps):
+    """[n, heads, D] tokens of one sequence as pages [pages, heads, ps, D], whose last slots hold NaN."""
+    n, heads, D = x.shape
+    pages = -(-n // ps)
+    out = torch.full((pages * ps, heads, D), math.nan, dtype=x.dtype)
+    out[:n] = x
+    return out.view(pages, ps, heads, D).transpose(1, 2).contiguous()
+
+
+def one_sequence(mk, q, keys, values, ps=64, **kw):
+    """Attention of q [heads, D] over keys and values [n, kv heads, D] in pages in order: out and lse, 64 bits."""
+    k, v = paged(keys, ps).cuda(), paged(values, ps).cuda()
+    table = torch.arange(k.shape[0], dtype=torch.int32, device="cuda")[None]
+    lengths = torch.tensor([len(keys)], dtype=torch.int32, device="cuda")
+    out, lse = mk.paged_attention(q[None].cuda(), k, v, table, lengths, return_lse=True, **kw)
+    return out[0].cpu().double(), lse[0].cpu().double()
+
+
+def exact(q, keys, values):
+    """out, lse and the bounds of their errors: weights held to WEIGHT and LOST, everything else as in kv_reference.py."""
+    heads, D = q.shape
+    kv_heads = keys.shape[1]
+    u, tiny = ref.U[q.dtype], ref.TINY[q.dtype]
+    out, tol = torch.zeros(heads, D, dtype=torch.float64), torch.zeros(heads, D, dtype=torch.float64)
+    lse, tol_lse = torch.zeros(heads, dtype=torch.float64), torch.zeros(heads, dtype=torch.float64)
+    for h in range(heads):
+        kvh = h // (heads // kv_heads)
+        products = keys[:, kvh].double() * q[h].double()
+        s = products.sum(1) * D ** -0.5
+        e = torch.exp(s - s.max())
+        total, v = e.sum(), values[:, kvh].double()
+        out[h] = (e[:, None] * v).sum(0) / total
+        lse[h] = s.max() + torch.log(total)
+        off = D * 2.0 ** -24 * float(products.abs().sum(1).max()) * D ** -0.5 + 2.0 ** -21 * float(s.abs().max())
+        spread = (e[:, None] * v.abs()).sum(0) / total
+        tol[h] = u * out[h].abs() + tiny + (WEIGHT[q.dtype] + 2 * off + 2.0 ** -18) * spread + LOST[q.dtype] * v.abs().sum(0) / total
+        tol_lse[h] = off + 2.0 ** -21 * (1 + abs(float(lse[h]))) + 2.0 ** -20
+    return out, lse, tol, tol_lse
+
+
+# ---- softmax weights ----
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("D", [64, 96, 128, 256])
+@pytest.mark.parametrize("n", [2, 40, 700])
+def test_attention_of_values_that_cancel(mk, dtype, D, n):
+    """Values of either sign around zero: an error of the weights stands out against the output's rounding."""
+    g = gen(D + n)
+    q = torch.randn(4, D, generator=g).to(dtype)
+    keys = torch.randn(n, 2, D, generator=g).to(dtype)
+    values = torch.randn(n, 2, D, generator=g).to(dtype)
+    out, _, _, _ = exact(q, keys, values)
+    # one more key of weight close to the rest's takes the sum to about zero
+    values[0] -= (out.view(2, 2, D).mean(1) * n / 2).to(dtype)
+    want, want_lse, tol, tol_lse = exact(q, keys, values)
+    got, lse = one_sequence(mk, q, keys, values)
+    assert ((got - want).abs() <= tol).all()
+    assert ((lse - want_lse).abs() <= tol_lse).all()
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("n,gap", [(131071, 17.5), (131071, 14.0), (20000, 16.0), (8192, 17.0), (100, 12.0)])
+@pytest.mark.parametrize("at", [0.0, 0.6])
+def test_attention_of_many_keys_far_below_one(mk, dtype, n, gap, at):
+    """One key whose value is zero, `gap` above all others: what the others' small weights add up to is the whole output."""
+    D, g = 64, gen(n)
+    q = torch.zeros(2, D).to(dtype)
+    q[:, 0] = 8.0
+    keys = torch.zeros(n, 1, D).to(dtype)
+    keys[int(at * n), 0, 0] = gap
+    values = (0.5 + torch.rand(n, 1, D, generator=g)).to(dtype)
+    values[int(at * n)] = 0
+    want, want_lse, tol, tol_lse = exact(q, keys, values)
+    got, lse = one_sequence(mk, q, keys, values)
+    assert ((got - want).abs() <= tol).all()
+    assert ((lse - want_lse).abs() <= tol_lse).all()
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("D", [64, 96, 128, 256])
+@pytest.mark.parametrize("n", [1, 40, 3000])
+@pytest.mark.parametrize("equal", [True, False])
+def test_attention_of_infinite_values(mk, dtype, D, n, equal):
+    """A weight above zero times an infinity is that infinity, whatever is left of the weight beside its first part
+    (`equal`: weights of one, of which nothing is left); of both signs it is no number; other channels do not see it."""
+    g = gen(D + n)
+    q = torch.zeros(2, D).to(dtype) if equal else torch.randn(2, D, generator=g).to(dtype)
+    keys = torch.randn(n, 1, D, generator=g).to(dtype)
+    values = torch.randn(n, 1, D, generator=g).to(dtype)
+    want, _, tol, _ = exact(q, keys, values)
+    values[n // 2, 0, 3] = math.inf
+    values[n // 3, 0, D - 1] = -math.inf
+    values[n // 2, 0, 9] = math.nan
+    if n > 1:
+        values[0, 0, 5], values[n - 1, 0, 5] = math.inf, -math.inf
+    got, _ = one_sequence(mk, q, keys, values)
+    assert (got[:, 3] == math.inf).all() and (got[:, D - 1] == -math.inf).all() and torch.isnan(got[:, 9]).all()
+    rest = [c for c in range(D) if c not in (3, 9, D - 1) + ((5,) if n > 1 else ())]
+    assert n == 1 or torch.isnan(got[:, 5]).all()
+    assert ((got - want).abs()[:, rest] <= tol[:, rest]).all()
