@@ -193,9 +193,10 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
         const int at = __builtin_ctzll(past);
         const int cb = __builtin_amdgcn_readlane(count, at);
         const int off = u - __builtin_amdgcn_readlane(ends, at) + (cb + cost) * rows;
-        // off / (cb + cost): the lanes count the rows that end by then
+        // off / (cb + cost): the lanes count the rows that end by then.  The last row's does not, and lanes from there on have none: their
+        // products pass 32 bits for 2^30 tokens of wide heads (64 * 2^26 steps), those of the others are units of the numbering.
         const int row = rows == 1 ? 0
-                        : rows <= 64 ? __popcll(__builtin_amdgcn_ballot_w64((uint32_t)(lane + 1) * (uint32_t)(cb + cost) <= (uint32_t)off))
+                        : rows <= 64 ? __popcll(__builtin_amdgcn_ballot_w64(lane + 1 < rows && (lane + 1) * (cb + cost) <= off))
                                      : (uint32_t)off / (uint32_t)(cb + cost);
         const int step = off - row * (cb + cost) - cost;
         return {b0 + at, row, step < 0 ? 0 : step, u - off - cost * (b0 + at) * rows + row * cb, cb, __builtin_amdgcn_readlane(length, at)};

@@ -130,3 +130,27 @@ def test_attention_of_infinite_values(mk, dtype, D, n, equal):
     rest = [c for c in range(D) if c not in (3, 9, D - 1) + ((5,) if n > 1 else ())]
     assert n == 1 or torch.isnan(got[:, 5]).all()
     assert ((got - want).abs()[:, rest] <= tol[:, rest]).all()
+
+
+# ---- limits ----
+
+@pytest.mark.parametrize("D,hkv,short", [(256, 2, 0), (256, 2, 47), (256, 5, 1), (128, 3, 0)])
+def test_attention_of_the_longest_sequence(mk, D, hkv, short):
+    """2^30 tokens (a table may name a page many times): the row that a step belongs to is found where the steps of 64 rows pass
+    32 bits.  Weights are all one and values small integers, so that sums are exact until pieces are joined."""
+    ps, n = 1024, (1 << 30) - short
+    g = gen(D + hkv)
+    values = torch.randint(-3, 4, (2, hkv, ps, D), generator=g)
+    table = torch.randint(0, 2, (1, n // ps + (n % ps > 0)), generator=g, dtype=torch.int32)
+    k = torch.zeros(2, hkv, ps, D, dtype=BF16, device="cuda")
+    lengths = torch.tensor([n], dtype=torch.int32, device="cuda")
+    q = torch.zeros(1, hkv, D, dtype=BF16, device="cuda")
+    out, lse = mk.paged_attention(q, k, values.to(BF16).cuda(), table.cuda(), lengths, return_lse=True)
+    torch.cuda.synchronize()
+    left = ps - short if short else ps
+    named = torch.bincount(table[0, :-1].long(), minlength=2).double()
+    total = (named[:, None, None] * values.sum(2)).sum(0) + values[table[0, -1], :, :left].sum(1)
+    size = (named[:, None, None] * values.abs().sum(2)).sum(0) + values[table[0, -1], :, :left].abs().sum(1)
+    want, spread = total.double() / n, size.double() / n
+    assert ((out[0].cpu().double() - want).abs() <= 2.0 ** -8 * want.abs() + 2.0 ** -18 * spread).all()
+    assert ((lse[0].cpu().double() - math.log(n)).abs() <= 2.0 ** -18).all()
