@@ -129,13 +129,14 @@ def _check_out(func: str, out: torch.Tensor, shape, dtype, device) -> None:
 _empty_like, _contiguous = torch.empty_like, torch.contiguous_format
 
 
-def _workspace(index: int, stream: int, workspace, nbytes: int) -> torch.Tensor:
+def _workspace(func: str, index: int, stream: int, workspace, nbytes: int) -> torch.Tensor:
     """The caller's workspace, or the one ``ops.gemm`` uses on this device and stream, of nbytes at least."""
     if workspace is None:
         workspace = ops._default_ws.get((index, stream))
         if workspace is None:
             workspace = ops._default_ws.setdefault((index, stream), ops.Workspace("cuda:%d" % index))
     buf = workspace.buf
+    _need(buf.is_cuda and buf.device.index == index and buf.is_contiguous(), func, "the workspace must be on the device of the tensors")
     return buf if buf.numel() >= nbytes else workspace.ensure(nbytes)
 
 
@@ -240,7 +241,7 @@ def paged_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tenso
     sizes = (n, heads, kv_heads, D, pages, page_size, ts[-1], 1.0 / math.sqrt(D) if scale is None else scale,
              _DTYPE[dtype])
     for nbytes in (0, B.marlin_paged_attention_workspace_bytes(D)):  # grown if the call says WORKSPACE_TOO_SMALL
-        buf = _workspace(dev, stream, workspace, nbytes)
+        buf = _workspace(f, dev, stream, workspace, nbytes)
         with torch.cuda.device(dev):
             status = B.lib().marlin_paged_attention(
                 B.pack_paged_attention(*ptrs, buf.data_ptr(), buf.numel(), *sizes), stream)
@@ -284,7 +285,7 @@ def select_pages(q: torch.Tensor, bounds: torch.Tensor, table: torch.Tensor, len
             tokens.data_ptr())
     sizes = (n, heads, kv_heads, D, pages, page_size, width, select, _DTYPE[dtype])
     for nbytes in (0, B.marlin_select_pages_workspace_bytes(n, kv_heads, width)):
-        buf = _workspace(dev, stream, workspace, nbytes)
+        buf = _workspace(f, dev, stream, workspace, nbytes)
         with torch.cuda.device(dev):
             status = B.lib().marlin_select_pages(B.pack_select_pages(*args, buf.data_ptr(), buf.numel(), *sizes), stream)
         if status != 5:

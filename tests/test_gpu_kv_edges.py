@@ -154,3 +154,16 @@ def test_attention_of_the_longest_sequence(mk, D, hkv, short):
     want, spread = total.double() / n, size.double() / n
     assert ((out[0].cpu().double() - want).abs() <= 2.0 ** -8 * want.abs() + 2.0 ** -18 * spread).all()
     assert ((lse[0].cpu().double() - math.log(n)).abs() <= 2.0 ** -18).all()
+
+
+# ---- refusals ----
+
+def test_a_workspace_elsewhere_is_refused(mk):
+    q = torch.zeros(1, 2, 64, dtype=F16, device="cuda")
+    k, v, bounds = mk.kv_cache(2, 1, 16, 64, bounds=True)
+    table, lengths = torch.zeros(1, 2, dtype=torch.int32, device="cuda"), torch.ones(1, dtype=torch.int32, device="cuda")
+    host = mk.Workspace("cpu", nbytes=1 << 24)
+    with pytest.raises(ValueError, match="workspace"):
+        mk.paged_attention(q, k, v, table, lengths, workspace=host)
+    with pytest.raises(ValueError, match="workspace"):
+        mk.select_pages(q, bounds, table, lengths, 16, 1, workspace=host)
