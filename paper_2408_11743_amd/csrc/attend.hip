@@ -344,14 +344,14 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
     auto write_row = [&](int b, int row) {
         if (r >= nh) return;
         const int64_t at = (int64_t)b * p.heads + head0_of(row) + r;
-        const float inv = l == 0.f ? 0.f : 1.f / (l * E::kWeightUnit);  // no key: zero
+        const float inv = 1.f / (l * E::kWeightUnit);
 #pragma unroll
         for (int hf = 0; hf < kHalves; ++hf)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 T y[kCh];
 #pragma unroll
-                for (int j = 0; j < kCh; ++j) y[j] = (T)(acc[hf * kCh + j][i] * inv);
+                for (int j = 0; j < kCh; ++j) y[j] = l == 0.f ? (T)0.f : (T)(acc[hf * kCh + j][i] * inv);  // no weight: zero, whatever the values
                 uint32_t w[kDw];
                 __builtin_memcpy(w, y, sizeof(y));
                 store_dwords<kDw>((T *)p.out + at * D + 128 * hf + kCh * (4 * g + i), w);
@@ -608,10 +608,10 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
         auto write = [&](int j, float4_t o, float top, float sum) {
             if (r >= nh) return;
             const int64_t at = (int64_t)b * p.heads + head0_of(row) + r;
-            const float inv = sum == 0.f ? 0.f : 1.f / (sum * E::kWeightUnit);
+            const float inv = 1.f / (sum * E::kWeightUnit);
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                ((T *)p.out)[at * D + 128 * (j / kCh) + kCh * (4 * g + i) + j % kCh] = (T)(o[i] * inv);
+                ((T *)p.out)[at * D + 128 * (j / kCh) + kCh * (4 * g + i) + j % kCh] = sum == 0.f ? (T)0.f : (T)(o[i] * inv);
             if (p.lse && g == 0 && j == 0) p.lse[at] = (top + __builtin_amdgcn_logf(sum)) * 0.693147180559945f;
         };
         // Contributors are joined in order, so that the bits are the same every time.  Of a few, a wave takes its channels at once

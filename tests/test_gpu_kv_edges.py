@@ -132,6 +132,20 @@ def test_attention_of_infinite_values(mk, dtype, D, n, equal):
     assert ((got - want).abs()[:, rest] <= tol[:, rest]).all()
 
 
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("n", [1, 40, 300, 3000, 12000])
+def test_attention_without_any_weight_is_zero(mk, dtype, D, n):
+    """Every score -inf: zero and -inf, also where the values are infinite or no numbers, in one piece or many."""
+    q = torch.ones(16, D).to(dtype)
+    keys = torch.full((n, 1, D), -math.inf).to(dtype)
+    values = torch.randn(n, 1, D, generator=gen(n)).to(dtype)
+    values[n // 2] = math.inf
+    values[n // 3, 0, ::2] = math.nan
+    out, lse = one_sequence(mk, q, keys, values)
+    assert (out == 0).all() and (lse == -math.inf).all()
+
+
 # ---- limits ----
 
 @pytest.mark.parametrize("D,hkv,short", [(256, 2, 0), (256, 2, 47), (256, 5, 1), (128, 3, 0)])
