@@ -3,7 +3,7 @@
 // query of the kv head's group,
 //
 //   score = max_h sum_c (q_hc > 0 ? q_hc hi_c : q_hc lo_c)
-//         = max_h (min(q_h, 0) . lo + max(q_h, 0) . hi),
+//         = max_h (min(q_h, 0) . lo + max(q_h, 0) . hi)   where the bounds are finite,
 //
 // a product over 2 D channels for the MFMAs, and the best `select` are kept in the
 // order of their positions.
@@ -73,7 +73,7 @@ __global__ void __launch_bounds__(64 * kScoreWaves) page_score_kernel(const Sele
         hi[t] = *(const vec8 *)(box + D + 32 * t);
     }
     float best = -INFINITY;
-    bool nan = false;
+    bool odd = false;
     for (int h0 = 0; h0 < p.group; h0 += 16) {
         if (h0 > 0)
 #pragma unroll
@@ -96,13 +96,38 @@ __global__ void __launch_bounds__(64 * kScoreWaves) page_score_kernel(const Sele
         for (int i = 0; i < 4; ++i)
             if (h0 + 4 * g + i < p.group) {
                 best = fmaxf(best, s[i]);
-                nan |= s[i] != s[i];
+                odd |= !(fabsf(s[i]) < INFINITY);
             }
     }
+    auto of_page = [&](bool x) -> bool {  // in any of the page's four lanes
+        const uint64_t in = __builtin_amdgcn_ballot_w64(x);
+        return (in >> r | in >> (r + 16) | in >> (r + 32) | in >> (r + 48)) & 1;
+    };
     best = max_over_groups(best);
-    const uint64_t nans = __builtin_amdgcn_ballot_w64(nan);
-    const bool any = (nans >> r | nans >> (r + 16) | nans >> (r + 32) | nans >> (r + 48)) & 1;
-    if (g == 0 && at < pages) p.scores[(int64_t)row * p.width + at] = !inside ? kNoPage : any ? kNan : score_key(best);
+    // The products also take what the formula leaves out, times zero: of a bound that is infinite or no number they are no number or
+    // infinite.  Such a page, a rare one, is scored anew as the formula says.
+    odd = of_page(odd) && inside;
+    bool nan = false;
+    if (__any(odd)) {
+        float anew = -INFINITY;
+#pragma unroll 1
+        for (int h = 0; h < p.group; ++h) {
+            const T *q = (const T *)p.q + b * p.q_row + (kvh * p.group + h) * p.q_head + 8 * g;
+            float sum = 0.f;
+#pragma unroll 1
+            for (int c = 0; c < D; c += 32) {
+                const vec8 x = *(const vec8 *)(q + c), least = *(const vec8 *)(box + c), most = *(const vec8 *)(box + D + c);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sum += (float)x[e] * (x[e] > (T)0.f ? (float)most[e] : (float)least[e]);
+            }
+            sum = sum_over_groups(sum);
+            anew = fmaxf(anew, sum);
+            nan |= sum != sum;
+        }
+        if (odd) best = anew;
+        nan &= odd;
+    }
+    if (g == 0 && at < pages) p.scores[(int64_t)row * p.width + at] = !inside ? kNoPage : nan ? kNan : score_key(best);
 }
 
 constexpr int kPickThreads = 512, kPickWaves = kPickThreads / 64;

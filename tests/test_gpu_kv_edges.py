@@ -146,6 +146,74 @@ def test_attention_without_any_weight_is_zero(mk, dtype, D, n):
     assert (out == 0).all() and (lse == -math.inf).all()
 
 
+# ---- page scores ----
+
+def select_by_definition(q, bounds, table, lengths, ps, count):
+    """marlin.h's formula as it stands, in 64 bits: the bound a channel's sign does not ask for is not looked at."""
+    kv_heads, group = bounds.shape[1], q.shape[1] // bounds.shape[1]
+    chosen = torch.full((len(lengths), kv_heads, count), -1, dtype=torch.int32)
+    for b, n in enumerate(lengths.tolist()):
+        used = -(-n // ps)
+        for h in range(kv_heads):
+            rank = []
+            for i in range(used):
+                page = int(table[b, i])
+                if not 0 <= page < bounds.shape[0]:
+                    rank.append((2, 0.0, i))
+                    continue
+                x = q[b, h * group:(h + 1) * group].double()
+                lo, hi = bounds[page, h].double()
+                s = torch.where(x > 0, x * hi, x * lo).sum(1)
+                rank.append((0 if torch.isnan(s).any() else 1, -float(s.max()), i))
+            rank = [(r, 0.0 if r != 1 else s, i) for r, s, i in rank]
+            best = list(range(used)) if used <= count else sorted([used - 1] + [i for _, _, i in sorted(rank[:-1])[:count - 1]])
+            chosen[b, h, :len(best)] = table[b, best]
+    return chosen
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("sign", [1, -1])
+def test_select_looks_at_the_bound_that_the_sign_asks_for(mk, dtype, sign):
+    """Six pages whose nearer bound is 0 .. 5, page 0's farther one infinite: the best are the last ones."""
+    q = torch.zeros(1, 1, 64).to(dtype)
+    q[0, 0, 0] = sign
+    bounds = torch.zeros(6, 1, 2, 64).to(dtype)
+    bounds[:, 0, 1 if sign > 0 else 0, 0] = sign * torch.arange(6).to(dtype)
+    bounds[0, 0, 0 if sign > 0 else 1, 0] = -sign * math.inf
+    table = torch.arange(6, dtype=torch.int32)[None]
+    lengths = torch.tensor([96], dtype=torch.int32)
+    got, _ = mk.select_pages(q.cuda(), bounds.cuda(), table.cuda(), lengths.cuda(), 16, 3)
+    assert got.flatten().tolist() == [3, 4, 5]
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("D", [64, 96, 128, 256])
+@pytest.mark.parametrize("hq,hkv", [(1, 1), (8, 2), (17, 1), (40, 2)])
+@pytest.mark.parametrize("zeros", [0.0, 0.8])
+def test_select_by_its_definition(mk, dtype, D, hq, hkv, zeros):
+    """Infinities and NaN in either bound or both, under queries of either sign and of zero; small integers elsewhere."""
+    g = gen(D + hq)
+    lengths, ps, count = torch.tensor([800, 33, 1500], dtype=torch.int32), 16, 9
+    used = [-(-n // ps) for n in lengths.tolist()]
+    pages = sum(used) + 1
+    table = torch.full((3, max(used)), -1, dtype=torch.int32)
+    perm = torch.randperm(pages, generator=g).int()
+    for b, n in enumerate(used):
+        table[b, :n] = perm[sum(used[:b]):sum(used[:b]) + n]
+    table[2, 4] = pages + 3
+    q = torch.randint(1, 3, (3, hq, D), generator=g) * (2 * torch.randint(0, 2, (3, 1, D), generator=g) - 1)
+    q = (q * (torch.rand(q.shape, generator=g) >= zeros)).to(dtype)
+    a, b = torch.randint(-3, 4, (2, pages, hkv, D), generator=g)
+    bounds = torch.stack([torch.minimum(a, b), torch.maximum(a, b)], 2).to(dtype)
+    odd = torch.tensor([math.inf, -math.inf, math.nan])
+    for p in range(0, pages, 3):
+        side, c = int(torch.randint(0, 3, (1,), generator=g)), int(torch.randint(0, D, (1,), generator=g))
+        for one in ((0,), (1,), (0, 1))[side]:
+            bounds[p, :, one, c] = odd[p // 3 % 3].to(dtype)
+    got, _ = mk.select_pages(q.cuda(), bounds.cuda(), table.cuda(), lengths.cuda(), ps, count)
+    assert torch.equal(got.cpu(), select_by_definition(q, bounds, table, lengths, ps, count))
+
+
 # ---- limits ----
 
 @pytest.mark.parametrize("D,hkv,short", [(256, 2, 0), (256, 2, 47), (256, 5, 1), (128, 3, 0)])
