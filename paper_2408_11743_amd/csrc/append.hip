@@ -354,18 +354,19 @@ __global__ void __launch_bounds__(256, 4) append_prompt_kernel(const AppendProbl
 template <typename T, int D>
 hipError_t launch_one(const AppendProblem &p, hipStream_t stream)
 {
+    AppendProblem q = p;
     if (!p.starts) {
         constexpr int kHeads = 256 / (D / 16);
         const int slabs = (p.heads + 2 * p.kv_heads + kHeads - 1) / kHeads;
-        hipLaunchKernelGGL((append_token_kernel<T, D>), dim3((uint32_t)p.B * slabs), dim3(256), 0, stream, p);
-    } else {
-        // a sequence of n tokens touches at most n / page size + 2 pages
-        const int pages = (p.tokens >> p.page_shift) + 2 * (p.B < p.tokens ? p.B : p.tokens);
-        const int slabs = (p.heads + kSlab - 1) / kSlab + 2 * ((p.kv_heads + kSlab - 1) / kSlab);
-        const bool once = D % 128 == 0 && (int64_t)p.tokens * (p.heads + 2 * p.kv_heads) * D * 2 > ((int64_t)128 << 20);
-        hipLaunchKernelGGL((append_prompt_kernel<T, D>), dim3((uint32_t)pages * slabs), dim3(256), 0, stream, p, once);
+        void *args[] = {&q};
+        return hipLaunchKernel((const void *)&append_token_kernel<T, D>, dim3((uint32_t)p.B * slabs), dim3(256), args, 0, stream);
     }
-    return hipGetLastError();
+    // a sequence of n tokens touches at most n / page size + 2 pages
+    const int pages = (p.tokens >> p.page_shift) + 2 * (p.B < p.tokens ? p.B : p.tokens);
+    const int slabs = (p.heads + kSlab - 1) / kSlab + 2 * ((p.kv_heads + kSlab - 1) / kSlab);
+    bool once = D % 128 == 0 && (int64_t)p.tokens * (p.heads + 2 * p.kv_heads) * D * 2 > ((int64_t)128 << 20);
+    void *args[] = {&q, &once};
+    return hipLaunchKernel((const void *)&append_prompt_kernel<T, D>, dim3((uint32_t)pages * slabs), dim3(256), args, 0, stream);
 }
 
 template <typename T>

@@ -716,8 +716,9 @@ hipError_t launch_one(const AttendProblem &p, int cus, hipStream_t stream)
     constexpr int kTiles = D > 128 ? 1 : 2;
     AttendProblem q = p;
     q.grid_reciprocal = ranges > 1 ? (uint32_t)(((uint64_t)1 << 32) / (uint64_t)ranges) : 0xFFFFFFFFu;
-    hipLaunchKernelGGL((paged_attention_kernel<T, D, kAttendWaves, kTiles>), dim3(ranges * p.head_tiles), dim3(64 * kAttendWaves), 0, stream, q);
-    return hipGetLastError();
+    void *args[] = {&q};
+    return hipLaunchKernel((const void *)&paged_attention_kernel<T, D, kAttendWaves, kTiles>, dim3(ranges * p.head_tiles),
+                           dim3(64 * kAttendWaves), args, 0, stream);
 }
 
 template <typename T>

@@ -1,9 +1,10 @@
 // The common case of the cache operators' Python calls (kv.py): tensors as they
 // nearly always are are checked, the output is allocated and the C entry point
 // called without a step in Python, since a decode step waits for the host
-// between these small launches.  Whatever is not so (or a call that the library
-// refuses) returns None with nothing done, and the Python side, which names
-// faults and copies views, takes it from there.
+// between these small launches.  Whatever is not so, or a call that the library's
+// own checks refuse, returns None with nothing done, and the Python side, which names
+// faults and copies views, takes it from there.  A HIP error raises: part of the
+// call may have reached the GPU, and it must not be made again.
 #include <Python.h>
 
 #include <torch/csrc/autograd/python_variable.h>
@@ -22,6 +23,7 @@ decltype(&marlin_kv_append) g_append;
 decltype(&marlin_paged_attention) g_attend;
 decltype(&marlin_select_pages) g_select;
 PyObject *g_raw_stream, *g_workspaces, *g_buf;  // current stream of a device; (device, stream) -> workspace; "buf"
+PyObject *g_error;                              // MarlinError(function, status)
 
 // A strided tensor of exactly PyTorch's type with memory of its own on a GPU, not lazily negated; else NULL.
 const at::Tensor *plain(PyObject *o)
@@ -115,6 +117,15 @@ PyObject *not_here()
     Py_RETURN_NONE;
 }
 
+PyObject *refused(const char *function, marlin_status_t status)
+{
+    if (status != MARLIN_ERR_HIP) return not_here();
+    PyObject *e = PyObject_CallFunction(g_error, "si", function, (int)status);
+    if (e) PyErr_SetObject(g_error, e);
+    Py_XDECREF(e);
+    return nullptr;
+}
+
 // q, k, v, k_cache, v_cache, table, lengths, cos_sin, starts, interleaved, bounds, out
 PyObject *kv_append(PyObject *, PyObject *const *o, Py_ssize_t n)
 try {
@@ -191,7 +202,7 @@ try {
     const c10::DeviceGuard guard(kc->device());
     const marlin_status_t status = g_append(&a, s);
     Py_DECREF(stream);
-    if (status != MARLIN_OK) return not_here();
+    if (status != MARLIN_OK) return refused("marlin_kv_append", status);
     if (o[11] != Py_None) {
         Py_INCREF(o[11]);
         return o[11];
@@ -250,7 +261,9 @@ try {
     const c10::DeviceGuard guard(kc->device());
     const bool ready = workspace_of(o[8], at.device, stream, a.workspace, a.workspace_bytes);
     Py_DECREF(stream);
-    if (!ready || g_attend(&a, s) != MARLIN_OK) return not_here();
+    if (!ready) return not_here();
+    const marlin_status_t status = g_attend(&a, s);
+    if (status != MARLIN_OK) return refused("marlin_paged_attention", status);
     PyObject *first = o[7];
     if (first != Py_None)
         Py_INCREF(first);
@@ -300,18 +313,20 @@ try {
     const c10::DeviceGuard guard(bounds->device());
     const bool ready = workspace_of(o[6], at.device, stream, a.workspace, a.workspace_bytes);
     Py_DECREF(stream);
-    if (!ready || g_select(&a, s) != MARLIN_OK) return not_here();
+    if (!ready) return not_here();
+    const marlin_status_t status = g_select(&a, s);
+    if (status != MARLIN_OK) return refused("marlin_select_pages", status);
     return Py_BuildValue("(NN)", THPVariable_Wrap(std::move(chosen)), THPVariable_Wrap(std::move(tokens)));
 } catch (const std::exception &) {
     return not_here();
 }
 
-// addresses of marlin_kv_append, marlin_paged_attention, marlin_select_pages; raw stream function; workspaces
+// addresses of marlin_kv_append, marlin_paged_attention, marlin_select_pages; raw stream function; workspaces; MarlinError
 PyObject *connect(PyObject *, PyObject *args)
 {
     unsigned long long append, attend, select;
-    PyObject *stream, *workspaces;
-    if (!PyArg_ParseTuple(args, "KKKOO!", &append, &attend, &select, &stream, &PyDict_Type, &workspaces)) return nullptr;
+    PyObject *stream, *workspaces, *error;
+    if (!PyArg_ParseTuple(args, "KKKOO!O", &append, &attend, &select, &stream, &PyDict_Type, &workspaces, &error)) return nullptr;
     g_append = reinterpret_cast<decltype(g_append)>(append);
     g_attend = reinterpret_cast<decltype(g_attend)>(attend);
     g_select = reinterpret_cast<decltype(g_select)>(select);
@@ -319,6 +334,8 @@ PyObject *connect(PyObject *, PyObject *args)
     Py_XSETREF(g_raw_stream, stream);
     Py_INCREF(workspaces);
     Py_XSETREF(g_workspaces, workspaces);
+    Py_INCREF(error);
+    Py_XSETREF(g_error, error);
     if (!g_buf && !(g_buf = PyUnicode_InternFromString("buf"))) return nullptr;
     Py_RETURN_NONE;
 }

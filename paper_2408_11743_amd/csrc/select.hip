@@ -335,24 +335,24 @@ hipError_t launch_one(const SelectProblem &p, hipStream_t stream)
     const int blocks = (p.width + kPer - 1) / kPer;
     // no scores where every sequence keeps all the pages it can have (one sequence of 21 tokens: 9.8 us with the
     // attention, 12.3 with a launch that finds nothing to do)
-    if (p.width > p.select)
-        hipLaunchKernelGGL((page_score_kernel<T, D>), dim3(blocks * p.B * p.kv_heads), dim3(64 * kScoreWaves), 0, stream, p, blocks);
-    const dim3 rows(p.B * p.kv_heads), threads(kPickThreads);
-    if (p.width <= kPickThreads)
-        hipLaunchKernelGGL(page_pick_kernel<1>, rows, threads, 0, stream, p);
-    else if (p.width <= 2 * kPickThreads)
-        hipLaunchKernelGGL(page_pick_kernel<2>, rows, threads, 0, stream, p);
-    else if (p.width <= 4 * kPickThreads)
-        hipLaunchKernelGGL(page_pick_kernel<4>, rows, threads, 0, stream, p);
-    else if (p.width <= 8 * kPickThreads)
-        hipLaunchKernelGGL(page_pick_kernel<8>, rows, threads, 0, stream, p);
-    else if (p.width <= 16 * kPickThreads)
-        hipLaunchKernelGGL(page_pick_kernel<16>, rows, threads, 0, stream, p);
-    else if (p.width <= 32 * kPickThreads)
-        hipLaunchKernelGGL(page_pick_kernel<32>, rows, threads, 0, stream, p);
-    else
-        hipLaunchKernelGGL(page_pick_kernel<0>, rows, threads, 0, stream, p);
-    return hipGetLastError();
+    SelectProblem q = p;
+    if (p.width > p.select) {
+        int n = blocks;
+        void *args[] = {&q, &n};
+        const hipError_t e = hipLaunchKernel((const void *)&page_score_kernel<T, D>, dim3(blocks * p.B * p.kv_heads),
+                                             dim3(64 * kScoreWaves), args, 0, stream);
+        if (e != hipSuccess) return e;
+    }
+    // entries and scores that a thread of the pick holds
+    const void *const pick = p.width <= kPickThreads        ? (const void *)&page_pick_kernel<1>
+                             : p.width <= 2 * kPickThreads  ? (const void *)&page_pick_kernel<2>
+                             : p.width <= 4 * kPickThreads  ? (const void *)&page_pick_kernel<4>
+                             : p.width <= 8 * kPickThreads  ? (const void *)&page_pick_kernel<8>
+                             : p.width <= 16 * kPickThreads ? (const void *)&page_pick_kernel<16>
+                             : p.width <= 32 * kPickThreads ? (const void *)&page_pick_kernel<32>
+                                                            : (const void *)&page_pick_kernel<0>;
+    void *args[] = {&q};
+    return hipLaunchKernel(pick, dim3(p.B * p.kv_heads), dim3(kPickThreads), args, 0, stream);
 }
 
 template <typename T>

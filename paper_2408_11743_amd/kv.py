@@ -68,7 +68,7 @@ def _need(ok: bool, func: str, what: str) -> None:
 # first handed to a native module (csrc/fast.cpp), which does it where the tensors are as
 # they nearly always are.  Anything else comes back as None, with nothing done,
 # to the checks below, which name what is wrong or copy a view that the kernels
-# cannot read.  A token of 32 + 16 heads appended: 11.4 us a call in Python.
+# cannot read; a HIP error raises there and then.  A token of 32 + 16 heads appended: 11.4 us a call in Python.
 _native = None
 
 
@@ -82,7 +82,7 @@ def _connect():
         raise RuntimeError("the native call module is missing: build it with `python -m paper_2408_11743_amd.build`") from e
     address = lambda f: ctypes.cast(f, ctypes.c_void_p).value  # noqa: E731
     _fast.connect(address(handle.marlin_kv_append), address(handle.marlin_paged_attention),
-                  address(handle.marlin_select_pages), _raw_stream, ops._default_ws)
+                  address(handle.marlin_select_pages), _raw_stream, ops._default_ws, B.MarlinError)
     _native = _fast
     return _fast
 

@@ -2,6 +2,7 @@
 crash: weights far below a row's maximum, infinite values, and the limits of
 sizes and lengths.  References are 64-bit forms written here or in kv_reference.py.
 """
+import ctypes
 import math
 
 import pytest
@@ -249,3 +250,58 @@ def test_a_workspace_elsewhere_is_refused(mk):
         mk.paged_attention(q, k, v, table, lengths, workspace=host)
     with pytest.raises(ValueError, match="workspace"):
         mk.select_pages(q, bounds, table, lengths, 16, 1, workspace=host)
+
+
+# ---- HIP errors ----
+
+def small_call(mk):
+    """Arguments of the three calls: two sequences of 40 and 50 tokens."""
+    q = torch.randn(2, 4, 64, device="cuda").half()
+    kv = torch.randn(2, 2, 64, device="cuda").half()
+    k, v, bounds = mk.kv_cache(8, 2, 16, 64, bounds=True)
+    table = torch.arange(8, dtype=torch.int32, device="cuda").view(2, 4)
+    lengths = torch.tensor([40, 50], dtype=torch.int32, device="cuda")
+    return q, kv, k, v, bounds, table, lengths
+
+
+def test_a_hip_error_raises_and_is_not_tried_again(mk):
+    from paper_2408_11743_amd import _fast, kv, ops
+    q, new, k, v, bounds, table, lengths = small_call(mk)
+    mk.paged_attention(q, k, v, table, lengths)  # the stream's workspace is there
+    mk.select_pages(q, bounds, table, lengths, 16, 2)
+    calls = []
+    stub = ctypes.CFUNCTYPE(ctypes.c_int, ctypes.c_void_p, ctypes.c_void_p)(lambda args, stream: calls.append(0) or 6)
+    at = ctypes.cast(stub, ctypes.c_void_p).value
+    _fast.connect(at, at, at, kv._raw_stream, ops._default_ws, mk.MarlinError)
+    try:
+        for n, call in enumerate((lambda: mk.kv_append(q, new, new, k, v, table, lengths),
+                                  lambda: mk.paged_attention(q, k, v, table, lengths, return_lse=True),
+                                  lambda: mk.select_pages(q, bounds, table, lengths, 16, 2))):
+            with pytest.raises(mk.MarlinError) as e:
+                call()
+            assert e.value.status == 6 and len(calls) == n + 1
+    finally:
+        kv._connect()
+    assert mk.kv_append(q, new, new, k, v, table, lengths).shape == q.shape
+
+
+def test_an_error_that_another_call_left_is_not_this_ones(mk):
+    """hipSetDevice of a device that there is not leaves an error on the thread; an append in place rotates once all the same."""
+    hip = next(line.split()[-1] for line in open("/proc/self/maps") if "libamdhip64" in line)
+    hip = ctypes.CDLL(hip)
+    q, new, k, v, bounds, table, lengths = small_call(mk)
+    angles = mk.rotation_table(64, 64)
+    want = mk.kv_append(q, new, new, k, v, table, lengths, angles)
+    o = mk.paged_attention(want, k, v, table, lengths)
+    pages, _ = mk.select_pages(want, bounds, table, lengths, 16, 2)
+    torch.cuda.synchronize()
+    try:
+        assert hip.hipSetDevice(9999) != 0
+        got = mk.kv_append(q, new, new, k, v, table, lengths, angles, out=q)
+        assert hip.hipSetDevice(9999) != 0
+        o2 = mk.paged_attention(q, k, v, table, lengths)
+        assert hip.hipSetDevice(9999) != 0
+        pages2, _ = mk.select_pages(q, bounds, table, lengths, 16, 2)
+    finally:
+        hip.hipGetLastError()
+    assert torch.equal(got, want) and torch.equal(o2, o) and torch.equal(pages2, pages)
