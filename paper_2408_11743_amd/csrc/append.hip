@@ -196,7 +196,7 @@ __global__ void __launch_bounds__(256) append_token_kernel(const AppendProblem p
 constexpr int kSlab = 4;
 
 template <typename T, int D>
-__global__ void __launch_bounds__(256, 4) append_prompt_kernel(const AppendProblem p, bool once)
+__global__ void __launch_bounds__(256, 4) append_prompt_kernel(const AppendProblem p, bool once, int page_base)
 {
     constexpr int kPairs = D / 16;
     constexpr int kTokens = D == 64 ? 16 : D == 256 ? 4 : 8;  // of a wave at a time
@@ -205,7 +205,7 @@ __global__ void __launch_bounds__(256, 4) append_prompt_kernel(const AppendProbl
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int pair = lane % kPairs, slot = lane / kPairs;
 
-    // the page: the blockIdx.x-th that the sequences touch, found among the sums of 64 sequences' pages, then among theirs
+    // the page: which of those that the sequences touch follows from blockIdx.x; found among the sums of 64 sequences' pages, then among theirs
     const int chunks = (p.B + 63) / 64;
     int begin = 0, count = 0, total = 0, pages = 0, incl = 0;  // of the lane's sequence: tokens, length, pages, pages up to it
     auto hold = [&](int chunk) {
@@ -224,7 +224,8 @@ __global__ void __launch_bounds__(256, 4) append_prompt_kernel(const AppendProbl
     };
     int chunk = 0, before = 0;
     const int q_slabs = (p.heads + kSlab - 1) / kSlab, kv_slabs = (p.kv_heads + kSlab - 1) / kSlab;
-    const int mine = blockIdx.x / (q_slabs + 2 * kv_slabs), y = blockIdx.x - mine * (q_slabs + 2 * kv_slabs);
+    const int in_launch = blockIdx.x / (q_slabs + 2 * kv_slabs), y = blockIdx.x - in_launch * (q_slabs + 2 * kv_slabs);
+    const int mine = page_base + in_launch;
     if (chunks == 1) {
         hold(0);
     } else {
@@ -365,8 +366,14 @@ hipError_t launch_one(const AppendProblem &p, hipStream_t stream)
     const int pages = (p.tokens >> p.page_shift) + 2 * (p.B < p.tokens ? p.B : p.tokens);
     const int slabs = (p.heads + kSlab - 1) / kSlab + 2 * ((p.kv_heads + kSlab - 1) / kSlab);
     bool once = D % 128 == 0 && (int64_t)p.tokens * (p.heads + 2 * p.kv_heads) * D * 2 > ((int64_t)128 << 20);
-    void *args[] = {&q, &once};
-    return hipLaunchKernel((const void *)&append_prompt_kernel<T, D>, dim3((uint32_t)pages * slabs), dim3(256), args, 0, stream);
+    const int most = (1 << 24) / slabs - 1;  // pages of a launch, which takes less than 2^32 threads
+    for (int base = 0; base < pages; base += most) {
+        void *args[] = {&q, &once, &base};
+        const uint32_t n = pages - base < most ? pages - base : most;
+        const hipError_t e = hipLaunchKernel((const void *)&append_prompt_kernel<T, D>, dim3(n * slabs), dim3(256), args, 0, stream);
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 template <typename T>

@@ -239,6 +239,33 @@ def test_attention_of_the_longest_sequence(mk, D, hkv, short):
     assert ((lse[0].cpu().double() - math.log(n)).abs() <= 2.0 ** -18).all()
 
 
+def test_append_of_more_threads_than_a_launch_takes(mk):
+    """22000 pages of 1024 + 1024 heads: 1.01 * 2^32 threads.  Most sequences' entries name no page; a few do, the last ones too."""
+    n, heads, D, ps = 11000, 1024, 64, 16
+    g = torch.Generator(device="cuda").manual_seed(5)
+    row = torch.randn(3, 1, heads, D, dtype=F16, device="cuda", generator=g)
+    q, k, v = (x.expand(2 * n, heads, D) for x in row)
+    real = [0, 1, 5000, n - 2, n - 1]
+    table = torch.full((n, 2), -1, dtype=torch.int32)
+    table[real] = torch.arange(2 * len(real), dtype=torch.int32).view(-1, 2)
+    kc, vc, bounds = mk.kv_cache(2 * len(real), heads, ps, D, bounds=True)
+    angles = mk.rotation_table(17, D)
+    lengths = torch.full((n,), 17, dtype=torch.int32, device="cuda")
+    starts = torch.arange(0, 2 * n + 1, 2, dtype=torch.int32, device="cuda")
+    out = mk.kv_append(q, k, v, kc, vc, table.cuda(), lengths, angles, starts, bounds=bounds)
+    # the same two tokens by themselves
+    kc1, vc1, bounds1 = mk.kv_cache(2, heads, ps, D, bounds=True)
+    one = mk.kv_append(q[:2], k[:2], v[:2], kc1, vc1, torch.tensor([[0, 1]], dtype=torch.int32, device="cuda"), lengths[:1], angles,
+                       starts[:2], bounds=bounds1)
+    torch.cuda.synchronize()
+    for i, b in enumerate(real):
+        assert torch.equal(out[2 * b:2 * b + 2], one)
+        for a, c in ((kc, kc1), (vc, vc1), (bounds, bounds1)):
+            assert torch.equal(a[2 * i:2 * i + 2], c)
+        out[2 * b:2 * b + 2] = 0
+    assert not out.any()
+
+
 # ---- refusals ----
 
 def test_a_workspace_elsewhere_is_refused(mk):
