@@ -189,15 +189,15 @@ __device__ __forceinline__ void load_unaligned(T (&to)[N], const T *from)
 }
 
 template <int HELD>
-__global__ void __launch_bounds__(kPickThreads) page_pick_kernel(const SelectProblem p)
+__global__ void __launch_bounds__(kPickThreads) page_pick_kernel(const SelectProblem p, int row_base)
 {
     __shared__ int bins[kPickBins], found[3];
     __shared__ Counts waves[2][kPickWaves];
     __shared__ uint32_t ends[2][kPickWaves];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int b = blockIdx.x / p.kv_heads, kvh = blockIdx.x % p.kv_heads;
+    const int row = row_base + blockIdx.x, b = row / p.kv_heads, kvh = row % p.kv_heads;
     const int32_t *table = p.table + b * p.table_row;
-    const uint32_t *scores = p.scores + (int64_t)blockIdx.x * p.width;
+    const uint32_t *scores = p.scores + (int64_t)row * p.width;
     uint32_t held[HELD ? HELD : 1];
     int32_t entry[HELD ? HELD : 1];
     if constexpr (HELD > 0) {
@@ -215,7 +215,7 @@ __global__ void __launch_bounds__(kPickThreads) page_pick_kernel(const SelectPro
         }
     }
     const int pages = pages_of(p, b);
-    int32_t *out = p.chosen + (int64_t)blockIdx.x * p.select;
+    int32_t *out = p.chosen + (int64_t)row * p.select;
     if (kvh == 0 && tid == 0) {
         const int n = p.lengths[b], cap = p.width << p.page_shift, len = n < 0 ? 0 : n < cap ? n : cap;
         p.chosen_lengths[b] = pages > p.select ? len - ((pages - p.select) << p.page_shift) : len;
@@ -351,8 +351,14 @@ hipError_t launch_one(const SelectProblem &p, hipStream_t stream)
                              : p.width <= 16 * kPickThreads ? (const void *)&page_pick_kernel<16>
                              : p.width <= 32 * kPickThreads ? (const void *)&page_pick_kernel<32>
                                                             : (const void *)&page_pick_kernel<0>;
-    void *args[] = {&q};
-    return hipLaunchKernel(pick, dim3(p.B * p.kv_heads), dim3(kPickThreads), args, 0, stream);
+    constexpr int kMost = 1 << 22;  // rows of a launch, which takes less than 2^32 threads
+    const int rows = p.B * p.kv_heads;
+    for (int base = 0; base < rows; base += kMost) {
+        void *args[] = {&q, &base};
+        const hipError_t e = hipLaunchKernel(pick, dim3(rows - base < kMost ? rows - base : kMost), dim3(kPickThreads), args, 0, stream);
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 template <typename T>

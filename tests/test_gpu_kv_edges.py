@@ -266,6 +266,20 @@ def test_append_of_more_threads_than_a_launch_takes(mk):
     assert not out.any()
 
 
+def test_select_of_more_threads_than_a_launch_takes(mk):
+    """2^23 rows of 512 threads, the most that marlin.h admits: the same 64 sequences over and over."""
+    times, n, heads, D, ps = 1024, 64, 128, 64, 16
+    g = torch.Generator(device="cuda").manual_seed(6)
+    q = torch.randn(1, heads, D, dtype=F16, device="cuda", generator=g)
+    bounds = torch.randn(20, heads, 2, D, dtype=F16, device="cuda", generator=g)
+    table = torch.randint(0, 20, (n, 4), device="cuda", generator=g).int()
+    lengths = torch.randint(0, 65, (n,), device="cuda", generator=g).int()
+    want, want_n = mk.select_pages(q.expand(n, heads, D), bounds, table, lengths, ps, 3)
+    got, got_n = mk.select_pages(q.expand(times * n, heads, D), bounds, table.repeat(times, 1), lengths.repeat(times), ps, 3)
+    assert torch.equal(got.view(times, n, heads, 3), want.expand(times, n, heads, 3))
+    assert torch.equal(got_n, want_n.repeat(times))
+
+
 # ---- refusals ----
 
 def test_a_workspace_elsewhere_is_refused(mk):
