@@ -353,7 +353,8 @@ marlin_status_t marlin_quantize(const uint16_t *W, int64_t K, int64_t N, int64_t
  * included, so one array serves the append and the attention of every layer
  * of a step.  It stays on the device: no entry point needs it on the host, so
  * all of them can be captured into a HIP graph and replayed as sequences grow.
- * A length below 0 counts as 0, one beyond width * page_size as that.
+ * A length below 0 counts as 0; what is read ends with the table, and a new
+ * token past it is not appended.
  *
  * Shapes: head_dim 64, 96, 128 or 256; page_size a power of two, 16 .. 1024;
  * heads a multiple of kv_heads, the query heads h * heads / kv_heads .. sharing

@@ -128,7 +128,12 @@ __device__ __forceinline__ Pieces rotate(const AppendProblem &p, const Pieces &x
     return __builtin_bit_cast(Pieces, y);
 }
 
-__device__ __forceinline__ int clamped(int n) { return n < 0 ? 0 : n < (1 << 30) ? n : (1 << 30); }
+// A table ends at 2^30 tokens at most, and 2^24 are appended: beyond the sum of both, every new token is past the table.
+__device__ __forceinline__ int clamped(int n)
+{
+    constexpr int kMost = (1 << 30) + (1 << 24);
+    return n < 0 ? 0 : n < kMost ? n : kMost;
+}
 
 // Slot (in rows of D of the cache, kv head 0) of sequence b's position, or -1:
 // the token is not appended.

@@ -280,6 +280,31 @@ def test_select_of_more_threads_than_a_launch_takes(mk):
     assert torch.equal(got_n, want_n.repeat(times))
 
 
+def test_append_past_the_largest_table(mk):
+    """A table of 2^30 tokens: positions from there on have no place, and do not take the last slot's."""
+    ps, width, D = 1024, 1 << 20, 64
+    kc, vc = mk.kv_cache(4, 1, ps, D)
+    table = torch.zeros(2, width, dtype=torch.int32, device="cuda")
+    table[0, -1], table[1, -1] = 2, 3
+    new = torch.randn(3, 6, 1, D, device="cuda").half()
+    for length in (2 ** 30 + 1, 2 ** 30 + 1024, 2 ** 31 - 1):
+        lengths = torch.tensor([length, 2 ** 30], dtype=torch.int32, device="cuda")
+        kc.zero_()
+        q = mk.kv_append(new[0, :2], new[1, :2], new[2, :2], kc, vc, table, lengths)
+        assert not q[0].any() and torch.equal(q[1], new[0, 1])
+        assert torch.equal(kc[3, 0, -1], new[1, 1, 0])
+        kc[3, 0, -1] = 0
+        assert not kc.any()
+    # prompts: four tokens of which two are past it, and two that are all
+    lengths = torch.tensor([2 ** 30 + 2, 2 ** 31 - 1], dtype=torch.int32, device="cuda")
+    starts = torch.tensor([0, 4, 6], dtype=torch.int32, device="cuda")
+    q = mk.kv_append(new[0], new[1], new[2], kc, vc, table, lengths, starts=starts)
+    assert torch.equal(q[:2], new[0, :2]) and not q[2:].any()
+    assert torch.equal(kc[2, 0, -2:], new[1, :2, 0])
+    kc[2, 0, -2:] = 0
+    assert not kc.any()
+
+
 # ---- refusals ----
 
 def test_a_workspace_elsewhere_is_refused(mk):
