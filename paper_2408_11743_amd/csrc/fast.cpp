@@ -9,8 +9,12 @@
 
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <ATen/TracerMode.h>
 #include <ATen/hip/EmptyTensor.h>
 #include <c10/core/DeviceGuard.h>
+#include <c10/core/GradMode.h>
+#include <c10/core/impl/LocalDispatchKeySet.h>
+#include <c10/core/impl/TorchDispatchModeTLS.h>
 
 #include <cmath>
 #include <cstring>
@@ -25,12 +29,23 @@ decltype(&marlin_select_pages) g_select;
 PyObject *g_raw_stream, *g_workspaces, *g_buf;  // current stream of a device; (device, stream) -> workspace; "buf"
 PyObject *g_error;                              // MarlinError(function, status)
 
-// A strided tensor of exactly PyTorch's type with memory of its own on a GPU, not lazily negated; else NULL.
+// A strided tensor of exactly PyTorch's type with memory of its own on a GPU, not lazily negated, without a gradient or
+// tangent to carry on; else NULL.
 const at::Tensor *plain(PyObject *o)
 {
     if (!THPVariable_CheckExact(o)) return nullptr;
     const at::Tensor &t = THPVariable_Unpack(o);
-    return t.is_cuda() && t.layout() == at::kStrided && t.has_storage() && !t.is_neg() ? &t : nullptr;
+    return t.is_cuda() && t.layout() == at::kStrided && t.has_storage() && !t.is_neg() &&
+                   !(t.requires_grad() && c10::GradMode::is_enabled()) && !t._fw_grad(0).defined()
+               ? &t
+               : nullptr;
+}
+
+// A dispatch mode, a trace or a transform is to see the call: it is the registered operator's.
+bool watched()
+{
+    return c10::impl::TorchDispatchModeTLS::any_modes_set() || at::tracer::impl::is_dispatch_enabled() ||
+           c10::impl::tls_is_dispatch_key_included(c10::DispatchKey::FuncTorchDynamicLayerFrontMode);
 }
 
 struct Place {
@@ -129,7 +144,7 @@ PyObject *refused(const char *function, marlin_status_t status)
 // q, k, v, k_cache, v_cache, table, lengths, cos_sin, starts, interleaved, bounds, out
 PyObject *kv_append(PyObject *, PyObject *const *o, Py_ssize_t n)
 try {
-    if (n != 12 || !g_append) return not_here();
+    if (n != 12 || !g_append || watched()) return not_here();
     const at::Tensor *q = plain(o[0]), *k = plain(o[1]), *v = plain(o[2]), *kc = plain(o[3]), *vc = plain(o[4]);
     const at::Tensor *table = plain(o[5]), *lengths = plain(o[6]);
     if (!kc) return not_here();
@@ -215,7 +230,7 @@ try {
 // q, k_cache, v_cache, table, lengths, scale, return_lse, out, workspace
 PyObject *paged_attention(PyObject *, PyObject *const *o, Py_ssize_t n)
 try {
-    if (n != 9 || !g_attend) return not_here();
+    if (n != 9 || !g_attend || watched()) return not_here();
     const at::Tensor *q = plain(o[0]), *kc = plain(o[1]), *vc = plain(o[2]), *table = plain(o[3]), *lengths = plain(o[4]);
     if (!kc || !table) return not_here();
     const Place at{kc->scalar_type(), kc->get_device()};
@@ -278,7 +293,7 @@ try {
 // q, bounds, table, lengths, page_size, select, workspace
 PyObject *select_pages(PyObject *, PyObject *const *o, Py_ssize_t n)
 try {
-    if (n != 7 || !g_select) return not_here();
+    if (n != 7 || !g_select || watched()) return not_here();
     const at::Tensor *q = plain(o[0]), *bounds = plain(o[1]), *table = plain(o[2]), *lengths = plain(o[3]);
     if (!bounds) return not_here();
     const Place at{bounds->scalar_type(), bounds->get_device()};

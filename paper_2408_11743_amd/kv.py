@@ -19,7 +19,9 @@ most promising pages alone:
 As in ``ops``, these functions check their arguments, allocate outputs and call the
 C entry points on the current stream.  They read no tensor on the host, so a
 step can be captured into a HIP graph (one eager call on the capturing stream first, which
-makes the workspace).  There is no autograd formula (inference only).
+makes the workspace).  There is no autograd formula (inference only): where a gradient is
+asked for, or a dispatch mode, trace or transform is to see the call, it becomes that of the
+operator registered in ``torch_op``, whose backward raises, and a tangent raises here.
 """
 from __future__ import annotations
 
@@ -85,6 +87,26 @@ def _connect():
                   address(handle.marlin_select_pages), _raw_stream, ops._default_ws, B.MarlinError)
     _native = _fast
     return _fast
+
+
+_dispatch_modes = torch._C._len_torch_dispatch_stack
+_transforms, _tracing = torch._C._functorch.peek_interpreter_stack, torch._C._get_tracing_state
+_forward_ad = torch.autograd.forward_ad
+
+
+def _watched(*args) -> bool:
+    """Something beside the kernels is to see a call with these arguments (see the module's docstring)."""
+    tensors = [x for x in args if isinstance(x, torch.Tensor)]
+    return (_dispatch_modes() > 0 or _transforms() is not None or _tracing() is not None
+            or any(type(x) not in (torch.Tensor, torch.nn.Parameter) for x in tensors)
+            or (torch.is_grad_enabled() and any(x.requires_grad for x in tensors)))
+
+
+def _no_tangents(func: str, *tensors) -> None:
+    if _forward_ad._current_level >= 0:
+        for x in tensors:
+            if isinstance(x, torch.Tensor) and _forward_ad.unpack_dual(x).tangent is not None:
+                raise RuntimeError("%s: there is no forward derivative" % func)
 
 
 def _rows(func: str, name: str, x: torch.Tensor, dtype, device) -> torch.Tensor:
@@ -158,6 +180,16 @@ def kv_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_cache: torch.
                                              bounds, out)
     if done is not None:
         return done
+    if _watched(q, k, v, k_cache, v_cache, table, lengths, cos_sin, starts, bounds, out):
+        y = torch.ops.marlin_mi355x.kv_append(q, k, v, k_cache, v_cache, bounds, table, lengths, cos_sin, starts,
+                                              bool(interleaved))
+        return y if out is None else out.copy_(y)
+    return _kv_append(q, k, v, k_cache, v_cache, table, lengths, cos_sin, starts, interleaved, bounds, out)
+
+
+def _kv_append(q, k, v, k_cache, v_cache, table, lengths, cos_sin, starts, interleaved, bounds, out):
+    """The call with its checks, which name what is wrong or copy a view that the kernels cannot read."""
+    _no_tangents("kv_append", q, k, v, k_cache, v_cache, cos_sin, bounds)
     f, dtype, device = "kv_append", k_cache.dtype, k_cache.device
     _check_caches(f, k_cache, v_cache)
     q, k, v = (_rows(f, name, x, dtype, device) for name, x in (("q", q), ("k", k), ("v", v)))
@@ -217,6 +249,15 @@ def paged_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tenso
     done = (_native or _connect()).paged_attention(q, k_cache, v_cache, table, lengths, scale, return_lse, out, workspace)
     if done is not None:
         return done
+    if _watched(q, k_cache, v_cache, table, lengths, out):
+        o, lse = torch.ops.marlin_mi355x.paged_attention(q, k_cache, v_cache, table, lengths, scale)
+        o = o if out is None else out.copy_(o)
+        return (o, lse) if return_lse else o
+    return _paged_attention(q, k_cache, v_cache, table, lengths, scale, return_lse, out, workspace)
+
+
+def _paged_attention(q, k_cache, v_cache, table, lengths, scale, return_lse, out, workspace):
+    _no_tangents("paged_attention", q, k_cache, v_cache)
     f, dtype, device = "paged_attention", k_cache.dtype, k_cache.device
     _check_caches(f, k_cache, v_cache)
     q = _rows(f, "q", q, dtype, device)
@@ -261,6 +302,12 @@ def select_pages(q: torch.Tensor, bounds: torch.Tensor, table: torch.Tensor, len
     done = (_native or _connect()).select_pages(q, bounds, table, lengths, page_size, select, workspace)
     if done is not None:
         return done
+    if _watched(q, bounds, table, lengths):
+        return torch.ops.marlin_mi355x.select_pages(q, bounds, table, lengths, page_size, select)
+    return _select_pages(q, bounds, table, lengths, page_size, select, workspace)
+
+
+def _select_pages(q, bounds, table, lengths, page_size, select, workspace):
     f, dtype, device = "select_pages", bounds.dtype, bounds.device
     if dtype not in _DTYPE or not bounds.is_cuda:
         raise TypeError("select_pages: bounds must be a float16 or bfloat16 device tensor")

@@ -18,7 +18,8 @@ packs it on the GPU, in one launch where it is contiguous (``ops.quantize_linear
 ``kv_append``, ``paged_attention`` and ``select_pages`` of ``kv`` are registered
 the same way under ``torch.ops.marlin_mi355x`` (``kv_append`` declares the caches and
 the bounds it writes), for code that is traced or compiled; eager callers save the
-dispatch by calling ``kv``'s functions.
+dispatch by calling ``kv``'s functions, which come here where a gradient, mode, trace or
+transform asks for it.
 
 HIP graphs: the operator enqueues kernels only, so it can be captured.  Its
 workspace is the per-(device, stream) one of ``ops.gemm``, allocated on first
@@ -56,7 +57,9 @@ def kv_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_cache: torch.
               bounds: Optional[torch.Tensor], table: torch.Tensor, lengths: torch.Tensor,
               cos_sin: Optional[torch.Tensor] = None, starts: Optional[torch.Tensor] = None,
               interleaved: bool = False) -> torch.Tensor:
-    return kv.kv_append(q, k, v, k_cache, v_cache, table, lengths, cos_sin, starts, interleaved, bounds)
+    args = q, k, v, k_cache, v_cache, table, lengths, cos_sin, starts, interleaved, bounds, None
+    done = (kv._native or kv._connect()).kv_append(*args)
+    return kv._kv_append(*args) if done is None else done
 
 
 @kv_append.register_fake
@@ -70,7 +73,9 @@ def _kv_append_fake(q, k, v, k_cache, v_cache, bounds, table, lengths, cos_sin=N
 def paged_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, table: torch.Tensor,
                     lengths: torch.Tensor, scale: Optional[float] = None) -> Tuple[torch.Tensor, torch.Tensor]:
     """(out, lse)"""
-    return kv.paged_attention(q, k_cache, v_cache, table, lengths, scale, return_lse=True)
+    args = q, k_cache, v_cache, table, lengths, scale, True, None, None
+    done = (kv._native or kv._connect()).paged_attention(*args)
+    return kv._paged_attention(*args) if done is None else done
 
 
 @paged_attention.register_fake
@@ -83,7 +88,9 @@ def _paged_attention_fake(q, k_cache, v_cache, table, lengths, scale=None):
 @torch.library.custom_op(_NS + "::select_pages", mutates_args=())
 def select_pages(q: torch.Tensor, bounds: torch.Tensor, table: torch.Tensor, lengths: torch.Tensor, page_size: int,
                  select: int) -> Tuple[torch.Tensor, torch.Tensor]:
-    return kv.select_pages(q, bounds, table, lengths, page_size, select)
+    args = q, bounds, table, lengths, page_size, select, None
+    done = (kv._native or kv._connect()).select_pages(*args)
+    return kv._select_pages(*args) if done is None else done
 
 
 @select_pages.register_fake

@@ -371,3 +371,66 @@ def test_an_error_that_another_call_left_is_not_this_ones(mk):
     finally:
         hip.hipGetLastError()
     assert torch.equal(got, want) and torch.equal(o2, o) and torch.equal(pages2, pages)
+
+
+# ---- gradients, tangents, modes, traces, transforms ----
+
+def test_a_gradient_is_not_dropped(mk):
+    q, new, k, v, bounds, table, lengths = small_call(mk)
+    want = mk.kv_append(q, new, new, k, v, table, lengths)
+    o, lse = mk.paged_attention(want, k, v, table, lengths, return_lse=True)
+    x = q.clone().requires_grad_()
+    for y in (mk.kv_append(x, new, new, k, v, table, lengths), mk.paged_attention(x, k, v, table, lengths),
+              mk.paged_attention(x, k, v, table, lengths, return_lse=True)[1],
+              mk.paged_attention(x * 1, k, v, table, lengths, out=torch.empty_like(q))):
+        assert y.requires_grad
+        with pytest.raises(RuntimeError, match="autograd"):
+            y.float().sum().backward()
+    with torch.no_grad():
+        assert torch.equal(mk.kv_append(x, new, new, k, v, table, lengths), want)
+        assert torch.equal(mk.paged_attention(want.clone().requires_grad_(), k, v, table, lengths), o)
+    with torch.inference_mode():
+        assert torch.equal(mk.paged_attention(x, k, v, table, lengths), mk.paged_attention(q, k, v, table, lengths))
+    pages, n = mk.select_pages(x, bounds, table, lengths, 16, 2)
+    assert not pages.requires_grad and pages.shape == (2, 2, 2)
+
+
+def test_a_tangent_is_refused(mk):
+    import torch.autograd.forward_ad as fwd
+    q, new, k, v, bounds, table, lengths = small_call(mk)
+    with fwd.dual_level():
+        x = fwd.make_dual(q, torch.ones_like(q))
+        for call in (lambda: mk.kv_append(x, new, new, k, v, table, lengths), lambda: mk.paged_attention(x, k, v, table, lengths),
+                     lambda: torch.ops.marlin_mi355x.paged_attention(x, k, v, table, lengths)):
+            with pytest.raises(RuntimeError, match="derivative"):
+                call()
+        assert mk.paged_attention(q, k, v, table, lengths).shape == q.shape
+
+
+def test_modes_traces_and_transforms_see_the_calls(mk):
+    from torch.utils._python_dispatch import TorchDispatchMode
+    q, new, k, v, bounds, table, lengths = small_call(mk)
+    seen = []
+
+    class Record(TorchDispatchMode):
+        def __torch_dispatch__(self, func, types, args=(), kwargs=None):
+            seen.append(str(func))
+            return func(*args, **(kwargs or {}))
+
+    def step(x):
+        y = mk.kv_append(x, new, new, k, v, table, lengths, bounds=bounds)
+        pages, n = mk.select_pages(y, bounds, table, lengths, 16, 2)
+        return mk.paged_attention(y, k, v, pages, n)
+
+    want = step(q)
+    with Record():
+        got = step(q)
+    assert torch.equal(got, want)
+    for name in ("kv_append", "select_pages", "paged_attention"):
+        assert any("marlin_mi355x.%s" % name in x for x in seen), name
+    other = torch.randn_like(q)
+    want = mk.paged_attention(other, k, v, table, lengths)
+    traced = torch.jit.trace(lambda x: mk.paged_attention(x, k, v, table, lengths), (q,), check_trace=False)
+    assert torch.equal(traced(other), want)
+    both = torch.vmap(lambda x: mk.paged_attention(x, k, v, table, lengths))(torch.stack([q, other]))
+    assert torch.equal(both[1], want) and torch.equal(both[0], mk.paged_attention(q, k, v, table, lengths))
