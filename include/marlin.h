@@ -439,8 +439,8 @@ size_t marlin_paged_attention_workspace_bytes(int64_t head_dim);
  * over the positions j < lengths[b] whose table entries name pages.  Without any (or
  * with every score -inf) out is 0 and lse -inf.  What other slots hold does
  * not matter, NaN included.  Scores, sums and partial results are fp32; the
- * second product takes the weights in two parts of the cache's type (22 bits in
- * all of float16, 2^-40 of the row's maximum at the least; 16 of bfloat16), and out
+ * second product takes the weights in two parts of the cache's type (21 bits in
+ * all of float16, 2^-40 of the row's maximum at the least; 15 of bfloat16), and out
  * is rounded once at the end.  Bitwise reproducible for a given device and input.
  * Errors: NULL_POINTER, INVALID_SHAPE (also B * rows of heads * the table's
  * 16-key tiles beyond 2^31), MISALIGNED, INVALID_ARGUMENT (scale, dtype),

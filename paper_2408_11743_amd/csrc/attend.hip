@@ -428,38 +428,19 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
                 for (int i = 0; i < 4; ++i) pr[u][i] = __builtin_amdgcn_exp2f(sc[u][i] - ref);
 #pragma unroll
             for (int u = 0; u < KT; ++u) l += (pr[u][0] + pr[u][1]) + (pr[u][2] + pr[u][3]);
-            // The second product takes the weights in the cache's type, as its MFMAs want them, in two parts: rounded, and what
-            // that left out, rounded.  Together they hold 22 bits of a float16 cache's weights and 16 of a bfloat16 one's,
+            // The second product takes the weights in the cache's type, as its MFMAs want them, in two parts: rounded down, and what
+            // that left out, rounded.  Together they hold 21 bits of a float16 cache's weights and 15 of a bfloat16 one's,
             // float16's times 2^15, so that those far below the maximum are no subnormals (an absolute 2^-40 of it is all that is lost).
+            // Both parts of a weight (that is not lost) are above zero, so that an infinite value stays what it is.  (Rounded to
+            // nearest, and parted anew where a value is infinite: 77 tokens of 32 heads 5.7 us, this 5.45, weights in one part 5.15.)
             weights_t pf, rest;
 #pragma unroll
-            for (int e = 0; e < 4 * KT; ++e) {
-                const float x = pr[e >> 2][e & 3] * E::kWeightUnit;
-                pf[e] = (T)x;
-                rest[e] = (T)(x - (float)pf[e]);
-            }
-            float odd = 0.f;
-#pragma unroll
-            for (int u = 0; u < KT; ++u)
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-#pragma unroll
-                    for (int hf = 0; hf < kHalves; ++hf)
-#pragma unroll
-                        for (int w = 0; w < kDw; ++w) odd = E::times_zero(vr[u][i][hf][w], odd);
-            if (__any(odd != 0.f)) {  // with an infinite value, both parts of a weight above zero have to be above zero
-#pragma unroll
-                for (int e = 0; e < 4 * KT; ++e) {
-                    const float x = pr[e >> 2][e & 3] * E::kWeightUnit;
-                    if (!(x > 0.f)) continue;
-                    T part = pf[e];  // named: a bit cast of a vector's element yields the first one
-                    uint16_t bits = __builtin_bit_cast(uint16_t, part);
-                    if ((float)part > x) --bits;  // towards zero
-                    part = __builtin_bit_cast(T, bits < E::kSmallest ? E::kSmallest : bits);
-                    const T left_out = (T)(x - (float)part);
-                    pf[e] = part;
-                    rest[e] = (float)left_out > 0.f ? left_out : __builtin_bit_cast(T, E::kSmallest);
-                }
+            for (int e = 0; e < 4 * KT; e += 2) {
+                const typename E::Parts x = E::part(pr[e >> 2][e & 3], pr[e >> 2][(e & 3) + 1]);
+                pf[e] = x.first[0];
+                pf[e + 1] = x.first[1];
+                rest[e] = x.rest[0];
+                rest[e + 1] = x.rest[1];
             }
 #pragma unroll
             for (int hf = 0; hf < kHalves; ++hf)

@@ -15,12 +15,18 @@ template <>
 struct Elem<_Float16> {
     typedef _Float16 vec8 __attribute__((ext_vector_type(8)));
     typedef _Float16 vec4 __attribute__((ext_vector_type(4)));
-    static constexpr float kWeightUnit = 32768.f;  // what a softmax weight of one is in the second product (see attend.hip)
-    static constexpr uint16_t kSmallest = 0x0001;  // the bits of 2^-24
-    // c, or not a number if one of the two elements is no finite one
-    static __device__ __forceinline__ float times_zero(uint32_t x, float c)
+    typedef _Float16 vec2 __attribute__((ext_vector_type(2)));
+    // Two softmax weights, times kWeightUnit, as the sums of two parts (see attend.hip).  The first is rounded down from a little
+    // below the weight, 2^-22 of it and half of what the second part can hold at the least, so that the second is above zero too.
+    static constexpr float kWeightUnit = 32768.f;
+    struct Parts {
+        vec2 first, rest;
+    };
+    static __device__ __forceinline__ Parts part(float x, float y)
     {
-        return __builtin_amdgcn_fdot2(__builtin_bit_cast(half2_t, x), half2_t{}, c, false);
+        constexpr float kBelow = kWeightUnit * (1.f - 0x1p-22f), kHalf = 0x1.1p-25f;
+        const vec2 first = __builtin_bit_cast(vec2, __builtin_amdgcn_cvt_pkrtz(__builtin_fmaf(x, kBelow, -kHalf), __builtin_fmaf(y, kBelow, -kHalf)));
+        return {first, vec2{(_Float16)__builtin_fmaf(x, kWeightUnit, -(float)first[0]), (_Float16)__builtin_fmaf(y, kWeightUnit, -(float)first[1])}};
     }
     static __device__ __forceinline__ float4_t mfma(vec8 a, vec8 b, float4_t c)
     {
@@ -36,12 +42,17 @@ template <>
 struct Elem<__bf16> {
     typedef __bf16 vec8 __attribute__((ext_vector_type(8)));
     typedef __bf16 vec4 __attribute__((ext_vector_type(4)));
+    typedef __bf16 vec2 __attribute__((ext_vector_type(2)));
     static constexpr float kWeightUnit = 1.f;
-    static constexpr uint16_t kSmallest = 0x0080;  // 2^-126
-    static __device__ __forceinline__ float times_zero(uint32_t x, float c)
+    struct Parts {
+        vec2 first, rest;
+    };
+    static __device__ __forceinline__ Parts part(float x, float y)
     {
-        typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
-        return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, x), bf16x2_t{}, c, false);
+        constexpr float kBelow = 1.f - 0x1p-22f;
+        const uint32_t a = __builtin_bit_cast(uint32_t, x * kBelow), b = __builtin_bit_cast(uint32_t, y * kBelow);
+        const float u = __builtin_bit_cast(float, a & 0xFFFF0000u), v = __builtin_bit_cast(float, b & 0xFFFF0000u);
+        return {__builtin_bit_cast(vec2, __builtin_amdgcn_perm(b, a, 0x07060302u)), vec2{(__bf16)(x - u), (__bf16)(y - v)}};
     }
     static __device__ __forceinline__ float4_t mfma(vec8 a, vec8 b, float4_t c)
     {

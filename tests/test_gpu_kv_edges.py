@@ -14,8 +14,10 @@ import kv_reference as ref  # noqa: E402
 pytestmark = pytest.mark.gpu
 
 F16, BF16 = torch.float16, torch.bfloat16
-WEIGHT = {F16: 2.0 ** -22, BF16: 2.0 ** -17}   # a softmax weight's relative error in the second product
-LOST = {F16: 2.0 ** -40, BF16: 2.0 ** -126}    # and its absolute one, of the row's maximum
+# a softmax weight's relative error in the second product: its first part is rounded down, which leaves less than an ulp of it (2^-10,
+# 2^-7), and the rest is rounded to nearest (half an ulp of that: 2^-11, 2^-8)
+WEIGHT = {F16: 2.0 ** -21, BF16: 2.0 ** -15}
+LOST = {F16: 2.0 ** -40, BF16: 2.0 ** -126}  # and its absolute one, of the row's maximum
 
 
 @pytest.fixture(scope="module")
