@@ -60,9 +60,11 @@ __device__ __forceinline__ Pieces load_pieces(const T *row, Where at)
     return x;
 }
 
-// The same of new tokens, of which nothing is read again: non-temporal (once) where they and what becomes of them are more than the last-level cache
-// holds, as what a projection has just written may still lie there, and where a piece's row of threads takes
-// whole lines of 128 bytes.  300 MB of prompts, heads of 128: 126 -> 111 us; 26 MB: 11.9 -> 15.5; heads of 64: 223 -> 242.
+// The same of new tokens, of which nothing is read again: non-temporal (once) where they and what becomes of them are more than the
+// last-level cache holds, as what a projection has just written may still lie there, and where a piece's row of threads takes
+// whole lines of 128 bytes.  Prompts of 32, 64, 128, 256 and 512 MB, 80 heads of 128 with bounds: 15.0, 34, 59, 114 and 214 us by
+// ordinary loads, 19.9, 34, 57, 99 and 217 so; heads of 256: 17.9, 32.5, 63, 121 and 221, so 22, 34, 61, 102 and 219; heads of 64 lose
+// at every size (256 MB: 121, 129).
 template <typename T>
 __device__ __forceinline__ Pieces load_new(const T *row, Where at, bool once)
 {

@@ -22,7 +22,7 @@ using namespace dev;
 
 // Waves are independent: small work-groups come and go faster (32 sequences of up to 60000 tokens selected and attended
 // in 63.5 us with two, 64.7 four, 65.9 eight, 83 sixteen).
-constexpr int kScoreWaves = 2, kFewBlocks = 4096;
+constexpr int kScoreWaves = 2;
 
 __device__ __forceinline__ int pages_of(const SelectProblem &p, int b)
 {
@@ -52,18 +52,15 @@ __global__ void __launch_bounds__(64 * kScoreWaves) page_score_kernel(const Sele
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
     const int row = blockIdx.x / blocks, b = row / p.kv_heads, kvh = row - b * p.kv_heads;
     const int page0 = ((int)(blockIdx.x - row * blocks) * kScoreWaves + wave) * 16, at = page0 + r;
-    // A few blocks have their table's entries and queries under way while the length is; of many, most may lie past
-    // the lengths, and end at once (8 sequences of 60000 tokens in pages of 64: 31.2 us with the attention, length first 32.8;
-    // 32 ragged ones in pages of 32: 72.7, 67.2).
+    // The length first: most of a ragged batch's work-groups lie past it (32 sequences of 300 .. 60000 tokens in pages of 32
+    // selected in 17.3 us, with entries and queries under way while the length is in 21.4; one of 32000 in 9.2 both ways).
     const int pages = pages_of(p, b);
-    if (gridDim.x > kFewBlocks && (pages <= p.select || page0 >= pages)) return;
-    const int entry = at < p.width ? p.table[b * p.table_row + at] : -1;
+    if (pages <= p.select || page0 >= pages) return;
+    const int page = at < pages ? p.table[b * p.table_row + at] : -1;
     const T *q0 = (const T *)p.q + b * p.q_row + (kvh * p.group + r) * p.q_head + 8 * g;
     vec8 qf[kQ];
 #pragma unroll
     for (int t = 0; t < kQ; ++t) qf[t] = r < p.group ? *(const vec8 *)(q0 + 32 * t) : vec8{};
-    if (pages <= p.select || page0 >= pages) return;
-    const int page = at < pages ? entry : -1;
     const bool inside = (uint32_t)page < (uint32_t)p.pages;
     const T *box = (const T *)p.bounds + ((int64_t)(inside ? page : 0) * p.kv_heads + kvh) * 2 * D + 8 * g;
     vec8 lo[kQ], hi[kQ];
