@@ -56,6 +56,8 @@ def kv_cache(pages: int, kv_heads: int, page_size: int, head_dim: int, dtype=tor
 def rotation_table(positions: int, rot: int, base: float = 10000.0, device="cuda") -> torch.Tensor:
     """float32 [positions, rot]: row j holds cos(j f_i), then sin(j f_i), f_i =
     base^(-2i / rot), the table ``kv_append`` rotates by (computed in 64 bits)."""
+    if rot < 0 or rot % 2 or positions < 0:
+        raise ValueError("rotation_table: rot must be even, and neither it nor positions negative")
     f = float(base) ** (-torch.arange(0, rot, 2, dtype=torch.float64, device=device) / rot)
     angle = torch.arange(positions, dtype=torch.float64, device=device)[:, None] * f
     return torch.cat([angle.cos(), angle.sin()], 1).float()

@@ -177,6 +177,13 @@ def test_rotation_table():
             assert abs(float(t[j, i]) - math.cos(a)) < 1e-7 and abs(float(t[j, 4 + i]) - math.sin(a)) < 1e-7
 
 
+def test_rotation_table_refusals():
+    for positions, rot in ((5, 7), (5, -2), (-1, 8)):
+        with pytest.raises(ValueError):
+            mk.rotation_table(positions, rot, device="cpu")
+    assert mk.rotation_table(0, 8, device="cpu").shape == (0, 8) and mk.rotation_table(3, 0, device="cpu").shape == (3, 0)
+
+
 def test_operators_are_registered_with_shapes():
     def meta(*shape, dtype=torch.float16):
         return torch.empty(*shape, dtype=dtype, device="meta")
