@@ -277,22 +277,17 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
         const int slot = (x.s * kStepKeys + kTileKeys * u) & ((1 << p.page_shift) - 1);
         return ((((int64_t)((uint32_t)e < (uint32_t)p.pages ? e : 0) * p.kv_heads + kvh) << p.page_shift) + slot) * D;
     };
-    // Values are read once, whole rows at a time: non-temporal.  A load of keys takes 64 bytes of a row, the
-    // other half of a line following at once; that goes better through the caches (values and keys non-temporal: 20 sequences
-    // of up to 9001 tokens, heads of 256, 30.3 us, values alone 29.1, neither 28.8), until
-    // the keys and values are more than the last-level cache holds (131071 tokens, 537 MB: 88, 90, 99 us).
-    // Rows of 192 bytes straddle lines (d = 96, 3 GB: 487, 462, 517 us), and the tiles of a larger group read the keys again.
-    const bool stream_keys = D != 96 && tiles == 1 && total * rows > ((256 << 20) / (kStepKeys * 4 * D));
+    // Values are read once, whole rows at a time: non-temporal (131071 tokens, 537 MB: 90.2 us, 98.5 through the caches; 16 sequences
+    // of up to 4001: 24.9, 27.3).  A load of keys takes 64 bytes of a row, the other half of a line following at once, and goes through
+    // the caches: non-temporal, it is within 2 % on large calls, some faster, some slower (128 ragged sequences, 867 MB: 141.0 us, not
+    // 143.2; 131071 tokens: 93.5, not 92.6; 64 sequences of 32768: 1315, not 1305), and slower on small ones (16 of up to 4001: 27.1).
     auto load_keys = [&](const Step &x) {
 #pragma unroll
         for (int u = 0; u < KT; ++u) {
             if (u > 0 && x.s * kStepKeys + kTileKeys * u >= x.tokens) break;  // masked, whatever the registers hold
             const T *k = (const T *)p.k + tile_at(x, u);
 #pragma unroll
-            for (int t = 0; t < kQ; ++t) {
-                const vec8 *at = (const vec8 *)(k + (r * D + 8 * g) + 32 * t);
-                kf[u][t] = stream_keys ? __builtin_nontemporal_load(at) : *at;
-            }
+            for (int t = 0; t < kQ; ++t) kf[u][t] = *(const vec8 *)(k + (r * D + 8 * g) + 32 * t);
         }
     };
     auto load_values = [&](const Step &x) {
