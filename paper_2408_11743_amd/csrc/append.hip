@@ -6,9 +6,9 @@
 // A head is D / 16 threads, each with two 16-byte pieces that hold eight pairs.
 // Nothing is read twice but the angles.  Prompts are bound by memory (24
 // prompts of up to 4096 tokens, 64 + 16 heads of 128 with bounds, 605 MB read and written:
-// 123 us, 4.9 TB/s, and 111 where the queries' last-level lines are written again; a large copy
-// reaches 4.8), a token per sequence by launch latency (32 + 16 heads: 2.7 us; 128
-// sequences of 64 + 16 heads with bounds: 3.7).
+// 124 us, 4.9 TB/s, and 111 where the queries' last-level lines are written again; a large copy
+// reaches 4.8), a token per sequence by launch latency (32 + 16 heads: 2.4 us; 128
+// sequences of 64 + 16 heads with bounds: 4.0).
 #include <hip/hip_runtime.h>
 
 #include "kv.h"
@@ -196,8 +196,8 @@ __global__ void __launch_bounds__(256) append_token_kernel(const AppendProblem p
 // of q, of k or of v: each wave some tokens, whose four heads it reads before
 // it writes any.  Keys with bounds are a head a wave instead, so that a page's
 // bounds are one wave's: kept in its registers and joined across its lanes (all
-// four heads' in every wave, joined in LDS: 64 registers, which spilled, 130 us for the
-// prompts above).  Neighbouring work-groups take the heads of one page, which lie side by side in
+// four heads' in every wave, joined in LDS: 64 registers, which spilled, 130 us where the
+// prompts above take 111).  Neighbouring work-groups take the heads of one page, which lie side by side in
 // the tokens' rows (neighbouring pages instead: 9 % more).
 // Slabs of two heads: 24 % more, of eight 5 % more.
 constexpr int kSlab = 4;

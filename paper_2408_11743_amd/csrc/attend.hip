@@ -26,12 +26,12 @@
 //
 // Bound by memory: a step's 16 KB (d = 128) take a compute unit 0.6 us of its
 // share of the bandwidth and 0.1 us of MFMA and vector work.  64 sequences of
-// 32768 tokens, 64 heads over 8 (8.6 GB): 1.26 ms, 6.8 TB/s, where a kernel that
-// only reads reaches 7.1; one of 131071 tokens: 89 us, 6.0.  Short
+// 32768 tokens, 64 heads over 8 (8.6 GB): 1.25 ms, 6.9 TB/s, where a kernel that
+// only reads reaches 7.1; one of 131071 tokens: 90 us, 6.0.  Short
 // calls are latency: 2 us to the first load of keys, a round trip a step, 4 to
-// 6 us where rows are cut between work-groups (77 tokens of 32 heads: 5.2 us,
-// one sequence of 8000 tokens over 8 kv heads, 33 MB: 14.0).  Four waves a work-group,
-// two work-groups a compute unit: 98 us for the 131071 tokens; eight and two: 100.
+// 6 us where rows are cut between work-groups (77 tokens of 32 heads: 5.4 us,
+// one sequence of 8000 tokens over 8 kv heads, 33 MB: 13.6).  Four waves a work-group,
+// two work-groups a compute unit: 96 us for the 131071 tokens; eight and two: 99.5.
 #include <hip/hip_runtime.h>
 
 #include "device.h"
@@ -47,8 +47,9 @@ using namespace dev;
 // A work-group border does not cut a row closer to its ends than min_cut
 // (it moves to the end): a cut costs a round trip through the workspace.
 // min_cut is a quarter of a range, so that no range grows much, between these: with 6
-// throughout, 256 sequences of 1 .. 1000 tokens take 43.7 us and not 42, with 16
-// throughout, one of 2000 takes 14.7 and not 12.7.
+// throughout, 200 sequences of 1 .. 400 tokens, 32 heads over 8, take 21.4 us and not 19.3 (256 of 1 .. 1000: 37.1,
+// 36.9).  Both of a range's borders may move towards each other, so twice min_cut stays within the shortest range, kMinTiles, and 6
+// is the most that it admits.
 constexpr int kMinCut = 6, kMaxCut = 16;
 // What a row costs beyond its steps (queries, output).
 constexpr int kRowTiles = 2;
@@ -136,9 +137,9 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
     // Range w starts at unit w * units / grid, rounded down, which puts borders between rows of one length; or, where
     // there are few, at w * kMinSteps.
     // A larger group's head tiles read the same keys: the work-groups of a range, one a tile, are neighbours on one XCD, whose L2
-    // they share (173 sequences of 4859 tokens, 32 heads over 1: 96 us; tiles one after the other as rows 120, and these spread over the XCDs
-    // 146 where they take 103 for 16 of up to 30000, 64 over 2). Other ranges share nothing, and large caches go faster spread over the XCDs (64
-    // sequences of 32768 tokens: 1.25 ms, 1.27).
+    // they share (173 sequences of 4859 tokens, 32 heads over 1: 98 us, spread over the XCDs 131; 16 of 300 .. 30000, 64 over 2: 33.3,
+    // 43.5).  Other ranges share nothing, and neighbours on one XCD are no different (64 sequences of 32768 tokens 1249 us, spread
+    // 1245; 16 of 500 .. 4001 25.0, 24.9; one of 2000 9.75, 9.8).
     const int tiles = p.head_tiles, grid = tiles == 1 ? gridDim.x : gridDim.x / tiles;
     const int place = tiles == 1 ? blockIdx.x : xcd_local_wg(blockIdx.x, gridDim.x);
     const int wg = tiles == 1 ? place : place / tiles, tile = place - wg * tiles;
@@ -218,8 +219,8 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
     };
     const Place wg_from = border(wg), wg_to = border(wg + 1);
     const int begin = wg_from.before + wg_from.step, steps = wg_to.before + wg_to.step - begin;
-    // Uneven shares: more to the first waves, whose loads are served first (77 tokens of 32 heads: 5.2 us, to the last
-    // waves 5.9; 20 sequences, heads of 256: 26.9, 28.4).
+    // Uneven shares: more to the first waves, whose loads are served first (77 tokens of 32 heads: 5.6 us, to the last
+    // waves 5.75; 20 sequences, heads of 256: 26.3, 27.7).
     const int share = steps / NW, odd = steps % NW;
     const int mine = share * wave + (wave < odd ? wave : odd);
     int left = share + (wave < odd ? 1 : 0);  // steps of this wave
@@ -427,7 +428,7 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
             // that left out, rounded.  Together they hold 21 bits of a float16 cache's weights and 15 of a bfloat16 one's,
             // float16's times 2^15, so that those far below the maximum are no subnormals (an absolute 2^-40 of it is all that is lost).
             // Both parts of a weight (that is not lost) are above zero, so that an infinite value stays what it is.  (Rounded to
-            // nearest, and parted anew where a value is infinite: 77 tokens of 32 heads 5.7 us, this 5.45, weights in one part 5.15.)
+            // nearest, and parted anew where a value is infinite: 77 tokens of 32 heads 5.70 us, this 5.45, weights in one part 5.15.)
             weights_t pf, rest;
 #pragma unroll
             for (int e = 0; e < 4 * KT; e += 2) {
@@ -546,8 +547,8 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
                 store_float(slot + kHeadTile * D + kHeadTile + r, sum);
             }
         };
-        // a row through the whole range, without branches: one sequence of 8000 tokens 13.9 us, 14.4 (ragged ones of
-        // heads of 256: 27 us, 25.5)
+        // a row through the whole range, without branches: one sequence of 8000 tokens 13.6 us, with them 14.0 (heads of
+        // 256: 20 ragged ones 27.7, with them 26.4, though 16 of 30000 157, with them 164)
         if (D <= 128 && slots == all)
             join_slots(all, put);
         else
@@ -555,7 +556,7 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
     }
     // Many contributors are joined in teams (beside each other, the last to arrive joins the team's pieces into its first
     // one's slot, and the last of those the teams'), as one compute unit reads 57 KB a us at most (one sequence of
-    // 102932 tokens, 5 heads of 256 over 1: 30.6 us, all by one work-group 54; 60000, 32 heads of 128 over 1: 21.1, 26.3; joins of 9 to
+    // 102932 tokens, 5 heads of 256 over 1: 30.5 us, all by one work-group 54; 60000, 32 heads of 128 over 1: 18.7, 24.7; joins of 9 to
     // 30 contributors, which take this path in one step, cost 0.2 us more for it).
     constexpr int kTeam = 2 * NW;
     auto in_teams = [&](int n) { return n * nh * D > kTeamFloats; };
@@ -591,7 +592,7 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
             if (p.lse && g == 0 && j == 0) p.lse[at] = (top + __builtin_amdgcn_logf(sum)) * 0.693147180559945f;
         };
         // Contributors are joined in order, so that the bits are the same every time.  Of a few, a wave takes its channels at once
-        // (16 sequences of up to 4001 tokens: 25.1 us, by LDS as below 26.4; the registers of both do not go together where heads are wide).
+        // (16 sequences of up to 4001 tokens: 24.9 us, by LDS as below 26.1; the registers of both do not go together where heads are wide).
         constexpr int kFew = 8;
         if (D <= 128 && last - first < kFew) {
             if (wave < kAcc && r < nh) {
@@ -687,8 +688,8 @@ hipError_t launch_one(const AttendProblem &p, int cus, hipStream_t stream)
     const int groups = (cus < kKvMaxCus ? cus : kKvMaxCus) * kAttendGroupsPerCu;
     const int ranges = groups > p.head_tiles ? groups / p.head_tiles : 1;  // at most 64 tiles
     // Wide heads: one tile a step, which keeps the registers and divides short ranges finer (heads of 256, 20 sequences of up
-    // to 9001 tokens 27.8 us, two tiles 30.6; 16 of 30000: 158, 168).  Narrower ones: two, fewer round trips in short
-    // ranges (one sequence of 2000, heads of 128: 10.4 us, one tile 11.1).
+    // to 9001 tokens 26.4 us, two tiles 29.0; 16 of 30000: 164.4, 165.4).  Narrower ones: two, fewer round trips in short
+    // ranges (one sequence of 2000, heads of 128: 9.8 us, one tile 10.7).
     constexpr int kTiles = D > 128 ? 1 : 2;
     AttendProblem q = p;
     q.grid_reciprocal = ranges > 1 ? (uint32_t)(((uint64_t)1 << 32) / (uint64_t)ranges) : 0xFFFFFFFFu;

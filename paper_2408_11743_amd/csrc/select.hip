@@ -8,8 +8,8 @@
 // a product over 2 D channels for the MFMAs, and the best `select` are kept in the
 // order of their positions.
 //
-// Latency bounds both kernels: 8 rows of 4063 pages are scored in 5.6 us (16.6
-// MB) and picked from in 5.9, 256 rows of 10 .. 1875 in 14.8 (48.7 MB) and 5.9.
+// Latency bounds both kernels: 8 rows of 4063 pages are scored in 6.2 us (16.6
+// MB) and picked from in 6.4, 256 rows of 10 .. 1875 in 14.6 (48.7 MB) and 6.1.
 #include <hip/hip_runtime.h>
 
 #include "kv.h"
@@ -21,7 +21,7 @@ namespace {
 using namespace dev;
 
 // Waves are independent: small work-groups come and go faster (32 sequences of up to 60000 tokens selected and attended
-// in 63.5 us with two, 64.7 four, 65.9 eight, 83 sixteen).
+// in 62.7 us with two, 64.1 four, 65.9 eight).
 constexpr int kScoreWaves = 2;
 
 __device__ __forceinline__ int pages_of(const SelectProblem &p, int b)
@@ -43,7 +43,7 @@ __device__ __forceinline__ uint32_t score_key(float x)
 // A wave scores 16 pages: lane (r = l % 16, g = l / 16) loads 16-byte pieces of
 // page r's bounds and gets the products of heads 4g .. 4g + 3 with it.  (Two,
 // four or eight tiles a wave, the queries loaded once: 32 sequences of up to 60000 tokens
-// selected and attended in 69.0, 77.8, 86.1 us, against 68.8.)
+// selected and attended in 69.0, 77.8, 86.1 us when one took 68.8.)
 template <typename T, int D>
 __global__ void __launch_bounds__(64 * kScoreWaves) page_score_kernel(const SelectProblem p, int blocks)
 {
@@ -330,8 +330,8 @@ hipError_t launch_one(const SelectProblem &p, hipStream_t stream)
 {
     constexpr int kPer = 16 * kScoreWaves;
     const int blocks = (p.width + kPer - 1) / kPer;
-    // no scores where every sequence keeps all the pages it can have (one sequence of 21 tokens: 9.8 us with the
-    // attention, 12.3 with a launch that finds nothing to do)
+    // no scores where every sequence keeps all the pages it can have (one sequence of 21 tokens: 9.0 us with the
+    // attention, 11.3 with a launch that finds nothing to do)
     SelectProblem q = p;
     if (p.width > p.select) {
         int n = blocks;
