@@ -21,7 +21,8 @@ C entry points on the current stream.  They read no tensor on the host, so a
 step can be captured into a HIP graph (one eager call on the capturing stream first, which
 makes the workspace).  There is no autograd formula (inference only): where a gradient is
 asked for, or a dispatch mode, trace or transform is to see the call, it becomes that of the
-operator registered in ``torch_op``, whose backward raises, and a tangent raises here.
+operator registered in ``torch_op``, whose backward raises (it uses the stream's own
+workspace, not one that is passed), and a tangent raises here.
 """
 from __future__ import annotations
 
@@ -150,6 +151,14 @@ def _check_out(func: str, out: torch.Tensor, shape, dtype, device) -> None:
           and not out.is_neg(), func, "out must be a contiguous tensor of q's shape, dtype and device")
 
 
+def _into(func: str, out, result: torch.Tensor) -> torch.Tensor:
+    """A registered operator's result, in the caller's tensor if there is one."""
+    if out is None:
+        return result
+    _check_out(func, out, result.shape, result.dtype, result.device)
+    return out.copy_(result)
+
+
 _empty_like, _contiguous = torch.empty_like, torch.contiguous_format
 
 
@@ -185,7 +194,7 @@ def kv_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_cache: torch.
     if _watched(q, k, v, k_cache, v_cache, table, lengths, cos_sin, starts, bounds, out):
         y = torch.ops.marlin_mi355x.kv_append(q, k, v, k_cache, v_cache, bounds, table, lengths, cos_sin, starts,
                                               bool(interleaved))
-        return y if out is None else out.copy_(y)
+        return _into("kv_append", out, y)
     return _kv_append(q, k, v, k_cache, v_cache, table, lengths, cos_sin, starts, interleaved, bounds, out)
 
 
@@ -253,7 +262,7 @@ def paged_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tenso
         return done
     if _watched(q, k_cache, v_cache, table, lengths, out):
         o, lse = torch.ops.marlin_mi355x.paged_attention(q, k_cache, v_cache, table, lengths, scale)
-        o = o if out is None else out.copy_(o)
+        o = _into("paged_attention", out, o)
         return (o, lse) if return_lse else o
     return _paged_attention(q, k_cache, v_cache, table, lengths, scale, return_lse, out, workspace)
 

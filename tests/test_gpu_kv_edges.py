@@ -393,6 +393,8 @@ def test_a_gradient_is_not_dropped(mk):
         assert torch.equal(mk.paged_attention(want.clone().requires_grad_(), k, v, table, lengths), o)
     with torch.inference_mode():
         assert torch.equal(mk.paged_attention(x, k, v, table, lengths), mk.paged_attention(q, k, v, table, lengths))
+    with pytest.raises(ValueError, match="out"):
+        mk.paged_attention(x, k, v, table, lengths, out=torch.empty(3, 2, 4, 64, dtype=F16, device="cuda"))
     pages, n = mk.select_pages(x, bounds, table, lengths, 16, 2)
     assert not pages.requires_grad and pages.shape == (2, 2, 2)
 
