@@ -485,6 +485,129 @@ size_t marlin_select_pages_workspace_bytes(int64_t B, int64_t kv_heads, int64_t 
  */
 marlin_status_t marlin_select_pages(const marlin_select_pages_args *args, hipStream_t stream);
 
+/*
+ * ---- 8-bit cache, windows, several new tokens a sequence, page tables ----
+ *
+ * An 8-bit cache holds keys and values as OCP e4m3 codes in the same pages,
+ * [pages][kv_heads][page_size][head_dim] bytes, with scales [pages][kv_heads][2]
+ * [page_size / 16]: one fp32 scale for the 16 keys of a block of slots, then one for its
+ * values.  An element is its code times its scale.  Scales are 2^-40 .. 2^40; a block
+ * with another one (a new cache's 0, a NaN) counts as masked when read.
+ */
+typedef struct {
+    const void *q, *k, *v;     /* as marlin_kv_append_args                                  */
+    int64_t q_row, q_head;
+    int64_t k_row, k_head;
+    int64_t v_row, v_head;
+    void *q_out;               /* may be q where q is dense                                 */
+    void *k_cache, *v_cache;   /* e4m3 codes                                                */
+    float *scales;             /* [pages][kv_heads][2][page_size / 16]                      */
+    const float *cos_sin;
+    int64_t positions, rot, interleaved;
+    const int32_t *table;
+    int64_t table_row;
+    const int32_t *lengths, *starts;
+    int64_t tokens;
+    int64_t B, heads, kv_heads, head_dim, pages, page_size, width;
+    int64_t dtype;             /* marlin_dtype_t of q, k, v and q_out                       */
+} marlin_kv_append8_args;
+
+/*
+ * marlin_kv_append8 - marlin_kv_append into an 8-bit cache (without bounds).
+ *
+ * Keys are rotated in fp32, each product and sum rounded.  Of a block of 16 slots that
+ * gets new tokens, a is the largest finite magnitude among theirs and s the least power of two,
+ * 2^-40 .. 2^40, with a <= 448 s.  If earlier tokens of the sequence lie in
+ * the block, s is no less than the block's scale so far (where that is 2^-40 .. 2^40), and
+ * where it grew their codes are rounded anew, code * (old / s).  A new element becomes
+ * the e4m3 number nearest to x / s (ties to even), at most 448 in magnitude (what 2^40
+ * cannot hold); an infinity or NaN becomes NaN.  Slots behind the last token keep what they hold.
+ * Errors: as marlin_kv_append.
+ */
+marlin_status_t marlin_kv_append8(const marlin_kv_append8_args *args, hipStream_t stream);
+
+typedef struct {
+    const void *q;               /* [tokens][heads][head_dim]                               */
+    int64_t q_row, q_head;
+    const void *k_cache, *v_cache; /* of dtype, or e4m3 codes where scales is given         */
+    const float *scales;         /* [pages][kv_heads][2][page_size / 16], or NULL           */
+    const int32_t *table;        /* [B][width] or, with table_head, [B][kv_heads][width]    */
+    int64_t table_row, table_head;
+    const int32_t *lengths;      /* [B], new tokens included                                */
+    const int32_t *starts;       /* [B + 1]: sequence b's tokens are rows starts[b] .. starts[b + 1] - 1; NULL: one each */
+    int64_t tokens;              /* rows of q, at most 2^24                                 */
+    int64_t window, sinks;       /* 0: no window, at most 2^30; first positions that stay visible, 0 .. 2^30 */
+    void *out;                   /* [tokens][heads][head_dim], written                      */
+    float *lse;                  /* [tokens][heads], written, or NULL                       */
+    void *workspace;             /* as for marlin_gemm (one buffer serves all)              */
+    uint64_t workspace_bytes;
+    int64_t B, heads, kv_heads, head_dim, pages, page_size, width;
+    double scale;                /* finite                                                  */
+    int64_t dtype;               /* of q and out                                            */
+} marlin_cache_attention_args;
+
+/* Bytes of workspace marlin_cache_attention needs for these sizes (starts: 0 where it is NULL; 0 for sizes it does not take). */
+size_t marlin_cache_attention_workspace_bytes(int64_t starts, int64_t tokens, int64_t B, int64_t heads, int64_t kv_heads,
+                                              int64_t head_dim);
+
+/*
+ * marlin_cache_attention - attention of any number of new tokens per sequence over
+ * a cache of 16 or 8 bits.
+ *
+ * The i-th of sequence b's n tokens has position p = lengths[b] - n + i and attends,
+ * by marlin_paged_attention's formula, to the positions j <= p with, where
+ * window > 0, j > p - window or j < sinks, of those that lie within the table, whose
+ * entries name pages and, in an 8-bit cache, whose blocks' scales are 2^-40 .. 2^40.  What other
+ * slots hold does not matter, NaN included.  A token that sees nothing gives 0 and -inf.
+ * Rows of out and lse that belong to no sequence are left as they are.
+ *
+ * Scores, sums and partial results are fp32.  One token per sequence (starts NULL): the weights are rounded as by
+ * marlin_paged_attention (to 21 bits, 15 of bfloat16).  Several: once to dtype.  Bitwise reproducible for a
+ * given device and input.
+ * Errors: as marlin_paged_attention (the limit of 2^31 without starts only); INVALID_SHAPE also for tokens, for
+ * tokens * heads / kv_heads beyond 2^30, for table_head with starts, and for tokens other than B without; INVALID_ARGUMENT
+ * also for window and sinks.
+ */
+marlin_status_t marlin_cache_attention(const marlin_cache_attention_args *args, hipStream_t stream);
+
+typedef struct {
+    int32_t *table;              /* [B][width], read and written                            */
+    int64_t table_row;
+    int32_t *lengths;            /* [B], read and written                                   */
+    const int32_t *new_tokens;   /* [B]: tokens the sequence gets; below 0: it ends         */
+    int32_t *free_pages;         /* [pages], its first free_count entries are free pages    */
+    int32_t *free_count;         /* [1]                                                     */
+    int32_t *starts;             /* [B + 1], written                                        */
+    int64_t *slots;              /* [tokens], written                                       */
+    void *workspace;             /* as for marlin_gemm (one buffer serves all)              */
+    uint64_t workspace_bytes;
+    int64_t B, width, pages, page_size, tokens, window, sinks;
+} marlin_assign_pages_args;
+
+/* Bytes of workspace marlin_assign_pages needs (0 for a B it does not take). */
+size_t marlin_assign_pages_workspace_bytes(int64_t B);
+
+/*
+ * marlin_assign_pages - the tables of a step: pages for its new tokens, pages given back.
+ *
+ * In the sequences' order, with L = lengths[b] (below 0: 0; past the table: its end) and n = new_tokens[b]:
+ *  1. n < 0: the sequence ends.  The entries of its ceil(L / page_size) pages that name pages are appended
+ *     to the free ones and become -1, and its length 0.  Otherwise, where window > 0, the same is done to the entries
+ *     below position L - window (whole pages) from there back to the first that names
+ *     no page, and at the most to the pages that hold the first `sinks` positions.
+ *  2. A sequence with n > 0 is served if L + n fits the table, and if the pages that it and the
+ *     fitting sequences before it need are among the free ones, their new tokens among `tokens`.  It takes pages from
+ *     the end of the free ones, the last first, and its length becomes L + n.  A sequence that is not served keeps its length and gets nothing.
+ *  starts: where each sequence's new tokens begin (those of a sequence not served: none), as the other entry
+ *  points take it.  slots[t]: page * page_size + slot of new token t, -1 where
+ *  the sequence's last page so far is no page, or behind the last token.
+ * A free_count outside 0 .. pages is clamped to it, and pages beyond `pages` free ones are not kept.  An entry of free_pages
+ * that names no page is handed out as it is, and its tokens count as masked.
+ * B 0 .. 2^16 (0: starts[0] and slots are written), tokens 0 .. 2^24; sizes as above.
+ * Errors: NULL_POINTER, INVALID_SHAPE, MISALIGNED, INVALID_ARGUMENT (window, sinks), WORKSPACE_TOO_SMALL, HIP.
+ */
+marlin_status_t marlin_assign_pages(const marlin_assign_pages_args *args, hipStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

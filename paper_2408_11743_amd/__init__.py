@@ -11,6 +11,8 @@ The compute runs in hand-written HIP kernels behind the C ABI of
   points);
 * ``kv_cache``, ``rotation_table``, ``kv_append``, ``paged_attention``,
   ``select_pages``: the paged key-value cache between a layer's projections (``kv``);
+* ``kv_cache8``, ``kv_append8``, ``cache_attention``, ``assign_pages``: the cache in 8
+  bits, windows and sinks, several new tokens per sequence, page tables (``cache``);
 * ``MarlinLinear`` and the operator ``torch.ops.marlin_mi355x.gemm``
   (``torch_op``), registered on import;
 * ``roofline``:  byte / FLOP accounting and MI355X peaks used by the bench.
@@ -22,12 +24,17 @@ from ._binding import (  # noqa: F401
     LAYOUT_VERSION,
     MarlinError,
     lib,
+    marlin_assign_pages,
+    marlin_assign_pages_workspace_bytes,
+    marlin_cache_attention,
+    marlin_cache_attention_workspace_bytes,
     marlin_describe,
     marlin_describe_sparse,
     marlin_gemm,
     marlin_gemm_no_alloc,
     marlin_gemm_sparse,
     marlin_kv_append,
+    marlin_kv_append8,
     marlin_layout_version,
     marlin_pack_sparse_weights,
     marlin_pack_weights,
@@ -44,6 +51,7 @@ from ._binding import (  # noqa: F401
     marlin_unpack_weights,
     marlin_workspace_bytes,
 )
+from .cache import assign_pages, cache_attention, kv_append8, kv_cache8  # noqa: F401
 from .kv import kv_append, kv_cache, paged_attention, rotation_table, select_pages  # noqa: F401
 from .ops import CLIP_RATIOS, Workspace, gemm, pack, quantize, unpack  # noqa: F401
 from .torch_op import MarlinLinear  # noqa: F401  (registers torch.ops.marlin_mi355x.gemm)

@@ -53,6 +53,11 @@ SIGNATURES = {
     "marlin_paged_attention": (ctypes.c_int, [_vp, _vp]),
     "marlin_select_pages_workspace_bytes": (_sz, [_i64, _i64, _i64]),
     "marlin_select_pages": (ctypes.c_int, [_vp, _vp]),
+    "marlin_kv_append8": (ctypes.c_int, [_vp, _vp]),
+    "marlin_cache_attention_workspace_bytes": (_sz, [_i64] * 6),
+    "marlin_cache_attention": (ctypes.c_int, [_vp, _vp]),
+    "marlin_assign_pages_workspace_bytes": (_sz, [_i64]),
+    "marlin_assign_pages": (ctypes.c_int, [_vp, _vp]),
     # marlin_quantize and marlin_pack_weights in one launch for a linear
     # layer's weight [N, K] (internal: not declared in marlin.h)
     "marlin_quantize_linear": (ctypes.c_int, [_vp, _i64, _i64, _i64, ctypes.POINTER(ctypes.c_float), ctypes.c_int,
@@ -217,9 +222,17 @@ PAGED_ATTENTION_FIELDS = ("q q_row q_head k_cache v_cache table table_row table_
                           "workspace_bytes B heads kv_heads head_dim pages page_size width scale dtype").split()
 SELECT_PAGES_FIELDS = ("q q_row q_head bounds table table_row lengths chosen chosen_lengths workspace workspace_bytes B "
                        "heads kv_heads head_dim pages page_size width select dtype").split()
+KV_APPEND8_FIELDS = ["scales" if f == "bounds" else f for f in KV_APPEND_FIELDS]
+CACHE_ATTENTION_FIELDS = ("q q_row q_head k_cache v_cache scales table table_row table_head lengths starts tokens window sinks "
+                          "out lse workspace workspace_bytes B heads kv_heads head_dim pages page_size width scale dtype").split()
+ASSIGN_PAGES_FIELDS = ("table table_row lengths new_tokens free_pages free_count starts slots workspace workspace_bytes B width "
+                       "pages page_size tokens window sinks").split()
 pack_kv_append = struct.Struct("%dq" % len(KV_APPEND_FIELDS)).pack
 pack_paged_attention = struct.Struct("20qdq").pack
 pack_select_pages = struct.Struct("%dq" % len(SELECT_PAGES_FIELDS)).pack
+pack_kv_append8 = pack_kv_append
+pack_cache_attention = struct.Struct("25qdq").pack
+pack_assign_pages = struct.Struct("%dq" % len(ASSIGN_PAGES_FIELDS)).pack
 
 
 def _fields(func: str, names, args: dict):
@@ -253,3 +266,29 @@ def marlin_select_pages(stream=None, **args) -> None:
     """args: the fields of marlin_select_pages_args by name."""
     _check("marlin_select_pages", lib().marlin_select_pages(
         pack_select_pages(*_fields("marlin_select_pages", SELECT_PAGES_FIELDS, args)), _stream(stream)))
+
+
+def marlin_kv_append8(stream=None, **args) -> None:
+    """args: the fields of marlin_kv_append8_args by name."""
+    _check("marlin_kv_append8", lib().marlin_kv_append8(
+        pack_kv_append8(*_fields("marlin_kv_append8", KV_APPEND8_FIELDS, args)), _stream(stream)))
+
+
+def marlin_cache_attention_workspace_bytes(starts: int, tokens: int, B: int, heads: int, kv_heads: int, head_dim: int) -> int:
+    return lib().marlin_cache_attention_workspace_bytes(starts, tokens, B, heads, kv_heads, head_dim)
+
+
+def marlin_cache_attention(stream=None, **args) -> None:
+    """args: the fields of marlin_cache_attention_args by name."""
+    _check("marlin_cache_attention", lib().marlin_cache_attention(
+        pack_cache_attention(*_fields("marlin_cache_attention", CACHE_ATTENTION_FIELDS, args)), _stream(stream)))
+
+
+def marlin_assign_pages_workspace_bytes(B: int) -> int:
+    return lib().marlin_assign_pages_workspace_bytes(B)
+
+
+def marlin_assign_pages(stream=None, **args) -> None:
+    """args: the fields of marlin_assign_pages_args by name."""
+    _check("marlin_assign_pages", lib().marlin_assign_pages(
+        pack_assign_pages(*_fields("marlin_assign_pages", ASSIGN_PAGES_FIELDS, args)), _stream(stream)))

@@ -24,7 +24,7 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(HERE, "libmarlin_mi355x.so")
 FAST = os.path.join(HERE, "_fast.so")
 SOURCES = ["api.cpp", "plan.cpp", "gemm.hip", "pair.hip", "tile.hip", "tile8.hip", "wide.hip", "pack.hip", "quant.hip", "noalloc.hip",
-           "kv_api.cpp", "append.hip", "attend.hip", "select.hip"]
+           "kv_api.cpp", "append.hip", "append8.hip", "attend.hip", "prompt.hip", "select.hip", "pages.hip"]
 ARCH = "gfx950"
 
 # Packed fp32 instructions are disabled for all device code: plain float code

@@ -63,6 +63,27 @@ __device__ __forceinline__ int cap_tokens(const AttendProblem &p, int n)
     return n < 0 ? 0 : n < cap ? n : cap;
 }
 
+// What a row's token sees through a window: positions below `sinks` and from `low` to before `end`, in steps of 2^shift keys that
+// leave out `skip` of them after the first `sink_steps`.
+struct Seen {
+    int end, low, sinks, sink_steps, skip, steps;
+};
+__device__ __forceinline__ Seen seen_of(const AttendProblem &p, int tokens, int shift)
+{
+    Seen x;
+    const int cap = p.width << p.page_shift, up = (1 << shift) - 1;
+    x.end = tokens < cap ? tokens : cap;
+    x.low = tokens > p.window ? tokens - p.window : 0;
+    x.sinks = p.sinks < x.low ? p.sinks : x.low;
+    const int all = (x.end + up) >> shift, first = x.low >> shift;
+    x.sink_steps = (x.sinks + up) >> shift;
+    if (x.sink_steps > all) x.sink_steps = all;
+    x.skip = (first < all ? first : all) - x.sink_steps;
+    if (x.skip < 0) x.skip = 0;
+    x.steps = all - x.skip;
+    return x;
+}
+
 // Where a range begins or ends: a step of a row.
 struct Place {
     int b, row;  // sequence, and its row: kv head
@@ -79,8 +100,14 @@ struct Step {
     int e[KT];
 };
 
-// KT: 16-key tiles of a step
-template <typename T, int D, int NW, int KT>
+// KT: 16-key tiles of a step; Eight: the cache holds e4m3 codes; Window: of a row p.window tokens and the first p.sinks are seen
+//
+// An 8-bit cache's codes become elements of T in the registers, exactly, and never meet their scales there.  A tile's keys share
+// one, which joins the scores' factor, and its values' scale s is a part of the weights: p' = exp2(score + log2 s - m'), where m' is
+// the maximum of score + log2 s, is what the second product takes, and the sum of the softmax takes p' / s.  With scales from
+// 2^-40 to 2^40 nothing of either sum is lost that fp32 would keep: a weight below 2^-126 in p' is below 2^-86 in the sum, whose
+// largest term is 2^-40 at the least.
+template <typename T, int D, int NW, int KT, bool Eight, bool Window>
 __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendProblem p)
 {
     typedef Elem<T> E;
@@ -88,9 +115,14 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
     typedef T weights_t __attribute__((ext_vector_type(4 * KT)));
     typedef Step<KT> Step;
     constexpr int kQ = D / 32;                // 16-byte pieces of a key's row per lane
-    constexpr int kHalves = D > 128 ? 2 : 1;  // pieces of a value's row per lane
+    constexpr int kHalves = D > 128 && !Eight ? 2 : 1;  // pieces of a value's row per lane
     constexpr int kCh = D / 16 / kHalves;     // channels in each
-    constexpr int kDw = kCh / 2;
+    constexpr int kDw = kCh / 2;              // dwords of output in each
+    // Dwords of a lane's piece of a row of values, of codes four channels each (96 channels: four of the first 64, two of the others),
+    // and of a key's row: with 16-bit elements 16 bytes of every 64; with codes 16 bytes of every 64 too (96 channels: 8 of every 32).
+    constexpr int kValueDw = Eight ? (kCh + 3) / 4 : kDw;
+    constexpr bool kBy32 = D % 64 != 0;
+    constexpr int kKeyDw = Eight ? D / 16 : kQ * 4;
     constexpr int kAcc = D / 16;
     constexpr int kSlotFloats = kHeadTile * D + 2 * kHeadTile;
 
@@ -104,8 +136,33 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
     const int r = lane & 15, g = lane >> 4;
     const int rows = p.kv_heads;  // of a sequence
     constexpr int kStepKeys = kTileKeys * KT, kRowCost = kRowTiles / KT, kMinSteps = kMinTiles / KT;
+    constexpr int kStepShift = KT == 2 ? 5 : 4;
+    static_assert(kStepKeys == 1 << kStepShift, "");
+    // tokens of a sequence as the rows carry them: with a window what lies past the table counts too
+    auto tokens_of = [&](int n) {
+        if constexpr (Window) return n < 0 ? 0 : n;
+        return cap_tokens(p, n);
+    };
     // a sequence without keys still has a step, in which its outputs are written
-    auto steps_of = [](int tokens) { return tokens > 0 ? (tokens + kStepKeys - 1) / kStepKeys : 1; };
+    auto steps_of = [&](int tokens) {
+        if constexpr (Window) {
+            const int steps = seen_of(p, tokens, kStepShift).steps;
+            return steps > 0 ? steps : 1;
+        }
+        return tokens > 0 ? (tokens + kStepKeys - 1) / kStepKeys : 1;
+    };
+    // first position of a row's step, and the end of what there is
+    auto position_of = [&](int tokens, int s) {
+        if constexpr (Window) {
+            const Seen x = seen_of(p, tokens, kStepShift);
+            return (s < x.sink_steps ? s : s + x.skip) * kStepKeys;
+        }
+        return s * kStepKeys;
+    };
+    auto end_of = [&](int tokens) {
+        if constexpr (Window) return cap_tokens(p, tokens);
+        return tokens;
+    };
 
     // ---- this work-group's range of steps, and this wave's share of it ----
     // Everything until the first loads of keys is latency: no divisions, the lengths of 64 sequences stay in the lanes,
@@ -115,7 +172,7 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
     auto hold = [&](int chunk) {
         held = chunk;
         const int b = chunk * 64 + lane;
-        length = b < p.B ? cap_tokens(p, p.lengths[b]) : 0;
+        length = b < p.B ? tokens_of(p.lengths[b]) : 0;
         count = b < p.B ? steps_of(length) : 0;
         incl = wave_scan(count);
     };
@@ -242,11 +299,11 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
     // the entries' loads (scalar) are issued a step before they are needed; past the row's tokens nothing is read
     auto entries = [&](Step &x) {
         const int32_t *table = table_of(x);
-        const int pos = x.s * kStepKeys;
+        const int pos = position_of(x.tokens, x.s), end = end_of(x.tokens);
 #pragma unroll
         for (int u = 0; u < KT; ++u) {
             x.e[u] = -1;
-            if (pos + kTileKeys * u < x.tokens) x.e[u] = scalar_load(table + ((pos + kTileKeys * u) >> p.page_shift));
+            if (pos + kTileKeys * u < end) x.e[u] = scalar_load(table + ((pos + kTileKeys * u) >> p.page_shift));
         }
     };
     auto advance = [&](Step x) -> Step {
@@ -257,24 +314,27 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
             if (++x.row == rows) {
                 x.row = 0;
                 ++x.b;
-                x.tokens = cap_tokens(p, scalar_load(p.lengths + x.b));
+                x.tokens = tokens_of(scalar_load(p.lengths + x.b));
             }
         }
         entries(x);
         return x;
     };
-    vec8 qf[kQ], kf[KT][kQ] = {};
-    uint32_t vr[KT][4][kHalves][kDw] = {};
+    vec8 qf[kQ];
+    uint32_t kf[KT][kKeyDw] = {};
+    uint32_t vr[KT][4][kHalves][kValueDw] = {};
+    float key_scale[KT], value_scale[KT];  // of the step whose keys are in the registers; of the other values are under way
     auto load_queries = [&](const Step &x) {
         const T *q = (const T *)p.q + x.b * p.q_row + (head0_of(x.row) + r) * p.q_head + 8 * g;
         const bool have = r < nh;
 #pragma unroll
-        for (int t = 0; t < kQ; ++t) qf[t] = have ? *(const vec8 *)(q + 32 * t) : vec8{};
+        for (int t = 0; t < kQ; ++t)  // of 16-byte pieces of codes, the halves one after the other
+            qf[t] = !have ? vec8{} : *(const vec8 *)(Eight && !kBy32 ? q + 8 * g + 64 * (t >> 1) + 8 * (t & 1) : q + 32 * t);
     };
     // a tile's first element in the caches; an entry that names no page is read as page 0 and masked
     auto tile_at = [&](const Step &x, int u) -> int64_t {
         const int e = x.e[u], kvh = x.row;
-        const int slot = (x.s * kStepKeys + kTileKeys * u) & ((1 << p.page_shift) - 1);
+        const int slot = (position_of(x.tokens, x.s) + kTileKeys * u) & ((1 << p.page_shift) - 1);
         return ((((int64_t)((uint32_t)e < (uint32_t)p.pages ? e : 0) * p.kv_heads + kvh) << p.page_shift) + slot) * D;
     };
     // Values are read once, whole rows at a time: non-temporal (131071 tokens, 537 MB: 90.2 us, 98.5 through the caches; 16 sequences
@@ -284,22 +344,55 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
     auto load_keys = [&](const Step &x) {
 #pragma unroll
         for (int u = 0; u < KT; ++u) {
-            if (u > 0 && x.s * kStepKeys + kTileKeys * u >= x.tokens) break;  // masked, whatever the registers hold
-            const T *k = (const T *)p.k + tile_at(x, u);
+            if (u > 0 && position_of(x.tokens, x.s) + kTileKeys * u >= end_of(x.tokens)) break;  // masked, whatever the registers hold
+            if constexpr (!Eight) {
+                const T *k = (const T *)p.k + tile_at(x, u);
 #pragma unroll
-            for (int t = 0; t < kQ; ++t) kf[u][t] = *(const vec8 *)(k + (r * D + 8 * g) + 32 * t);
+                for (int t = 0; t < kQ; ++t)
+                    __builtin_memcpy(&kf[u][4 * t], __builtin_assume_aligned(k + (r * D + 8 * g) + 32 * t, 16), 16);
+            } else {
+                const uint8_t *k = (const uint8_t *)p.k + tile_at(x, u) + r * D;
+                constexpr int kPiece = kBy32 ? 8 : 16;
+#pragma unroll
+                for (int t = 0; t < D / (4 * kPiece); ++t)
+                    __builtin_memcpy(&kf[u][kPiece / 4 * t], __builtin_assume_aligned(k + kPiece * (g + 4 * t), kPiece), kPiece);
+            }
         }
     };
     auto load_values = [&](const Step &x) {
 #pragma unroll
         for (int u = 0; u < KT; ++u) {
-            if (u > 0 && x.s * kStepKeys + kTileKeys * u >= x.tokens) break;
-            const T *v = (const T *)p.v + tile_at(x, u);
+            if (u > 0 && position_of(x.tokens, x.s) + kTileKeys * u >= end_of(x.tokens)) break;
+            if constexpr (!Eight) {
+                const T *v = (const T *)p.v + tile_at(x, u);
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+                for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int hf = 0; hf < kHalves; ++hf)
-                    load_dwords_once<kDw>(vr[u][i][hf], v + (4 * g * D + kCh * r) + i * D + 128 * hf);
+                    for (int hf = 0; hf < kHalves; ++hf)
+                        load_dwords_once<kDw>(vr[u][i][hf], v + (4 * g * D + kCh * r) + i * D + 128 * hf);
+            } else {
+                const uint8_t *v = (const uint8_t *)p.v + tile_at(x, u) + 4 * g * D;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if constexpr (kBy32) {
+                        vr[u][i][0][0] = __builtin_nontemporal_load((const uint32_t *)(v + i * D + 4 * r));
+                        vr[u][i][0][1] = __builtin_nontemporal_load((const uint16_t *)(v + i * D + 64 + 2 * r));
+                    } else {
+                        load_dwords_once<kValueDw>(vr[u][i][0], v + i * D + kCh * r);
+                    }
+                }
+            }
+        }
+    };
+    auto load_scales = [&](const Step &x, float (&of_keys)[KT], float (&of_values)[KT]) {
+#pragma unroll
+        for (int u = 0; u < KT; ++u) {
+            const int e = x.e[u], per_shift = p.page_shift - 4;  // blocks of a page
+            const int slot = (position_of(x.tokens, x.s) + kTileKeys * u) & ((1 << p.page_shift) - 1);
+            const int64_t head = (int64_t)((uint32_t)e < (uint32_t)p.pages ? e : 0) * p.kv_heads + x.row;
+            const float *s = p.scales + ((head * 2) << per_shift) + (slot >> 4);
+            of_keys[u] = scalar_load(s);
+            of_values[u] = scalar_load(s + (1 << per_shift));
         }
     };
     float4_t acc[kAcc];
@@ -349,7 +442,13 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
                 for (int j = 0; j < kCh; ++j) y[j] = l == 0.f ? (T)0.f : (T)(acc[hf * kCh + j][i] * inv);  // no weight: zero, whatever the values
                 uint32_t w[kDw];
                 __builtin_memcpy(w, y, sizeof(y));
-                store_dwords<kDw>((T *)p.out + at * D + 128 * hf + kCh * (4 * g + i), w);
+                T *const to = (T *)p.out + at * D;
+                if constexpr (Eight && kBy32) {
+                    __builtin_memcpy(__builtin_assume_aligned(to + 4 * (4 * g + i), 8), w, 8);
+                    __builtin_memcpy(__builtin_assume_aligned(to + 64 + 2 * (4 * g + i), 4), w + 2, 4);
+                } else {
+                    store_dwords<kDw>(to + 128 * hf + kCh * (4 * g + i), w);
+                }
             }
         if (p.lse && g == 0) p.lse[at] = (m + __builtin_amdgcn_logf(l)) * 0.693147180559945f;
     };
@@ -357,11 +456,12 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
     bool begun_before = from.step > 0;  // the row at hand began in another wave
     clear();  // a wave without steps between two that share a row adds nothing to it
     if (left > 0) {
-        Step cur{from.b, from.row, from.tokens >= 0 ? from.tokens : cap_tokens(p, scalar_load(p.lengths + from.b)), from.step, {}}, next;
+        Step cur{from.b, from.row, from.tokens >= 0 ? from.tokens : tokens_of(scalar_load(p.lengths + from.b)), from.step, {}}, next;
         entries(cur);
         load_queries(cur);
         load_keys(cur);
         load_values(cur);
+        if constexpr (Eight) load_scales(cur, key_scale, value_scale);
         if (left > 1) next = advance(cur);
         while (true) {
             float4_t sc[KT];
@@ -369,36 +469,72 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
             for (int u = 0; u < KT; ++u) {
                 sc[u] = float4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int t = 0; t < kQ; ++t) sc[u] = E::mfma(kf[u][t], qf[t], sc[u]);
+                for (int t = 0; t < kQ; ++t) {
+                    vec8 x;
+                    if constexpr (Eight)
+                        x = E::of_codes(kf[u][2 * t], kf[u][2 * t + 1]);
+                    else
+                        __builtin_memcpy(&x, &kf[u][4 * t], 16);
+                    sc[u] = E::mfma(x, qf[t], sc[u]);
+                }
             }
             // The next step's keys are under way while this one's scores and values are dealt with,
             // its values while the next scores are.
             const bool row_ends = cur.s + 1 == steps_of(cur.tokens);
             Step ahead;
+            float next_key_scale[KT] = {}, next_value_scale[KT] = {};
             issue_order_point();
             if (left > 1) {
                 if (row_ends) load_queries(next);
                 load_keys(next);
+                if constexpr (Eight) load_scales(next, next_key_scale, next_value_scale);
                 if (left > 2) ahead = advance(next);
+            }
+            bool none = (uint32_t)cur.e[0] >= (uint32_t)p.pages || (uint32_t)cur.e[KT - 1] >= (uint32_t)p.pages;
+            float add[KT] = {}, times[KT] = {};  // of a tile's scores, of its weights in the sum
+            if constexpr (Eight) {
+#pragma unroll
+                for (int u = 0; u < KT; ++u) {
+                    const bool fine = key_scale[u] >= kLeastScale && key_scale[u] <= kMostScale && value_scale[u] >= kLeastScale &&
+                                      value_scale[u] <= kMostScale;
+                    if (!fine) cur.e[u] = -1;
+                    none |= !fine;
+                    add[u] = fine ? __builtin_amdgcn_logf(value_scale[u]) : 0.f;
+                    times[u] = fine ? __builtin_amdgcn_rcpf(value_scale[u]) : 0.f;
+                }
             }
 #pragma unroll
             for (int u = 0; u < KT; ++u)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) sc[u][i] *= p.scale_log2;
-            const int pos = cur.s * kStepKeys;
-            if (pos + kStepKeys > cur.tokens || (uint32_t)cur.e[0] >= (uint32_t)p.pages || (uint32_t)cur.e[KT - 1] >= (uint32_t)p.pages) {
+                for (int i = 0; i < 4; ++i) {
+                    if constexpr (Eight)
+                        sc[u][i] = __builtin_fmaf(sc[u][i], p.scale_log2 * key_scale[u], add[u]);
+                    else
+                        sc[u][i] *= p.scale_log2;
+                }
+            const int pos = position_of(cur.tokens, cur.s), end = end_of(cur.tokens);
+            bool cut = pos + kStepKeys > end || none;
+            int low = 0, sinks = 0;
+            if constexpr (Window) {
+                const Seen x = seen_of(p, cur.tokens, kStepShift);
+                low = x.low;
+                sinks = x.sinks;
+                cut |= pos < low && pos + kStepKeys > sinks;
+            }
+            if (cut) {
                 // whatever a masked slot holds (an infinity, not a number) stays out of both products
 #pragma unroll
                 for (int u = 0; u < KT; ++u) {
-                    const int valid = (uint32_t)cur.e[u] < (uint32_t)p.pages ? cur.tokens - pos - kTileKeys * u : 0;
+                    const int from_tile = pos + kTileKeys * u;
+                    const int valid = (uint32_t)cur.e[u] < (uint32_t)p.pages ? end - from_tile : 0;
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
-                        if (4 * g + i >= valid) {
+                        if (4 * g + i >= valid || (Window && from_tile + 4 * g + i < low && from_tile + 4 * g + i >= sinks)) {
                             sc[u][i] = -INFINITY;
 #pragma unroll
                             for (int hf = 0; hf < kHalves; ++hf)
 #pragma unroll
-                                for (int w = 0; w < kDw; ++w) vr[u][i][hf][w] = 0;
+                                for (int w = 0; w < kValueDw; ++w) vr[u][i][hf][w] = 0;
                         }
                 }
             }
@@ -422,7 +558,10 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
 #pragma unroll
                 for (int i = 0; i < 4; ++i) pr[u][i] = __builtin_amdgcn_exp2f(sc[u][i] - ref);
 #pragma unroll
-            for (int u = 0; u < KT; ++u) l += (pr[u][0] + pr[u][1]) + (pr[u][2] + pr[u][3]);
+            for (int u = 0; u < KT; ++u) {
+                const float sum = (pr[u][0] + pr[u][1]) + (pr[u][2] + pr[u][3]);
+                l += Eight ? sum * times[u] : sum;
+            }
             // The second product takes the weights in the cache's type, as its MFMAs want them, in two parts: rounded down, and what
             // that left out, rounded.  Together they hold 21 bits of a float16 cache's weights and 15 of a bfloat16 one's,
             // float16's times 2^15, so that those far below the maximum are no subnormals (an absolute 2^-40 of it is all that is lost).
@@ -443,9 +582,14 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
                 for (int j = 0; j < kCh; ++j) {
                     uint32_t w[2 * KT];
 #pragma unroll
-                    for (int e = 0; e < 2 * KT; ++e)
-                        w[e] = __builtin_amdgcn_perm(vr[e >> 1][2 * (e & 1) + 1][hf][j >> 1], vr[e >> 1][2 * (e & 1)][hf][j >> 1],
-                                                     (j & 1) ? 0x07060302u : 0x05040100u);
+                    for (int e = 0; e < 2 * KT; ++e) {
+                        if constexpr (Eight)  // two keys' codes of channels j and j ^ 1 beside each other, of which one pair becomes elements
+                            w[e] = E::of_two_codes(__builtin_amdgcn_perm(vr[e >> 1][2 * (e & 1) + 1][hf][j >> 2], vr[e >> 1][2 * (e & 1)][hf][j >> 2],
+                                                                         (j & 2) ? 0x07030602u : 0x05010400u), j & 1);
+                        else
+                            w[e] = __builtin_amdgcn_perm(vr[e >> 1][2 * (e & 1) + 1][hf][j >> 1], vr[e >> 1][2 * (e & 1)][hf][j >> 1],
+                                                         (j & 1) ? 0x07060302u : 0x05040100u);
+                    }
                     const weights_t x = __builtin_bit_cast(weights_t, w);
                     acc[hf * kCh + j] = E::mfma(x, pf, acc[hf * kCh + j]);
                     acc[hf * kCh + j] = E::mfma(x, rest, acc[hf * kCh + j]);
@@ -464,6 +608,13 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
             if (--left == 0) break;
             cur = next;
             next = ahead;
+            if constexpr (Eight) {
+#pragma unroll
+                for (int u = 0; u < KT; ++u) {
+                    key_scale[u] = next_key_scale[u];
+                    value_scale[u] = next_value_scale[u];
+                }
+            }
         }
     }
 
@@ -586,8 +737,11 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
             const int64_t at = (int64_t)b * p.heads + head0_of(row) + r;
             const float inv = 1.f / (sum * E::kWeightUnit);
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                ((T *)p.out)[at * D + 128 * (j / kCh) + kCh * (4 * g + i) + j % kCh] = sum == 0.f ? (T)0.f : (T)(o[i] * inv);
+            for (int i = 0; i < 4; ++i) {
+                const int x = 4 * g + i;
+                const int ch = Eight && kBy32 ? (j < 4 ? 4 * x + j : 60 + 2 * x + j) : 128 * (j / kCh) + kCh * x + j % kCh;
+                ((T *)p.out)[at * D + ch] = sum == 0.f ? (T)0.f : (T)(o[i] * inv);
+            }
             if (p.lse && g == 0 && j == 0) p.lse[at] = (top + __builtin_amdgcn_logf(sum)) * 0.693147180559945f;
         };
         // Contributors are joined in order, so that the bits are the same every time.  Of a few, a wave takes its channels at once
@@ -681,7 +835,7 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
     }
 }
 
-template <typename T, int D>
+template <typename T, int D, bool Eight, bool Window>
 hipError_t launch_one(const AttendProblem &p, int cus, hipStream_t stream)
 {
     const int groups = (cus < kKvMaxCus ? cus : kKvMaxCus) * kAttendGroupsPerCu;
@@ -693,18 +847,25 @@ hipError_t launch_one(const AttendProblem &p, int cus, hipStream_t stream)
     AttendProblem q = p;
     q.grid_reciprocal = ranges > 1 ? (uint32_t)(((uint64_t)1 << 32) / (uint64_t)ranges) : 0xFFFFFFFFu;
     void *args[] = {&q};
-    return hipLaunchKernel((const void *)&paged_attention_kernel<T, D, kAttendWaves, kTiles>, dim3(ranges * p.head_tiles),
+    return hipLaunchKernel((const void *)&paged_attention_kernel<T, D, kAttendWaves, kTiles, Eight, Window>, dim3(ranges * p.head_tiles),
                            dim3(64 * kAttendWaves), args, 0, stream);
+}
+
+template <typename T, int D>
+hipError_t launch_cache(const AttendProblem &p, int cus, hipStream_t stream)
+{
+    if (p.scales) return p.window ? launch_one<T, D, true, true>(p, cus, stream) : launch_one<T, D, true, false>(p, cus, stream);
+    return p.window ? launch_one<T, D, false, true>(p, cus, stream) : launch_one<T, D, false, false>(p, cus, stream);
 }
 
 template <typename T>
 hipError_t launch_typed(const AttendProblem &p, int head_dim, int cus, hipStream_t stream)
 {
     switch (head_dim) {
-    case 64: return launch_one<T, 64>(p, cus, stream);
-    case 96: return launch_one<T, 96>(p, cus, stream);
-    case 128: return launch_one<T, 128>(p, cus, stream);
-    case 256: return launch_one<T, 256>(p, cus, stream);
+    case 64: return launch_cache<T, 64>(p, cus, stream);
+    case 96: return launch_cache<T, 96>(p, cus, stream);
+    case 128: return launch_cache<T, 128>(p, cus, stream);
+    case 256: return launch_cache<T, 256>(p, cus, stream);
     }
     return hipErrorInvalidValue;
 }

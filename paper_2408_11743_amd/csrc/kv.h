@@ -1,7 +1,7 @@
 // Internal declarations of the paged key-value cache operators: rotating and
-// appending new tokens (append.hip), attention of one token per sequence
-// (attend.hip), the choice of pages to attend to (select.hip).  Argument
-// checks are in kv_api.cpp.
+// appending new tokens (append.hip, append8.hip), attention of one token per sequence
+// (attend.hip) and of several (prompt.hip), the choice of pages to attend to
+// (select.hip), pages for new tokens (pages.hip).  Argument checks are in kv_api.cpp.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -37,6 +37,8 @@ struct AttendProblem {
     int page_shift, width, pages;
     float scale_log2;  // scale * log2(e)
     uint32_t grid_reciprocal;  // floor(2^32 / ranges)
+    const float *scales;       // [pages][kv_heads][2][page size / 16] of an 8-bit cache, or NULL
+    int window, sinks;         // 0: no window
 };
 
 hipError_t launch_attend(const AttendProblem &p, int head_dim, marlin_dtype_t dtype, int cus, hipStream_t stream);
@@ -54,6 +56,13 @@ struct AppendProblem {
     int page_shift, width, pages;
 };
 
+// The same into an 8-bit cache with scales.
+struct Append8Problem : AppendProblem {
+    float *scales;  // [pages][kv_heads][2][page size / 16]
+};
+
+hipError_t launch_append8(const Append8Problem &p, int head_dim, marlin_dtype_t dtype, hipStream_t stream);
+
 hipError_t launch_append(const AppendProblem &p, int head_dim, marlin_dtype_t dtype, hipStream_t stream);
 
 struct SelectProblem {
@@ -70,5 +79,53 @@ struct SelectProblem {
 };
 
 hipError_t launch_select(const SelectProblem &p, int head_dim, marlin_dtype_t dtype, hipStream_t stream);
+
+constexpr int kBlockSlots = 16;  // slots of an 8-bit cache that share a scale
+static_assert(kBlockSlots == kTileKeys, "a tile of keys has one scale");
+constexpr float kLeastScale = 0x1p-40f, kMostScale = 0x1p40f;
+
+// Attention of several tokens per sequence.
+struct PromptProblem {
+    const void *q;  // [tokens][heads][D], strides below (elements)
+    int64_t q_row, q_head;
+    const void *k, *v;
+    const float *scales;
+    const int32_t *table;  // [B][width]
+    int64_t table_row;
+    const int32_t *lengths, *starts;
+    void *out;
+    float *lse;
+    float *partials;
+    uint32_t *counters;
+    int tokens, B, heads, kv_heads, group;
+    int page_shift, width, pages;
+    int window, sinks;
+    float scale_log2;
+    int splits;     // work-groups that may share a tile's keys
+    int base;       // the launch's first work-group
+    int tiles;      // of all sequences, at most
+};
+
+// How a call of these sizes is split: rows of a tile, tiles at most, work-groups a tile, workspace floats a work-group.
+struct PromptPlan {
+    bool few;  // the kernel for few rows a sequence
+    int rows, tiles, splits, slot_floats;
+};
+PromptPlan plan_prompt(int64_t tokens, int64_t B, int64_t heads, int64_t kv_heads, int head_dim);
+
+hipError_t launch_prompt(const PromptProblem &p, const PromptPlan &plan, int head_dim, marlin_dtype_t dtype, hipStream_t stream);
+
+struct PagesProblem {
+    int32_t *table;
+    int64_t table_row;
+    int32_t *lengths;
+    const int32_t *new_tokens;
+    int32_t *free_pages, *free_count, *starts;
+    int64_t *slots;
+    int32_t *before;  // workspace: [B] pages taken before the sequence, then the free ones' count
+    int B, width, pages, page_shift, tokens, window, sinks;
+};
+
+hipError_t launch_pages(const PagesProblem &p, hipStream_t stream);
 
 }  // namespace marlin

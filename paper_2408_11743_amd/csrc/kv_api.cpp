@@ -45,6 +45,16 @@ bool scores_ok(int64_t B, int64_t kv_heads, int64_t width)
     return width <= (1 << 29) && (width + 63) / 64 * B * kv_heads <= (1 << 23);
 }
 
+constexpr int64_t kMaxTokens = 1 << 24;  // of a call
+
+// Rows of a kv head: new tokens by the heads that share it.
+bool rows_of_tokens_ok(int64_t tokens, int64_t heads, int64_t kv_heads)
+{
+    return tokens >= 0 && tokens <= kMaxTokens && tokens * (heads / kv_heads) <= (1 << 30);
+}
+
+bool visible_ok(int64_t window, int64_t sinks) { return window >= 0 && window <= (1 << 30) && sinks >= 0 && sinks <= (1 << 30); }
+
 }  // namespace
 
 extern "C" {
@@ -153,6 +163,8 @@ marlin_status_t marlin_paged_attention(const marlin_paged_attention_args *a, hip
     p.width = (int)a->width;
     p.pages = (int)a->pages;
     p.scale_log2 = (float)(a->scale * 1.4426950408889634);
+    p.scales = nullptr;
+    p.window = p.sinks = 0;
     return launch_attend(p, (int)a->head_dim, (marlin_dtype_t)a->dtype, cus, stream) == hipSuccess ? MARLIN_OK : MARLIN_ERR_HIP;
 }
 
@@ -198,6 +210,195 @@ marlin_status_t marlin_select_pages(const marlin_select_pages_args *a, hipStream
     p.pages = (int)a->pages;
     p.select = (int)a->select;
     return launch_select(p, (int)a->head_dim, (marlin_dtype_t)a->dtype, stream) == hipSuccess ? MARLIN_OK : MARLIN_ERR_HIP;
+}
+
+marlin_status_t marlin_kv_append8(const marlin_kv_append8_args *a, hipStream_t stream)
+{
+    if (!a) return MARLIN_ERR_NULL_POINTER;
+    if (!shape_ok(a->B, a->heads, a->kv_heads, a->head_dim, a->pages, a->page_size, a->width)) return MARLIN_ERR_INVALID_SHAPE;
+    if (a->tokens < 0 || a->tokens > kMaxTokens || (!a->starts && a->tokens != a->B)) return MARLIN_ERR_INVALID_SHAPE;
+    if (!strides_ok(a->q_row, a->q_head) || !strides_ok(a->k_row, a->k_head) || !strides_ok(a->v_row, a->v_head) ||
+        a->table_row < 0)
+        return MARLIN_ERR_INVALID_SHAPE;
+    if (!dtype_ok(a->dtype) || a->rot < 0 || a->rot > a->head_dim || a->rot % 16 != 0 || a->interleaved < 0 ||
+        a->interleaved > 1)
+        return MARLIN_ERR_INVALID_ARGUMENT;
+    if (a->rot > 0 && (a->positions < 1 || a->positions > (1 << 30))) return MARLIN_ERR_INVALID_SHAPE;
+    if (a->B == 0 || a->tokens == 0) return MARLIN_OK;
+    if (!a->q || !a->k || !a->v || !a->q_out || !a->k_cache || !a->v_cache || !a->scales || !a->table || !a->lengths ||
+        (a->rot > 0 && !a->cos_sin))
+        return MARLIN_ERR_NULL_POINTER;
+    if (!aligned16(a->q) || !aligned16(a->k) || !aligned16(a->v) || !aligned16(a->q_out) || !aligned16(a->k_cache) ||
+        !aligned16(a->v_cache) || !aligned16(a->cos_sin) || !aligned(a->scales, 4) || !aligned(a->table, 4) ||
+        !aligned(a->lengths, 4) || !aligned(a->starts, 4))
+        return MARLIN_ERR_MISALIGNED;
+
+    Append8Problem p;
+    p.q = a->q;
+    p.k = a->k;
+    p.v = a->v;
+    p.q_row = a->q_row;
+    p.q_head = a->q_head;
+    p.k_row = a->k_row;
+    p.k_head = a->k_head;
+    p.v_row = a->v_row;
+    p.v_head = a->v_head;
+    p.q_out = a->q_out;
+    p.k_cache = a->k_cache;
+    p.v_cache = a->v_cache;
+    p.bounds = nullptr;
+    p.scales = a->scales;
+    p.cos_sin = a->cos_sin;
+    p.positions = (int)(a->rot > 0 ? a->positions : 0);
+    p.rot = (int)a->rot;
+    p.interleaved = (int)a->interleaved;
+    p.table = a->table;
+    p.table_row = a->table_row;
+    p.lengths = a->lengths;
+    p.starts = a->starts;
+    p.tokens = (int)a->tokens;
+    p.B = (int)a->B;
+    p.heads = (int)a->heads;
+    p.kv_heads = (int)a->kv_heads;
+    p.page_shift = shift_of(a->page_size);
+    p.width = (int)a->width;
+    p.pages = (int)a->pages;
+    return launch_append8(p, (int)a->head_dim, (marlin_dtype_t)a->dtype, stream) == hipSuccess ? MARLIN_OK : MARLIN_ERR_HIP;
+}
+
+size_t marlin_cache_attention_workspace_bytes(int64_t starts, int64_t tokens, int64_t B, int64_t heads, int64_t kv_heads,
+                                              int64_t head_dim)
+{
+    if (!shape_ok(B, heads, kv_heads, head_dim, 1, 16, 1) || !rows_of_tokens_ok(tokens, heads, kv_heads)) return 0;
+    if (!starts) return marlin_paged_attention_workspace_bytes(head_dim);
+    const PromptPlan plan = plan_prompt(tokens, B, heads, kv_heads, (int)head_dim);
+    const size_t slots = plan.splits > 1 ? (size_t)plan.tiles * (size_t)kv_heads * (size_t)plan.splits : 0;
+    return kCounterRegionBytes + slots * (size_t)plan.slot_floats * sizeof(float);
+}
+
+marlin_status_t marlin_cache_attention(const marlin_cache_attention_args *a, hipStream_t stream)
+{
+    if (!a) return MARLIN_ERR_NULL_POINTER;
+    if (!shape_ok(a->B, a->heads, a->kv_heads, a->head_dim, a->pages, a->page_size, a->width)) return MARLIN_ERR_INVALID_SHAPE;
+    if (!strides_ok(a->q_row, a->q_head) || a->table_row < 0 || a->table_head < 0) return MARLIN_ERR_INVALID_SHAPE;
+    if (!rows_of_tokens_ok(a->tokens, a->heads, a->kv_heads)) return MARLIN_ERR_INVALID_SHAPE;
+    if (a->starts ? a->table_head != 0 : a->tokens != a->B) return MARLIN_ERR_INVALID_SHAPE;
+    const int64_t group = a->heads / a->kv_heads, head_tiles = (group + kHeadTile - 1) / kHeadTile;
+    const int64_t tiles = a->width * a->page_size / kTileKeys;
+    if (!a->starts && a->B > 0 && tiles + 2 > INT32_MAX / (a->B * a->kv_heads * head_tiles)) return MARLIN_ERR_INVALID_SHAPE;
+    if (!dtype_ok(a->dtype) || !std::isfinite(a->scale) || !std::isfinite((float)(a->scale * 1.4426950408889634)) ||
+        !visible_ok(a->window, a->sinks))
+        return MARLIN_ERR_INVALID_ARGUMENT;
+    if (a->B == 0 || a->tokens == 0) return MARLIN_OK;
+    if (!a->q || !a->k_cache || !a->v_cache || !a->table || !a->lengths || !a->out || !a->workspace)
+        return MARLIN_ERR_NULL_POINTER;
+    if (!aligned16(a->q) || !aligned16(a->k_cache) || !aligned16(a->v_cache) || !aligned16(a->out) ||
+        !aligned16(a->workspace) || !aligned(a->scales, 4) || !aligned(a->table, 4) || !aligned(a->lengths, 4) ||
+        !aligned(a->starts, 4) || !aligned(a->lse, 4))
+        return MARLIN_ERR_MISALIGNED;
+    if (a->workspace_bytes <
+        marlin_cache_attention_workspace_bytes(a->starts != nullptr, a->tokens, a->B, a->heads, a->kv_heads, a->head_dim))
+        return MARLIN_ERR_WORKSPACE_TOO_SMALL;
+
+    if (a->starts) {
+        PromptProblem p;
+        p.q = a->q;
+        p.q_row = a->q_row;
+        p.q_head = a->q_head;
+        p.k = a->k_cache;
+        p.v = a->v_cache;
+        p.scales = a->scales;
+        p.table = a->table;
+        p.table_row = a->table_row;
+        p.lengths = a->lengths;
+        p.starts = a->starts;
+        p.out = a->out;
+        p.lse = a->lse;
+        p.counters = (uint32_t *)a->workspace;
+        p.partials = (float *)((char *)a->workspace + kCounterRegionBytes);
+        p.tokens = (int)a->tokens;
+        p.B = (int)a->B;
+        p.heads = (int)a->heads;
+        p.kv_heads = (int)a->kv_heads;
+        p.group = (int)group;
+        p.page_shift = shift_of(a->page_size);
+        p.width = (int)a->width;
+        p.pages = (int)a->pages;
+        p.window = (int)a->window;
+        p.sinks = (int)a->sinks;
+        p.scale_log2 = (float)(a->scale * 1.4426950408889634);
+        const PromptPlan plan = plan_prompt(a->tokens, a->B, a->heads, a->kv_heads, (int)a->head_dim);
+        return launch_prompt(p, plan, (int)a->head_dim, (marlin_dtype_t)a->dtype, stream) == hipSuccess ? MARLIN_OK : MARLIN_ERR_HIP;
+    }
+    int device = 0;
+    if (hipGetDevice(&device) != hipSuccess) return MARLIN_ERR_HIP;
+    const int cus = device_cu_count(device);
+    if (cus <= 0) return MARLIN_ERR_HIP;
+    AttendProblem p;
+    p.q = a->q;
+    p.q_row = a->q_row;
+    p.q_head = a->q_head;
+    p.k = a->k_cache;
+    p.v = a->v_cache;
+    p.scales = a->scales;
+    p.table = a->table;
+    p.table_row = a->table_row;
+    p.table_head = a->table_head;
+    p.lengths = a->lengths;
+    p.out = a->out;
+    p.lse = a->lse;
+    p.counters = (uint32_t *)a->workspace;
+    p.partials = (float *)((char *)a->workspace + kCounterRegionBytes);
+    p.B = (int)a->B;
+    p.heads = (int)a->heads;
+    p.kv_heads = (int)a->kv_heads;
+    p.group = (int)group;
+    p.head_tiles = (int)head_tiles;
+    p.page_shift = shift_of(a->page_size);
+    p.width = (int)a->width;
+    p.pages = (int)a->pages;
+    p.window = (int)a->window;
+    p.sinks = (int)a->sinks;
+    p.scale_log2 = (float)(a->scale * 1.4426950408889634);
+    return launch_attend(p, (int)a->head_dim, (marlin_dtype_t)a->dtype, cus, stream) == hipSuccess ? MARLIN_OK : MARLIN_ERR_HIP;
+}
+
+size_t marlin_assign_pages_workspace_bytes(int64_t B)
+{
+    return B < 0 || B > kKvMaxBatch ? 0 : kCounterRegionBytes + ((size_t)B + 1) * sizeof(int32_t);
+}
+
+marlin_status_t marlin_assign_pages(const marlin_assign_pages_args *a, hipStream_t stream)
+{
+    if (!a) return MARLIN_ERR_NULL_POINTER;
+    if (!shape_ok(a->B, 1, 1, 64, a->pages, a->page_size, a->width) || a->table_row < 0 || a->tokens < 0 || a->tokens > kMaxTokens)
+        return MARLIN_ERR_INVALID_SHAPE;
+    if (!visible_ok(a->window, a->sinks)) return MARLIN_ERR_INVALID_ARGUMENT;
+    if ((a->B > 0 && (!a->table || !a->lengths || !a->new_tokens)) || !a->free_pages || !a->free_count || !a->starts ||
+        (a->tokens > 0 && !a->slots) || !a->workspace)
+        return MARLIN_ERR_NULL_POINTER;
+    if (!aligned(a->table, 4) || !aligned(a->lengths, 4) || !aligned(a->new_tokens, 4) || !aligned(a->free_pages, 4) ||
+        !aligned(a->free_count, 4) || !aligned(a->starts, 4) || !aligned(a->slots, 8) || !aligned16(a->workspace))
+        return MARLIN_ERR_MISALIGNED;
+    if (a->workspace_bytes < marlin_assign_pages_workspace_bytes(a->B)) return MARLIN_ERR_WORKSPACE_TOO_SMALL;
+    PagesProblem p;
+    p.table = a->table;
+    p.table_row = a->table_row;
+    p.lengths = a->lengths;
+    p.new_tokens = a->new_tokens;
+    p.free_pages = a->free_pages;
+    p.free_count = a->free_count;
+    p.starts = a->starts;
+    p.slots = a->slots;
+    p.before = (int32_t *)((char *)a->workspace + kCounterRegionBytes);
+    p.B = (int)a->B;
+    p.width = (int)a->width;
+    p.pages = (int)a->pages;
+    p.page_shift = shift_of(a->page_size);
+    p.tokens = (int)a->tokens;
+    p.window = (int)a->window;
+    p.sinks = (int)a->sinks;
+    return launch_pages(p, stream) == hipSuccess ? MARLIN_OK : MARLIN_ERR_HIP;
 }
 
 }  // extern "C"

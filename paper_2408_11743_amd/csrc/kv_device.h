@@ -36,6 +36,17 @@ struct Elem<_Float16> {
     {
         return __builtin_amdgcn_mfma_f32_16x16x16f16(a, b, c, 0, 0, 0);
     }
+    // e4m3 codes as numbers, exactly: the first or the second two of a dword; eight.
+    static __device__ __forceinline__ uint32_t of_two_codes(uint32_t x, bool second)
+    {
+        return __builtin_bit_cast(uint32_t, second ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(x, 1.f, true)
+                                                   : __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(x, 1.f, false));
+    }
+    static __device__ __forceinline__ vec8 of_codes(uint32_t x, uint32_t y)
+    {
+        const u32x4_t w = {of_two_codes(x, false), of_two_codes(x, true), of_two_codes(y, false), of_two_codes(y, true)};
+        return __builtin_bit_cast(vec8, w);
+    }
 };
 
 template <>
@@ -62,6 +73,16 @@ struct Elem<__bf16> {
     {
         typedef short short4_t __attribute__((ext_vector_type(4)));
         return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(short4_t, a), __builtin_bit_cast(short4_t, b), c, 0, 0, 0);
+    }
+    static __device__ __forceinline__ uint32_t of_two_codes(uint32_t x, bool second)
+    {
+        return __builtin_bit_cast(uint32_t, second ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, 1.f, true)
+                                                   : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, 1.f, false));
+    }
+    static __device__ __forceinline__ vec8 of_codes(uint32_t x, uint32_t y)
+    {
+        const u32x4_t w = {of_two_codes(x, false), of_two_codes(x, true), of_two_codes(y, false), of_two_codes(y, true)};
+        return __builtin_bit_cast(vec8, w);
     }
 };
 
@@ -100,6 +121,10 @@ __device__ __forceinline__ void store_dwords(void *to, const uint32_t (&from)[N]
 __device__ __forceinline__ int scalar_load(const int32_t *p)
 {
     return *(const __attribute__((address_space(4))) int32_t *)(uintptr_t)p;
+}
+__device__ __forceinline__ float scalar_load(const float *p)
+{
+    return *(const __attribute__((address_space(4))) float *)(uintptr_t)p;
 }
 
 // x of lane l and of lane l ^ D, D = 32 or 16, in the same order in both: an

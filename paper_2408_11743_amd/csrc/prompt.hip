@@ -1,0 +1,1006 @@
+// Attention of several new tokens per sequence over a paged key-value cache: prompts,
+// their chunks, drafted tokens.
+//
+//   o_t = sum_j p_tj v_j,  p_tj = exp(scale q_t . k_j) / sum_i exp(scale q_t . k_i),  j up to t's position, and through a window
+//
+// A tile of work is rows of one sequence and kv head: its tokens by the query heads that share the
+// kv head (row r: token r / group, head r % group), so keys and values are read once for all of
+// them.  Both products are MFMAs with the rows as columns,
+//
+//   S^T [keys x rows] = K Q^T,  O^T [channels x rows] += V^T P^T,
+//
+// so a row's scores lie in few lanes, which need no exchange but for the maximum, and a lane's
+// scores are the operand of the second product as they are: the contraction's order is free, and V^T
+// is laid out in the order in which the lanes hold the keys.
+//
+// The tiles of a call are numbered from the sequences' starts on the device; a work-group finds its tile by
+// scans, the longest of a sequence first.  Where there are few tiles, several work-groups share a tile's
+// keys and leave partial results in the workspace, which the last to arrive joins in order.
+//
+// Weights go to the second product rounded once to the cache's type (float16's times 2^15, so that
+// they are no subnormals until 2^-29 of the maximum, and lost below 2^-40): an error of half a step of each weight, as the output's own,
+// and averaged over the keys.  Scores, maxima, sums and results are fp32.
+#include <hip/hip_runtime.h>
+
+#include "device.h"
+#include "kv.h"
+#include "kv_device.h"
+
+namespace marlin {
+namespace {
+
+using namespace dev;
+
+typedef float float16_t __attribute__((ext_vector_type(16)));
+
+constexpr int kWaves = 4;
+
+__device__ __forceinline__ float16_t mfma32(Elem<_Float16>::vec8 a, Elem<_Float16>::vec8 b, float16_t c)
+{
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ float16_t mfma32(Elem<__bf16>::vec8 a, Elem<__bf16>::vec8 b, float16_t c)
+{
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+
+// A masked key's value may be anything, and its weight of zero does not take an infinity or NaN away.  In steps in which some rows
+// do not see all keys what is not finite is left out of the second product, and added by itself for the rows that do see it.
+//
+// A dword of elements, or of codes, without those that are not finite.
+template <typename T, bool Eight>
+__device__ __forceinline__ uint32_t finite_of(uint32_t w)
+{
+    if constexpr (Eight) {
+        const uint32_t odd = ((w & 0x7F7F7F7Fu) + 0x01010101u) >> 7 & 0x01010101u;
+        return w & ~(odd * 0xFFu);
+    }
+    constexpr uint32_t exponent = (__is_same(T, _Float16) ? 0x7C00u : 0x7F80u) * 0x10001u;
+    constexpr uint32_t unit = (__is_same(T, _Float16) ? 0x0400u : 0x0080u) * 0x10001u;
+    const uint32_t odd = ((w & exponent) + unit) >> 15 & 0x00010001u;
+    return w & ~(odd * 0xFFFFu);
+}
+// One element of the cache, or zero where it is finite.
+template <typename T, bool Eight>
+__device__ __forceinline__ float odd_at(const void *cache, int64_t at)
+{
+    float x;
+    if constexpr (Eight)
+        x = (((const uint8_t *)cache)[at] & 0x7F) == 0x7F ? __builtin_nanf("") : 0.f;
+    else
+        x = (float)((const T *)cache)[at];
+    return __builtin_fabsf(x) < INFINITY ? 0.f : x;
+}
+
+// A tile of rows: tokens from + row / group of a sequence.
+struct Tile {
+    int b, from, tokens, start;  // sequence, its first row of q, its new tokens, the first one's position
+    int row0;                    // the tile's first row; -1: there is no such tile
+};
+
+// The mine-th tile of `rows` rows of the sequences, by a work-group: found among the sums of 64 sequences' tiles, then among theirs.
+__device__ __forceinline__ Tile find_tile(const PromptProblem &p, int rows, int mine, int lane, int wave, int *lds_chunks)
+{
+    const int chunks = (p.B + 63) / 64;
+    int begin = 0, count = 0, length = 0, tiles = 0, incl = 0;
+    auto hold = [&](int chunk) {
+        const int b = chunk * 64 + lane;
+        begin = count = length = tiles = 0;
+        if (b < p.B) {
+            begin = p.starts[b];
+            int end = p.starts[b + 1];
+            begin = begin < 0 ? 0 : begin < p.tokens ? begin : p.tokens;
+            end = end < begin ? begin : end < p.tokens ? end : p.tokens;
+            count = end - begin;
+            length = p.lengths[b];
+            if (length < 0) length = 0;
+            tiles = (int)(((int64_t)count * p.group + rows - 1) / rows);
+        }
+        incl = wave_scan(tiles);
+    };
+    int chunk = 0, before = 0;
+    Tile x{0, 0, 0, 0, -1};
+    if (chunks == 1) {
+        hold(0);
+    } else {
+        for (int c = wave; c < chunks; c += kWaves) {
+            hold(c);
+            if (lane == 63) lds_chunks[c] = incl;
+        }
+        __syncthreads();
+        chunk = -1;
+        for (int c0 = 0; c0 < chunks && chunk < 0; c0 += 64) {
+            const int c = c0 + lane < chunks ? lds_chunks[c0 + lane] : 0, i = wave_scan(c);
+            const uint64_t past = __builtin_amdgcn_ballot_w64(before + i > mine);
+            const int at = past ? __builtin_ctzll(past) : 63;
+            if (past) chunk = c0 + at;
+            before += __builtin_amdgcn_readlane(i, at) - (past ? __builtin_amdgcn_readlane(c, at) : 0);
+        }
+        if (chunk < 0) return x;
+        hold(chunk);
+    }
+    const uint64_t past = __builtin_amdgcn_ballot_w64(before + incl > mine);
+    if (!past) return x;
+    const int at = __builtin_ctzll(past);
+    x.b = chunk * 64 + at;
+    x.from = __builtin_amdgcn_readlane(begin, at);
+    x.tokens = __builtin_amdgcn_readlane(count, at);
+    x.start = __builtin_amdgcn_readlane(length, at) - x.tokens;
+    x.row0 = (mine - before - (__builtin_amdgcn_readlane(incl, at) - __builtin_amdgcn_readlane(tiles, at))) * rows;
+    return x;
+}
+
+// The keys that a tile's rows see, in steps of 2^shift: [0, sinks) and [low, end), of which steps the first sink_steps and those
+// from skip further on.
+struct Keys {
+    int first, last;  // the rows' first and last position
+    int end, low, sinks, sink_steps, skip, steps;
+};
+__device__ __forceinline__ Keys keys_of(const PromptProblem &p, const Tile &t, int rows, int shift)
+{
+    Keys k;
+    const int64_t all_rows = (int64_t)t.tokens * p.group;
+    const int last_row = (int)(t.row0 + rows < all_rows ? t.row0 + rows : all_rows) - 1;
+    const int cap = p.width << p.page_shift, up = (1 << shift) - 1;
+    k.first = t.start + t.row0 / p.group;
+    k.last = t.start + last_row / p.group;
+    k.end = k.last + 1 < cap ? k.last + 1 : cap;
+    if (k.end < 0) k.end = 0;
+    k.low = k.sinks = 0;
+    if (p.window) {
+        k.low = k.first >= p.window ? k.first - p.window + 1 : 0;
+        k.sinks = p.sinks < k.low ? p.sinks : k.low;
+    }
+    const int all = (k.end + up) >> shift, first = k.low >> shift;
+    k.sink_steps = (k.sinks + up) >> shift;
+    if (k.sink_steps > all) k.sink_steps = all;
+    k.skip = (first < all ? first : all) - k.sink_steps;
+    if (k.skip < 0) k.skip = 0;
+    k.steps = all - k.skip;
+    return k;
+}
+
+// A row's part of what is seen: positions up to `last`, above `above` or below `sinks`.
+struct Sight {
+    int last, above, sinks;
+    __device__ __forceinline__ bool sees(int j) const { return j <= last && (j > above || j < sinks); }
+};
+__device__ __forceinline__ Sight sight_of(const PromptProblem &p, const Tile &t, int row)
+{
+    const bool have = row < (int64_t)t.tokens * p.group;
+    const int pos = have ? t.start + row / p.group : -1;
+    return {pos, p.window ? pos - p.window : -1, p.sinks};
+}
+
+__device__ __forceinline__ bool is_scale(float s) { return s >= kLeastScale && s <= kMostScale; }
+
+// N tiles of 16 keys of a step: where they lie in the caches (elements); which are there (bits) and, in an 8-bit cache, what their
+// scales make of the scores (times factor, plus add) and of the weights in the sum (times).
+template <int N>
+struct Places {
+    int64_t at[N];
+};
+template <int N, bool Eight>
+struct Block {
+    uint32_t ok;
+};
+template <int N>
+struct Block<N, true> {
+    uint32_t ok;
+    float factor[N], add[N], times[N];
+};
+template <int N>
+struct Entries {
+    int e[N];
+};
+template <int N>
+__device__ __forceinline__ Entries<N> load_entries(const PromptProblem &p, const int32_t *table, int pos, int end)
+{
+    Entries<N> x;
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+        x.e[u] = -1;
+        if (pos + kTileKeys * u < end) x.e[u] = scalar_load(table + ((pos + kTileKeys * u) >> p.page_shift));
+    }
+    return x;
+}
+template <int N, bool Eight>
+__device__ __forceinline__ Block<N, Eight> block_of(const PromptProblem &p, const Entries<N> &x, int head, int pos, int D, Places<N> &places)
+{
+    Block<N, Eight> k;
+    k.ok = 0;
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+        const bool named = (uint32_t)x.e[u] < (uint32_t)p.pages;
+        const int slot = (pos + kTileKeys * u) & ((1 << p.page_shift) - 1);
+        const int64_t page_head = (int64_t)(named ? x.e[u] : 0) * p.kv_heads + head;
+        places.at[u] = ((page_head << p.page_shift) + slot) * D;
+        bool fine = named;
+        if constexpr (Eight) {
+            const int per_shift = p.page_shift - 4;
+            const float *s = p.scales + ((page_head * 2) << per_shift) + (slot >> 4);
+            const float ks = scalar_load(s), vs = scalar_load(s + (1 << per_shift));
+            fine = named && is_scale(ks) && is_scale(vs);
+            k.factor[u] = fine ? ks * p.scale_log2 : 0.f;
+            k.add[u] = fine ? __builtin_amdgcn_logf(vs) : 0.f;
+            k.times[u] = fine ? __builtin_amdgcn_rcpf(vs) : 0.f;
+        }
+        k.ok |= (fine ? 1u : 0u) << u;
+    }
+    return k;
+}
+// One of four by arithmetic: a select by a lane's index of a vector's elements goes through memory.
+__device__ __forceinline__ int64_t one_of(int u, int64_t a, int64_t b, int64_t c, int64_t d)
+{
+    const int64_t first = -(int64_t)(u == 0), second = -(int64_t)(u == 1), third = -(int64_t)(u == 2), fourth = -(int64_t)(u == 3);
+    return (a & first) | (b & second) | (c & third) | (d & fourth);
+}
+
+// ---- many rows: keys and values through LDS ----
+
+constexpr int kStep = 64;
+
+template <typename T, int D, int RT>
+constexpr int kWideFloats = 64 * kWaves * 4 * (RT * (D / 32) * 4 + RT);
+
+// RT: 32-row columns of a wave.  K lies in LDS as [key][channel], its 16-byte pieces swapped by the key's last three bits; V^T as
+// [channel][key], each 16 keys in the order 0-3, 8-11, 4-7, 12-15, its pieces swapped by bits of the channel: every read and write is
+// of distinct banks.
+template <typename T, int D, int RT, bool Eight>
+__global__ void __launch_bounds__(64 * kWaves, RT == 1 && D <= 128 ? 2 : 1) prompt_kernel(const PromptProblem p)
+{
+    typedef Elem<T> E;
+    typedef typename E::vec8 vec8;
+    constexpr int kRows = 32 * RT * kWaves, kThreads = 64 * kWaves;
+    constexpr int kOct = D / 8;                       // pieces of eight channels of a row
+    constexpr int kKeyRow = (D == 96 ? 128 : D) * 2;  // bytes
+    constexpr int kKeyBytes = kStep * kKeyRow, kValueBytes = D * kStep * 2;
+    constexpr int kKeyPasses = kStep * kOct / kThreads, kQuads = kStep / 4;
+    constexpr int kValuePasses = (kQuads * kOct + kThreads - 1) / kThreads;
+    constexpr int kPiece = Eight ? 2 : 4;  // dwords of eight elements
+    constexpr int kCt = D / 32, kC = D / 16;
+    constexpr float kUnit = __is_same(T, _Float16) ? 15.f : 0.f;  // log2 of what a weight of 1 is
+    static_assert(kStep * kOct % kThreads == 0, "");
+
+    __shared__ __attribute__((aligned(16))) uint8_t lds[2][kKeyBytes + kValueBytes];
+    __shared__ int lds_odd[2][kWaves];
+    __shared__ int lds_last;
+    static_assert(sizeof(lds) >= kKvMaxBatch / 64 * 4, "");
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int col = lane & 31, half = lane >> 5;
+    const int index = p.base + blockIdx.x;
+    const int head = index % p.kv_heads, rest = index / p.kv_heads;
+    const int split = rest % p.splits, tile_no = p.tiles - 1 - rest / p.splits;
+    const Tile tile = find_tile(p, kRows, tile_no, lane, wave, (int *)&lds[0][0]);
+    if (tile.row0 < 0) return;
+    const Keys keys = keys_of(p, tile, kRows, 6);
+    int parts = keys.steps / 4;  // work-groups that share the tile, each four steps at the least
+    parts = parts < 1 ? 1 : parts < p.splits ? parts : p.splits;
+    if (split >= parts) return;
+    const int s0 = (int)((int64_t)keys.steps * split / parts), s1 = (int)((int64_t)keys.steps * (split + 1) / parts);
+    __syncthreads();
+
+    const int32_t *const table = p.table + (int64_t)tile.b * p.table_row;
+    auto position_of = [&](int s) { return (s < keys.sink_steps ? s : s + keys.skip) * kStep; };
+
+    // this lane's rows
+    Sight sight[RT];
+    vec8 qf[RT][kC];
+    int64_t out_at[RT];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        const int row = tile.row0 + (wave * RT + rt) * 32 + col;
+        sight[rt] = sight_of(p, tile, row);
+        const bool have = row < (int64_t)tile.tokens * p.group;
+        const int token = tile.from + (have ? row / p.group : 0), h = head * p.group + (have ? row % p.group : 0);
+        out_at[rt] = have ? (int64_t)token * p.heads + h : -1;
+        const T *q = (const T *)p.q + token * p.q_row + h * p.q_head + 8 * half;
+#pragma unroll
+        for (int c = 0; c < kC; ++c) qf[rt][c] = have ? *(const vec8 *)(q + 16 * c) : vec8{};
+    }
+
+    uint32_t kreg[kKeyPasses][kPiece], vreg[kValuePasses][4][kPiece];
+    auto load_step = [&](const Places<4> &places, uint32_t ok, int pos) {
+        constexpr int kSize = Eight ? 1 : 2;
+        const int64_t a0 = places.at[0], a1 = places.at[1], a2 = places.at[2], a3 = places.at[3];
+#pragma unroll
+        for (int i = 0; i < kKeyPasses; ++i) {
+            const int n = tid + kThreads * i, key = n / kOct, oct = n % kOct;
+            const uint8_t *from = (const uint8_t *)p.k + (one_of(key >> 4, a0, a1, a2, a3) + (key & 15) * D + 8 * oct) * kSize;
+            if (ok >> (key >> 4) & 1) __builtin_memcpy(kreg[i], __builtin_assume_aligned(from, 8 * kSize), 8 * kSize);
+        }
+#pragma unroll
+        for (int i = 0; i < kValuePasses; ++i) {
+            const int n = tid + kThreads * i, quad = n / kOct, oct = n % kOct;
+            const bool have = quad < kQuads && (ok >> (quad >> 2) & 1);
+            const uint8_t *from = (const uint8_t *)p.v + (one_of(quad >> 2, a0, a1, a2, a3) + (quad & 3) * 4 * D + 8 * oct) * kSize;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+#pragma unroll
+                for (int w = 0; w < kPiece; ++w) vreg[i][j][w] = 0;
+                if (have && pos + 4 * quad + j < keys.end)
+                    __builtin_memcpy(vreg[i][j], __builtin_assume_aligned(from + j * D * kSize, 8 * kSize), 8 * kSize);
+            }
+        }
+    };
+    // whether every row sees every key of a step
+    auto whole = [&](uint32_t ok, int pos) {
+        return ok == 15u && pos + kStep - 1 <= keys.first && pos + kStep <= keys.end &&
+               (!p.window || pos > keys.last - p.window || pos + kStep <= p.sinks);
+    };
+    auto store_step = [&](int buf, bool check) {
+        if (check) {
+            uint32_t odd = 0;
+#pragma unroll
+            for (int i = 0; i < kValuePasses; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int w = 0; w < kPiece; ++w) {
+                        const uint32_t x = finite_of<T, Eight>(vreg[i][j][w]);
+                        odd |= x ^ vreg[i][j][w];
+                        vreg[i][j][w] = x;
+                    }
+            const bool any = __any(odd != 0);
+            if (lane == 0) lds_odd[buf][wave] = any;
+        }
+        uint8_t *const to_keys = lds[buf], *const to_values = lds[buf] + kKeyBytes;
+#pragma unroll
+        for (int i = 0; i < kKeyPasses; ++i) {
+            const int n = tid + kThreads * i, key = n / kOct, oct = n % kOct;
+            vec8 x;
+            if constexpr (Eight)
+                x = E::of_codes(kreg[i][0], kreg[i][1]);
+            else
+                __builtin_memcpy(&x, kreg[i], 16);
+            *(vec8 *)(to_keys + key * kKeyRow + ((oct ^ (key & 7)) * 16)) = x;
+        }
+#pragma unroll
+        for (int i = 0; i < kValuePasses; ++i) {
+            const int n = tid + kThreads * i, quad = n / kOct, oct = n % kOct;
+            if (quad < kQuads) {
+                const int chunk = (quad >> 2) * 2 + (quad & 1), upper = (quad >> 1) & 1;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    uint32_t w[2];
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        if constexpr (Eight)
+                            w[h] = E::of_two_codes(__builtin_amdgcn_perm(vreg[i][2 * h + 1][j >> 2], vreg[i][2 * h][j >> 2],
+                                                                         (j & 2) ? 0x07030602u : 0x05010400u), j & 1);
+                        else
+                            w[h] = __builtin_amdgcn_perm(vreg[i][2 * h + 1][j >> 1], vreg[i][2 * h][j >> 1], (j & 1) ? 0x07060302u : 0x05040100u);
+                    }
+                    const int ch = 8 * oct + j;
+                    __builtin_memcpy(__builtin_assume_aligned(to_values + ch * (kStep * 2) + ((chunk ^ ((ch ^ (ch >> 3)) & 7)) * 16) + upper * 8, 8), w, 8);
+                }
+            }
+        }
+    };
+
+    float16_t acc[RT][kCt];
+    float m[RT], l[RT];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        m[rt] = -INFINITY;
+        l[rt] = 0.f;
+#pragma unroll
+        for (int ct = 0; ct < kCt; ++ct) acc[rt][ct] = float16_t{};
+    }
+
+    auto value_at = [&](int buf, int ct, int g16) -> vec8 {
+        const int ch = 32 * ct + col;
+        return *(const vec8 *)(lds[buf] + kKeyBytes + ch * (kStep * 2) + (((2 * g16 + half) ^ ((ch ^ (ch >> 3)) & 7)) * 16));
+    };
+    auto compute = [&](int buf, const Block<4, Eight> &k, int pos) {
+        float16_t s[RT][2];
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) s[rt][0] = s[rt][1] = float16_t{};
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt) {
+            const int key = 32 * kt + col;
+#pragma unroll
+            for (int c = 0; c < kC; ++c) {
+                const vec8 a = *(const vec8 *)(lds[buf] + key * kKeyRow + (((2 * c + half) ^ (key & 7)) * 16));
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) s[rt][kt] = mfma32(a, qf[rt][c], s[rt][kt]);
+            }
+        }
+        const bool all = whole(k.ok, pos);
+        // key of a lane's score i of 32: the tile's, then this
+        auto key_of = [&](int kt, int i) { return 32 * kt + 8 * (i >> 2) + 4 * half + (i & 3); };
+        vec8 weights[RT][4];
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    if constexpr (Eight)
+                        s[rt][kt][i] = __builtin_fmaf(s[rt][kt][i], k.factor[2 * kt + (i >> 3)], k.add[2 * kt + (i >> 3)]);
+                    else
+                        s[rt][kt][i] *= p.scale_log2;
+                }
+            if (!all) {
+#pragma unroll
+                for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (!(k.ok >> (2 * kt + (i >> 3)) & 1) || !sight[rt].sees(pos + key_of(kt, i)) || pos + key_of(kt, i) >= keys.end)
+                            s[rt][kt][i] = -INFINITY;
+            }
+            float top = m[rt];
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) top = fmaxf(top, s[rt][kt][i]);
+            const Pair halves = exchange<32>(top);
+            top = fmaxf(halves.a, halves.b);
+            const float ref = top == -INFINITY ? 0.f : top;
+            if (__any(top > m[rt])) {
+                const float keep = __builtin_amdgcn_exp2f(m[rt] - ref);
+                l[rt] *= keep;
+#pragma unroll
+                for (int ct = 0; ct < kCt; ++ct) acc[rt][ct] *= keep;
+            }
+            m[rt] = top;
+#pragma unroll
+            for (int g16 = 0; g16 < 4; ++g16) {
+                float sum = 0.f;
+#pragma unroll
+                for (int e = 0; e < 8; e += 2) {
+                    const float x = __builtin_amdgcn_exp2f(s[rt][g16 >> 1][8 * (g16 & 1) + e] - (ref - kUnit));
+                    const float y = __builtin_amdgcn_exp2f(s[rt][g16 >> 1][8 * (g16 & 1) + e + 1] - (ref - kUnit));
+                    sum += x + y;
+                    weights[rt][g16][e] = (T)x;
+                    weights[rt][g16][e + 1] = (T)y;
+                }
+                if constexpr (Eight) sum *= k.times[g16];
+                l[rt] += sum;
+            }
+        }
+#pragma unroll
+        for (int g16 = 0; g16 < 4; ++g16)
+#pragma unroll
+            for (int ct = 0; ct < kCt; ++ct) {
+                const vec8 a = value_at(buf, ct, g16);
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) acc[rt][ct] = mfma32(a, weights[rt][g16], acc[rt][ct]);
+            }
+        if (!all) {
+            int odd = 0;
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) odd |= lds_odd[buf][w];
+            if (__builtin_amdgcn_readfirstlane(odd)) {
+#pragma unroll 1
+                for (int n = 0; n < kStep; ++n) {
+                    const int j = pos + n;
+                    if (!(k.ok >> (n >> 4) & 1) || j >= keys.end) continue;
+                    const int page = scalar_load(table + (j >> p.page_shift)), slot = j & ((1 << p.page_shift) - 1);
+                    const int64_t at = ((((int64_t)page * p.kv_heads + head) << p.page_shift) + slot) * D + 4 * half;
+#pragma unroll
+                    for (int ct = 0; ct < kCt; ++ct)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            const float x = odd_at<T, Eight>(p.v, at + 32 * ct + 8 * (i >> 2) + (i & 3));
+#pragma unroll
+                            for (int rt = 0; rt < RT; ++rt)
+                                if (sight[rt].sees(j)) acc[rt][ct][i] += x;
+                        }
+                }
+            }
+        }
+    };
+
+    if (s0 < s1) {
+        Entries<4> entries = load_entries<4>(p, table, position_of(s0), keys.end), ahead{};
+        Places<4> places;
+        Block<4, Eight> block = block_of<4, Eight>(p, entries, head, position_of(s0), D, places);
+        load_step(places, block.ok, position_of(s0));
+        if (s0 + 1 < s1) ahead = load_entries<4>(p, table, position_of(s0 + 1), keys.end);
+        store_step(0, !whole(block.ok, position_of(s0)));
+        int buf = 0;
+#pragma unroll 1
+        for (int s = s0; s < s1; ++s) {
+            Block<4, Eight> next = block;
+            const bool more = s + 1 < s1;
+            if (more) {
+                next = block_of<4, Eight>(p, ahead, head, position_of(s + 1), D, places);
+                load_step(places, next.ok, position_of(s + 1));
+                if (s + 2 < s1) ahead = load_entries<4>(p, table, position_of(s + 2), keys.end);
+            }
+            __syncthreads();
+            compute(buf, block, position_of(s));
+            if (more) store_step(buf ^ 1, !whole(next.ok, position_of(s + 1)));
+            block = next;
+            buf ^= 1;
+        }
+    }
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        const Pair halves = exchange<32>(l[rt]);
+        l[rt] = halves.a + halves.b;
+    }
+
+    // ---- pieces of a tile's keys ----
+    if (parts > 1) {
+        const int item = tile_no * p.kv_heads + head;
+        constexpr int kPer = RT * kCt * 4 + RT;  // 16-byte pieces of a lane
+        float *const slot = p.partials + (int64_t)(item * p.splits + split) * kWideFloats<T, D, RT>;
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+#pragma unroll
+            for (int ct = 0; ct < kCt; ++ct)
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    store_partial16(slot, wave * kPer + (rt * kCt + ct) * 4 + q, lane,
+                                    float4_t{acc[rt][ct][4 * q], acc[rt][ct][4 * q + 1], acc[rt][ct][4 * q + 2], acc[rt][ct][4 * q + 3]});
+            store_partial16(slot, wave * kPer + RT * kCt * 4 + rt, lane, float4_t{m[rt], l[rt], 0.f, 0.f});
+        }
+        wait_vmcnt<0>();
+        __syncthreads();
+        if (tid == 0) {
+            uint32_t *const ctr = p.counters + kCounterStride * item;
+            const bool done = __hip_atomic_fetch_add(ctr, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)(parts - 1);
+            if (done) __hip_atomic_store(ctr, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            lds_last = done;
+        }
+        __syncthreads();
+        if (!__builtin_amdgcn_readfirstlane(lds_last)) return;
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            m[rt] = -INFINITY;
+            l[rt] = 0.f;
+#pragma unroll
+            for (int ct = 0; ct < kCt; ++ct) acc[rt][ct] = float16_t{};
+        }
+#pragma unroll 1
+        for (int k = 0; k < parts; ++k) {
+            const float *const from = p.partials + (int64_t)(item * p.splits + k) * kWideFloats<T, D, RT>;
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) {
+                const float4_t ml = load_partial16(from, wave * kPer + RT * kCt * 4 + rt, lane);
+                const float top = fmaxf(m[rt], ml[0]), ref = top == -INFINITY ? 0.f : top;
+                const float f = __builtin_amdgcn_exp2f(m[rt] - ref), f2 = __builtin_amdgcn_exp2f(ml[0] - ref);
+                m[rt] = top;
+                l[rt] = l[rt] * f + ml[1] * f2;
+#pragma unroll
+                for (int ct = 0; ct < kCt; ++ct)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const float4_t x = load_partial16(from, wave * kPer + (rt * kCt + ct) * 4 + q, lane);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) acc[rt][ct][4 * q + i] = acc[rt][ct][4 * q + i] * f + x[i] * f2;
+                    }
+            }
+        }
+    }
+
+    // ---- the finished rows: a lane holds four adjacent channels of every eight ----
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        if (out_at[rt] < 0) continue;
+        const float inv = 1.f / l[rt];
+        T *const to = (T *)p.out + out_at[rt] * D + 4 * half;
+#pragma unroll
+        for (int ct = 0; ct < kCt; ++ct)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                typename E::vec4 y;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) y[i] = l[rt] == 0.f ? (T)0.f : (T)(acc[rt][ct][4 * q + i] * inv);
+                *(typename E::vec4 *)(to + 32 * ct + 8 * q) = y;
+            }
+        if (p.lse && half == 0) p.lse[out_at[rt]] = (m[rt] + __builtin_amdgcn_logf(l[rt]) - kUnit) * 0.693147180559945f;
+    }
+}
+
+// ---- few rows: keys and values straight to registers, the waves share the keys ----
+
+template <typename T, int D, int RT>
+constexpr int kFewFloats = RT * (kHeadTile * D + 2 * kHeadTile);
+
+// RT: 16-row columns of the tile.  A wave takes steps of 32 keys as the kernel of one token per sequence does (attend.hip), with the
+// rows for its heads.
+template <typename T, int D, int RT, bool Eight>
+__global__ void __launch_bounds__(64 * kWaves, D > 128 ? 1 : 2) prompt_few_kernel(const PromptProblem p)
+{
+    typedef Elem<T> E;
+    typedef typename E::vec8 vec8;
+    constexpr int kRows = 16 * RT, KT = 2, kKeys = 32;
+    constexpr int kQ = D / 32;
+    constexpr int kHalves = D > 128 && !Eight ? 2 : 1;
+    constexpr int kCh = D / 16 / kHalves;
+    constexpr int kValueDw = Eight ? (kCh + 3) / 4 : kCh / 2;
+    constexpr bool kBy32 = D % 64 != 0;
+    constexpr int kKeyDw = Eight ? D / 16 : kQ * 4;
+    constexpr int kAcc = D / 16;
+    constexpr float kUnit = __is_same(T, _Float16) ? 15.f : 0.f;
+    constexpr int kSlot = kFewFloats<T, D, RT>;
+
+    __shared__ float4_t lds_acc[kWaves][kAcc][64];
+    __shared__ float lds_m[kWaves][kHeadTile], lds_l[kWaves][kHeadTile];
+    __shared__ int lds_last;
+    static_assert(sizeof(lds_acc) >= kKvMaxBatch / 64 * 4, "");
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int r = lane & 15, g = lane >> 4;
+    const int index = p.base + blockIdx.x;
+    const int head = index % p.kv_heads, rest = index / p.kv_heads;
+    const int split = rest % p.splits, tile_no = p.tiles - 1 - rest / p.splits;
+    const Tile tile = find_tile(p, kRows, tile_no, lane, wave, (int *)&lds_acc[0][0][0]);
+    if (tile.row0 < 0) return;
+    const Keys keys = keys_of(p, tile, kRows, 5);
+    int parts = keys.steps / (4 * kWaves);  // each wave four steps at the least
+    parts = parts < 1 ? 1 : parts < p.splits ? parts : p.splits;
+    if (split >= parts) return;
+    const int s0 = (int)((int64_t)keys.steps * split / parts), s1 = (int)((int64_t)keys.steps * (split + 1) / parts);
+    __syncthreads();
+
+    const int32_t *const table = p.table + (int64_t)tile.b * p.table_row;
+    auto position_of = [&](int s) { return (s < keys.sink_steps ? s : s + keys.skip) * kKeys; };
+    Sight sight[RT];
+    vec8 qf[RT][kQ];
+    int64_t out_at[RT];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        const int row = tile.row0 + rt * 16 + r;
+        sight[rt] = sight_of(p, tile, row);
+        const bool have = row < (int64_t)tile.tokens * p.group;
+        const int token = tile.from + (have ? row / p.group : 0), h = head * p.group + (have ? row % p.group : 0);
+        out_at[rt] = have ? (int64_t)token * p.heads + h : -1;
+        const T *q = (const T *)p.q + token * p.q_row + h * p.q_head;
+#pragma unroll
+        for (int t = 0; t < kQ; ++t)
+            qf[rt][t] = !have ? vec8{} : *(const vec8 *)(Eight && !kBy32 ? q + 16 * g + 64 * (t >> 1) + 8 * (t & 1) : q + 8 * g + 32 * t);
+    }
+
+    uint32_t kf[KT][kKeyDw] = {}, vr[KT][4][kHalves][kValueDw] = {};
+    auto load_keys = [&](const Places<KT> &k, uint32_t ok) {
+#pragma unroll
+        for (int u = 0; u < KT; ++u) {
+            if (!(ok >> u & 1)) continue;
+            if constexpr (!Eight) {
+                const T *from = (const T *)p.k + k.at[u] + (r * D + 8 * g);
+#pragma unroll
+                for (int t = 0; t < kQ; ++t) __builtin_memcpy(&kf[u][4 * t], __builtin_assume_aligned(from + 32 * t, 16), 16);
+            } else {
+                constexpr int kPiece = kBy32 ? 8 : 16;
+                const uint8_t *from = (const uint8_t *)p.k + k.at[u] + r * D;
+#pragma unroll
+                for (int t = 0; t < D / (4 * kPiece); ++t)
+                    __builtin_memcpy(&kf[u][kPiece / 4 * t], __builtin_assume_aligned(from + kPiece * (g + 4 * t), kPiece), kPiece);
+            }
+        }
+    };
+    auto load_values = [&](const Places<KT> &k, uint32_t ok) {
+#pragma unroll
+        for (int u = 0; u < KT; ++u) {
+            if (!(ok >> u & 1)) continue;
+            if constexpr (!Eight) {
+                const T *v = (const T *)p.v + k.at[u] + (4 * g * D + kCh * r);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int hf = 0; hf < kHalves; ++hf) load_dwords<kValueDw>(vr[u][i][hf], v + i * D + 128 * hf);
+            } else {
+                const uint8_t *v = (const uint8_t *)p.v + k.at[u] + 4 * g * D;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if constexpr (kBy32) {
+                        vr[u][i][0][0] = *(const uint32_t *)(v + i * D + 4 * r);
+                        vr[u][i][0][1] = *(const uint16_t *)(v + i * D + 64 + 2 * r);
+                    } else {
+                        load_dwords<kValueDw>(vr[u][i][0], v + i * D + kCh * r);
+                    }
+                }
+            }
+        }
+    };
+    float4_t acc[RT][kAcc];
+    float m[RT], l[RT];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        m[rt] = -INFINITY;
+        l[rt] = 0.f;
+#pragma unroll
+        for (int j = 0; j < kAcc; ++j) acc[rt][j] = float4_t{0.f, 0.f, 0.f, 0.f};
+    }
+    // the channel that row x of accumulator j stands for
+    auto channel_of = [](int j, int x) {
+        return Eight && kBy32 ? (j < 4 ? 4 * x + j : 60 + 2 * x + j) : 128 * (j / kCh) + kCh * x + j % kCh;
+    };
+    // four keys' elements of channel piece hf, j of both tiles, as the second product's operand
+    auto values_of = [&](int hf, int j) -> vec8 {
+        u32x4_t w;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if constexpr (Eight)
+                w[e] = E::of_two_codes(__builtin_amdgcn_perm(vr[e >> 1][2 * (e & 1) + 1][hf][j >> 2], vr[e >> 1][2 * (e & 1)][hf][j >> 2],
+                                                             (j & 2) ? 0x07030602u : 0x05010400u), j & 1);
+            else
+                w[e] = __builtin_amdgcn_perm(vr[e >> 1][2 * (e & 1) + 1][hf][j >> 1], vr[e >> 1][2 * (e & 1)][hf][j >> 1],
+                                             (j & 1) ? 0x07060302u : 0x05040100u);
+        }
+        return __builtin_bit_cast(vec8, w);
+    };
+
+    int s = s0 + wave;
+    if (s < s1) {
+        Places<KT> places;
+        Block<KT, Eight> cur = block_of<KT, Eight>(p, load_entries<KT>(p, table, position_of(s), keys.end), head, position_of(s), D, places), next = cur;
+        load_keys(places, cur.ok);
+        load_values(places, cur.ok);
+        Entries<KT> ahead{};
+        if (s + kWaves < s1) ahead = load_entries<KT>(p, table, position_of(s + kWaves), keys.end);
+#pragma unroll 1
+        while (true) {
+            float4_t sc[RT][KT];
+#pragma unroll
+            for (int u = 0; u < KT; ++u) {
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) sc[rt][u] = float4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int t = 0; t < kQ; ++t) {
+                    vec8 x;
+                    if constexpr (Eight)
+                        x = E::of_codes(kf[u][2 * t], kf[u][2 * t + 1]);
+                    else
+                        __builtin_memcpy(&x, &kf[u][4 * t], 16);
+#pragma unroll
+                    for (int rt = 0; rt < RT; ++rt) sc[rt][u] = E::mfma(x, qf[rt][t], sc[rt][u]);
+                }
+            }
+            const int pos = position_of(s);
+            const bool more = s + kWaves < s1;
+            issue_order_point();
+            if (more) {
+                next = block_of<KT, Eight>(p, ahead, head, position_of(s + kWaves), D, places);
+                load_keys(places, next.ok);
+                if (s + 2 * kWaves < s1) ahead = load_entries<KT>(p, table, position_of(s + 2 * kWaves), keys.end);
+            }
+            const bool all = cur.ok == 3u && pos + kKeys - 1 <= keys.first && pos + kKeys <= keys.end &&
+                             (!p.window || pos > keys.last - p.window || pos + kKeys <= p.sinks);
+            if (!all) {  // what no row sees: zero
+#pragma unroll
+                for (int u = 0; u < KT; ++u)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (!(cur.ok >> u & 1) || pos + 16 * u + 4 * g + i >= keys.end) {
+#pragma unroll
+                            for (int hf = 0; hf < kHalves; ++hf)
+#pragma unroll
+                                for (int w = 0; w < kValueDw; ++w) vr[u][i][hf][w] = 0;
+                        }
+            }
+            vec8 weights[RT];
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) {
+#pragma unroll
+                for (int u = 0; u < KT; ++u)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        if constexpr (Eight)
+                            sc[rt][u][i] = __builtin_fmaf(sc[rt][u][i], cur.factor[u], cur.add[u]);
+                        else
+                            sc[rt][u][i] *= p.scale_log2;
+                        if (!all) {
+                            const int j = pos + 16 * u + 4 * g + i;
+                            if (!(cur.ok >> u & 1) || !sight[rt].sees(j) || j >= keys.end) sc[rt][u][i] = -INFINITY;
+                        }
+                    }
+                float top = m[rt];
+#pragma unroll
+                for (int u = 0; u < KT; ++u)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) top = fmaxf(top, sc[rt][u][i]);
+                top = max_over_groups(top);
+                const float ref = top == -INFINITY ? 0.f : top;
+                if (__any(top > m[rt])) {
+                    const float keep = __builtin_amdgcn_exp2f(m[rt] - ref);
+                    l[rt] *= keep;
+#pragma unroll
+                    for (int j = 0; j < kAcc; ++j) acc[rt][j] *= keep;
+                }
+                m[rt] = top;
+#pragma unroll
+                for (int u = 0; u < KT; ++u) {
+                    float sum = 0.f;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float x = __builtin_amdgcn_exp2f(sc[rt][u][i] - (ref - kUnit));
+                        sum += x;
+                        weights[rt][4 * u + i] = (T)x;
+                    }
+                    if constexpr (Eight) sum *= cur.times[u];
+                    l[rt] += sum;
+                }
+            }
+            if (!all) {
+                uint32_t odd = 0;
+#pragma unroll
+                for (int u = 0; u < KT; ++u)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+#pragma unroll
+                        for (int hf = 0; hf < kHalves; ++hf)
+#pragma unroll
+                            for (int w = 0; w < kValueDw; ++w) {
+                                const uint32_t x = finite_of<T, Eight>(vr[u][i][hf][w]);
+                                odd |= x ^ vr[u][i][hf][w];
+                                vr[u][i][hf][w] = x;
+                            }
+                if (__any(odd != 0)) {
+#pragma unroll 1
+                    for (int n = 0; n < kKeys; ++n) {
+                        const int j = pos + n;
+                        if (!(cur.ok >> (n >> 4) & 1) || j >= keys.end) continue;
+                        const int page = scalar_load(table + (j >> p.page_shift)), slot = j & ((1 << p.page_shift) - 1);
+                        const int64_t at = ((((int64_t)page * p.kv_heads + head) << p.page_shift) + slot) * D;
+#pragma unroll
+                        for (int c = 0; c < kAcc; ++c)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                const float x = odd_at<T, Eight>(p.v, at + channel_of(c, 4 * g + i));
+#pragma unroll
+                                for (int rt = 0; rt < RT; ++rt)
+                                    if (sight[rt].sees(j)) acc[rt][c][i] += x;
+                            }
+                    }
+                }
+            }
+#pragma unroll
+            for (int hf = 0; hf < kHalves; ++hf)
+#pragma unroll
+                for (int j = 0; j < kCh; ++j) {
+                    const vec8 x = values_of(hf, j);
+#pragma unroll
+                    for (int rt = 0; rt < RT; ++rt) acc[rt][hf * kCh + j] = E::mfma(x, weights[rt], acc[rt][hf * kCh + j]);
+                }
+            issue_order_point();
+            if (!more) break;
+            load_values(places, next.ok);
+            cur = next;
+            s += kWaves;
+        }
+    }
+
+    // ---- the waves' pieces, then the work-groups' ----
+    const int item = tile_no * p.kv_heads + head;
+    float *const slot = p.partials + (int64_t)(item * p.splits + split) * kSlot;
+    auto write = [&](int rt, int j, float4_t o, float top, float sum) {
+        if (out_at[rt] < 0) return;
+        const float inv = 1.f / sum;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            ((T *)p.out)[out_at[rt] * D + channel_of(j, 4 * g + i)] = sum == 0.f ? (T)0.f : (T)(o[i] * inv);
+        }
+        if (p.lse && g == 0 && j == 0) p.lse[out_at[rt]] = (top + __builtin_amdgcn_logf(sum) - kUnit) * 0.693147180559945f;
+    };
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < kAcc; ++j) lds_acc[wave][j][lane] = acc[rt][j];
+        const float sum_l = sum_over_groups(l[rt]);
+        if (g == 0) {
+            lds_m[wave][r] = m[rt];
+            lds_l[wave][r] = sum_l;
+        }
+        __syncthreads();
+        float top = -INFINITY, sum = 0.f, f[kWaves];
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) top = fmaxf(top, lds_m[w][r]);
+        const float ref = top == -INFINITY ? 0.f : top;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            f[w] = __builtin_amdgcn_exp2f(lds_m[w][r] - ref);
+            sum += lds_l[w][r] * f[w];
+        }
+#pragma unroll 1
+        for (int j = wave; j < kAcc; j += kWaves) {
+            float4_t o{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) o += lds_acc[w][j][lane] * f[w];
+            if (parts == 1) {
+                write(rt, j, o, top, sum);
+            } else {
+                store_partial16(slot, rt * kAcc + j, lane, o);
+                if (j == 0 && g == 0) {
+                    store_float(slot + RT * kHeadTile * D + rt * 2 * kHeadTile + r, top);
+                    store_float(slot + RT * kHeadTile * D + rt * 2 * kHeadTile + kHeadTile + r, sum);
+                }
+            }
+        }
+    }
+    if (parts == 1) return;
+    wait_vmcnt<0>();
+    __syncthreads();
+    if (tid == 0) {
+        uint32_t *const ctr = p.counters + kCounterStride * item;
+        const bool done = __hip_atomic_fetch_add(ctr, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)(parts - 1);
+        if (done) __hip_atomic_store(ctr, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        lds_last = done;
+    }
+    __syncthreads();
+    if (!__builtin_amdgcn_readfirstlane(lds_last)) return;
+    const float *const slots = p.partials + (int64_t)item * p.splits * kSlot;
+    const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc((void *)slots, (short)0, 0x7fffffffu, kBufferFlags);
+#pragma unroll 1
+    for (int n = wave; n < RT * kAcc; n += kWaves) {
+        const int rt = n / kAcc, j = n - rt * kAcc;
+        float top = -INFINITY, sum = 0.f;
+        float4_t o{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+        for (int k = 0; k < parts; ++k) {
+            const int at = k * kSlot * 4, ml = (RT * kHeadTile * D + rt * 2 * kHeadTile + r) * 4;
+            const float m2 = load_slot4(rsrc, at, ml), l2 = load_slot4(rsrc, at, ml + kHeadTile * 4);
+            const float4_t x = load_slot16(rsrc, at, n * 1024 + lane * 16);
+            const float t = fmaxf(top, m2), ref = t == -INFINITY ? 0.f : t;
+            const float f = __builtin_amdgcn_exp2f(top - ref), f2 = __builtin_amdgcn_exp2f(m2 - ref);
+            top = t;
+            sum = sum * f + l2 * f2;
+            o = o * f + x * f2;
+        }
+#pragma unroll
+        for (int i = 0; i < RT; ++i)
+            if (i == rt) write(i, j, o, top, sum);
+    }
+}
+
+constexpr int kWideGroups = 512, kFewGroups = 1024;  // work-groups that share a call's keys
+
+template <typename T, int D, bool Eight>
+hipError_t launch_one(const PromptProblem &p, const PromptPlan &plan, hipStream_t stream)
+{
+    PromptProblem q = p;
+    q.tiles = plan.tiles;
+    q.splits = plan.splits;
+    const void *kernel = (const void *)(plan.few ? (plan.rows == 16 ? &prompt_few_kernel<T, D, 1, Eight> : &prompt_few_kernel<T, D, 2, Eight>)
+                                                 : &prompt_kernel<T, D, 1, Eight>);
+    const int64_t all = (int64_t)plan.tiles * p.kv_heads * plan.splits, most = ((int64_t)1 << 24) / p.kv_heads * p.kv_heads - p.kv_heads;
+    for (int64_t base = 0; base < all; base += most) {  // a launch takes less than 2^32 threads
+        q.base = (int)base;
+        void *args[] = {&q};
+        const uint32_t n = (uint32_t)(all - base < most ? all - base : most);
+        const hipError_t e = hipLaunchKernel(kernel, dim3(n), dim3(64 * kWaves), args, 0, stream);
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
+template <typename T>
+hipError_t launch_typed(const PromptProblem &p, const PromptPlan &plan, int head_dim, hipStream_t stream)
+{
+    switch (head_dim) {
+    case 64: return p.scales ? launch_one<T, 64, true>(p, plan, stream) : launch_one<T, 64, false>(p, plan, stream);
+    case 96: return p.scales ? launch_one<T, 96, true>(p, plan, stream) : launch_one<T, 96, false>(p, plan, stream);
+    case 128: return p.scales ? launch_one<T, 128, true>(p, plan, stream) : launch_one<T, 128, false>(p, plan, stream);
+    case 256: return p.scales ? launch_one<T, 256, true>(p, plan, stream) : launch_one<T, 256, false>(p, plan, stream);
+    }
+    return hipErrorInvalidValue;
+}
+
+}  // namespace
+
+PromptPlan plan_prompt(int64_t tokens, int64_t B, int64_t heads, int64_t kv_heads, int head_dim)
+{
+    PromptPlan x;
+    const int64_t rows = tokens * (heads / kv_heads);  // of one kv head
+    const int64_t sequences = B < tokens ? B : tokens;
+    x.few = rows <= 64 * sequences;
+    x.rows = x.few ? (rows <= 16 * sequences ? 16 : 32) : 32 * kWaves;
+    x.tiles = (int)(rows / x.rows + sequences);
+    const int64_t groups = (int64_t)x.tiles * kv_heads, most = x.few ? kFewGroups : kWideGroups;
+    x.splits = (int)(groups == 0 || groups > most ? 1 : most / groups);
+    x.slot_floats = x.few ? (x.rows / 16) * (kHeadTile * head_dim + 2 * kHeadTile) : 64 * kWaves * 4 * (head_dim / 32 * 4 + 1);
+    return x;
+}
+
+hipError_t launch_prompt(const PromptProblem &p, const PromptPlan &plan, int head_dim, marlin_dtype_t dtype, hipStream_t stream)
+{
+    return dtype == MARLIN_BF16 ? launch_typed<__bf16>(p, plan, head_dim, stream) : launch_typed<_Float16>(p, plan, head_dim, stream);
+}
+
+}  // namespace marlin

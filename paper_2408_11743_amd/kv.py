@@ -112,11 +112,11 @@ def _no_tangents(func: str, *tensors) -> None:
                 raise RuntimeError("%s: there is no forward derivative" % func)
 
 
-def _rows(func: str, name: str, x: torch.Tensor, dtype, device) -> torch.Tensor:
+def _rows(func: str, name: str, x: torch.Tensor, dtype, device, kind: str = "of the cache's dtype") -> torch.Tensor:
     """x [rows, heads, head dim] as the kernels read it: channels contiguous, rows
     and heads at multiples of 16 bytes (any other view is copied)."""
     if x.dtype != dtype or not x.is_cuda:
-        raise TypeError("%s: %s must be a device tensor of the cache's dtype" % (func, name))
+        raise TypeError("%s: %s must be a device tensor %s" % (func, name, kind))
     _need(x.dim() == 3, func, "%s must be [tokens, heads, head_dim]" % name)
     _need(x.device == device, func, "all tensors must be on one device")
     if x.is_neg():

@@ -21,6 +21,8 @@ the bounds it writes), for code that is traced or compiled; eager callers save t
 dispatch by calling ``kv``'s functions, which come here where a gradient, mode, trace or
 transform asks for it.
 
+``kv_append8``, ``cache_attention`` and ``assign_pages`` of ``cache`` are registered likewise.
+
 HIP graphs: the operator enqueues kernels only, so it can be captured.  Its
 workspace is the per-(device, stream) one of ``ops.gemm``, allocated on first
 use; call the layer once eagerly on the capturing stream before capturing so
@@ -32,7 +34,7 @@ from typing import Optional, Tuple
 
 import torch
 
-from . import kv, ops
+from . import cache, kv, ops
 
 _NS = "marlin_mi355x"
 
@@ -98,6 +100,54 @@ def _select_pages_fake(q, bounds, table, lengths, page_size, select):
     if q.dim() != 3 or bounds.dim() != 4:
         raise ValueError("marlin_mi355x::select_pages: q must be [sequences, heads, head_dim], bounds [pages, kv_heads, 2, head_dim]")
     return (table.new_empty((q.shape[0], bounds.shape[1], select)), lengths.new_empty(lengths.shape))
+
+
+@torch.library.custom_op(_NS + "::kv_append8", mutates_args=("k_cache", "v_cache", "scales"))
+def kv_append8(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor,
+               scales: torch.Tensor, table: torch.Tensor, lengths: torch.Tensor, cos_sin: Optional[torch.Tensor] = None,
+               starts: Optional[torch.Tensor] = None, interleaved: bool = False) -> torch.Tensor:
+    args = q, k, v, k_cache, v_cache, scales, table, lengths, cos_sin, starts, interleaved, None
+    done = (cache._native or cache._connect()).kv_append8(*args)
+    return cache._kv_append8(*args) if done is None else done
+
+
+@kv_append8.register_fake
+def _kv_append8_fake(q, k, v, k_cache, v_cache, scales, table, lengths, cos_sin=None, starts=None, interleaved=False):
+    if q.dim() != 3 or q.dtype not in (torch.float16, torch.bfloat16):
+        raise TypeError("marlin_mi355x::kv_append8: q must be [tokens, heads, head_dim], float16 or bfloat16")
+    return q.new_empty(q.shape)
+
+
+@torch.library.custom_op(_NS + "::cache_attention", mutates_args=())
+def cache_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, table: torch.Tensor, lengths: torch.Tensor,
+                    scales: Optional[torch.Tensor] = None, starts: Optional[torch.Tensor] = None, window: int = 0, sinks: int = 0,
+                    scale: Optional[float] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """(out, lse); window 0: none"""
+    args = q, k_cache, v_cache, table, lengths, scales, starts, window or None, sinks, scale, True, None, None
+    done = (cache._native or cache._connect()).cache_attention(*args)
+    return cache._cache_attention(*args) if done is None else done
+
+
+@cache_attention.register_fake
+def _cache_attention_fake(q, k_cache, v_cache, table, lengths, scales=None, starts=None, window=0, sinks=0, scale=None):
+    if q.dim() != 3 or q.dtype not in (torch.float16, torch.bfloat16):
+        raise TypeError("marlin_mi355x::cache_attention: q must be [tokens, heads, head_dim], float16 or bfloat16")
+    return q.new_empty(q.shape), q.new_empty(q.shape[:2], dtype=torch.float32)
+
+
+@torch.library.custom_op(_NS + "::assign_pages", mutates_args=("table", "lengths", "free", "free_count"))
+def assign_pages(table: torch.Tensor, lengths: torch.Tensor, new: torch.Tensor, free: torch.Tensor, free_count: torch.Tensor,
+                 page_size: int, tokens: int, window: int = 0, sinks: int = 0) -> Tuple[torch.Tensor, torch.Tensor]:
+    args = table, lengths, new, free, free_count, page_size, tokens, window or None, sinks, None
+    done = (cache._native or cache._connect()).assign_pages(*args)
+    return cache._assign_pages(*args) if done is None else done
+
+
+@assign_pages.register_fake
+def _assign_pages_fake(table, lengths, new, free, free_count, page_size, tokens, window=0, sinks=0):
+    if table.dim() != 2 or tokens < 0:
+        raise ValueError("marlin_mi355x::assign_pages: table must be [sequences, width], tokens at least 0")
+    return table.new_empty(table.shape[0] + 1), table.new_empty(tokens, dtype=torch.int64)
 
 
 # What the check below asks of torch, bound once: looking the names up took as
