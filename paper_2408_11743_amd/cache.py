@@ -134,9 +134,11 @@ def _kv_append8(q, k, v, k_cache, v_cache, scales, table, lengths, cos_sin, star
 
 
 def _visible(func: str, window, sinks) -> tuple[int, int]:
-    window = 0 if window is None else operator.index(window)
     sinks = operator.index(sinks)
-    _need(window >= 0, func, "window must be None or at least 1")
+    if window is None:
+        return 0, sinks
+    window = operator.index(window)
+    _need(window >= 1, func, "window must be None or at least 1")
     return window, sinks
 
 

@@ -160,10 +160,11 @@ __device__ __forceinline__ Keys keys_of(const PromptProblem &p, const Tile &t, i
     return k;
 }
 
-// A row's part of what is seen: positions up to `last`, above `above` or below `sinks`.
+// A row's part of what is seen: positions up to `last`, above `above` or below `sinks`.  No branches: what follows from it are
+// selects of elements of MFMA results, and the compiler (ROCm 7.2) drops assignments to those in divergent branches.
 struct Sight {
     int last, above, sinks;
-    __device__ __forceinline__ bool sees(int j) const { return j <= last && (j > above || j < sinks); }
+    __device__ __forceinline__ bool sees(int j) const { return (j <= last) & ((j > above) | (j < sinks)); }
 };
 __device__ __forceinline__ Sight sight_of(const PromptProblem &p, const Tile &t, int row)
 {
@@ -426,9 +427,11 @@ __global__ void __launch_bounds__(64 * kWaves, RT == 1 && D <= 128 ? 2 : 1) prom
 #pragma unroll
                 for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        if (!(k.ok >> (2 * kt + (i >> 3)) & 1) || !sight[rt].sees(pos + key_of(kt, i)) || pos + key_of(kt, i) >= keys.end)
-                            s[rt][kt][i] = -INFINITY;
+                    for (int i = 0; i < 16; ++i) {
+                        const int j = pos + key_of(kt, i);
+                        const bool seen = ((k.ok >> (2 * kt + (i >> 3)) & 1) != 0) & sight[rt].sees(j) & (j < keys.end);
+                        s[rt][kt][i] = seen ? s[rt][kt][i] : -INFINITY;
+                    }
             }
             float top = m[rt];
 #pragma unroll
@@ -485,8 +488,7 @@ __global__ void __launch_bounds__(64 * kWaves, RT == 1 && D <= 128 ? 2 : 1) prom
                         for (int i = 0; i < 16; ++i) {
                             const float x = odd_at<T, Eight>(p.v, at + 32 * ct + 8 * (i >> 2) + (i & 3));
 #pragma unroll
-                            for (int rt = 0; rt < RT; ++rt)
-                                if (sight[rt].sees(j)) acc[rt][ct][i] += x;
+                            for (int rt = 0; rt < RT; ++rt) acc[rt][ct][i] += sight[rt].sees(j) ? x : 0.f;
                         }
                 }
             }
@@ -785,11 +787,17 @@ __global__ void __launch_bounds__(64 * kWaves, D > 128 ? 1 : 2) prompt_few_kerne
                             sc[rt][u][i] = __builtin_fmaf(sc[rt][u][i], cur.factor[u], cur.add[u]);
                         else
                             sc[rt][u][i] *= p.scale_log2;
-                        if (!all) {
-                            const int j = pos + 16 * u + 4 * g + i;
-                            if (!(cur.ok >> u & 1) || !sight[rt].sees(j) || j >= keys.end) sc[rt][u][i] = -INFINITY;
-                        }
                     }
+                if (!all) {
+#pragma unroll
+                    for (int u = 0; u < KT; ++u)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const int j = pos + 16 * u + 4 * g + i;
+                            const bool seen = ((cur.ok >> u & 1) != 0) & sight[rt].sees(j) & (j < keys.end);
+                            sc[rt][u][i] = seen ? sc[rt][u][i] : -INFINITY;
+                        }
+                }
                 float top = m[rt];
 #pragma unroll
                 for (int u = 0; u < KT; ++u)
@@ -844,8 +852,7 @@ __global__ void __launch_bounds__(64 * kWaves, D > 128 ? 1 : 2) prompt_few_kerne
                             for (int i = 0; i < 4; ++i) {
                                 const float x = odd_at<T, Eight>(p.v, at + channel_of(c, 4 * g + i));
 #pragma unroll
-                                for (int rt = 0; rt < RT; ++rt)
-                                    if (sight[rt].sees(j)) acc[rt][c][i] += x;
+                                for (int rt = 0; rt < RT; ++rt) acc[rt][c][i] += sight[rt].sees(j) ? x : 0.f;
                             }
                     }
                 }
