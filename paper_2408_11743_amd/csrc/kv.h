@@ -100,7 +100,8 @@ struct PromptProblem {
     int tokens, B, heads, kv_heads, group;
     int page_shift, width, pages;
     int window, sinks;
-    float scale_log2;
+    float scale_log2;           // |scale| * log2(e), above zero
+    uint32_t q_and, q_xor;      // of two elements of q: the scale's sign, or nothing left where it is zero
     int splits;     // work-groups that may share a tile's keys
     int base;       // the launch's first work-group
     int tiles;      // of all sequences, at most

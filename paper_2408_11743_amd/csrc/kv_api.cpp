@@ -326,7 +326,11 @@ marlin_status_t marlin_cache_attention(const marlin_cache_attention_args *a, hip
         p.pages = (int)a->pages;
         p.window = (int)a->window;
         p.sinks = (int)a->sinks;
-        p.scale_log2 = (float)(a->scale * 1.4426950408889634);
+        // the maximum is taken of the products before they are scaled, by a factor above zero
+        const float scale = (float)(a->scale * 1.4426950408889634), least = 0x1p-126f;
+        p.scale_log2 = std::fabs(scale) > least ? std::fabs(scale) : least;
+        p.q_and = std::fabs(scale) > 0 ? 0xFFFFFFFFu : 0u;
+        p.q_xor = scale < 0 ? 0x80008000u : 0u;
         const PromptPlan plan = plan_prompt(a->tokens, a->B, a->heads, a->kv_heads, (int)a->head_dim);
         return launch_prompt(p, plan, (int)a->head_dim, (marlin_dtype_t)a->dtype, stream) == hipSuccess ? MARLIN_OK : MARLIN_ERR_HIP;
     }

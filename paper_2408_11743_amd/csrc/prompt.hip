@@ -175,12 +175,18 @@ __device__ __forceinline__ Sight sight_of(const PromptProblem &p, const Tile &t,
 
 __device__ __forceinline__ bool is_scale(float s) { return s >= kLeastScale && s <= kMostScale; }
 
-// N tiles of 16 keys of a step: where they lie in the caches (elements); which are there (bits) and, in an 8-bit cache, what their
-// scales make of the scores (times factor, plus add) and of the weights in the sum (times).
-template <int N>
-struct Places {
-    int64_t at[N];
+// N tiles of 16 keys of a step as they are loaded: which have pages (bits) and, in an 8-bit cache, their scales.  What follows
+// from the scales is found when they are used, a step later, so that nothing waits for them.
+template <int N, bool Eight>
+struct Raw {
+    uint32_t named;
 };
+template <int N>
+struct Raw<N, true> {
+    uint32_t named;
+    float ks[N], vs[N];
+};
+// Which tiles are seen at all; and, in an 8-bit cache, factor and summand of their scores and the factor of their weights in the sum.
 template <int N, bool Eight>
 struct Block {
     uint32_t ok;
@@ -205,65 +211,90 @@ __device__ __forceinline__ Entries<N> load_entries(const PromptProblem &p, const
     }
     return x;
 }
-template <int N, bool Eight>
-__device__ __forceinline__ Block<N, Eight> block_of(const PromptProblem &p, const Entries<N> &x, int head, int pos, int D, Places<N> &places)
+// Pages of a kv head before an entry's (0 for an entry that names no page).
+__device__ __forceinline__ int64_t page_head(const PromptProblem &p, int entry, int head)
 {
-    Block<N, Eight> k;
-    k.ok = 0;
+    return (int64_t)((uint32_t)entry < (uint32_t)p.pages ? entry : 0) * p.kv_heads + head;
+}
+// A position's element in the caches.
+__device__ __forceinline__ int64_t place_of(const PromptProblem &p, int entry, int head, int pos, int D)
+{
+    return ((page_head(p, entry, head) << p.page_shift) + (pos & ((1 << p.page_shift) - 1))) * D;
+}
+template <int N, bool Eight>
+__device__ __forceinline__ Raw<N, Eight> raw_of(const PromptProblem &p, const Entries<N> &x, int head, int pos)
+{
+    Raw<N, Eight> k;
+    k.named = 0;
 #pragma unroll
     for (int u = 0; u < N; ++u) {
-        const bool named = (uint32_t)x.e[u] < (uint32_t)p.pages;
-        const int slot = (pos + kTileKeys * u) & ((1 << p.page_shift) - 1);
-        const int64_t page_head = (int64_t)(named ? x.e[u] : 0) * p.kv_heads + head;
-        places.at[u] = ((page_head << p.page_shift) + slot) * D;
-        bool fine = named;
+        k.named |= ((uint32_t)x.e[u] < (uint32_t)p.pages ? 1u : 0u) << u;
         if constexpr (Eight) {
-            const int per_shift = p.page_shift - 4;
-            const float *s = p.scales + ((page_head * 2) << per_shift) + (slot >> 4);
-            const float ks = scalar_load(s), vs = scalar_load(s + (1 << per_shift));
-            fine = named && is_scale(ks) && is_scale(vs);
-            k.factor[u] = fine ? ks * p.scale_log2 : 0.f;
-            k.add[u] = fine ? __builtin_amdgcn_logf(vs) : 0.f;
-            k.times[u] = fine ? __builtin_amdgcn_rcpf(vs) : 0.f;
+            const int per_shift = p.page_shift - 4, slot = (pos + kTileKeys * u) & ((1 << p.page_shift) - 1);
+            const float *s = p.scales + ((page_head(p, x.e[u], head) * 2) << per_shift) + (slot >> 4);
+            k.ks[u] = scalar_load(s);
+            k.vs[u] = scalar_load(s + (1 << per_shift));
         }
-        k.ok |= (fine ? 1u : 0u) << u;
     }
     return k;
 }
-// One of four by arithmetic: a select by a lane's index of a vector's elements goes through memory.
-__device__ __forceinline__ int64_t one_of(int u, int64_t a, int64_t b, int64_t c, int64_t d)
+template <int N, bool Eight>
+__device__ __forceinline__ Block<N, Eight> block_of(const PromptProblem &p, const Raw<N, Eight> &x)
 {
-    const int64_t first = -(int64_t)(u == 0), second = -(int64_t)(u == 1), third = -(int64_t)(u == 2), fourth = -(int64_t)(u == 3);
-    return (a & first) | (b & second) | (c & third) | (d & fourth);
+    Block<N, Eight> k;
+    k.ok = x.named;
+    if constexpr (Eight) {
+#pragma unroll
+        for (int u = 0; u < N; ++u) {
+            const bool fine = is_scale(x.ks[u]) && is_scale(x.vs[u]);
+            if (!fine) k.ok &= ~(1u << u);
+            k.factor[u] = fine ? fmaxf(x.ks[u] * p.scale_log2, 0x1p-126f) : 1.f;
+            k.add[u] = fine ? __builtin_amdgcn_logf(x.vs[u]) : 0.f;
+            k.times[u] = fine ? __builtin_amdgcn_rcpf(x.vs[u]) : 0.f;
+        }
+    }
+    return k;
+}
+// Eight elements of q, of a row that there is: with the scale's sign, or zero where that is zero.
+template <typename V, typename T>
+__device__ __forceinline__ V query_of(const PromptProblem &p, const T *q, bool have)
+{
+    const u32x4_t w = have ? *(const u32x4_t *)q : u32x4_t{};
+    return __builtin_bit_cast(V, (w & p.q_and) ^ p.q_xor);
 }
 
 // ---- many rows: keys and values through LDS ----
 
 constexpr int kStep = 64;
 
-template <typename T, int D, int RT>
+template <int D, int RT>
 constexpr int kWideFloats = 64 * kWaves * 4 * (RT * (D / 32) * 4 + RT);
 
-// RT: 32-row columns of a wave.  K lies in LDS as [key][channel], its 16-byte pieces swapped by the key's last three bits; V^T as
-// [channel][key], each 16 keys in the order 0-3, 8-11, 4-7, 12-15, its pieces swapped by bits of the channel: every read and write is
-// of distinct banks.
+// RT: 32-row columns of a wave.  A wave brings 16 keys of a step, whose page is the same in all lanes, and all waves read all of them.
+// K lies in LDS as [key][channel], V^T as [channel][key] with each 16 keys in the order 0-3, 8-11, 4-7, 12-15, rows 16 bytes further
+// apart than they are long, an odd number of 16-byte pieces: reads are of distinct banks, and at constant distances.  V^T's
+// rows are in an order of their own, eight-channel pieces side by side, so that the writes are of distinct banks too, and a
+// lane's results are whole pieces: row 8 * oct + j of the channels is row j * (D / 8) + oct (96 channels: four-channel pieces, below).
 template <typename T, int D, int RT, bool Eight>
 __global__ void __launch_bounds__(64 * kWaves, RT == 1 && D <= 128 ? 2 : 1) prompt_kernel(const PromptProblem p)
 {
     typedef Elem<T> E;
     typedef typename E::vec8 vec8;
-    constexpr int kRows = 32 * RT * kWaves, kThreads = 64 * kWaves;
-    constexpr int kOct = D / 8;                       // pieces of eight channels of a row
-    constexpr int kKeyRow = (D == 96 ? 128 : D) * 2;  // bytes
-    constexpr int kKeyBytes = kStep * kKeyRow, kValueBytes = D * kStep * 2;
-    constexpr int kKeyPasses = kStep * kOct / kThreads, kQuads = kStep / 4;
-    constexpr int kValuePasses = (kQuads * kOct + kThreads - 1) / kThreads;
-    constexpr int kPiece = Eight ? 2 : 4;  // dwords of eight elements
+    constexpr int kRows = 32 * RT * kWaves;
+    constexpr int kOct = D / 8;                            // eight-channel pieces of a row
+    constexpr int kSize = Eight ? 1 : 2;                   // bytes of an element in the cache
+    constexpr int kKeyRow = D * 2 + 16, kValueRow = kStep * 2 + 16;  // bytes in LDS
+    constexpr int kKeyBytes = kStep * kKeyRow, kBufBytes = kKeyBytes + D * kValueRow;
+    constexpr int kLoad = Eight && D % 64 ? 8 : 16;        // bytes of keys a lane loads at a time
+    constexpr int kElems = kLoad / kSize;                  // elements
+    constexpr int kKeyPasses = 16 * D / kElems / 64;       // of a wave over its 16 keys
+    constexpr int kValueItems = 4 * kOct, kValuePasses = (kValueItems + 63) / 64;  // four keys, eight channels
+    constexpr int kPiece = 2 * kSize;                      // dwords of eight elements in the cache
     constexpr int kCt = D / 32, kC = D / 16;
     constexpr float kUnit = __is_same(T, _Float16) ? 15.f : 0.f;  // log2 of what a weight of 1 is
-    static_assert(kStep * kOct % kThreads == 0, "");
+    static_assert(16 * D % (kElems * 64) == 0, "");
 
-    __shared__ __attribute__((aligned(16))) uint8_t lds[2][kKeyBytes + kValueBytes];
+    __shared__ __attribute__((aligned(16))) uint8_t lds[2 * kBufBytes];
     __shared__ int lds_odd[2][kWaves];
     __shared__ int lds_last;
     static_assert(sizeof(lds) >= kKvMaxBatch / 64 * 4, "");
@@ -273,7 +304,7 @@ __global__ void __launch_bounds__(64 * kWaves, RT == 1 && D <= 128 ? 2 : 1) prom
     const int index = p.base + blockIdx.x;
     const int head = index % p.kv_heads, rest = index / p.kv_heads;
     const int split = rest % p.splits, tile_no = p.tiles - 1 - rest / p.splits;
-    const Tile tile = find_tile(p, kRows, tile_no, lane, wave, (int *)&lds[0][0]);
+    const Tile tile = find_tile(p, kRows, tile_no, lane, wave, (int *)lds);
     if (tile.row0 < 0) return;
     const Keys keys = keys_of(p, tile, kRows, 6);
     int parts = keys.steps / 4;  // work-groups that share the tile, each four steps at the least
@@ -298,70 +329,80 @@ __global__ void __launch_bounds__(64 * kWaves, RT == 1 && D <= 128 ? 2 : 1) prom
         out_at[rt] = have ? (int64_t)token * p.heads + h : -1;
         const T *q = (const T *)p.q + token * p.q_row + h * p.q_head + 8 * half;
 #pragma unroll
-        for (int c = 0; c < kC; ++c) qf[rt][c] = have ? *(const vec8 *)(q + 16 * c) : vec8{};
+        for (int c = 0; c < kC; ++c) qf[rt][c] = query_of<vec8>(p, q + 16 * c, have);
     }
 
-    uint32_t kreg[kKeyPasses][kPiece], vreg[kValuePasses][4][kPiece];
-    auto load_step = [&](const Places<4> &places, uint32_t ok, int pos) {
-        constexpr int kSize = Eight ? 1 : 2;
-        const int64_t a0 = places.at[0], a1 = places.at[1], a2 = places.at[2], a3 = places.at[3];
-#pragma unroll
-        for (int i = 0; i < kKeyPasses; ++i) {
-            const int n = tid + kThreads * i, key = n / kOct, oct = n % kOct;
-            const uint8_t *from = (const uint8_t *)p.k + (one_of(key >> 4, a0, a1, a2, a3) + (key & 15) * D + 8 * oct) * kSize;
-            if (ok >> (key >> 4) & 1) __builtin_memcpy(kreg[i], __builtin_assume_aligned(from, 8 * kSize), 8 * kSize);
-        }
-#pragma unroll
-        for (int i = 0; i < kValuePasses; ++i) {
-            const int n = tid + kThreads * i, quad = n / kOct, oct = n % kOct;
-            const bool have = quad < kQuads && (ok >> (quad >> 2) & 1);
-            const uint8_t *from = (const uint8_t *)p.v + (one_of(quad >> 2, a0, a1, a2, a3) + (quad & 3) * 4 * D + 8 * oct) * kSize;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-#pragma unroll
-                for (int w = 0; w < kPiece; ++w) vreg[i][j][w] = 0;
-                if (have && pos + 4 * quad + j < keys.end)
-                    __builtin_memcpy(vreg[i][j], __builtin_assume_aligned(from + j * D * kSize, 8 * kSize), 8 * kSize);
-            }
-        }
+    // ---- a step's keys and values: this wave's tile of 16 keys, to registers and from there to LDS ----
+    uint32_t kreg[kKeyPasses][kLoad / 4], vreg[kValuePasses][4][kPiece];
+    const uint32_t key_from = lane * kLoad, value_from = ((lane / kOct) * 4 * D + (lane % kOct) * 8) * kSize;
+    // whether every row sees every key of a step, as far as its position says
+    auto within = [&](int pos) {
+        return pos + kStep - 1 <= keys.first && pos + kStep <= keys.end && (!p.window || pos > keys.last - p.window || pos + kStep <= p.sinks);
     };
-    // whether every row sees every key of a step
-    auto whole = [&](uint32_t ok, int pos) {
-        return ok == 15u && pos + kStep - 1 <= keys.first && pos + kStep <= keys.end &&
-               (!p.window || pos > keys.last - p.window || pos + kStep <= p.sinks);
-    };
-    auto store_step = [&](int buf, bool check) {
-        if (check) {
-            uint32_t odd = 0;
+    auto load_step = [&](const Entries<4> &e, int pos) {
+        int entry = wave == 0 ? e.e[0] : wave == 1 ? e.e[1] : wave == 2 ? e.e[2] : e.e[3];
+        entry = __builtin_amdgcn_readfirstlane(entry);
+        if ((uint32_t)entry >= (uint32_t)p.pages) {  // weights of zero want values that are numbers
 #pragma unroll
             for (int i = 0; i < kValuePasses; ++i)
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
 #pragma unroll
+                    for (int w = 0; w < kPiece; ++w) vreg[i][j][w] = 0;
+            return;
+        }
+        const int64_t at = place_of(p, entry, head, pos + kTileKeys * wave, D) * kSize;
+        const uint8_t *const k = (const uint8_t *)p.k + at, *const v = (const uint8_t *)p.v + at;
+#pragma unroll
+        for (int i = 0; i < kKeyPasses; ++i)
+            __builtin_memcpy(kreg[i], __builtin_assume_aligned(k + key_from + i * 64 * kLoad, kLoad), kLoad);
+#pragma unroll
+        for (int i = 0; i < kValuePasses; ++i)
+            if (kValueItems % 64 == 0 || lane + 64 * i < kValueItems) {
+                static_assert(kValuePasses == 1 || 64 % kOct == 0, "");
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    __builtin_memcpy(vreg[i][j], __builtin_assume_aligned(v + value_from + (i * (64 / kOct) * 4 + j) * D * kSize, 8 * kSize), 8 * kSize);
+            }
+    };
+    auto store_step = [&](int buf, int pos, uint32_t ok) {
+        uint8_t *const to_keys = lds + buf * kBufBytes, *const to_values = to_keys + kKeyBytes;
+        if (!(within(pos) && ok == 15u)) {
+            // what no row sees is zero; of the rest what is finite
+            uint32_t odd = 0;
+#pragma unroll
+            for (int i = 0; i < kValuePasses; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const bool seen = pos + kTileKeys * wave + ((lane + 64 * i) / kOct) * 4 + j < keys.end;
+#pragma unroll
                     for (int w = 0; w < kPiece; ++w) {
-                        const uint32_t x = finite_of<T, Eight>(vreg[i][j][w]);
-                        odd |= x ^ vreg[i][j][w];
-                        vreg[i][j][w] = x;
+                        const uint32_t x = seen ? vreg[i][j][w] : 0, y = finite_of<T, Eight>(x);
+                        odd |= x ^ y;
+                        vreg[i][j][w] = y;
                     }
-            const bool any = __any(odd != 0);
+                }
+            const bool any = __any((kValueItems % 64 == 0 || lane < kValueItems) & (odd != 0));
             if (lane == 0) lds_odd[buf][wave] = any;
         }
-        uint8_t *const to_keys = lds[buf], *const to_values = lds[buf] + kKeyBytes;
 #pragma unroll
         for (int i = 0; i < kKeyPasses; ++i) {
-            const int n = tid + kThreads * i, key = n / kOct, oct = n % kOct;
-            vec8 x;
-            if constexpr (Eight)
-                x = E::of_codes(kreg[i][0], kreg[i][1]);
-            else
-                __builtin_memcpy(&x, kreg[i], 16);
-            *(vec8 *)(to_keys + key * kKeyRow + ((oct ^ (key & 7)) * 16)) = x;
+            const int n = (lane + 64 * i) * kElems, key = kTileKeys * wave + n / D, ch = n % D;
+#pragma unroll
+            for (int j = 0; j < kElems / 8; ++j) {
+                vec8 x;
+                if constexpr (Eight)
+                    x = E::of_codes(kreg[i][2 * j], kreg[i][2 * j + 1]);
+                else
+                    __builtin_memcpy(&x, kreg[i], 16);
+                *(vec8 *)(to_keys + key * kKeyRow + (ch + 8 * j) * 2) = x;
+            }
         }
 #pragma unroll
         for (int i = 0; i < kValuePasses; ++i) {
-            const int n = tid + kThreads * i, quad = n / kOct, oct = n % kOct;
-            if (quad < kQuads) {
-                const int chunk = (quad >> 2) * 2 + (quad & 1), upper = (quad >> 1) & 1;
+            if (kValueItems % 64 == 0 || lane + 64 * i < kValueItems) {
+                const int quad = (lane + 64 * i) / kOct, oct = (lane + 64 * i) % kOct;
+                uint8_t *const to = to_values + (2 * wave + (quad & 1)) * 16 + (quad >> 1) * 8;
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     uint32_t w[2];
@@ -373,11 +414,18 @@ __global__ void __launch_bounds__(64 * kWaves, RT == 1 && D <= 128 ? 2 : 1) prom
                         else
                             w[h] = __builtin_amdgcn_perm(vreg[i][2 * h + 1][j >> 1], vreg[i][2 * h][j >> 1], (j & 1) ? 0x07060302u : 0x05040100u);
                     }
-                    const int ch = 8 * oct + j;
-                    __builtin_memcpy(__builtin_assume_aligned(to_values + ch * (kStep * 2) + ((chunk ^ ((ch ^ (ch >> 3)) & 7)) * 16) + upper * 8, 8), w, 8);
+                    // channel 8 oct + j; with 96 of them the fours are side by side, by eight of them
+                    const int four = 2 * oct + (j >> 2), row = D == 96 ? 32 * (four >> 3) + 8 * (j & 3) + (four & 7) : j * kOct + oct;
+                    __builtin_memcpy(__builtin_assume_aligned(to + row * kValueRow, 8), w, 8);
                 }
             }
         }
+    };
+    // the channel of element i of accumulator ct
+    auto channel_of = [&](int ct, int i) {
+        if (D == 96) return 4 * (8 * ct + 4 * half + (i & 3)) + (i >> 2);
+        const int row = 32 * ct + 8 * (i >> 2) + (i & 3);
+        return 8 * (row % kOct) + row / kOct + 32 * half;
     };
 
     float16_t acc[RT][kCt];
@@ -390,54 +438,50 @@ __global__ void __launch_bounds__(64 * kWaves, RT == 1 && D <= 128 ? 2 : 1) prom
         for (int ct = 0; ct < kCt; ++ct) acc[rt][ct] = float16_t{};
     }
 
-    auto value_at = [&](int buf, int ct, int g16) -> vec8 {
-        const int ch = 32 * ct + col;
-        return *(const vec8 *)(lds[buf] + kKeyBytes + ch * (kStep * 2) + (((2 * g16 + half) ^ ((ch ^ (ch >> 3)) & 7)) * 16));
-    };
     auto compute = [&](int buf, const Block<4, Eight> &k, int pos) {
+        const uint8_t *const from_keys = lds + buf * kBufBytes + col * kKeyRow + half * 16;
+        const uint8_t *const from_values = lds + buf * kBufBytes + kKeyBytes + col * kValueRow + half * 16;
         float16_t s[RT][2];
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) s[rt][0] = s[rt][1] = float16_t{};
 #pragma unroll
-        for (int kt = 0; kt < 2; ++kt) {
-            const int key = 32 * kt + col;
+        for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
             for (int c = 0; c < kC; ++c) {
-                const vec8 a = *(const vec8 *)(lds[buf] + key * kKeyRow + (((2 * c + half) ^ (key & 7)) * 16));
+                const vec8 a = *(const vec8 *)(from_keys + 32 * kt * kKeyRow + c * 32);
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt) s[rt][kt] = mfma32(a, qf[rt][c], s[rt][kt]);
             }
-        }
-        const bool all = whole(k.ok, pos);
-        // key of a lane's score i of 32: the tile's, then this
-        auto key_of = [&](int kt, int i) { return 32 * kt + 8 * (i >> 2) + 4 * half + (i & 3); };
+        const bool all = within(pos) && k.ok == 15u;
         vec8 weights[RT][4];
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
-#pragma unroll
-            for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    if constexpr (Eight)
-                        s[rt][kt][i] = __builtin_fmaf(s[rt][kt][i], k.factor[2 * kt + (i >> 3)], k.add[2 * kt + (i >> 3)]);
-                    else
-                        s[rt][kt][i] *= p.scale_log2;
-                }
             if (!all) {
 #pragma unroll
                 for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
-                        const int j = pos + key_of(kt, i);
+                        const int j = pos + 32 * kt + 8 * (i >> 2) + 4 * half + (i & 3);
                         const bool seen = ((k.ok >> (2 * kt + (i >> 3)) & 1) != 0) & sight[rt].sees(j) & (j < keys.end);
                         s[rt][kt][i] = seen ? s[rt][kt][i] : -INFINITY;
                     }
             }
+            // the maximum, of what the factors make of the scores
             float top = m[rt];
+            if constexpr (Eight) {
 #pragma unroll
-            for (int kt = 0; kt < 2; ++kt)
+                for (int g16 = 0; g16 < 4; ++g16) {
+                    float x = s[rt][g16 >> 1][8 * (g16 & 1)];
 #pragma unroll
-                for (int i = 0; i < 16; ++i) top = fmaxf(top, s[rt][kt][i]);
+                    for (int e = 1; e < 8; ++e) x = fmaxf(x, s[rt][g16 >> 1][8 * (g16 & 1) + e]);
+                    top = fmaxf(top, __builtin_fmaf(x, k.factor[g16], k.add[g16]));
+                }
+            } else {
+                float x = s[rt][0][0];
+#pragma unroll
+                for (int e = 1; e < 32; ++e) x = fmaxf(x, s[rt][e >> 4][e & 15]);
+                top = fmaxf(top, x * p.scale_log2);
+            }
             const Pair halves = exchange<32>(top);
             top = fmaxf(halves.a, halves.b);
             const float ref = top == -INFINITY ? 0.f : top;
@@ -450,11 +494,15 @@ __global__ void __launch_bounds__(64 * kWaves, RT == 1 && D <= 128 ? 2 : 1) prom
             m[rt] = top;
 #pragma unroll
             for (int g16 = 0; g16 < 4; ++g16) {
-                float sum = 0.f;
+                float f = p.scale_log2, to_unit = kUnit - ref, sum = 0.f;
+                if constexpr (Eight) {
+                    f = k.factor[g16];
+                    to_unit += k.add[g16];
+                }
 #pragma unroll
                 for (int e = 0; e < 8; e += 2) {
-                    const float x = __builtin_amdgcn_exp2f(s[rt][g16 >> 1][8 * (g16 & 1) + e] - (ref - kUnit));
-                    const float y = __builtin_amdgcn_exp2f(s[rt][g16 >> 1][8 * (g16 & 1) + e + 1] - (ref - kUnit));
+                    const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rt][g16 >> 1][8 * (g16 & 1) + e], f, to_unit));
+                    const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rt][g16 >> 1][8 * (g16 & 1) + e + 1], f, to_unit));
                     sum += x + y;
                     weights[rt][g16][e] = (T)x;
                     weights[rt][g16][e + 1] = (T)y;
@@ -467,7 +515,7 @@ __global__ void __launch_bounds__(64 * kWaves, RT == 1 && D <= 128 ? 2 : 1) prom
         for (int g16 = 0; g16 < 4; ++g16)
 #pragma unroll
             for (int ct = 0; ct < kCt; ++ct) {
-                const vec8 a = value_at(buf, ct, g16);
+                const vec8 a = *(const vec8 *)(from_values + 32 * ct * kValueRow + g16 * 32);
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt) acc[rt][ct] = mfma32(a, weights[rt][g16], acc[rt][ct]);
             }
@@ -480,13 +528,12 @@ __global__ void __launch_bounds__(64 * kWaves, RT == 1 && D <= 128 ? 2 : 1) prom
                 for (int n = 0; n < kStep; ++n) {
                     const int j = pos + n;
                     if (!(k.ok >> (n >> 4) & 1) || j >= keys.end) continue;
-                    const int page = scalar_load(table + (j >> p.page_shift)), slot = j & ((1 << p.page_shift) - 1);
-                    const int64_t at = ((((int64_t)page * p.kv_heads + head) << p.page_shift) + slot) * D + 4 * half;
+                    const int64_t at = place_of(p, scalar_load(table + (j >> p.page_shift)), head, j, D);
 #pragma unroll
                     for (int ct = 0; ct < kCt; ++ct)
 #pragma unroll
                         for (int i = 0; i < 16; ++i) {
-                            const float x = odd_at<T, Eight>(p.v, at + 32 * ct + 8 * (i >> 2) + (i & 3));
+                            const float x = odd_at<T, Eight>(p.v, at + channel_of(ct, i));
 #pragma unroll
                             for (int rt = 0; rt < RT; ++rt) acc[rt][ct][i] += sight[rt].sees(j) ? x : 0.f;
                         }
@@ -496,26 +543,27 @@ __global__ void __launch_bounds__(64 * kWaves, RT == 1 && D <= 128 ? 2 : 1) prom
     };
 
     if (s0 < s1) {
-        Entries<4> entries = load_entries<4>(p, table, position_of(s0), keys.end), ahead{};
-        Places<4> places;
-        Block<4, Eight> block = block_of<4, Eight>(p, entries, head, position_of(s0), D, places);
-        load_step(places, block.ok, position_of(s0));
+        Entries<4> ahead = load_entries<4>(p, table, position_of(s0), keys.end);
+        load_step(ahead, position_of(s0));
+        Block<4, Eight> block = block_of<4, Eight>(p, raw_of<4, Eight>(p, ahead, head, position_of(s0)));
         if (s0 + 1 < s1) ahead = load_entries<4>(p, table, position_of(s0 + 1), keys.end);
-        store_step(0, !whole(block.ok, position_of(s0)));
+        store_step(0, position_of(s0), block.ok);
         int buf = 0;
 #pragma unroll 1
         for (int s = s0; s < s1; ++s) {
-            Block<4, Eight> next = block;
+            Raw<4, Eight> raw;
             const bool more = s + 1 < s1;
             if (more) {
-                next = block_of<4, Eight>(p, ahead, head, position_of(s + 1), D, places);
-                load_step(places, next.ok, position_of(s + 1));
+                load_step(ahead, position_of(s + 1));
+                raw = raw_of<4, Eight>(p, ahead, head, position_of(s + 1));
                 if (s + 2 < s1) ahead = load_entries<4>(p, table, position_of(s + 2), keys.end);
             }
             __syncthreads();
             compute(buf, block, position_of(s));
-            if (more) store_step(buf ^ 1, !whole(next.ok, position_of(s + 1)));
-            block = next;
+            if (more) {
+                block = block_of<4, Eight>(p, raw);
+                store_step(buf ^ 1, position_of(s + 1), block.ok);
+            }
             buf ^= 1;
         }
     }
@@ -529,7 +577,7 @@ __global__ void __launch_bounds__(64 * kWaves, RT == 1 && D <= 128 ? 2 : 1) prom
     if (parts > 1) {
         const int item = tile_no * p.kv_heads + head;
         constexpr int kPer = RT * kCt * 4 + RT;  // 16-byte pieces of a lane
-        float *const slot = p.partials + (int64_t)(item * p.splits + split) * kWideFloats<T, D, RT>;
+        float *const slot = p.partials + (int64_t)(item * p.splits + split) * kWideFloats<D, RT>;
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
 #pragma unroll
@@ -559,7 +607,7 @@ __global__ void __launch_bounds__(64 * kWaves, RT == 1 && D <= 128 ? 2 : 1) prom
         }
 #pragma unroll 1
         for (int k = 0; k < parts; ++k) {
-            const float *const from = p.partials + (int64_t)(item * p.splits + k) * kWideFloats<T, D, RT>;
+            const float *const from = p.partials + (int64_t)(item * p.splits + k) * kWideFloats<D, RT>;
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) {
                 const float4_t ml = load_partial16(from, wave * kPer + RT * kCt * 4 + rt, lane);
@@ -579,21 +627,25 @@ __global__ void __launch_bounds__(64 * kWaves, RT == 1 && D <= 128 ? 2 : 1) prom
         }
     }
 
-    // ---- the finished rows: a lane holds four adjacent channels of every eight ----
+    // ---- the finished rows: a lane holds pieces of eight channels (96: of four) ----
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
         if (out_at[rt] < 0) continue;
         const float inv = 1.f / l[rt];
-        T *const to = (T *)p.out + out_at[rt] * D + 4 * half;
+        T *const to = (T *)p.out + out_at[rt] * D;
+        auto result = [&](int ct, int i) { return l[rt] == 0.f ? (T)0.f : (T)(acc[rt][ct][i] * inv); };
+        constexpr int kPieces = D == 96 ? 12 : D / 16, kChannels = D == 96 ? 4 : 8;  // a lane's
 #pragma unroll
-        for (int ct = 0; ct < kCt; ++ct)
+        for (int n = 0; n < kPieces; ++n) {
+            T y[kChannels];
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                typename E::vec4 y;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) y[i] = l[rt] == 0.f ? (T)0.f : (T)(acc[rt][ct][4 * q + i] * inv);
-                *(typename E::vec4 *)(to + 32 * ct + 8 * q) = y;
+            for (int j = 0; j < kChannels; ++j) {
+                // D = 96: four 8 ct + 4 half + i, its channels in q = j; else piece 8 (n / 4) + 4 half + n % 4, channel j in row j * kOct + piece
+                const int row = j * kOct + 8 * (n >> 2) + (n & 3);
+                y[j] = D == 96 ? result(n >> 2, 4 * j + (n & 3)) : result(row >> 5, 4 * ((row & 31) >> 3) + (n & 3));
             }
+            __builtin_memcpy(__builtin_assume_aligned(to + kChannels * (8 * (n >> 2) + 4 * half + (n & 3)), 2 * kChannels), y, 2 * kChannels);
+        }
         if (p.lse && half == 0) p.lse[out_at[rt]] = (m[rt] + __builtin_amdgcn_logf(l[rt]) - kUnit) * 0.693147180559945f;
     }
 }
@@ -654,15 +706,24 @@ __global__ void __launch_bounds__(64 * kWaves, D > 128 ? 1 : 2) prompt_few_kerne
         out_at[rt] = have ? (int64_t)token * p.heads + h : -1;
         const T *q = (const T *)p.q + token * p.q_row + h * p.q_head;
 #pragma unroll
-        for (int t = 0; t < kQ; ++t)
-            qf[rt][t] = !have ? vec8{} : *(const vec8 *)(Eight && !kBy32 ? q + 16 * g + 64 * (t >> 1) + 8 * (t & 1) : q + 8 * g + 32 * t);
+        for (int t = 0; t < kQ; ++t) qf[rt][t] = query_of<vec8>(p, Eight && !kBy32 ? q + 16 * g + 64 * (t >> 1) + 8 * (t & 1) : q + 8 * g + 32 * t, have);
     }
 
     uint32_t kf[KT][kKeyDw] = {}, vr[KT][4][kHalves][kValueDw] = {};
-    auto load_keys = [&](const Places<KT> &k, uint32_t ok) {
+    struct Places {
+        int64_t at[KT];
+    };
+    auto places_of = [&](const Entries<KT> &x, int pos) {
+        Places k;
+#pragma unroll
+        for (int u = 0; u < KT; ++u) k.at[u] = place_of(p, x.e[u], head, pos + kTileKeys * u, D);
+        return k;
+    };
+    // of tiles without a page the registers keep what they hold, which is masked
+    auto load_keys = [&](const Places &k, uint32_t named) {
 #pragma unroll
         for (int u = 0; u < KT; ++u) {
-            if (!(ok >> u & 1)) continue;
+            if (!(named >> u & 1)) continue;
             if constexpr (!Eight) {
                 const T *from = (const T *)p.k + k.at[u] + (r * D + 8 * g);
 #pragma unroll
@@ -676,10 +737,10 @@ __global__ void __launch_bounds__(64 * kWaves, D > 128 ? 1 : 2) prompt_few_kerne
             }
         }
     };
-    auto load_values = [&](const Places<KT> &k, uint32_t ok) {
+    auto load_values = [&](const Places &k, uint32_t named) {
 #pragma unroll
         for (int u = 0; u < KT; ++u) {
-            if (!(ok >> u & 1)) continue;
+            if (!(named >> u & 1)) continue;
             if constexpr (!Eight) {
                 const T *v = (const T *)p.v + k.at[u] + (4 * g * D + kCh * r);
 #pragma unroll
@@ -730,10 +791,11 @@ __global__ void __launch_bounds__(64 * kWaves, D > 128 ? 1 : 2) prompt_few_kerne
 
     int s = s0 + wave;
     if (s < s1) {
-        Places<KT> places;
-        Block<KT, Eight> cur = block_of<KT, Eight>(p, load_entries<KT>(p, table, position_of(s), keys.end), head, position_of(s), D, places), next = cur;
-        load_keys(places, cur.ok);
-        load_values(places, cur.ok);
+        const Entries<KT> first = load_entries<KT>(p, table, position_of(s), keys.end);
+        Raw<KT, Eight> raw = raw_of<KT, Eight>(p, first, head, position_of(s)), next = raw;
+        Places places = places_of(first, position_of(s));
+        load_keys(places, raw.named);
+        load_values(places, raw.named);
         Entries<KT> ahead{};
         if (s + kWaves < s1) ahead = load_entries<KT>(p, table, position_of(s + kWaves), keys.end);
 #pragma unroll 1
@@ -758,10 +820,12 @@ __global__ void __launch_bounds__(64 * kWaves, D > 128 ? 1 : 2) prompt_few_kerne
             const bool more = s + kWaves < s1;
             issue_order_point();
             if (more) {
-                next = block_of<KT, Eight>(p, ahead, head, position_of(s + kWaves), D, places);
-                load_keys(places, next.ok);
+                next = raw_of<KT, Eight>(p, ahead, head, position_of(s + kWaves));
+                places = places_of(ahead, position_of(s + kWaves));
+                load_keys(places, next.named);
                 if (s + 2 * kWaves < s1) ahead = load_entries<KT>(p, table, position_of(s + 2 * kWaves), keys.end);
             }
+            const Block<KT, Eight> cur = block_of<KT, Eight>(p, raw);
             const bool all = cur.ok == 3u && pos + kKeys - 1 <= keys.first && pos + kKeys <= keys.end &&
                              (!p.window || pos > keys.last - p.window || pos + kKeys <= p.sinks);
             if (!all) {  // what no row sees: zero
@@ -844,8 +908,7 @@ __global__ void __launch_bounds__(64 * kWaves, D > 128 ? 1 : 2) prompt_few_kerne
                     for (int n = 0; n < kKeys; ++n) {
                         const int j = pos + n;
                         if (!(cur.ok >> (n >> 4) & 1) || j >= keys.end) continue;
-                        const int page = scalar_load(table + (j >> p.page_shift)), slot = j & ((1 << p.page_shift) - 1);
-                        const int64_t at = ((((int64_t)page * p.kv_heads + head) << p.page_shift) + slot) * D;
+                        const int64_t at = place_of(p, scalar_load(table + (j >> p.page_shift)), head, j, D);
 #pragma unroll
                         for (int c = 0; c < kAcc; ++c)
 #pragma unroll
@@ -867,8 +930,8 @@ __global__ void __launch_bounds__(64 * kWaves, D > 128 ? 1 : 2) prompt_few_kerne
                 }
             issue_order_point();
             if (!more) break;
-            load_values(places, next.ok);
-            cur = next;
+            load_values(places, next.named);
+            raw = next;
             s += kWaves;
         }
     }
