@@ -284,7 +284,7 @@ __global__ void __launch_bounds__(64 * kWaves, RT == 1 && D <= 128 ? 2 : 1) prom
     constexpr int kOct = D / 8;                            // eight-channel pieces of a row
     constexpr int kSize = Eight ? 1 : 2;                   // bytes of an element in the cache
     constexpr int kKeyRow = D * 2 + 16, kValueRow = kStep * 2 + 16;  // bytes in LDS
-    constexpr int kKeyBytes = kStep * kKeyRow, kBufBytes = kKeyBytes + D * kValueRow;
+    constexpr int kKeyBytes = kStep * kKeyRow, kValueBytes = D * kValueRow;
     constexpr int kLoad = Eight && D % 64 ? 8 : 16;        // bytes of keys a lane loads at a time
     constexpr int kElems = kLoad / kSize;                  // elements
     constexpr int kKeyPasses = 16 * D / kElems / 64;       // of a wave over its 16 keys
@@ -294,8 +294,14 @@ __global__ void __launch_bounds__(64 * kWaves, RT == 1 && D <= 128 ? 2 : 1) prom
     constexpr float kUnit = __is_same(T, _Float16) ? 15.f : 0.f;  // log2 of what a weight of 1 is
     static_assert(16 * D % (kElems * 64) == 0, "");
 
-    __shared__ __attribute__((aligned(16))) uint8_t lds[2 * kBufBytes];
-    __shared__ int lds_odd[2][kWaves];
+    __shared__ __attribute__((aligned(16))) uint8_t lds[2 * (kKeyBytes + kValueBytes)];
+    // of a step's four tiles, kept for four steps: whether there is one, whether its values are not all finite, and what its scales
+    // make of scores (factor, then add) and of weights in the sum (times)
+    struct Info {
+        int ok[kWaves], odd[kWaves];
+        float factor[kWaves], add[kWaves], times[kWaves];
+    };
+    __shared__ Info lds_info[4];
     __shared__ int lds_last;
     static_assert(sizeof(lds) >= kKvMaxBatch / 64 * 4, "");
 
@@ -333,29 +339,48 @@ __global__ void __launch_bounds__(64 * kWaves, RT == 1 && D <= 128 ? 2 : 1) prom
     }
 
     // ---- a step's keys and values: this wave's tile of 16 keys, to registers and from there to LDS ----
+    // Keys are a step ahead of values: while a step's weights are found and its values summed up, the next one's scores are.
     uint32_t kreg[kKeyPasses][kLoad / 4], vreg[kValuePasses][4][kPiece];
     const uint32_t key_from = lane * kLoad, value_from = ((lane / kOct) * 4 * D + (lane % kOct) * 8) * kSize;
     // whether every row sees every key of a step, as far as its position says
     auto within = [&](int pos) {
         return pos + kStep - 1 <= keys.first && pos + kStep <= keys.end && (!p.window || pos > keys.last - p.window || pos + kStep <= p.sinks);
     };
-    auto load_step = [&](const Entries<4> &e, int pos) {
-        int entry = wave == 0 ? e.e[0] : wave == 1 ? e.e[1] : wave == 2 ? e.e[2] : e.e[3];
+    // this wave's tile of a step: its page's entry, where it lies (bytes), whether there is one, its scales
+    struct Mine {
+        int64_t at;
+        bool named;
+        float ks, vs;
+    };
+    auto entry_of = [&](int s) {
+        const int pos = position_of(s) + kTileKeys * wave;
+        int e = -1;
+        if (s < s1 && pos < keys.end) e = scalar_load(table + (pos >> p.page_shift));
+        return e;
+    };
+    auto load_keys = [&](int s, int entry) {
+        Mine x;
         entry = __builtin_amdgcn_readfirstlane(entry);
-        if ((uint32_t)entry >= (uint32_t)p.pages) {  // weights of zero want values that are numbers
-#pragma unroll
-            for (int i = 0; i < kValuePasses; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-#pragma unroll
-                    for (int w = 0; w < kPiece; ++w) vreg[i][j][w] = 0;
-            return;
+        x.named = (uint32_t)entry < (uint32_t)p.pages;
+        const int pos = position_of(s) + kTileKeys * wave;
+        x.at = place_of(p, entry, head, pos, D) * kSize;
+        if constexpr (Eight) {
+            const int per_shift = p.page_shift - 4, slot = pos & ((1 << p.page_shift) - 1);
+            const float *scale = p.scales + ((page_head(p, entry, head) * 2) << per_shift) + (slot >> 4);
+            x.ks = scalar_load(scale);
+            x.vs = scalar_load(scale + (1 << per_shift));
         }
-        const int64_t at = place_of(p, entry, head, pos + kTileKeys * wave, D) * kSize;
-        const uint8_t *const k = (const uint8_t *)p.k + at, *const v = (const uint8_t *)p.v + at;
+        if (x.named) {
+            const uint8_t *const k = (const uint8_t *)p.k + x.at;
 #pragma unroll
-        for (int i = 0; i < kKeyPasses; ++i)
-            __builtin_memcpy(kreg[i], __builtin_assume_aligned(k + key_from + i * 64 * kLoad, kLoad), kLoad);
+            for (int i = 0; i < kKeyPasses; ++i)
+                __builtin_memcpy(kreg[i], __builtin_assume_aligned(k + key_from + i * 64 * kLoad, kLoad), kLoad);
+        }
+        return x;
+    };
+    auto load_values = [&](const Mine &x) {
+        if (!x.named) return;
+        const uint8_t *const v = (const uint8_t *)p.v + x.at;
 #pragma unroll
         for (int i = 0; i < kValuePasses; ++i)
             if (kValueItems % 64 == 0 || lane + 64 * i < kValueItems) {
@@ -365,39 +390,57 @@ __global__ void __launch_bounds__(64 * kWaves, RT == 1 && D <= 128 ? 2 : 1) prom
                     __builtin_memcpy(vreg[i][j], __builtin_assume_aligned(v + value_from + (i * (64 / kOct) * 4 + j) * D * kSize, 8 * kSize), 8 * kSize);
             }
     };
-    auto store_step = [&](int buf, int pos, uint32_t ok) {
-        uint8_t *const to_keys = lds + buf * kBufBytes, *const to_values = to_keys + kKeyBytes;
-        if (!(within(pos) && ok == 15u)) {
-            // what no row sees is zero; of the rest what is finite
-            uint32_t odd = 0;
-#pragma unroll
-            for (int i = 0; i < kValuePasses; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const bool seen = pos + kTileKeys * wave + ((lane + 64 * i) / kOct) * 4 + j < keys.end;
-#pragma unroll
-                    for (int w = 0; w < kPiece; ++w) {
-                        const uint32_t x = seen ? vreg[i][j][w] : 0, y = finite_of<T, Eight>(x);
-                        odd |= x ^ y;
-                        vreg[i][j][w] = y;
-                    }
-                }
-            const bool any = __any((kValueItems % 64 == 0 || lane < kValueItems) & (odd != 0));
-            if (lane == 0) lds_odd[buf][wave] = any;
+    auto is_fine = [&](const Mine &x) {
+        if constexpr (Eight) return x.named && is_scale(x.ks) && is_scale(x.vs);
+        return x.named;
+    };
+    auto store_keys = [&](int s, const Mine &x) {
+        uint8_t *const to = lds + (s & 1) * kKeyBytes;
+        const bool fine = is_fine(x);
+        if (lane == 0) {
+            Info &info = lds_info[s & 3];
+            info.ok[wave] = fine;
+            if constexpr (Eight) {
+                info.factor[wave] = fine ? fmaxf(x.ks * p.scale_log2, 0x1p-126f) : 1.f;
+                info.add[wave] = fine ? __builtin_amdgcn_logf(x.vs) : 0.f;
+                info.times[wave] = fine ? __builtin_amdgcn_rcpf(x.vs) : 0.f;
+            }
         }
 #pragma unroll
         for (int i = 0; i < kKeyPasses; ++i) {
             const int n = (lane + 64 * i) * kElems, key = kTileKeys * wave + n / D, ch = n % D;
 #pragma unroll
             for (int j = 0; j < kElems / 8; ++j) {
-                vec8 x;
+                vec8 y;
                 if constexpr (Eight)
-                    x = E::of_codes(kreg[i][2 * j], kreg[i][2 * j + 1]);
+                    y = E::of_codes(kreg[i][2 * j], kreg[i][2 * j + 1]);
                 else
-                    __builtin_memcpy(&x, kreg[i], 16);
-                *(vec8 *)(to_keys + key * kKeyRow + (ch + 8 * j) * 2) = x;
+                    __builtin_memcpy(&y, kreg[i], 16);
+                *(vec8 *)(to + key * kKeyRow + (ch + 8 * j) * 2) = y;
             }
         }
+    };
+    auto store_values = [&](int s, const Mine &x) {
+        const int pos = position_of(s);
+        if (!(within(pos) && is_fine(x))) {
+            // what no row sees is zero; of the rest what is finite
+            uint32_t odd = 0;
+#pragma unroll
+            for (int i = 0; i < kValuePasses; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const bool seen = x.named & (pos + kTileKeys * wave + ((lane + 64 * i) / kOct) * 4 + j < keys.end);
+#pragma unroll
+                    for (int w = 0; w < kPiece; ++w) {
+                        const uint32_t y = seen ? vreg[i][j][w] : 0, z = finite_of<T, Eight>(y);
+                        odd |= y ^ z;
+                        vreg[i][j][w] = z;
+                    }
+                }
+            const bool any = __any((kValueItems % 64 == 0 || lane < kValueItems) & (odd != 0));
+            if (lane == 0) lds_info[s & 3].odd[wave] = any;
+        }
+        uint8_t *const to_values = lds + 2 * kKeyBytes + (s & 1) * kValueBytes;
 #pragma unroll
         for (int i = 0; i < kValuePasses; ++i) {
             if (kValueItems % 64 == 0 || lane + 64 * i < kValueItems) {
@@ -438,134 +481,173 @@ __global__ void __launch_bounds__(64 * kWaves, RT == 1 && D <= 128 ? 2 : 1) prom
         for (int ct = 0; ct < kCt; ++ct) acc[rt][ct] = float16_t{};
     }
 
-    auto compute = [&](int buf, const Block<4, Eight> &k, int pos) {
-        const uint8_t *const from_keys = lds + buf * kBufBytes + col * kKeyRow + half * 16;
-        const uint8_t *const from_values = lds + buf * kBufBytes + kKeyBytes + col * kValueRow + half * 16;
-        float16_t s[RT][2];
+    typedef float16_t scores_t[RT][2];
+    const uint32_t key_at = col * kKeyRow + half * 16, value_at = 2 * kKeyBytes + col * kValueRow + half * 16;
+    auto score = [&](int s, scores_t &x) {
+        const uint8_t *const from = lds + (s & 1) * kKeyBytes + key_at;
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt) s[rt][0] = s[rt][1] = float16_t{};
+        for (int rt = 0; rt < RT; ++rt) x[rt][0] = x[rt][1] = float16_t{};
 #pragma unroll
-        for (int kt = 0; kt < 2; ++kt)
+        for (int c = 0; c < kC; ++c)
 #pragma unroll
-            for (int c = 0; c < kC; ++c) {
-                const vec8 a = *(const vec8 *)(from_keys + 32 * kt * kKeyRow + c * 32);
+            for (int kt = 0; kt < 2; ++kt) {
+                const vec8 a = *(const vec8 *)(from + 32 * kt * kKeyRow + c * 32);
 #pragma unroll
-                for (int rt = 0; rt < RT; ++rt) s[rt][kt] = mfma32(a, qf[rt][c], s[rt][kt]);
+                for (int rt = 0; rt < RT; ++rt) x[rt][kt] = mfma32(a, qf[rt][c], x[rt][kt]);
             }
-        const bool all = within(pos) && k.ok == 15u;
-        vec8 weights[RT][4];
+    };
+    // which of a step's tiles are there
+    auto ok_of = [&](int s) { return (uint32_t)__builtin_amdgcn_ballot_w64(lds_info[s & 3].ok[lane & 3] != 0) & 15u; };
+    // scores that are not seen, then the maximum (of what the factors make of them) with the sums brought to it
+    auto look = [&](int s, scores_t &x, float (&top)[RT]) {
+        const int pos = position_of(s);
+        const uint32_t ok = ok_of(s);
+        if (!(within(pos) && ok == 15u)) {
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt) {
-            if (!all) {
+            for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
                 for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
                         const int j = pos + 32 * kt + 8 * (i >> 2) + 4 * half + (i & 3);
-                        const bool seen = ((k.ok >> (2 * kt + (i >> 3)) & 1) != 0) & sight[rt].sees(j) & (j < keys.end);
-                        s[rt][kt][i] = seen ? s[rt][kt][i] : -INFINITY;
+                        const bool seen = ((ok >> (2 * kt + (i >> 3)) & 1) != 0) & sight[rt].sees(j) & (j < keys.end);
+                        x[rt][kt][i] = seen ? x[rt][kt][i] : -INFINITY;
                     }
-            }
-            // the maximum, of what the factors make of the scores
-            float top = m[rt];
+        }
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            float t = m[rt];
             if constexpr (Eight) {
+                const Info &info = lds_info[s & 3];
 #pragma unroll
                 for (int g16 = 0; g16 < 4; ++g16) {
-                    float x = s[rt][g16 >> 1][8 * (g16 & 1)];
+                    float y = x[rt][g16 >> 1][8 * (g16 & 1)];
 #pragma unroll
-                    for (int e = 1; e < 8; ++e) x = fmaxf(x, s[rt][g16 >> 1][8 * (g16 & 1) + e]);
-                    top = fmaxf(top, __builtin_fmaf(x, k.factor[g16], k.add[g16]));
+                    for (int e = 1; e < 8; ++e) y = fmaxf(y, x[rt][g16 >> 1][8 * (g16 & 1) + e]);
+                    t = fmaxf(t, __builtin_fmaf(y, info.factor[g16], info.add[g16]));
                 }
             } else {
-                float x = s[rt][0][0];
+                float y = x[rt][0][0];
 #pragma unroll
-                for (int e = 1; e < 32; ++e) x = fmaxf(x, s[rt][e >> 4][e & 15]);
-                top = fmaxf(top, x * p.scale_log2);
+                for (int e = 1; e < 32; ++e) y = fmaxf(y, x[rt][e >> 4][e & 15]);
+                t = fmaxf(t, y * p.scale_log2);
             }
-            const Pair halves = exchange<32>(top);
-            top = fmaxf(halves.a, halves.b);
-            const float ref = top == -INFINITY ? 0.f : top;
-            if (__any(top > m[rt])) {
-                const float keep = __builtin_amdgcn_exp2f(m[rt] - ref);
+            const Pair halves = exchange<32>(t);
+            top[rt] = fmaxf(halves.a, halves.b);
+        }
+    };
+    auto rescale = [&](const float (&top)[RT]) {
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            if (__any(top[rt] > m[rt])) {
+                const float keep = __builtin_amdgcn_exp2f(m[rt] - (top[rt] == -INFINITY ? 0.f : top[rt]));
                 l[rt] *= keep;
 #pragma unroll
                 for (int ct = 0; ct < kCt; ++ct) acc[rt][ct] *= keep;
             }
-            m[rt] = top;
+            m[rt] = top[rt];
+        }
+    };
+    auto weigh = [&](int s, const scores_t &x, vec8 (&weights)[RT][4]) {
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            const float unit = kUnit - (m[rt] == -INFINITY ? 0.f : m[rt]);
 #pragma unroll
             for (int g16 = 0; g16 < 4; ++g16) {
-                float f = p.scale_log2, to_unit = kUnit - ref, sum = 0.f;
+                float f = p.scale_log2, add = unit, sum = 0.f;
                 if constexpr (Eight) {
-                    f = k.factor[g16];
-                    to_unit += k.add[g16];
+                    f = lds_info[s & 3].factor[g16];
+                    add += lds_info[s & 3].add[g16];
                 }
 #pragma unroll
                 for (int e = 0; e < 8; e += 2) {
-                    const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rt][g16 >> 1][8 * (g16 & 1) + e], f, to_unit));
-                    const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rt][g16 >> 1][8 * (g16 & 1) + e + 1], f, to_unit));
-                    sum += x + y;
-                    weights[rt][g16][e] = (T)x;
-                    weights[rt][g16][e + 1] = (T)y;
+                    const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(x[rt][g16 >> 1][8 * (g16 & 1) + e], f, add));
+                    const float z = __builtin_amdgcn_exp2f(__builtin_fmaf(x[rt][g16 >> 1][8 * (g16 & 1) + e + 1], f, add));
+                    sum += y + z;
+                    weights[rt][g16][e] = (T)y;
+                    weights[rt][g16][e + 1] = (T)z;
                 }
-                if constexpr (Eight) sum *= k.times[g16];
+                if constexpr (Eight) sum *= lds_info[s & 3].times[g16];
                 l[rt] += sum;
             }
         }
+    };
+    auto add_values = [&](int s, const vec8 (&weights)[RT][4]) {
+        const uint8_t *const from = lds + (s & 1) * kValueBytes + value_at;
 #pragma unroll
         for (int g16 = 0; g16 < 4; ++g16)
 #pragma unroll
             for (int ct = 0; ct < kCt; ++ct) {
-                const vec8 a = *(const vec8 *)(from_values + 32 * ct * kValueRow + g16 * 32);
+                const vec8 a = *(const vec8 *)(from + 32 * ct * kValueRow + g16 * 32);
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt) acc[rt][ct] = mfma32(a, weights[rt][g16], acc[rt][ct]);
             }
-        if (!all) {
-            int odd = 0;
-#pragma unroll
-            for (int w = 0; w < kWaves; ++w) odd |= lds_odd[buf][w];
-            if (__builtin_amdgcn_readfirstlane(odd)) {
+    };
+    // values of a step that are not finite, where some rows do not see all keys
+    auto add_odd = [&](int s) {
+        const int pos = position_of(s);
+        const uint32_t ok = ok_of(s);
+        if (within(pos) && ok == 15u) return;
+        // a wave whose tile every row sees has not looked
+        uint32_t odd = (uint32_t)__builtin_amdgcn_ballot_w64(lds_info[s & 3].odd[lane & 3] != 0) & 15u;
+        if (within(pos)) odd &= ~ok;
+        if (odd == 0) return;
 #pragma unroll 1
-                for (int n = 0; n < kStep; ++n) {
-                    const int j = pos + n;
-                    if (!(k.ok >> (n >> 4) & 1) || j >= keys.end) continue;
-                    const int64_t at = place_of(p, scalar_load(table + (j >> p.page_shift)), head, j, D);
+        for (int n = 0; n < kStep; ++n) {
+            const int j = pos + n;
+            if (!(ok >> (n >> 4) & 1) || j >= keys.end) continue;
+            const int64_t at = place_of(p, scalar_load(table + (j >> p.page_shift)), head, j, D);
 #pragma unroll
-                    for (int ct = 0; ct < kCt; ++ct)
+            for (int ct = 0; ct < kCt; ++ct)
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            const float x = odd_at<T, Eight>(p.v, at + channel_of(ct, i));
+                for (int i = 0; i < 16; ++i) {
+                    const float x = odd_at<T, Eight>(p.v, at + channel_of(ct, i));
 #pragma unroll
-                            for (int rt = 0; rt < RT; ++rt) acc[rt][ct][i] += sight[rt].sees(j) ? x : 0.f;
-                        }
+                    for (int rt = 0; rt < RT; ++rt) acc[rt][ct][i] += sight[rt].sees(j) ? x : 0.f;
                 }
-            }
         }
     };
 
     if (s0 < s1) {
-        Entries<4> ahead = load_entries<4>(p, table, position_of(s0), keys.end);
-        load_step(ahead, position_of(s0));
-        Block<4, Eight> block = block_of<4, Eight>(p, raw_of<4, Eight>(p, ahead, head, position_of(s0)));
-        if (s0 + 1 < s1) ahead = load_entries<4>(p, table, position_of(s0 + 1), keys.end);
-        store_step(0, position_of(s0), block.ok);
-        int buf = 0;
+        scores_t x, ahead;
+        vec8 weights[RT][4];
+        float top[RT];
+        int entry = entry_of(s0 + 1);
+        Mine values = load_keys(s0, entry_of(s0)), next = values;  // of the step whose values are to come next; of the one after it
+        store_keys(s0, values);
+        load_values(values);
+        next = load_keys(s0 + 1, entry);
+        entry = entry_of(s0 + 2);
+        __syncthreads();
+        score(s0, x);
+        look(s0, x, top);
+        rescale(top);
+        store_values(s0, values);
+        store_keys(s0 + 1, next);
 #pragma unroll 1
-        for (int s = s0; s < s1; ++s) {
-            Raw<4, Eight> raw;
-            const bool more = s + 1 < s1;
-            if (more) {
-                load_step(ahead, position_of(s + 1));
-                raw = raw_of<4, Eight>(p, ahead, head, position_of(s + 1));
-                if (s + 2 < s1) ahead = load_entries<4>(p, table, position_of(s + 2), keys.end);
-            }
+        for (int s = s0; s + 1 < s1; ++s) {
             __syncthreads();
-            compute(buf, block, position_of(s));
-            if (more) {
-                block = block_of<4, Eight>(p, raw);
-                store_step(buf ^ 1, position_of(s + 1), block.ok);
-            }
-            buf ^= 1;
+            values = next;
+            load_values(values);
+            next = load_keys(s + 2, entry);
+            entry = entry_of(s + 3);
+            score(s + 1, ahead);
+            weigh(s, x, weights);
+            add_values(s, weights);
+            look(s + 1, ahead, top);
+            add_odd(s);
+            rescale(top);
+            store_values(s + 1, values);
+            store_keys(s + 2, next);
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                for (int kt = 0; kt < 2; ++kt) x[rt][kt] = ahead[rt][kt];
         }
+        __syncthreads();
+        weigh(s1 - 1, x, weights);
+        add_values(s1 - 1, weights);
+        add_odd(s1 - 1);
     }
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
