@@ -96,23 +96,25 @@ struct PromptProblem {
     void *out;
     float *lse;
     float *partials;
-    uint32_t *counters;
+    void *records;
     int tokens, B, heads, kv_heads, group;
     int page_shift, width, pages;
     int window, sinks;
     float scale_log2;           // |scale| * log2(e), above zero
     uint32_t q_and, q_xor;      // of two elements of q: the scale's sign, or nothing left where it is zero
-    int splits;     // work-groups that may share a tile's keys
+    int target;     // work-groups to split the keys for; 0: a tile is one's
     int base;       // the launch's first work-group
-    int tiles;      // of all sequences, at most
 };
 
-// How a call of these sizes is split: rows of a tile, tiles at most, work-groups a tile, workspace floats a work-group.
+// How a call of these sizes is split: rows of a tile, work-groups to split the keys for (or 0) and at the most, workspace floats of one.
 struct PromptPlan {
     bool few;  // the kernel for few rows a sequence
-    int rows, tiles, splits, slot_floats;
+    int rows, target, slot_floats;
+    int64_t groups;
 };
-PromptPlan plan_prompt(int64_t tokens, int64_t B, int64_t heads, int64_t kv_heads, int head_dim);
+// positions: of a table's row, at most.
+PromptPlan plan_prompt(int64_t tokens, int64_t B, int64_t heads, int64_t kv_heads, int head_dim, int64_t positions);
+size_t prompt_workspace(const PromptPlan &plan);  // bytes behind the counters
 
 hipError_t launch_prompt(const PromptProblem &p, const PromptPlan &plan, int head_dim, marlin_dtype_t dtype, hipStream_t stream);
 

@@ -45,7 +45,8 @@ bool scores_ok(int64_t B, int64_t kv_heads, int64_t width)
     return width <= (1 << 29) && (width + 63) / 64 * B * kv_heads <= (1 << 23);
 }
 
-constexpr int64_t kMaxTokens = 1 << 24;  // of a call
+constexpr int64_t kMaxTokens = 1 << 24;     // of a call
+constexpr int64_t kMaxPositions = 1 << 30;  // of a table's row
 
 // Rows of a kv head: new tokens by the heads that share it.
 bool rows_of_tokens_ok(int64_t tokens, int64_t heads, int64_t kv_heads)
@@ -271,9 +272,7 @@ size_t marlin_cache_attention_workspace_bytes(int64_t starts, int64_t tokens, in
 {
     if (!shape_ok(B, heads, kv_heads, head_dim, 1, 16, 1) || !rows_of_tokens_ok(tokens, heads, kv_heads)) return 0;
     if (!starts) return marlin_paged_attention_workspace_bytes(head_dim);
-    const PromptPlan plan = plan_prompt(tokens, B, heads, kv_heads, (int)head_dim);
-    const size_t slots = plan.splits > 1 ? (size_t)plan.tiles * (size_t)kv_heads * (size_t)plan.splits : 0;
-    return kCounterRegionBytes + slots * (size_t)plan.slot_floats * sizeof(float);
+    return kCounterRegionBytes + prompt_workspace(plan_prompt(tokens, B, heads, kv_heads, (int)head_dim, kMaxPositions));
 }
 
 marlin_status_t marlin_cache_attention(const marlin_cache_attention_args *a, hipStream_t stream)
@@ -314,7 +313,6 @@ marlin_status_t marlin_cache_attention(const marlin_cache_attention_args *a, hip
         p.starts = a->starts;
         p.out = a->out;
         p.lse = a->lse;
-        p.counters = (uint32_t *)a->workspace;
         p.partials = (float *)((char *)a->workspace + kCounterRegionBytes);
         p.tokens = (int)a->tokens;
         p.B = (int)a->B;
@@ -331,7 +329,7 @@ marlin_status_t marlin_cache_attention(const marlin_cache_attention_args *a, hip
         p.scale_log2 = std::fabs(scale) > least ? std::fabs(scale) : least;
         p.q_and = std::fabs(scale) > 0 ? 0xFFFFFFFFu : 0u;
         p.q_xor = scale < 0 ? 0x80008000u : 0u;
-        const PromptPlan plan = plan_prompt(a->tokens, a->B, a->heads, a->kv_heads, (int)a->head_dim);
+        const PromptPlan plan = plan_prompt(a->tokens, a->B, a->heads, a->kv_heads, (int)a->head_dim, a->width * a->page_size);
         return launch_prompt(p, plan, (int)a->head_dim, (marlin_dtype_t)a->dtype, stream) == hipSuccess ? MARLIN_OK : MARLIN_ERR_HIP;
     }
     int device = 0;

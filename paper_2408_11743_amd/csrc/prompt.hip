@@ -14,8 +14,8 @@
 // is laid out in the order in which the lanes hold the keys.
 //
 // The tiles of a call are numbered from the sequences' starts on the device; a work-group finds its tile by
-// scans, the longest of a sequence first.  Where there are few tiles, several work-groups share a tile's
-// keys and leave partial results in the workspace, which the last to arrive joins in order.
+// scans, the longest of a sequence first.  Where there are few tiles, their keys are split into parts of one length, a work-group
+// each, which leave partial results in the workspace; a second launch joins those in order.
 //
 // Weights go to the second product rounded once to the cache's type (float16's times 2^15, so that
 // they are no subnormals until 2^-29 of the maximum, and lost below 2^-40): an error of half a step of each weight, as the output's own,
@@ -34,6 +34,12 @@ using namespace dev;
 typedef float float16_t __attribute__((ext_vector_type(16)));
 
 constexpr int kWaves = 4;
+
+// Work-groups that a call's keys are split for where there are fewer tiles: of many rows two a compute unit, as many as it holds; of
+// few rows it holds three, and tiles' last parts, which are not whole ones, come on top (32 sequences of up to 8000 tokens, four new
+// ones each, 8 bits, 32 heads over 8: 41.7 us, for 768 work-groups 48, for 1024 47).
+constexpr int kWideGroups = 512, kFewGroups = 640;
+constexpr int kWideLeast = 4, kFewLeast = 4 * kWaves;  // steps of a part
 
 __device__ __forceinline__ float16_t mfma32(Elem<_Float16>::vec8 a, Elem<_Float16>::vec8 b, float16_t c)
 {
@@ -72,78 +78,19 @@ __device__ __forceinline__ float odd_at(const void *cache, int64_t at)
     return __builtin_fabsf(x) < INFINITY ? 0.f : x;
 }
 
-// A tile of rows: tokens from + row / group of a sequence.
-struct Tile {
-    int b, from, tokens, start;  // sequence, its first row of q, its new tokens, the first one's position
-    int row0;                    // the tile's first row; -1: there is no such tile
-};
-
-// The mine-th tile of `rows` rows of the sequences, by a work-group: found among the sums of 64 sequences' tiles, then among theirs.
-__device__ __forceinline__ Tile find_tile(const PromptProblem &p, int rows, int mine, int lane, int wave, int *lds_chunks)
-{
-    const int chunks = (p.B + 63) / 64;
-    int begin = 0, count = 0, length = 0, tiles = 0, incl = 0;
-    auto hold = [&](int chunk) {
-        const int b = chunk * 64 + lane;
-        begin = count = length = tiles = 0;
-        if (b < p.B) {
-            begin = p.starts[b];
-            int end = p.starts[b + 1];
-            begin = begin < 0 ? 0 : begin < p.tokens ? begin : p.tokens;
-            end = end < begin ? begin : end < p.tokens ? end : p.tokens;
-            count = end - begin;
-            length = p.lengths[b];
-            if (length < 0) length = 0;
-            tiles = (int)(((int64_t)count * p.group + rows - 1) / rows);
-        }
-        incl = wave_scan(tiles);
-    };
-    int chunk = 0, before = 0;
-    Tile x{0, 0, 0, 0, -1};
-    if (chunks == 1) {
-        hold(0);
-    } else {
-        for (int c = wave; c < chunks; c += kWaves) {
-            hold(c);
-            if (lane == 63) lds_chunks[c] = incl;
-        }
-        __syncthreads();
-        chunk = -1;
-        for (int c0 = 0; c0 < chunks && chunk < 0; c0 += 64) {
-            const int c = c0 + lane < chunks ? lds_chunks[c0 + lane] : 0, i = wave_scan(c);
-            const uint64_t past = __builtin_amdgcn_ballot_w64(before + i > mine);
-            const int at = past ? __builtin_ctzll(past) : 63;
-            if (past) chunk = c0 + at;
-            before += __builtin_amdgcn_readlane(i, at) - (past ? __builtin_amdgcn_readlane(c, at) : 0);
-        }
-        if (chunk < 0) return x;
-        hold(chunk);
-    }
-    const uint64_t past = __builtin_amdgcn_ballot_w64(before + incl > mine);
-    if (!past) return x;
-    const int at = __builtin_ctzll(past);
-    x.b = chunk * 64 + at;
-    x.from = __builtin_amdgcn_readlane(begin, at);
-    x.tokens = __builtin_amdgcn_readlane(count, at);
-    x.start = __builtin_amdgcn_readlane(length, at) - x.tokens;
-    x.row0 = (mine - before - (__builtin_amdgcn_readlane(incl, at) - __builtin_amdgcn_readlane(tiles, at))) * rows;
-    return x;
-}
-
 // The keys that a tile's rows see, in steps of 2^shift: [0, sinks) and [low, end), of which steps the first sink_steps and those
 // from skip further on.
 struct Keys {
     int first, last;  // the rows' first and last position
     int end, low, sinks, sink_steps, skip, steps;
 };
-__device__ __forceinline__ Keys keys_of(const PromptProblem &p, const Tile &t, int rows, int shift)
+__device__ __forceinline__ Keys keys_of(const PromptProblem &p, int start, int tokens, int row0, int rows, int shift)
 {
     Keys k;
-    const int64_t all_rows = (int64_t)t.tokens * p.group;
-    const int last_row = (int)(t.row0 + rows < all_rows ? t.row0 + rows : all_rows) - 1;
+    const int all_rows = tokens * p.group, last_row = (row0 + rows < all_rows ? row0 + rows : all_rows) - 1;
     const int cap = p.width << p.page_shift, up = (1 << shift) - 1;
-    k.first = t.start + t.row0 / p.group;
-    k.last = t.start + last_row / p.group;
+    k.first = start + row0 / p.group;
+    k.last = start + last_row / p.group;
     k.end = k.last + 1 < cap ? k.last + 1 : cap;
     if (k.end < 0) k.end = 0;
     k.low = k.sinks = 0;
@@ -160,15 +107,124 @@ __device__ __forceinline__ Keys keys_of(const PromptProblem &p, const Tile &t, i
     return k;
 }
 
+// What a work-group did, for those that join the pieces of tiles whose keys were split: pieces first, first + p.kv_heads ..
+struct Record {
+    int parts, part, first;  // parts 0: nothing
+    int row0, from, tokens;
+};
+__device__ __forceinline__ Record *record_of(const PromptProblem &p, int index) { return (Record *)p.records + index; }
+
+// What is the same in all lanes, in scalar registers (quotients come from vector ones).
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ Keys uniform(const Keys &k)
+{
+    return {uniform(k.first), uniform(k.last), uniform(k.end), uniform(k.low), uniform(k.sinks), uniform(k.sink_steps), uniform(k.skip), uniform(k.steps)};
+}
+
+// What a work-group does: a tile of rows (tokens from + row / group of a sequence), and which part of its keys.
+struct Work {
+    int b, from, tokens, start;  // sequence, its first row of q, its new tokens, the first one's position
+    int row0;                    // the tile's first row; -1: nothing
+    int part, chunk;             // steps chunk * part .. of the tile's keys
+    int first;                   // the work-group of the tile's first part; the others' are p.kv_heads apart
+};
+
+// The work of one of a kv head's work-groups, found from the sequences' starts and lengths: tiles of `rows` rows, the last of a
+// sequence first, as it sees the most, in parts of `chunk` steps of 2^shift keys, which is what all tiles' steps make for each of p.target work-groups
+// (where there are as many tiles as that, a part is all of a tile).
+// 64 sequences are held in the lanes; of more, the waves share the sums.
+__device__ __forceinline__ Work find_work(const PromptProblem &p, int rows, int shift, int least, int index, int lane, int wave, int *lds_chunks)
+{
+    const int chunks = (p.B + 63) / 64, head = uniform(index % p.kv_heads), mine = uniform(index / p.kv_heads);
+    int held = -1, begin = 0, count = 0, length = 0, tiles = 0, steps = 0;
+    auto hold = [&](int at) {
+        if (at == held) return;
+        held = at;
+        const int b = at * 64 + lane;
+        begin = count = length = tiles = steps = 0;
+        if (b < p.B) {
+            begin = p.starts[b];
+            int end = p.starts[b + 1];
+            begin = begin < 0 ? 0 : begin < p.tokens ? begin : p.tokens;
+            end = end < begin ? begin : end < p.tokens ? end : p.tokens;
+            count = end - begin;
+            length = p.lengths[b];
+            if (length < 0) length = 0;
+            tiles = (count * p.group + rows - 1) / rows;
+            if (p.target > 0 && tiles > 0) steps = keys_of(p, length - count, count, (tiles - 1) * rows, rows, shift).steps;
+        }
+    };
+    // steps of a part: float sums, in the same order in every work-group
+    int chunk = 1 << 30;
+    if (p.target > 0) {
+        float total = 0.f;
+        for (int at = chunks == 1 ? 0 : wave; at < chunks; at += chunks == 1 ? 1 : kWaves) {
+            hold(at);
+            float x = (float)tiles * (float)steps;
+#pragma unroll
+            for (int d = 32; d > 0; d >>= 1) x += __shfl_xor(x, d);
+            total += x;
+        }
+        if (chunks > 1) {
+            if (lane == 0) lds_chunks[wave] = __builtin_bit_cast(int, total);
+            __syncthreads();
+            total = 0.f;
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) total += __builtin_bit_cast(float, lds_chunks[w]);
+            __syncthreads();
+        }
+        const float each = total * (float)p.kv_heads / (float)p.target;
+        chunk = each < 1e9f ? (int)each + 1 : 1 << 30;
+        if (chunk < least) chunk = least;
+        chunk = __builtin_amdgcn_readfirstlane(chunk);
+    }
+    auto parts_of = [&](int n) { return n <= chunk ? 1 : (n + chunk - 1) / chunk; };
+    int at_chunk = 0, before = 0;
+    Work x{0, 0, 0, 0, -1, 0, chunk, 0};
+    if (chunks == 1) {
+        hold(0);
+    } else {
+        for (int at = wave; at < chunks; at += kWaves) {
+            hold(at);
+            const int sum = wave_scan(tiles * parts_of(steps));
+            if (lane == 63) lds_chunks[at] = sum;
+        }
+        __syncthreads();
+        at_chunk = -1;
+        for (int c0 = 0; c0 < chunks && at_chunk < 0; c0 += 64) {
+            const int c = c0 + lane < chunks ? lds_chunks[c0 + lane] : 0, i = wave_scan(c);
+            const uint64_t past = __builtin_amdgcn_ballot_w64(before + i > mine);
+            const int at = past ? __builtin_ctzll(past) : 63;
+            if (past) at_chunk = c0 + at;
+            before += __builtin_amdgcn_readlane(i, at) - (past ? __builtin_amdgcn_readlane(c, at) : 0);
+        }
+        if (at_chunk < 0) return x;
+        hold(at_chunk);
+    }
+    const int parts = parts_of(steps), items = tiles * parts, incl = wave_scan(items);
+    const uint64_t past = __builtin_amdgcn_ballot_w64(before + incl > mine);
+    if (!past) return x;
+    const int at = __builtin_ctzll(past);
+    const int n = __builtin_amdgcn_readlane(parts, at), local = mine - before - (__builtin_amdgcn_readlane(incl, at) - __builtin_amdgcn_readlane(items, at));
+    x.b = at_chunk * 64 + at;
+    x.from = __builtin_amdgcn_readlane(begin, at);
+    x.tokens = __builtin_amdgcn_readlane(count, at);
+    x.start = __builtin_amdgcn_readlane(length, at) - x.tokens;
+    x.part = uniform(local % n);
+    x.row0 = uniform((__builtin_amdgcn_readlane(tiles, at) - 1 - local / n) * rows);
+    x.first = uniform((mine - x.part) * p.kv_heads + head);
+    return x;
+}
+
 // A row's part of what is seen: positions up to `last`, above `above` or below `sinks`.  No branches: what follows from it are
 // selects of elements of MFMA results, and the compiler (ROCm 7.2) drops assignments to those in divergent branches.
 struct Sight {
     int last, above, sinks;
     __device__ __forceinline__ bool sees(int j) const { return (j <= last) & ((j > above) | (j < sinks)); }
 };
-__device__ __forceinline__ Sight sight_of(const PromptProblem &p, const Tile &t, int row)
+__device__ __forceinline__ Sight sight_of(const PromptProblem &p, const Work &t, int row)
 {
-    const bool have = row < (int64_t)t.tokens * p.group;
+    const bool have = row < t.tokens * p.group;
     const int pos = have ? t.start + row / p.group : -1;
     return {pos, p.window ? pos - p.window : -1, p.sinks};
 }
@@ -302,21 +358,20 @@ __global__ void __launch_bounds__(64 * kWaves, RT == 1 && D <= 128 ? 2 : 1) prom
         float factor[kWaves], add[kWaves], times[kWaves];
     };
     __shared__ Info lds_info[4];
-    __shared__ int lds_last;
     static_assert(sizeof(lds) >= kKvMaxBatch / 64 * 4, "");
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 31, half = lane >> 5;
     const int index = p.base + blockIdx.x;
-    const int head = index % p.kv_heads, rest = index / p.kv_heads;
-    const int split = rest % p.splits, tile_no = p.tiles - 1 - rest / p.splits;
-    const Tile tile = find_tile(p, kRows, tile_no, lane, wave, (int *)lds);
+    const int head = uniform(index % p.kv_heads);
+    const Work tile = find_work(p, kRows, 6, kWideLeast, index, lane, wave, (int *)lds);
+    if (p.target > 0 && tid == 0) record_of(p, index)->parts = 0;
     if (tile.row0 < 0) return;
-    const Keys keys = keys_of(p, tile, kRows, 6);
-    int parts = keys.steps / 4;  // work-groups that share the tile, each four steps at the least
-    parts = parts < 1 ? 1 : parts < p.splits ? parts : p.splits;
-    if (split >= parts) return;
-    const int s0 = (int)((int64_t)keys.steps * split / parts), s1 = (int)((int64_t)keys.steps * (split + 1) / parts);
+    const Keys keys = uniform(keys_of(p, tile.start, tile.tokens, tile.row0, kRows, 6));
+    const int parts = uniform(keys.steps <= tile.chunk ? 1 : (keys.steps + tile.chunk - 1) / tile.chunk);  // work-groups that share the tile
+    if (tile.part >= parts) return;
+    if (parts > 1 && tid == 0) *record_of(p, index) = {parts, tile.part, tile.first, tile.row0, tile.from, tile.tokens};
+    const int s0 = uniform((int)((int64_t)keys.steps * tile.part / parts)), s1 = uniform((int)((int64_t)keys.steps * (tile.part + 1) / parts));
     __syncthreads();
 
     const int32_t *const table = p.table + (int64_t)tile.b * p.table_row;
@@ -330,7 +385,7 @@ __global__ void __launch_bounds__(64 * kWaves, RT == 1 && D <= 128 ? 2 : 1) prom
     for (int rt = 0; rt < RT; ++rt) {
         const int row = tile.row0 + (wave * RT + rt) * 32 + col;
         sight[rt] = sight_of(p, tile, row);
-        const bool have = row < (int64_t)tile.tokens * p.group;
+        const bool have = row < tile.tokens * p.group;
         const int token = tile.from + (have ? row / p.group : 0), h = head * p.group + (have ? row % p.group : 0);
         out_at[rt] = have ? (int64_t)token * p.heads + h : -1;
         const T *q = (const T *)p.q + token * p.q_row + h * p.q_head + 8 * half;
@@ -655,58 +710,21 @@ __global__ void __launch_bounds__(64 * kWaves, RT == 1 && D <= 128 ? 2 : 1) prom
         l[rt] = halves.a + halves.b;
     }
 
-    // ---- pieces of a tile's keys ----
+    // ---- a part of the tile's keys: left for the joining kernel ----
     if (parts > 1) {
-        const int item = tile_no * p.kv_heads + head;
-        constexpr int kPer = RT * kCt * 4 + RT;  // 16-byte pieces of a lane
-        float *const slot = p.partials + (int64_t)(item * p.splits + split) * kWideFloats<D, RT>;
+        float4_t *const slot = (float4_t *)(p.partials + (int64_t)index * kWideFloats<D, RT>) + lane;
+        constexpr int kPer = RT * (kCt * 4 + 1);  // blocks of 64 float4 of a wave
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
 #pragma unroll
             for (int ct = 0; ct < kCt; ++ct)
 #pragma unroll
                 for (int q = 0; q < 4; ++q)
-                    store_partial16(slot, wave * kPer + (rt * kCt + ct) * 4 + q, lane,
-                                    float4_t{acc[rt][ct][4 * q], acc[rt][ct][4 * q + 1], acc[rt][ct][4 * q + 2], acc[rt][ct][4 * q + 3]});
-            store_partial16(slot, wave * kPer + RT * kCt * 4 + rt, lane, float4_t{m[rt], l[rt], 0.f, 0.f});
+                    slot[(wave * kPer + rt * (kCt * 4 + 1) + ct * 4 + q) * 64] =
+                        float4_t{acc[rt][ct][4 * q], acc[rt][ct][4 * q + 1], acc[rt][ct][4 * q + 2], acc[rt][ct][4 * q + 3]};
+            slot[(wave * kPer + rt * (kCt * 4 + 1) + kCt * 4) * 64] = float4_t{m[rt], l[rt], 0.f, 0.f};
         }
-        wait_vmcnt<0>();
-        __syncthreads();
-        if (tid == 0) {
-            uint32_t *const ctr = p.counters + kCounterStride * item;
-            const bool done = __hip_atomic_fetch_add(ctr, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)(parts - 1);
-            if (done) __hip_atomic_store(ctr, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            lds_last = done;
-        }
-        __syncthreads();
-        if (!__builtin_amdgcn_readfirstlane(lds_last)) return;
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt) {
-            m[rt] = -INFINITY;
-            l[rt] = 0.f;
-#pragma unroll
-            for (int ct = 0; ct < kCt; ++ct) acc[rt][ct] = float16_t{};
-        }
-#pragma unroll 1
-        for (int k = 0; k < parts; ++k) {
-            const float *const from = p.partials + (int64_t)(item * p.splits + k) * kWideFloats<D, RT>;
-#pragma unroll
-            for (int rt = 0; rt < RT; ++rt) {
-                const float4_t ml = load_partial16(from, wave * kPer + RT * kCt * 4 + rt, lane);
-                const float top = fmaxf(m[rt], ml[0]), ref = top == -INFINITY ? 0.f : top;
-                const float f = __builtin_amdgcn_exp2f(m[rt] - ref), f2 = __builtin_amdgcn_exp2f(ml[0] - ref);
-                m[rt] = top;
-                l[rt] = l[rt] * f + ml[1] * f2;
-#pragma unroll
-                for (int ct = 0; ct < kCt; ++ct)
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        const float4_t x = load_partial16(from, wave * kPer + (rt * kCt + ct) * 4 + q, lane);
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) acc[rt][ct][4 * q + i] = acc[rt][ct][4 * q + i] * f + x[i] * f2;
-                    }
-            }
-        }
+        return;
     }
 
     // ---- the finished rows: a lane holds pieces of eight channels (96: of four) ----
@@ -734,8 +752,8 @@ __global__ void __launch_bounds__(64 * kWaves, RT == 1 && D <= 128 ? 2 : 1) prom
 
 // ---- few rows: keys and values straight to registers, the waves share the keys ----
 
-template <typename T, int D, int RT>
-constexpr int kFewFloats = RT * (kHeadTile * D + 2 * kHeadTile);
+template <int D, int RT>
+constexpr int kFewFloats = 64 * 4 * RT * (D / 16 + 1);
 
 // RT: 16-row columns of the tile.  A wave takes steps of 32 keys as the kernel of one token per sequence does (attend.hip), with the
 // rows for its heads.
@@ -753,25 +771,24 @@ __global__ void __launch_bounds__(64 * kWaves, D > 128 ? 1 : 2) prompt_few_kerne
     constexpr int kKeyDw = Eight ? D / 16 : kQ * 4;
     constexpr int kAcc = D / 16;
     constexpr float kUnit = __is_same(T, _Float16) ? 15.f : 0.f;
-    constexpr int kSlot = kFewFloats<T, D, RT>;
+    constexpr int kSlot = kFewFloats<D, RT>;
 
     __shared__ float4_t lds_acc[kWaves][kAcc][64];
     __shared__ float lds_m[kWaves][kHeadTile], lds_l[kWaves][kHeadTile];
-    __shared__ int lds_last;
     static_assert(sizeof(lds_acc) >= kKvMaxBatch / 64 * 4, "");
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int r = lane & 15, g = lane >> 4;
     const int index = p.base + blockIdx.x;
-    const int head = index % p.kv_heads, rest = index / p.kv_heads;
-    const int split = rest % p.splits, tile_no = p.tiles - 1 - rest / p.splits;
-    const Tile tile = find_tile(p, kRows, tile_no, lane, wave, (int *)&lds_acc[0][0][0]);
+    const int head = uniform(index % p.kv_heads);
+    const Work tile = find_work(p, kRows, 5, kFewLeast, index, lane, wave, (int *)&lds_acc[0][0][0]);
+    if (p.target > 0 && tid == 0) record_of(p, index)->parts = 0;
     if (tile.row0 < 0) return;
-    const Keys keys = keys_of(p, tile, kRows, 5);
-    int parts = keys.steps / (4 * kWaves);  // each wave four steps at the least
-    parts = parts < 1 ? 1 : parts < p.splits ? parts : p.splits;
-    if (split >= parts) return;
-    const int s0 = (int)((int64_t)keys.steps * split / parts), s1 = (int)((int64_t)keys.steps * (split + 1) / parts);
+    const Keys keys = uniform(keys_of(p, tile.start, tile.tokens, tile.row0, kRows, 5));
+    const int parts = uniform(keys.steps <= tile.chunk ? 1 : (keys.steps + tile.chunk - 1) / tile.chunk);  // work-groups that share the tile
+    if (tile.part >= parts) return;
+    if (parts > 1 && tid == 0) *record_of(p, index) = {parts, tile.part, tile.first, tile.row0, tile.from, tile.tokens};
+    const int s0 = uniform((int)((int64_t)keys.steps * tile.part / parts)), s1 = uniform((int)((int64_t)keys.steps * (tile.part + 1) / parts));
     __syncthreads();
 
     const int32_t *const table = p.table + (int64_t)tile.b * p.table_row;
@@ -783,7 +800,7 @@ __global__ void __launch_bounds__(64 * kWaves, D > 128 ? 1 : 2) prompt_few_kerne
     for (int rt = 0; rt < RT; ++rt) {
         const int row = tile.row0 + rt * 16 + r;
         sight[rt] = sight_of(p, tile, row);
-        const bool have = row < (int64_t)tile.tokens * p.group;
+        const bool have = row < tile.tokens * p.group;
         const int token = tile.from + (have ? row / p.group : 0), h = head * p.group + (have ? row % p.group : 0);
         out_at[rt] = have ? (int64_t)token * p.heads + h : -1;
         const T *q = (const T *)p.q + token * p.q_row + h * p.q_head;
@@ -1018,18 +1035,8 @@ __global__ void __launch_bounds__(64 * kWaves, D > 128 ? 1 : 2) prompt_few_kerne
         }
     }
 
-    // ---- the waves' pieces, then the work-groups' ----
-    const int item = tile_no * p.kv_heads + head;
-    float *const slot = p.partials + (int64_t)(item * p.splits + split) * kSlot;
-    auto write = [&](int rt, int j, float4_t o, float top, float sum) {
-        if (out_at[rt] < 0) return;
-        const float inv = 1.f / sum;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            ((T *)p.out)[out_at[rt] * D + channel_of(j, 4 * g + i)] = sum == 0.f ? (T)0.f : (T)(o[i] * inv);
-        }
-        if (p.lse && g == 0 && j == 0) p.lse[out_at[rt]] = (top + __builtin_amdgcn_logf(sum) - kUnit) * 0.693147180559945f;
-    };
+    // ---- the waves' pieces; a part of the tile's keys is left for the joining kernel ----
+    float *const slot = p.partials + (int64_t)index * kSlot;
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
         __syncthreads();
@@ -1050,73 +1057,164 @@ __global__ void __launch_bounds__(64 * kWaves, D > 128 ? 1 : 2) prompt_few_kerne
             f[w] = __builtin_amdgcn_exp2f(lds_m[w][r] - ref);
             sum += lds_l[w][r] * f[w];
         }
+        const float inv = 1.f / sum;
 #pragma unroll 1
         for (int j = wave; j < kAcc; j += kWaves) {
             float4_t o{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int w = 0; w < kWaves; ++w) o += lds_acc[w][j][lane] * f[w];
-            if (parts == 1) {
-                write(rt, j, o, top, sum);
-            } else {
-                store_partial16(slot, rt * kAcc + j, lane, o);
-                if (j == 0 && g == 0) {
-                    store_float(slot + RT * kHeadTile * D + rt * 2 * kHeadTile + r, top);
-                    store_float(slot + RT * kHeadTile * D + rt * 2 * kHeadTile + kHeadTile + r, sum);
-                }
+            if (parts > 1) {
+                ((float4_t *)slot)[(rt * (kAcc + 1) + j) * 64 + lane] = o;
+                if (j == 0) ((float4_t *)slot)[(rt * (kAcc + 1) + kAcc) * 64 + lane] = float4_t{top, sum, 0.f, 0.f};
+                continue;
             }
-        }
-    }
-    if (parts == 1) return;
-    wait_vmcnt<0>();
-    __syncthreads();
-    if (tid == 0) {
-        uint32_t *const ctr = p.counters + kCounterStride * item;
-        const bool done = __hip_atomic_fetch_add(ctr, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)(parts - 1);
-        if (done) __hip_atomic_store(ctr, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        lds_last = done;
-    }
-    __syncthreads();
-    if (!__builtin_amdgcn_readfirstlane(lds_last)) return;
-    const float *const slots = p.partials + (int64_t)item * p.splits * kSlot;
-    const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc((void *)slots, (short)0, 0x7fffffffu, kBufferFlags);
-#pragma unroll 1
-    for (int n = wave; n < RT * kAcc; n += kWaves) {
-        const int rt = n / kAcc, j = n - rt * kAcc;
-        float top = -INFINITY, sum = 0.f;
-        float4_t o{0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-        for (int k = 0; k < parts; ++k) {
-            const int at = k * kSlot * 4, ml = (RT * kHeadTile * D + rt * 2 * kHeadTile + r) * 4;
-            const float m2 = load_slot4(rsrc, at, ml), l2 = load_slot4(rsrc, at, ml + kHeadTile * 4);
-            const float4_t x = load_slot16(rsrc, at, n * 1024 + lane * 16);
-            const float t = fmaxf(top, m2), ref = t == -INFINITY ? 0.f : t;
-            const float f = __builtin_amdgcn_exp2f(top - ref), f2 = __builtin_amdgcn_exp2f(m2 - ref);
-            top = t;
-            sum = sum * f + l2 * f2;
-            o = o * f + x * f2;
-        }
+            if (out_at[rt] < 0) continue;
 #pragma unroll
-        for (int i = 0; i < RT; ++i)
-            if (i == rt) write(i, j, o, top, sum);
+            for (int i = 0; i < 4; ++i) ((T *)p.out)[out_at[rt] * D + channel_of(j, 4 * g + i)] = sum == 0.f ? (T)0.f : (T)(o[i] * inv);
+            if (p.lse && g == 0 && j == 0) p.lse[out_at[rt]] = (top + __builtin_amdgcn_logf(sum) - kUnit) * 0.693147180559945f;
+        }
     }
 }
 
-constexpr int kWideGroups = 512, kFewGroups = 1024;  // work-groups that share a call's keys
+// ---- pieces of tiles whose keys were split ----
+
+// A piece is blocks of 64 float4, kBlocks of a lane's results and one of its row's maximum and sum, RT times of each wave.  The
+// work-groups that made a tile's pieces join a share of its blocks each: few pieces a wave a block, in order; of many
+// the waves take some each, in order, and are added up in LDS.  So the pieces of any number are read side by side, and the
+// same bits come of them every time.
+template <typename T, int D, int RT, bool Few, bool Eight>
+__global__ void __launch_bounds__(64 * kWaves) prompt_join_kernel(const PromptProblem p)
+{
+    constexpr int kBlocks = Few ? D / 16 : D / 8;  // of a wave's rows
+    constexpr int kAll = (Few ? 1 : kWaves) * RT * kBlocks;
+    constexpr int kFloats = Few ? kFewFloats<D, RT> : kWideFloats<D, RT>;
+    constexpr int kHalves = D > 128 && !Eight ? 2 : 1, kCh = D / 16 / kHalves, kOct = D / 8;
+    constexpr float kUnit = __is_same(T, _Float16) ? 15.f : 0.f;
+    __shared__ float4_t lds_o[kWaves][64];
+    __shared__ float lds_top[kWaves][64], lds_sum[kWaves][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int index = p.base + blockIdx.x, head = uniform(index % p.kv_heads);
+    const Record x = *record_of(p, index);
+    const int parts = uniform(x.parts), part = uniform(x.part);
+    if (parts == 0) return;
+    const float4_t *const pieces = (const float4_t *)(p.partials + (int64_t)x.first * kFloats) + lane;
+    const int64_t stride = (int64_t)p.kv_heads * kFloats / 4;
+    const int from = kAll * part / parts, to = kAll * (part + 1) / parts;
+    // pieces k0, k0 + step .. of a block: their results added up, brought to their maximum; eight under way together
+    struct Joined {
+        float top, sum;
+        float4_t y;
+    };
+    auto join = [&](const float4_t *ml, const float4_t *o, int k0, int step) {
+        Joined x{-INFINITY, 0.f, float4_t{0.f, 0.f, 0.f, 0.f}};
+        constexpr int kAhead = 8;
+#pragma unroll 1
+        for (int k = k0; k < parts; k += kAhead * step) {
+            float4_t v[kAhead], z[kAhead];
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                const bool have = k + i * step < parts;  // or the first again, without a weight
+                const int64_t at = (have ? k + i * step : k) * stride;
+                v[i] = ml[at];
+                z[i] = o[at];
+                v[i][0] = have ? v[i][0] : -INFINITY;
+            }
+            float top = x.top;
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) top = fmaxf(top, v[i][0]);
+            const float ref = top == -INFINITY ? 0.f : top, keep = __builtin_amdgcn_exp2f(x.top - ref);
+            x.top = top;
+            x.sum *= keep;
+            x.y *= keep;
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                const float f = __builtin_amdgcn_exp2f(v[i][0] - ref);
+                x.sum += v[i][1] * f;
+                x.y += z[i] * f;
+            }
+        }
+        return x;
+    };
+    auto write = [&](int group, int j, float top, float sum, float4_t y) {
+        const int row = x.row0 + (Few ? group * 16 + (lane & 15) : group * 32 + (lane & 31));
+        if (row >= x.tokens * p.group) return;
+        const int64_t at = (int64_t)(x.from + row / p.group) * p.heads + head * p.group + row % p.group;
+        const float inv = 1.f / sum;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            int ch;
+            if constexpr (Few) {
+                const int c = 4 * (lane >> 4) + i;
+                ch = Eight && D % 64 ? (j < 4 ? 4 * c + j : 60 + 2 * c + j) : 128 * (j / kCh) + kCh * c + j % kCh;
+            } else {
+                const int r = 32 * (j >> 2) + 8 * (j & 3) + 4 * (lane >> 5) + i;
+                ch = D == 96 ? 4 * (8 * (j >> 2) + 4 * (lane >> 5) + i) + (j & 3) : 8 * (r % kOct) + r / kOct;
+            }
+            ((T *)p.out)[at * D + ch] = sum == 0.f ? (T)0.f : (T)(y[i] * inv);
+        }
+        if (p.lse && j == 0 && (Few ? lane < 16 : lane < 32)) p.lse[at] = (top + __builtin_amdgcn_logf(sum) - kUnit) * 0.693147180559945f;
+    };
+    constexpr int kFewPieces = 16;
+    if (parts <= kFewPieces) {
+#pragma unroll 1
+        for (int n = from + wave; n < to; n += kWaves) {
+            const int group = n / kBlocks, j = n - group * kBlocks;  // of rows, and the block
+            const float4_t *const ml = pieces + (group * (kBlocks + 1) + kBlocks) * 64, *const o = pieces + (group * (kBlocks + 1) + j) * 64;
+            const Joined a = join(ml, o, 0, 1);
+            write(group, j, a.top, a.sum, a.y);
+        }
+        return;
+    }
+#pragma unroll 1
+    for (int n = from; n < to; ++n) {
+        const int group = n / kBlocks, j = n - group * kBlocks;
+        const float4_t *const ml = pieces + (group * (kBlocks + 1) + kBlocks) * 64, *const o = pieces + (group * (kBlocks + 1) + j) * 64;
+        const Joined a = join(ml, o, wave, kWaves);
+        __syncthreads();  // of the last block's readers
+        lds_top[wave][lane] = a.top;
+        lds_sum[wave][lane] = a.sum;
+        lds_o[wave][lane] = a.y;
+        __syncthreads();
+        if (wave != n % kWaves) continue;
+        float top = -INFINITY, sum = 0.f;
+        float4_t y{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) top = fmaxf(top, lds_top[w][lane]);
+        const float ref = top == -INFINITY ? 0.f : top;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            const float f = __builtin_amdgcn_exp2f(lds_top[w][lane] - ref);
+            sum += lds_sum[w][lane] * f;
+            y += lds_o[w][lane] * f;
+        }
+        write(group, j, top, sum, y);
+    }
+}
 
 template <typename T, int D, bool Eight>
 hipError_t launch_one(const PromptProblem &p, const PromptPlan &plan, hipStream_t stream)
 {
     PromptProblem q = p;
-    q.tiles = plan.tiles;
-    q.splits = plan.splits;
-    const void *kernel = (const void *)(plan.few ? (plan.rows == 16 ? &prompt_few_kernel<T, D, 1, Eight> : &prompt_few_kernel<T, D, 2, Eight>)
-                                                 : &prompt_kernel<T, D, 1, Eight>);
-    const int64_t all = (int64_t)plan.tiles * p.kv_heads * plan.splits, most = ((int64_t)1 << 24) / p.kv_heads * p.kv_heads - p.kv_heads;
-    for (int64_t base = 0; base < all; base += most) {  // a launch takes less than 2^32 threads
+    q.target = plan.target;
+    q.records = (char *)p.partials + (size_t)plan.groups * plan.slot_floats * sizeof(float);  // behind the pieces
+    const void *kernel, *join;
+    if (!plan.few) {
+        kernel = (const void *)&prompt_kernel<T, D, 1, Eight>;
+        join = (const void *)&prompt_join_kernel<T, D, 1, false, Eight>;
+    } else if (plan.rows == 16) {
+        kernel = (const void *)&prompt_few_kernel<T, D, 1, Eight>;
+        join = (const void *)&prompt_join_kernel<T, D, 1, true, Eight>;
+    } else {
+        kernel = (const void *)&prompt_few_kernel<T, D, 2, Eight>;
+        join = (const void *)&prompt_join_kernel<T, D, 2, true, Eight>;
+    }
+    const int64_t most = ((int64_t)1 << 24) / p.kv_heads * p.kv_heads - p.kv_heads;
+    for (int64_t base = 0; base < plan.groups; base += most) {  // a launch takes less than 2^32 threads
         q.base = (int)base;
         void *args[] = {&q};
-        const uint32_t n = (uint32_t)(all - base < most ? all - base : most);
-        const hipError_t e = hipLaunchKernel(kernel, dim3(n), dim3(64 * kWaves), args, 0, stream);
+        const uint32_t n = (uint32_t)(plan.groups - base < most ? plan.groups - base : most);
+        hipError_t e = hipLaunchKernel(kernel, dim3(n), dim3(64 * kWaves), args, 0, stream);
+        if (e == hipSuccess && plan.target) e = hipLaunchKernel(join, dim3(n), dim3(64 * kWaves), args, 0, stream);
         if (e != hipSuccess) return e;
     }
     return hipSuccess;
@@ -1136,18 +1234,24 @@ hipError_t launch_typed(const PromptProblem &p, const PromptPlan &plan, int head
 
 }  // namespace
 
-PromptPlan plan_prompt(int64_t tokens, int64_t B, int64_t heads, int64_t kv_heads, int head_dim)
+PromptPlan plan_prompt(int64_t tokens, int64_t B, int64_t heads, int64_t kv_heads, int head_dim, int64_t positions)
 {
     PromptPlan x;
     const int64_t rows = tokens * (heads / kv_heads);  // of one kv head
     const int64_t sequences = B < tokens ? B : tokens;
     x.few = rows <= 64 * sequences;
     x.rows = x.few ? (rows <= 16 * sequences ? 16 : 32) : 32 * kWaves;
-    x.tiles = (int)(rows / x.rows + sequences);
-    const int64_t groups = (int64_t)x.tiles * kv_heads, most = x.few ? kFewGroups : kWideGroups;
-    x.splits = (int)(groups == 0 || groups > most ? 1 : most / groups);
-    x.slot_floats = x.few ? (x.rows / 16) * (kHeadTile * head_dim + 2 * kHeadTile) : 64 * kWaves * 4 * (head_dim / 32 * 4 + 1);
+    const int64_t tiles = (rows / x.rows + sequences) * kv_heads, target = x.few ? kFewGroups : kWideGroups;  // tiles at the most
+    const int64_t least = x.few ? (int64_t)kFewLeast << 5 : (int64_t)kWideLeast << 6;  // keys of a part at the least
+    x.target = tiles < target && positions > least ? (int)target : 0;
+    x.groups = tiles + x.target;  // a tile's last part is not a whole one
+    x.slot_floats = x.few ? 64 * 4 * (x.rows / 16) * (head_dim / 16 + 1) : 64 * kWaves * 4 * (head_dim / 32 * 4 + 1);
     return x;
+}
+
+size_t prompt_workspace(const PromptPlan &x)
+{
+    return x.target ? (size_t)x.groups * (sizeof(Record) + (size_t)x.slot_floats * sizeof(float)) : 0;
 }
 
 hipError_t launch_prompt(const PromptProblem &p, const PromptPlan &plan, int head_dim, marlin_dtype_t dtype, hipStream_t stream)
