@@ -23,24 +23,26 @@ using namespace dev;
 constexpr int kThreads = 1024, kSums = kThreads / 64;
 constexpr int kFusedTokens = 2048;
 
-__device__ __forceinline__ uint32_t add_up(uint32_t a, uint32_t b) { return __builtin_elementwise_add_sat(a, b); }
-
-// Sums over the work-group's threads up to and with each, on top of `before`, which becomes the sum of all; saturating.
-__device__ __forceinline__ uint32_t block_scan(uint32_t x, uint32_t &before, uint32_t *lds, int lane, int wave)
+// Two sums over the work-group's threads up to and with each, on top of `before`, which becomes the sums of all; saturating.
+struct Two {
+    uint32_t a, b;
+};
+__device__ __forceinline__ Two add_up(Two x, Two y) { return {__builtin_elementwise_add_sat(x.a, y.a), __builtin_elementwise_add_sat(x.b, y.b)}; }
+__device__ __forceinline__ Two block_scan(Two x, Two &before, Two *lds, int lane, int wave, int waves)
 {
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
-        const uint32_t y = __shfl_up(x, d);
+        const Two y{(uint32_t)__shfl_up(x.a, d), (uint32_t)__shfl_up(x.b, d)};
         if (lane >= d) x = add_up(x, y);
     }
     __syncthreads();  // of the last scan's readers
     if (lane == 63) lds[wave] = x;
     __syncthreads();
-    uint32_t mine = before, all = before;
-#pragma unroll
-    for (int w = 0; w < kSums; ++w) {
-        if (w < wave) mine = add_up(mine, lds[w]);
-        all = add_up(all, lds[w]);
+    Two mine = before, all = before;
+    for (int w = 0; w < waves; ++w) {
+        const Two y = lds[w];
+        if (w < wave) mine = add_up(mine, y);
+        all = add_up(all, y);
     }
     before = all;
     return add_up(mine, x);
@@ -79,9 +81,10 @@ __device__ __forceinline__ int64_t slot_of_token(const PagesProblem &p, int b, i
 template <bool Fused>
 __global__ void __launch_bounds__(kThreads) assign_kernel(const PagesProblem p)
 {
-    __shared__ uint32_t lds_sums[kSums];
-    __shared__ uint32_t lds_served[2][kSums];
+    __shared__ Two lds_sums[kSums], lds_served[kSums];
     __shared__ int lds_starts[kThreads + 1], lds_before[kThreads], lds_had[kThreads];  // of up to 1024 sequences
+    // sequences whose entries are looked at: thread, first entry, last (with the sign bit: all of them count); what is given back
+    __shared__ int lds_works, lds_of[kThreads], lds_first[kThreads], lds_last[kThreads], lds_given[kThreads], lds_upto[kThreads];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int ps = 1 << p.page_shift, cap = p.width << p.page_shift;
     int count = *p.free_count;
@@ -93,15 +96,22 @@ __global__ void __launch_bounds__(kThreads) assign_kernel(const PagesProblem p)
     };
 
     // ---- given back ----
-    uint32_t returned = 0;
+    Two returned{0, 0};
+    int had0 = 0, new0 = 0;  // of the first 1024 sequences
     for (int b0 = 0; b0 < p.B; b0 += kThreads) {
         const int b = b0 + tid;
+        if (tid == 0) lds_works = 0;
+        __syncthreads();
         // entries first .. last - 1 are looked at, all of them (an ended sequence's) or from the last down to one that names no page
         int first = 0, last = 0;
         bool ends = false;
         if (b < p.B) {
-            const int had = length_of(b);
-            ends = p.new_tokens[b] < 0;
+            const int had = length_of(b), fresh = p.new_tokens[b];
+            if (b0 == 0) {
+                had0 = had;
+                new0 = fresh;
+            }
+            ends = fresh < 0;
             if (ends) {
                 last = (had + ps - 1) >> p.page_shift;
             } else if (p.window > 0 && had > p.window) {
@@ -109,20 +119,26 @@ __global__ void __launch_bounds__(kThreads) assign_kernel(const PagesProblem p)
                 last = (had - p.window) >> p.page_shift;
                 if (last > first && (uint32_t)p.table[b * p.table_row + last - 1] >= (uint32_t)p.pages) last = 0;
             }
-            if (last <= first) last = first = 0;
         }
-        // a wave looks at its 64 sequences' entries one after another, 64 entries at a time
-        uint32_t mine = 0;
-        const uint64_t work = __builtin_amdgcn_ballot_w64(last > first);
-        for (uint64_t left = work; left; left &= left - 1) {
-            const int of = __builtin_ctzll(left);
-            const int f = __builtin_amdgcn_readlane(first, of), l = __builtin_amdgcn_readlane(last, of);
-            const bool whole = __builtin_amdgcn_readlane(ends, of);
-            const int32_t *const row = p.table + (int64_t)(b0 + wave * 64 + of) * p.table_row;
-            uint32_t n = 0;
+        lds_given[tid] = 0;
+        if (last > first) {
+            const int at = atomicAdd(&lds_works, 1);  // in any order
+            lds_of[at] = tid;
+            lds_first[at] = first;
+            lds_last[at] = ends ? last | 1 << 31 : last;
+        }
+        __syncthreads();
+        const int works = lds_works;
+        if (works == 0) continue;
+        // a sequence is a wave's, 64 entries at a time
+        for (int i = wave; i < works; i += kSums) {
+            const int of = lds_of[i], f = lds_first[i], l = lds_last[i] & 0x7FFFFFFF;
+            const bool whole = lds_last[i] < 0;
+            const int32_t *const row = p.table + (int64_t)(b0 + of) * p.table_row;
+            int n = 0;
             for (int at = l; at > f; at -= 64) {
-                const int i = at - 1 - lane;
-                const uint64_t named = __builtin_amdgcn_ballot_w64(i >= f && (uint32_t)row[i >= f ? i : f] < (uint32_t)p.pages);
+                const int e = at - 1 - lane;
+                const uint64_t named = __builtin_amdgcn_ballot_w64(e >= f && (uint32_t)row[e >= f ? e : f] < (uint32_t)p.pages);
                 if (whole) {
                     n += __popcll(named);
                 } else {
@@ -131,66 +147,60 @@ __global__ void __launch_bounds__(kThreads) assign_kernel(const PagesProblem p)
                     if (run < 64) break;
                 }
             }
-            if (lane == of) mine = n;
+            if (lane == 0) lds_given[of] = n;
         }
-        const uint32_t upto = block_scan(mine, returned, lds_sums, lane, wave);
-        // written in ascending order: the run below a window's end is its last `mine` entries
-        for (uint64_t left = work; left; left &= left - 1) {
-            const int of = __builtin_ctzll(left);
-            const int l = __builtin_amdgcn_readlane(last, of), n = __builtin_amdgcn_readlane(mine, of);
-            const bool whole = __builtin_amdgcn_readlane(ends, of);
-            const int f = whole ? __builtin_amdgcn_readlane(first, of) : l - n;
-            int32_t *const row = p.table + (int64_t)(b0 + wave * 64 + of) * p.table_row;
-            int64_t to = (int64_t)count + (uint32_t)__builtin_amdgcn_readlane(upto, of) - n;
+        __syncthreads();
+        const Two upto = block_scan({(uint32_t)lds_given[tid], 0}, returned, lds_sums, lane, wave, kSums);
+        lds_upto[tid] = (int)upto.a;
+        __syncthreads();
+        // written in ascending order: the run below a window's end is its last entries
+        for (int i = wave; i < works; i += kSums) {
+            const int of = lds_of[i], l = lds_last[i] & 0x7FFFFFFF, n = lds_given[of], f = lds_last[i] < 0 ? lds_first[i] : l - n;
+            int32_t *const row = p.table + (int64_t)(b0 + of) * p.table_row;
+            int64_t to = (int64_t)count + (uint32_t)lds_upto[of] - n;
             for (int at = f; at < l; at += 64) {
-                const int i = at + lane;
-                const int page = i < l ? row[i] : -1;
+                const int e = at + lane;
+                const int page = e < l ? row[e] : -1;
                 const bool named = (uint32_t)page < (uint32_t)p.pages;
                 const uint64_t all = __builtin_amdgcn_ballot_w64(named);
                 const int64_t at_free = to + __popcll(all & (((uint64_t)1 << lane) - 1));
                 if (named) {
                     if (at_free < p.pages) p.free_pages[at_free] = page;
-                    row[i] = -1;
+                    row[e] = -1;
                 }
                 to += __popcll(all);
             }
         }
     }
-    const int room = (int)((int64_t)count + returned < p.pages ? count + returned : p.pages);
+    const int room = (int)((int64_t)count + returned.a < p.pages ? count + returned.a : p.pages);
 
     // ---- served ----
-    uint32_t pages_sum = 0, tokens_sum = 0, pages_served = 0, tokens_served = 0;
+    Two sums{0, 0};
+    uint32_t pages_served = 0, tokens_served = 0;
     if (tid == 0) p.starts[0] = 0;
     if (Fused && tid == 0) lds_starts[0] = 0;
     for (int b0 = 0; b0 < p.B; b0 += kThreads) {
         const int b = b0 + tid;
-        int had = 0, n = 0;
-        if (b < p.B) {
-            had = length_of(b);
-            n = p.new_tokens[b];
+        int had = had0, n = new0;
+        if (b0 > 0) {
+            had = b < p.B ? length_of(b) : 0;
+            n = b < p.B ? p.new_tokens[b] : 0;
         }
         const bool fits = n > 0 && n <= cap - had;
         const uint32_t need = fits ? ((had + n + ps - 1) >> p.page_shift) - ((had + ps - 1) >> p.page_shift) : 0;
-        const uint32_t pages = block_scan(need, pages_sum, lds_sums, lane, wave);
-        const uint32_t tokens = block_scan(fits ? n : 0, tokens_sum, lds_sums, lane, wave);
+        const Two upto = block_scan({need, fits ? (uint32_t)n : 0}, sums, lds_sums, lane, wave, kSums);
+        const uint32_t pages = upto.a, tokens = upto.b;
         const bool served = fits && pages <= (uint32_t)room && tokens <= (uint32_t)p.tokens;
-        // the last served one's sums
-        uint32_t a = served ? pages : 0, c = served ? tokens : 0;
-#pragma unroll
-        for (int d = 32; d > 0; d >>= 1) {
-            const uint32_t a2 = __shfl_xor(a, d), c2 = __shfl_xor(c, d);
-            a = a2 > a ? a2 : a;
-            c = c2 > c ? c2 : c;
-        }
-        if (lane == 0) {
-            lds_served[0][wave] = a;
-            lds_served[1][wave] = c;
-        }
+        // the last served one's sums: of a wave the last lane's that is
+        const uint64_t any = __builtin_amdgcn_ballot_w64(served);
+        const int at = any ? 63 - __builtin_clzll(any) : 0;
+        const Two most{any ? (uint32_t)__builtin_amdgcn_readlane(pages, at) : 0u, any ? (uint32_t)__builtin_amdgcn_readlane(tokens, at) : 0u};
+        if (lane == 0) lds_served[wave] = most;
         __syncthreads();
-#pragma unroll
         for (int w = 0; w < kSums; ++w) {
-            pages_served = lds_served[0][w] > pages_served ? lds_served[0][w] : pages_served;
-            tokens_served = lds_served[1][w] > tokens_served ? lds_served[1][w] : tokens_served;
+            const Two x = lds_served[w];
+            pages_served = x.a > pages_served ? x.a : pages_served;
+            tokens_served = x.b > tokens_served ? x.b : tokens_served;
         }
         if (b < p.B) {
             const uint32_t end = tokens < tokens_served ? tokens : tokens_served;
