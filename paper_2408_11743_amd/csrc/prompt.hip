@@ -78,32 +78,36 @@ __device__ __forceinline__ float odd_at(const void *cache, int64_t at)
     return __builtin_fabsf(x) < INFINITY ? 0.f : x;
 }
 
-// The keys that a tile's rows see, in steps of 2^shift: [0, sinks) and [low, end), of which steps the first sink_steps and those
-// from skip further on.
+// The keys that a tile's rows see: those below `sinks` and from a window's lower end on, in tiles of 16 of which the first `sink_tiles`
+// and those `skip` further on are taken, 2^shift to a step.
 struct Keys {
     int first, last;  // the rows' first and last position
-    int end, low, sinks, sink_steps, skip, steps;
+    int end, sinks;   // of what there is, of the sinks below the window
+    int sink_tiles, skip, steps;
+    // first position of tile t
+    __device__ __forceinline__ int position(int t) const { return (t < sink_tiles ? t : t + skip) * kTileKeys; }
 };
 __device__ __forceinline__ Keys keys_of(const PromptProblem &p, int start, int tokens, int row0, int rows, int shift)
 {
     Keys k;
     const int all_rows = tokens * p.group, last_row = (row0 + rows < all_rows ? row0 + rows : all_rows) - 1;
-    const int cap = p.width << p.page_shift, up = (1 << shift) - 1;
+    const int cap = p.width << p.page_shift;
     k.first = start + row0 / p.group;
     k.last = start + last_row / p.group;
     k.end = k.last + 1 < cap ? k.last + 1 : cap;
     if (k.end < 0) k.end = 0;
-    k.low = k.sinks = 0;
+    int low = 0;
+    k.sinks = 0;
     if (p.window) {
-        k.low = k.first >= p.window ? k.first - p.window + 1 : 0;
-        k.sinks = p.sinks < k.low ? p.sinks : k.low;
+        low = k.first >= p.window ? k.first - p.window + 1 : 0;
+        k.sinks = p.sinks < low ? p.sinks : low;
     }
-    const int all = (k.end + up) >> shift, first = k.low >> shift;
-    k.sink_steps = (k.sinks + up) >> shift;
-    if (k.sink_steps > all) k.sink_steps = all;
-    k.skip = (first < all ? first : all) - k.sink_steps;
+    const int all = (k.end + kTileKeys - 1) / kTileKeys, from = low / kTileKeys;
+    k.sink_tiles = (k.sinks + kTileKeys - 1) / kTileKeys;
+    if (k.sink_tiles > all) k.sink_tiles = all;
+    k.skip = (from < all ? from : all) - k.sink_tiles;
     if (k.skip < 0) k.skip = 0;
-    k.steps = all - k.skip;
+    k.steps = (all - k.skip + (1 << shift) - 1) >> shift;
     return k;
 }
 
@@ -118,7 +122,7 @@ __device__ __forceinline__ Record *record_of(const PromptProblem &p, int index) 
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 __device__ __forceinline__ Keys uniform(const Keys &k)
 {
-    return {uniform(k.first), uniform(k.last), uniform(k.end), uniform(k.low), uniform(k.sinks), uniform(k.sink_steps), uniform(k.skip), uniform(k.steps)};
+    return {uniform(k.first), uniform(k.last), uniform(k.end), uniform(k.sinks), uniform(k.sink_tiles), uniform(k.skip), uniform(k.steps)};
 }
 
 // What a work-group does: a tile of rows (tokens from + row / group of a sequence), and which part of its keys.
@@ -130,7 +134,7 @@ struct Work {
 };
 
 // The work of one of a kv head's work-groups, found from the sequences' starts and lengths: tiles of `rows` rows, the last of a
-// sequence first, as it sees the most, in parts of `chunk` steps of 2^shift keys, which is what all tiles' steps make for each of p.target work-groups
+// sequence first, as it sees the most, in parts of `chunk` steps of 2^shift 16-key tiles, which is what all tiles' steps make for each of p.target work-groups
 // (where there are as many tiles as that, a part is all of a tile).
 // 64 sequences are held in the lanes; of more, the waves share the sums.
 __device__ __forceinline__ Work find_work(const PromptProblem &p, int rows, int shift, int least, int index, int lane, int wave, int *lds_chunks)
@@ -256,14 +260,16 @@ template <int N>
 struct Entries {
     int e[N];
 };
+// of the tiles of step s
 template <int N>
-__device__ __forceinline__ Entries<N> load_entries(const PromptProblem &p, const int32_t *table, int pos, int end)
+__device__ __forceinline__ Entries<N> load_entries(const PromptProblem &p, const int32_t *table, const Keys &keys, int s)
 {
     Entries<N> x;
 #pragma unroll
     for (int u = 0; u < N; ++u) {
+        const int pos = keys.position(N * s + u);
         x.e[u] = -1;
-        if (pos + kTileKeys * u < end) x.e[u] = scalar_load(table + ((pos + kTileKeys * u) >> p.page_shift));
+        if (pos < keys.end) x.e[u] = scalar_load(table + (pos >> p.page_shift));
     }
     return x;
 }
@@ -278,7 +284,7 @@ __device__ __forceinline__ int64_t place_of(const PromptProblem &p, int entry, i
     return ((page_head(p, entry, head) << p.page_shift) + (pos & ((1 << p.page_shift) - 1))) * D;
 }
 template <int N, bool Eight>
-__device__ __forceinline__ Raw<N, Eight> raw_of(const PromptProblem &p, const Entries<N> &x, int head, int pos)
+__device__ __forceinline__ Raw<N, Eight> raw_of(const PromptProblem &p, const Entries<N> &x, int head, const Keys &keys, int s)
 {
     Raw<N, Eight> k;
     k.named = 0;
@@ -286,10 +292,10 @@ __device__ __forceinline__ Raw<N, Eight> raw_of(const PromptProblem &p, const En
     for (int u = 0; u < N; ++u) {
         k.named |= ((uint32_t)x.e[u] < (uint32_t)p.pages ? 1u : 0u) << u;
         if constexpr (Eight) {
-            const int per_shift = p.page_shift - 4, slot = (pos + kTileKeys * u) & ((1 << p.page_shift) - 1);
-            const float *s = p.scales + ((page_head(p, x.e[u], head) * 2) << per_shift) + (slot >> 4);
-            k.ks[u] = scalar_load(s);
-            k.vs[u] = scalar_load(s + (1 << per_shift));
+            const int per_shift = p.page_shift - 4, slot = keys.position(N * s + u) & ((1 << p.page_shift) - 1);
+            const float *scale = p.scales + ((page_head(p, x.e[u], head) * 2) << per_shift) + (slot >> 4);
+            k.ks[u] = scalar_load(scale);
+            k.vs[u] = scalar_load(scale + (1 << per_shift));
         }
     }
     return k;
@@ -364,10 +370,10 @@ __global__ void __launch_bounds__(64 * kWaves, RT == 1 && D <= 128 ? 2 : 1) prom
     const int col = lane & 31, half = lane >> 5;
     const int index = p.base + blockIdx.x;
     const int head = uniform(index % p.kv_heads);
-    const Work tile = find_work(p, kRows, 6, kWideLeast, index, lane, wave, (int *)lds);
+    const Work tile = find_work(p, kRows, 2, kWideLeast, index, lane, wave, (int *)lds);
     if (p.target > 0 && tid == 0) record_of(p, index)->parts = 0;
     if (tile.row0 < 0) return;
-    const Keys keys = uniform(keys_of(p, tile.start, tile.tokens, tile.row0, kRows, 6));
+    const Keys keys = uniform(keys_of(p, tile.start, tile.tokens, tile.row0, kRows, 2));
     const int parts = uniform(keys.steps <= tile.chunk ? 1 : (keys.steps + tile.chunk - 1) / tile.chunk);  // work-groups that share the tile
     if (tile.part >= parts) return;
     if (parts > 1 && tid == 0) *record_of(p, index) = {parts, tile.part, tile.first, tile.row0, tile.from, tile.tokens};
@@ -375,7 +381,7 @@ __global__ void __launch_bounds__(64 * kWaves, RT == 1 && D <= 128 ? 2 : 1) prom
     __syncthreads();
 
     const int32_t *const table = p.table + (int64_t)tile.b * p.table_row;
-    auto position_of = [&](int s) { return (s < keys.sink_steps ? s : s + keys.skip) * kStep; };
+    auto position_of = [&](int s, int u) { return keys.position(4 * s + u); };  // of a step's tile
 
     // this lane's rows
     Sight sight[RT];
@@ -398,17 +404,24 @@ __global__ void __launch_bounds__(64 * kWaves, RT == 1 && D <= 128 ? 2 : 1) prom
     uint32_t kreg[kKeyPasses][kLoad / 4], vreg[kValuePasses][4][kPiece];
     const uint32_t key_from = lane * kLoad, value_from = ((lane / kOct) * 4 * D + (lane % kOct) * 8) * kSize;
     // whether every row sees every key of a step, as far as its position says
-    auto within = [&](int pos) {
-        return pos + kStep - 1 <= keys.first && pos + kStep <= keys.end && (!p.window || pos > keys.last - p.window || pos + kStep <= p.sinks);
+    auto within = [&](int s) {
+        const int t0 = 4 * s, t3 = t0 + 3, last = keys.position(t3);
+        bool all = last + kTileKeys - 1 <= keys.first && last + kTileKeys <= keys.end;
+        if (p.window) {  // the first tile of the window, the last of the sinks
+            const int low = t0 > keys.sink_tiles ? t0 : keys.sink_tiles, sink = t3 < keys.sink_tiles ? t3 : keys.sink_tiles - 1;
+            all = all && (low > t3 || keys.position(low) > keys.last - p.window) && (sink < t0 || keys.position(sink) + kTileKeys <= p.sinks);
+        }
+        return all;
     };
     // this wave's tile of a step: its page's entry, where it lies (bytes), whether there is one, its scales
     struct Mine {
         int64_t at;
         bool named;
+        bool within;
         float ks, vs;
     };
     auto entry_of = [&](int s) {
-        const int pos = position_of(s) + kTileKeys * wave;
+        const int pos = position_of(s, wave);
         int e = -1;
         if (s < s1 && pos < keys.end) e = scalar_load(table + (pos >> p.page_shift));
         return e;
@@ -417,7 +430,8 @@ __global__ void __launch_bounds__(64 * kWaves, RT == 1 && D <= 128 ? 2 : 1) prom
         Mine x;
         entry = __builtin_amdgcn_readfirstlane(entry);
         x.named = (uint32_t)entry < (uint32_t)p.pages;
-        const int pos = position_of(s) + kTileKeys * wave;
+        x.within = within(s);
+        const int pos = position_of(s, wave);
         x.at = place_of(p, entry, head, pos, D) * kSize;
         if constexpr (Eight) {
             const int per_shift = p.page_shift - 4, slot = pos & ((1 << p.page_shift) - 1);
@@ -476,15 +490,15 @@ __global__ void __launch_bounds__(64 * kWaves, RT == 1 && D <= 128 ? 2 : 1) prom
         }
     };
     auto store_values = [&](int s, const Mine &x) {
-        const int pos = position_of(s);
-        if (!(within(pos) && is_fine(x))) {
+        if (!(x.within && is_fine(x))) {
+            const int pos = position_of(s, wave);
             // what no row sees is zero; of the rest what is finite
             uint32_t odd = 0;
 #pragma unroll
             for (int i = 0; i < kValuePasses; ++i)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const bool seen = x.named & (pos + kTileKeys * wave + ((lane + 64 * i) / kOct) * 4 + j < keys.end);
+                    const bool seen = x.named & (pos + ((lane + 64 * i) / kOct) * 4 + j < keys.end);
 #pragma unroll
                     for (int w = 0; w < kPiece; ++w) {
                         const uint32_t y = seen ? vreg[i][j][w] : 0, z = finite_of<T, Eight>(y);
@@ -554,17 +568,16 @@ __global__ void __launch_bounds__(64 * kWaves, RT == 1 && D <= 128 ? 2 : 1) prom
     // which of a step's tiles are there
     auto ok_of = [&](int s) { return (uint32_t)__builtin_amdgcn_ballot_w64(lds_info[s & 3].ok[lane & 3] != 0) & 15u; };
     // scores that are not seen, then the maximum (of what the factors make of them) with the sums brought to it
-    auto look = [&](int s, scores_t &x, float (&top)[RT]) {
-        const int pos = position_of(s);
+    auto look = [&](int s, bool inside, scores_t &x, float (&top)[RT]) {
         const uint32_t ok = ok_of(s);
-        if (!(within(pos) && ok == 15u)) {
+        if (!(inside && ok == 15u)) {
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
                 for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
-                        const int j = pos + 32 * kt + 8 * (i >> 2) + 4 * half + (i & 3);
+                        const int j = position_of(s, 2 * kt + (i >> 3)) + 8 * ((i >> 2) & 1) + 4 * half + (i & 3);
                         const bool seen = ((ok >> (2 * kt + (i >> 3)) & 1) != 0) & sight[rt].sees(j) & (j < keys.end);
                         x[rt][kt][i] = seen ? x[rt][kt][i] : -INFINITY;
                     }
@@ -639,17 +652,16 @@ __global__ void __launch_bounds__(64 * kWaves, RT == 1 && D <= 128 ? 2 : 1) prom
             }
     };
     // values of a step that are not finite, where some rows do not see all keys
-    auto add_odd = [&](int s) {
-        const int pos = position_of(s);
+    auto add_odd = [&](int s, bool inside) {
         const uint32_t ok = ok_of(s);
-        if (within(pos) && ok == 15u) return;
+        if (inside && ok == 15u) return;
         // a wave whose tile every row sees has not looked
         uint32_t odd = (uint32_t)__builtin_amdgcn_ballot_w64(lds_info[s & 3].odd[lane & 3] != 0) & 15u;
-        if (within(pos)) odd &= ~ok;
+        if (inside) odd &= ~ok;
         if (odd == 0) return;
 #pragma unroll 1
         for (int n = 0; n < kStep; ++n) {
-            const int j = pos + n;
+            const int j = position_of(s, n >> 4) + (n & 15);
             if (!(ok >> (n >> 4) & 1) || j >= keys.end) continue;
             const int64_t at = place_of(p, scalar_load(table + (j >> p.page_shift)), head, j, D);
 #pragma unroll
@@ -675,7 +687,8 @@ __global__ void __launch_bounds__(64 * kWaves, RT == 1 && D <= 128 ? 2 : 1) prom
         entry = entry_of(s0 + 2);
         __syncthreads();
         score(s0, x);
-        look(s0, x, top);
+        bool inside = values.within;  // of the step at hand
+        look(s0, inside, x, top);
         rescale(top);
         store_values(s0, values);
         store_keys(s0 + 1, next);
@@ -689,8 +702,9 @@ __global__ void __launch_bounds__(64 * kWaves, RT == 1 && D <= 128 ? 2 : 1) prom
             score(s + 1, ahead);
             weigh(s, x, weights);
             add_values(s, weights);
-            look(s + 1, ahead, top);
-            add_odd(s);
+            look(s + 1, values.within, ahead, top);
+            add_odd(s, inside);
+            inside = values.within;
             rescale(top);
             store_values(s + 1, values);
             store_keys(s + 2, next);
@@ -702,7 +716,7 @@ __global__ void __launch_bounds__(64 * kWaves, RT == 1 && D <= 128 ? 2 : 1) prom
         __syncthreads();
         weigh(s1 - 1, x, weights);
         add_values(s1 - 1, weights);
-        add_odd(s1 - 1);
+        add_odd(s1 - 1, inside);
     }
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
@@ -781,10 +795,10 @@ __global__ void __launch_bounds__(64 * kWaves, D > 128 ? 1 : 2) prompt_few_kerne
     const int r = lane & 15, g = lane >> 4;
     const int index = p.base + blockIdx.x;
     const int head = uniform(index % p.kv_heads);
-    const Work tile = find_work(p, kRows, 5, kFewLeast, index, lane, wave, (int *)&lds_acc[0][0][0]);
+    const Work tile = find_work(p, kRows, 1, kFewLeast, index, lane, wave, (int *)&lds_acc[0][0][0]);
     if (p.target > 0 && tid == 0) record_of(p, index)->parts = 0;
     if (tile.row0 < 0) return;
-    const Keys keys = uniform(keys_of(p, tile.start, tile.tokens, tile.row0, kRows, 5));
+    const Keys keys = uniform(keys_of(p, tile.start, tile.tokens, tile.row0, kRows, 1));
     const int parts = uniform(keys.steps <= tile.chunk ? 1 : (keys.steps + tile.chunk - 1) / tile.chunk);  // work-groups that share the tile
     if (tile.part >= parts) return;
     if (parts > 1 && tid == 0) *record_of(p, index) = {parts, tile.part, tile.first, tile.row0, tile.from, tile.tokens};
@@ -792,7 +806,7 @@ __global__ void __launch_bounds__(64 * kWaves, D > 128 ? 1 : 2) prompt_few_kerne
     __syncthreads();
 
     const int32_t *const table = p.table + (int64_t)tile.b * p.table_row;
-    auto position_of = [&](int s) { return (s < keys.sink_steps ? s : s + keys.skip) * kKeys; };
+    auto position_of = [&](int s, int u) { return keys.position(2 * s + u); };  // of a step's tile
     Sight sight[RT];
     vec8 qf[RT][kQ];
     int64_t out_at[RT];
@@ -812,10 +826,10 @@ __global__ void __launch_bounds__(64 * kWaves, D > 128 ? 1 : 2) prompt_few_kerne
     struct Places {
         int64_t at[KT];
     };
-    auto places_of = [&](const Entries<KT> &x, int pos) {
+    auto places_of = [&](const Entries<KT> &x, int s) {
         Places k;
 #pragma unroll
-        for (int u = 0; u < KT; ++u) k.at[u] = place_of(p, x.e[u], head, pos + kTileKeys * u, D);
+        for (int u = 0; u < KT; ++u) k.at[u] = place_of(p, x.e[u], head, position_of(s, u), D);
         return k;
     };
     // of tiles without a page the registers keep what they hold, which is masked
@@ -890,13 +904,13 @@ __global__ void __launch_bounds__(64 * kWaves, D > 128 ? 1 : 2) prompt_few_kerne
 
     int s = s0 + wave;
     if (s < s1) {
-        const Entries<KT> first = load_entries<KT>(p, table, position_of(s), keys.end);
-        Raw<KT, Eight> raw = raw_of<KT, Eight>(p, first, head, position_of(s)), next = raw;
-        Places places = places_of(first, position_of(s));
+        const Entries<KT> first = load_entries<KT>(p, table, keys, s);
+        Raw<KT, Eight> raw = raw_of<KT, Eight>(p, first, head, keys, s), next = raw;
+        Places places = places_of(first, s);
         load_keys(places, raw.named);
         load_values(places, raw.named);
         Entries<KT> ahead{};
-        if (s + kWaves < s1) ahead = load_entries<KT>(p, table, position_of(s + kWaves), keys.end);
+        if (s + kWaves < s1) ahead = load_entries<KT>(p, table, keys, s + kWaves);
 #pragma unroll 1
         while (true) {
             float4_t sc[RT][KT];
@@ -915,24 +929,27 @@ __global__ void __launch_bounds__(64 * kWaves, D > 128 ? 1 : 2) prompt_few_kerne
                     for (int rt = 0; rt < RT; ++rt) sc[rt][u] = E::mfma(x, qf[rt][t], sc[rt][u]);
                 }
             }
-            const int pos = position_of(s);
+            const int pos[KT] = {position_of(s, 0), position_of(s, 1)};
             const bool more = s + kWaves < s1;
             issue_order_point();
             if (more) {
-                next = raw_of<KT, Eight>(p, ahead, head, position_of(s + kWaves));
-                places = places_of(ahead, position_of(s + kWaves));
+                next = raw_of<KT, Eight>(p, ahead, head, keys, s + kWaves);
+                places = places_of(ahead, s + kWaves);
                 load_keys(places, next.named);
-                if (s + 2 * kWaves < s1) ahead = load_entries<KT>(p, table, position_of(s + 2 * kWaves), keys.end);
+                if (s + 2 * kWaves < s1) ahead = load_entries<KT>(p, table, keys, s + 2 * kWaves);
             }
             const Block<KT, Eight> cur = block_of<KT, Eight>(p, raw);
-            const bool all = cur.ok == 3u && pos + kKeys - 1 <= keys.first && pos + kKeys <= keys.end &&
-                             (!p.window || pos > keys.last - p.window || pos + kKeys <= p.sinks);
+            bool all = cur.ok == 3u && pos[1] + kTileKeys - 1 <= keys.first && pos[1] + kTileKeys <= keys.end;
+            if (p.window) {
+#pragma unroll
+                for (int u = 0; u < KT; ++u) all = all && (pos[u] > keys.last - p.window || pos[u] + kTileKeys <= p.sinks);
+            }
             if (!all) {  // what no row sees: zero
 #pragma unroll
                 for (int u = 0; u < KT; ++u)
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
-                        if (!(cur.ok >> u & 1) || pos + 16 * u + 4 * g + i >= keys.end) {
+                        if (!(cur.ok >> u & 1) || pos[u] + 4 * g + i >= keys.end) {
 #pragma unroll
                             for (int hf = 0; hf < kHalves; ++hf)
 #pragma unroll
@@ -956,7 +973,7 @@ __global__ void __launch_bounds__(64 * kWaves, D > 128 ? 1 : 2) prompt_few_kerne
                     for (int u = 0; u < KT; ++u)
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
-                            const int j = pos + 16 * u + 4 * g + i;
+                            const int j = pos[u] + 4 * g + i;
                             const bool seen = ((cur.ok >> u & 1) != 0) & sight[rt].sees(j) & (j < keys.end);
                             sc[rt][u][i] = seen ? sc[rt][u][i] : -INFINITY;
                         }
@@ -1005,7 +1022,7 @@ __global__ void __launch_bounds__(64 * kWaves, D > 128 ? 1 : 2) prompt_few_kerne
                 if (__any(odd != 0)) {
 #pragma unroll 1
                     for (int n = 0; n < kKeys; ++n) {
-                        const int j = pos + n;
+                        const int j = position_of(s, n >> 4) + (n & 15);
                         if (!(cur.ok >> (n >> 4) & 1) || j >= keys.end) continue;
                         const int64_t at = place_of(p, scalar_load(table + (j >> p.page_shift)), head, j, D);
 #pragma unroll

@@ -665,10 +665,10 @@ def test_steps_as_graphs(mk, bits):
     g = gen(2)
     rows = {n: torch.randn(n, hq + 2 * hkv, D, generator=g).half().cuda() for n in (6, 90)}
     new = {6: torch.ones(6, dtype=torch.int32).cuda(), 90: torch.tensor([20, 3, 40, 0, 26, 1], dtype=torch.int32).cuda()}
-    side = torch.cuda.Stream()
-    side.wait_stream(torch.cuda.current_stream())
     graphs, outs = {}, {}
     keep = {k: x.clone() for k, x in st.items() if isinstance(x, torch.Tensor)}
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())  # the copies are made before the first steps change what they are of
     with torch.cuda.stream(side):
         for n in (6, 90):
             step(rows[n], new[n], n)
