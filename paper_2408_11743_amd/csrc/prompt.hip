@@ -17,9 +17,9 @@
 // scans, the longest of a sequence first.  Where there are few tiles, their keys are split into parts of one length, a work-group
 // each, which leave partial results in the workspace; a second launch joins those in order.
 //
-// Weights go to the second product rounded once to the cache's type (float16's times 2^15, so that
-// they are no subnormals until 2^-29 of the maximum, and lost below 2^-40): an error of half a step of each weight, as the output's own,
-// and averaged over the keys.  Scores, maxima, sums and results are fp32.
+// Weights go to the second product rounded once to the cache's type: an error of half a step of each weight, as the output's
+// own, and averaged over the keys.  float16's are times 2^11 (few rows: 2^15), so that they are no subnormals until 2^-25 of the maximum, and lost
+// below 2^-36: 2^20 keys that are lost are less than half a step of the sum.  Scores, maxima, sums and results are fp32.
 #include <hip/hip_runtime.h>
 
 #include "device.h"
@@ -329,6 +329,12 @@ __device__ __forceinline__ V query_of(const PromptProblem &p, const T *q, bool h
 
 constexpr int kStep = 64;
 
+// Weights are taken against a row's maximum as it was when the results were last brought to it: doing so takes a multiplication of
+// every result, and of 32 rows some one's maximum grows by a little in most steps.  float16's weights are times 2^11, 2^15 at the most.
+constexpr float kWideSlack = 4.f;  // log2
+template <typename T>
+constexpr float kWideUnit = __is_same(T, _Float16) ? 11.f : 0.f;
+
 template <int D, int RT>
 constexpr int kWideFloats = 64 * kWaves * 4 * (RT * (D / 32) * 4 + RT);
 
@@ -353,7 +359,7 @@ __global__ void __launch_bounds__(64 * kWaves, RT == 1 && D <= 128 ? 2 : 1) prom
     constexpr int kValueItems = 4 * kOct, kValuePasses = (kValueItems + 63) / 64;  // four keys, eight channels
     constexpr int kPiece = 2 * kSize;                      // dwords of eight elements in the cache
     constexpr int kCt = D / 32, kC = D / 16;
-    constexpr float kUnit = __is_same(T, _Float16) ? 15.f : 0.f;  // log2 of what a weight of 1 is
+    constexpr float kUnit = kWideUnit<T>;  // log2 of what a weight of 1 is, against a maximum that may be kWideSlack too low
     static_assert(16 * D % (kElems * 64) == 0, "");
 
     __shared__ __attribute__((aligned(16))) uint8_t lds[2 * (kKeyBytes + kValueBytes)];
@@ -607,13 +613,15 @@ __global__ void __launch_bounds__(64 * kWaves, RT == 1 && D <= 128 ? 2 : 1) prom
     auto rescale = [&](const float (&top)[RT]) {
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
-            if (__any(top[rt] > m[rt])) {
-                const float keep = __builtin_amdgcn_exp2f(m[rt] - (top[rt] == -INFINITY ? 0.f : top[rt]));
+            // the maximum that weights are taken against moves only where it is more than the slack too low
+            const bool moves = top[rt] > m[rt] + kWideSlack;
+            if (__any(moves)) {
+                const float to = moves ? top[rt] : m[rt], keep = moves ? __builtin_amdgcn_exp2f(m[rt] - to) : 1.f;
                 l[rt] *= keep;
 #pragma unroll
                 for (int ct = 0; ct < kCt; ++ct) acc[rt][ct] *= keep;
+                m[rt] = to;
             }
-            m[rt] = top[rt];
         }
     };
     auto weigh = [&](int s, const scores_t &x, vec8 (&weights)[RT][4]) {
@@ -1106,7 +1114,7 @@ __global__ void __launch_bounds__(64 * kWaves) prompt_join_kernel(const PromptPr
     constexpr int kAll = (Few ? 1 : kWaves) * RT * kBlocks;
     constexpr int kFloats = Few ? kFewFloats<D, RT> : kWideFloats<D, RT>;
     constexpr int kHalves = D > 128 && !Eight ? 2 : 1, kCh = D / 16 / kHalves, kOct = D / 8;
-    constexpr float kUnit = __is_same(T, _Float16) ? 15.f : 0.f;
+    constexpr float kUnit = !Few ? kWideUnit<T> : __is_same(T, _Float16) ? 15.f : 0.f;
     __shared__ float4_t lds_o[kWaves][64];
     __shared__ float lds_top[kWaves][64], lds_sum[kWaves][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
