@@ -103,6 +103,7 @@ struct PromptProblem {
     float scale_log2;           // |scale| * log2(e), above zero
     uint32_t q_and, q_xor;      // of two elements of q: the scale's sign, or nothing left where it is zero
     int target;     // work-groups to split the keys for; 0: a tile is one's
+    int64_t groups; // of all launches
     int base;       // the launch's first work-group
 };
 

@@ -129,7 +129,7 @@ __device__ __forceinline__ Keys uniform(const Keys &k)
 struct Work {
     int b, from, tokens, start;  // sequence, its first row of q, its new tokens, the first one's position
     int row0;                    // the tile's first row; -1: nothing
-    int part, chunk;             // steps chunk * part .. of the tile's keys
+    int part, parts, chunk;      // which of its parts, how many there are work-groups for, steps of one
     int first;                   // the work-group of the tile's first part; the others' are p.kv_heads apart
 };
 
@@ -184,7 +184,7 @@ __device__ __forceinline__ Work find_work(const PromptProblem &p, int rows, int 
     }
     auto parts_of = [&](int n) { return n <= chunk ? 1 : (n + chunk - 1) / chunk; };
     int at_chunk = 0, before = 0;
-    Work x{0, 0, 0, 0, -1, 0, chunk, 0};
+    Work x{0, 0, 0, 0, -1, 0, 1, chunk, 0};
     if (chunks == 1) {
         hold(0);
     } else {
@@ -215,9 +215,19 @@ __device__ __forceinline__ Work find_work(const PromptProblem &p, int rows, int 
     x.tokens = __builtin_amdgcn_readlane(count, at);
     x.start = __builtin_amdgcn_readlane(length, at) - x.tokens;
     x.part = uniform(local % n);
+    x.parts = n;
     x.row0 = uniform((__builtin_amdgcn_readlane(tiles, at) - 1 - local / n) * rows);
     x.first = uniform((mine - x.part) * p.kv_heads + head);
     return x;
+}
+
+// Work-groups that share a tile: by its own steps, which through a window may be more than the last tile's, for which work-groups were
+// counted.  0 if those are not all in the launch (starts that are none).
+__device__ __forceinline__ int parts_of(const PromptProblem &p, const Work &x, const Keys &k)
+{
+    int n = k.steps <= x.chunk ? 1 : (k.steps + x.chunk - 1) / x.chunk;
+    n = uniform(n < x.parts ? n : x.parts);
+    return n == 1 || (int64_t)x.first + (int64_t)(n - 1) * p.kv_heads < p.groups ? n : 0;
 }
 
 // A row's part of what is seen: positions up to `last`, above `above` or below `sinks`.  No branches: what follows from it are
@@ -380,7 +390,7 @@ __global__ void __launch_bounds__(64 * kWaves, RT == 1 && D <= 128 ? 2 : 1) prom
     if (p.target > 0 && tid == 0) record_of(p, index)->parts = 0;
     if (tile.row0 < 0) return;
     const Keys keys = uniform(keys_of(p, tile.start, tile.tokens, tile.row0, kRows, 2));
-    const int parts = uniform(keys.steps <= tile.chunk ? 1 : (keys.steps + tile.chunk - 1) / tile.chunk);  // work-groups that share the tile
+    const int parts = parts_of(p, tile, keys);
     if (tile.part >= parts) return;
     if (parts > 1 && tid == 0) *record_of(p, index) = {parts, tile.part, tile.first, tile.row0, tile.from, tile.tokens};
     const int s0 = uniform((int)((int64_t)keys.steps * tile.part / parts)), s1 = uniform((int)((int64_t)keys.steps * (tile.part + 1) / parts));
@@ -807,7 +817,7 @@ __global__ void __launch_bounds__(64 * kWaves, D > 128 ? 1 : 2) prompt_few_kerne
     if (p.target > 0 && tid == 0) record_of(p, index)->parts = 0;
     if (tile.row0 < 0) return;
     const Keys keys = uniform(keys_of(p, tile.start, tile.tokens, tile.row0, kRows, 1));
-    const int parts = uniform(keys.steps <= tile.chunk ? 1 : (keys.steps + tile.chunk - 1) / tile.chunk);  // work-groups that share the tile
+    const int parts = parts_of(p, tile, keys);
     if (tile.part >= parts) return;
     if (parts > 1 && tid == 0) *record_of(p, index) = {parts, tile.part, tile.first, tile.row0, tile.from, tile.tokens};
     const int s0 = uniform((int)((int64_t)keys.steps * tile.part / parts)), s1 = uniform((int)((int64_t)keys.steps * (tile.part + 1) / parts));
@@ -1221,6 +1231,7 @@ hipError_t launch_one(const PromptProblem &p, const PromptPlan &plan, hipStream_
 {
     PromptProblem q = p;
     q.target = plan.target;
+    q.groups = plan.groups;
     q.records = (char *)p.partials + (size_t)plan.groups * plan.slot_floats * sizeof(float);  // behind the pieces
     const void *kernel, *join;
     if (!plan.few) {
@@ -1269,7 +1280,8 @@ PromptPlan plan_prompt(int64_t tokens, int64_t B, int64_t heads, int64_t kv_head
     const int64_t tiles = (rows / x.rows + sequences) * kv_heads, target = x.few ? kFewGroups : kWideGroups;  // tiles at the most
     const int64_t least = x.few ? (int64_t)kFewLeast << 5 : (int64_t)kWideLeast << 6;  // keys of a part at the least
     x.target = tiles < target && positions > least ? (int)target : 0;
-    x.groups = tiles + x.target;  // a tile's last part is not a whole one
+    // a tile's last part is not a whole one; and the steps are added up in floats
+    x.groups = tiles + (x.target ? x.target + 2 * kv_heads : 0);
     x.slot_floats = x.few ? 64 * 4 * (x.rows / 16) * (head_dim / 16 + 1) : 64 * kWaves * 4 * (head_dim / 32 * 4 + 1);
     return x;
 }

@@ -224,6 +224,20 @@ def test_keys_shared_by_work_groups(mk, new, cached, hq, hkv, D, bits):
     check(mk, args, window=2000, sinks=70)
 
 
+@pytest.mark.parametrize("new,hq", [(130, 1), (18, 2)])
+def test_shared_keys_behind_windows(mk, new, hq):
+    """The last tile of a sequence has two rows, whose window is of fewer steps than that of those before; at every remainder."""
+    for window in range(1500, 2140, 33):
+        check(mk, make(window, [2600], [new], hq, 1, 64, 16, F16, 16), window=window, sinks=window % 40)
+
+
+@pytest.mark.parametrize("new", [None, [5, 3], [90, 70]])
+@pytest.mark.parametrize("bits", [8, 16])
+@pytest.mark.parametrize("scale", [0.0, -0.2, 1e-42, 3.0])
+def test_scales_of_the_softmax(mk, new, bits, scale):
+    check(mk, make(3, [100, 90], new, 4, 2, 64, 16, F16, bits), scale=scale)
+
+
 @pytest.mark.parametrize("n", [63, 64, 65, 500, 4200])
 def test_many_sequences(mk, n):
     new = [(i * 7) % 4 if i % 50 else 20 for i in range(n)]
