@@ -114,7 +114,7 @@ struct PromptPlan {
     int64_t groups;
 };
 // positions: of a table's row, at most.
-PromptPlan plan_prompt(int64_t tokens, int64_t B, int64_t heads, int64_t kv_heads, int head_dim, int64_t positions);
+PromptPlan plan_prompt(int64_t tokens, int64_t B, int64_t heads, int64_t kv_heads, int head_dim, bool eight, int64_t positions);
 size_t prompt_workspace(const PromptPlan &plan);  // bytes behind the counters
 
 hipError_t launch_prompt(const PromptProblem &p, const PromptPlan &plan, int head_dim, marlin_dtype_t dtype, hipStream_t stream);

@@ -272,7 +272,12 @@ size_t marlin_cache_attention_workspace_bytes(int64_t starts, int64_t tokens, in
 {
     if (!shape_ok(B, heads, kv_heads, head_dim, 1, 16, 1) || !rows_of_tokens_ok(tokens, heads, kv_heads)) return 0;
     if (!starts) return marlin_paged_attention_workspace_bytes(head_dim);
-    return kCounterRegionBytes + prompt_workspace(plan_prompt(tokens, B, heads, kv_heads, (int)head_dim, kMaxPositions));
+    size_t most = 0;
+    for (const bool eight : {false, true}) {
+        const size_t x = prompt_workspace(plan_prompt(tokens, B, heads, kv_heads, (int)head_dim, eight, kMaxPositions));
+        if (x > most) most = x;
+    }
+    return kCounterRegionBytes + most;
 }
 
 marlin_status_t marlin_cache_attention(const marlin_cache_attention_args *a, hipStream_t stream)
@@ -329,7 +334,7 @@ marlin_status_t marlin_cache_attention(const marlin_cache_attention_args *a, hip
         p.scale_log2 = std::fabs(scale) > least ? std::fabs(scale) : least;
         p.q_and = std::fabs(scale) > 0 ? 0xFFFFFFFFu : 0u;
         p.q_xor = scale < 0 ? 0x80008000u : 0u;
-        const PromptPlan plan = plan_prompt(a->tokens, a->B, a->heads, a->kv_heads, (int)a->head_dim, a->width * a->page_size);
+        const PromptPlan plan = plan_prompt(a->tokens, a->B, a->heads, a->kv_heads, (int)a->head_dim, a->scales != nullptr, a->width * a->page_size);
         return launch_prompt(p, plan, (int)a->head_dim, (marlin_dtype_t)a->dtype, stream) == hipSuccess ? MARLIN_OK : MARLIN_ERR_HIP;
     }
     int device = 0;

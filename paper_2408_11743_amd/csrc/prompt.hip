@@ -34,12 +34,21 @@ using namespace dev;
 typedef float float16_t __attribute__((ext_vector_type(16)));
 
 constexpr int kWaves = 4;
+template <int N>
+struct Constant {
+    static constexpr int value = N;
+};
+constexpr int kSearch = 6;  // tries to find how large parts are
 
-// Work-groups that a call's keys are split for where there are fewer tiles: of many rows two a compute unit, as many as it holds; of
-// few rows it holds three, and tiles' last parts, which are not whole ones, come on top (32 sequences of up to 8000 tokens, four new
-// ones each, 8 bits, 32 heads over 8: 41.7 us, for 768 work-groups 48, for 1024 47).
-constexpr int kWideGroups = 512, kFewGroups = 640;
-constexpr int kWideLeast = 4, kFewLeast = 4 * kWaves;  // steps of a part
+// Parts of a tile's keys, counted in steps of many rows, in rounds of the four waves' steps of few: at most the root of kRoot times
+// as many, as joining takes longer the more there are, and none of less than kLeast.  One sequence, 32 heads over 8 of 128 channels, 16 bits, four
+// new tokens: 2000 long 12.0 us (half the parts: 14.3, parts of four rounds: 14.0), 20000 long 22.7 (half the root's square 24.3, double 27.9); 64 new ones behind 8000: 30.2 (33.5 and 31.3).
+struct Many {
+    static constexpr int kShift = 2, kLeast = 3, kRoot = 2;  // 16-key tiles of a step (log2)
+};
+struct Few {
+    static constexpr int kShift = 3, kLeast = 2, kRoot = 4;  // of a round
+};
 
 __device__ __forceinline__ float16_t mfma32(Elem<_Float16>::vec8 a, Elem<_Float16>::vec8 b, float16_t c)
 {
@@ -129,15 +138,44 @@ __device__ __forceinline__ Keys uniform(const Keys &k)
 struct Work {
     int b, from, tokens, start;  // sequence, its first row of q, its new tokens, the first one's position
     int row0;                    // the tile's first row; -1: nothing
-    int part, parts, chunk;      // which of its parts, how many there are work-groups for, steps of one
+    int part, parts, chunk;      // which of its parts, how many there are work-groups for, steps (rounds) of one
     int first;                   // the work-group of the tile's first part; the others' are p.kv_heads apart
 };
 
+// The sum over the lanes.
+__device__ __forceinline__ float wave_sum(float x)
+{
+    auto moved = [](float y, auto control, auto rows) {
+        return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, y), control.value, rows.value, 0xf, true));
+    };
+    x += moved(x, Constant<0x111>{}, Constant<0xf>{});  // row_shr:1
+    x += moved(x, Constant<0x112>{}, Constant<0xf>{});
+    x += moved(x, Constant<0x114>{}, Constant<0xf>{});
+    x += moved(x, Constant<0x118>{}, Constant<0xf>{});
+    x += moved(x, Constant<0x142>{}, Constant<0xa>{});  // row_bcast:15 into rows 1 and 3
+    x += moved(x, Constant<0x143>{}, Constant<0xc>{});  // row_bcast:31 into rows 2 and 3
+    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), 63));
+}
+
+// Parts that n steps (rounds) are split into, of `chunk` where they may be as small.
+template <typename Kind>
+__device__ __forceinline__ int parts_for(int n, int chunk)
+{
+    if (n <= chunk) return 1;
+    int x = (n + chunk - 1) / chunk;
+    const int root = (int)__builtin_amdgcn_sqrtf((float)Kind::kRoot * (float)n), most = n / Kind::kLeast;
+    if (x > root) x = root;
+    if (x > most) x = most;
+    return x < 1 ? 1 : x;
+}
+
 // The work of one of a kv head's work-groups, found from the sequences' starts and lengths: tiles of `rows` rows, the last of a
-// sequence first, as it sees the most, in parts of `chunk` steps of 2^shift 16-key tiles, which is what all tiles' steps make for each of p.target work-groups
-// (where there are as many tiles as that, a part is all of a tile).
+// sequence first, as it sees the most, in parts.  A part is as small as it can be with all of them running at once (p.target work-groups):
+// 256 new tokens behind 8000 to 30000, four sequences, 32 heads over 8: 395 us, in parts of what all make for each of 512 work-groups 427.
+// Where there are as many tiles as that, it is all of a tile.
 // 64 sequences are held in the lanes; of more, the waves share the sums.
-__device__ __forceinline__ Work find_work(const PromptProblem &p, int rows, int shift, int least, int index, int lane, int wave, int *lds_chunks)
+template <typename Kind>
+__device__ __forceinline__ Work find_work(const PromptProblem &p, int rows, int index, int lane, int wave, int *lds_chunks)
 {
     const int chunks = (p.B + 63) / 64, head = uniform(index % p.kv_heads), mine = uniform(index / p.kv_heads);
     int held = -1, begin = 0, count = 0, length = 0, tiles = 0, steps = 0;
@@ -155,34 +193,48 @@ __device__ __forceinline__ Work find_work(const PromptProblem &p, int rows, int 
             length = p.lengths[b];
             if (length < 0) length = 0;
             tiles = (count * p.group + rows - 1) / rows;
-            if (p.target > 0 && tiles > 0) steps = keys_of(p, length - count, count, (tiles - 1) * rows, rows, shift).steps;
+            if (p.target > 0 && tiles > 0) steps = keys_of(p, length - count, count, (tiles - 1) * rows, rows, Kind::kShift).steps;
         }
     };
-    // steps of a part: float sums, in the same order in every work-group
-    int chunk = 1 << 30;
-    if (p.target > 0) {
-        float total = 0.f;
+    // two sums over the sequences, in the same order in every work-group
+    auto sums_of = [&](auto of) {
+        Pair total{0.f, 0.f};
         for (int at = chunks == 1 ? 0 : wave; at < chunks; at += chunks == 1 ? 1 : kWaves) {
             hold(at);
-            float x = (float)tiles * (float)steps;
-#pragma unroll
-            for (int d = 32; d > 0; d >>= 1) x += __shfl_xor(x, d);
-            total += x;
+            const Pair x = of();
+            total.a += wave_sum(x.a);
+            total.b += wave_sum(x.b);
         }
         if (chunks > 1) {
-            if (lane == 0) lds_chunks[wave] = __builtin_bit_cast(int, total);
+            if (lane == 0) {
+                lds_chunks[2 * wave] = __builtin_bit_cast(int, total.a);
+                lds_chunks[2 * wave + 1] = __builtin_bit_cast(int, total.b);
+            }
             __syncthreads();
-            total = 0.f;
+            total = {0.f, 0.f};
 #pragma unroll
-            for (int w = 0; w < kWaves; ++w) total += __builtin_bit_cast(float, lds_chunks[w]);
+            for (int w = 0; w < kWaves; ++w) {
+                total.a += __builtin_bit_cast(float, lds_chunks[2 * w]);
+                total.b += __builtin_bit_cast(float, lds_chunks[2 * w + 1]);
+            }
             __syncthreads();
         }
-        const float each = total * (float)p.kv_heads / (float)p.target;
-        chunk = each < 1e9f ? (int)each + 1 : 1 << 30;
-        if (chunk < least) chunk = least;
-        chunk = __builtin_amdgcn_readfirstlane(chunk);
+        return Pair{total.a * (float)p.kv_heads, total.b * (float)p.kv_heads};
+    };
+    int chunk = 1 << 30;
+    if (p.target > 0) {
+        const float target = (float)p.target;
+        const Pair all = sums_of([&] { return Pair{(float)tiles, (float)tiles * (float)steps}; });
+        // half of a tile's last part is not there
+        const float each = all.b / fmaxf(target - 0.5f * all.a, 0.5f * target);
+        if (each < 1e8f) chunk = uniform((int)each + 1);
+        for (int i = 0; i < kSearch && chunk < 1 << 28; ++i) {
+            const float parts = sums_of([&] { return Pair{(float)tiles * (float)parts_for<Kind>(steps, chunk), 0.f}; }).a;
+            if (parts <= target) break;
+            const int next = (int)((float)chunk * (parts / target));
+            chunk = uniform(next > chunk ? next : chunk + 1);
+        }
     }
-    auto parts_of = [&](int n) { return n <= chunk ? 1 : (n + chunk - 1) / chunk; };
     int at_chunk = 0, before = 0;
     Work x{0, 0, 0, 0, -1, 0, 1, chunk, 0};
     if (chunks == 1) {
@@ -190,7 +242,7 @@ __device__ __forceinline__ Work find_work(const PromptProblem &p, int rows, int 
     } else {
         for (int at = wave; at < chunks; at += kWaves) {
             hold(at);
-            const int sum = wave_scan(tiles * parts_of(steps));
+            const int sum = wave_scan(tiles * parts_for<Kind>(steps, chunk));
             if (lane == 63) lds_chunks[at] = sum;
         }
         __syncthreads();
@@ -205,7 +257,7 @@ __device__ __forceinline__ Work find_work(const PromptProblem &p, int rows, int 
         if (at_chunk < 0) return x;
         hold(at_chunk);
     }
-    const int parts = parts_of(steps), items = tiles * parts, incl = wave_scan(items);
+    const int parts = parts_for<Kind>(steps, chunk), items = tiles * parts, incl = wave_scan(items);
     const uint64_t past = __builtin_amdgcn_ballot_w64(before + incl > mine);
     if (!past) return x;
     const int at = __builtin_ctzll(past);
@@ -221,11 +273,12 @@ __device__ __forceinline__ Work find_work(const PromptProblem &p, int rows, int 
     return x;
 }
 
-// Work-groups that share a tile: by its own steps, which through a window may be more than the last tile's, for which work-groups were
-// counted.  0 if those are not all in the launch (starts that are none).
-__device__ __forceinline__ int parts_of(const PromptProblem &p, const Work &x, const Keys &k)
+// Work-groups that share a tile: by its own steps (rounds), which through a window may be more than the last tile's, for which
+// work-groups were counted.  0 if those are not all in the launch (starts that are none).
+template <typename Kind>
+__device__ __forceinline__ int parts_of(const PromptProblem &p, const Work &x, int steps)
 {
-    int n = k.steps <= x.chunk ? 1 : (k.steps + x.chunk - 1) / x.chunk;
+    int n = parts_for<Kind>(steps, x.chunk);
     n = uniform(n < x.parts ? n : x.parts);
     return n == 1 || (int64_t)x.first + (int64_t)(n - 1) * p.kv_heads < p.groups ? n : 0;
 }
@@ -345,20 +398,20 @@ constexpr float kWideSlack = 4.f;  // log2
 template <typename T>
 constexpr float kWideUnit = __is_same(T, _Float16) ? 11.f : 0.f;
 
-template <int D, int RT>
-constexpr int kWideFloats = 64 * kWaves * 4 * (RT * (D / 32) * 4 + RT);
+template <int D>
+constexpr int kWideFloats = 64 * kWaves * 4 * ((D / 32) * 4 + 1);
 
-// RT: 32-row columns of a wave.  A wave brings 16 keys of a step, whose page is the same in all lanes, and all waves read all of them.
+// A wave has 32 rows.  It brings 16 keys of a step, whose page is the same in all lanes, and all waves read all of them.
 // K lies in LDS as [key][channel], V^T as [channel][key] with each 16 keys in the order 0-3, 8-11, 4-7, 12-15, rows 16 bytes further
 // apart than they are long, an odd number of 16-byte pieces: reads are of distinct banks, and at constant distances.  V^T's
-// rows are in an order of their own, eight-channel pieces side by side, so that the writes are of distinct banks too, and a
-// lane's results are whole pieces: row 8 * oct + j of the channels is row j * (D / 8) + oct (96 channels: four-channel pieces, below).
-template <typename T, int D, int RT, bool Eight>
-__global__ void __launch_bounds__(64 * kWaves, RT == 1 && D <= 128 ? 2 : 1) prompt_kernel(const PromptProblem p)
+// rows are in an order of their own, eight-channel pieces side by side, so that most writes are too (conflicts take 14 % of
+// the LDS's busy cycles, 22 % in an 8-bit cache; an order of the lanes without them took the same time), and a lane's results are whole pieces: row 8 * oct + j of the channels is row j * (D / 8) + oct (96 channels: four-channel pieces, below).
+template <typename T, int D, bool Eight>
+__global__ void __launch_bounds__(64 * kWaves, D <= 128 ? 2 : 1) prompt_kernel(const PromptProblem p)
 {
     typedef Elem<T> E;
     typedef typename E::vec8 vec8;
-    constexpr int kRows = 32 * RT * kWaves;
+    constexpr int kRows = 32 * kWaves;
     constexpr int kOct = D / 8;                            // eight-channel pieces of a row
     constexpr int kSize = Eight ? 1 : 2;                   // bytes of an element in the cache
     constexpr int kKeyRow = D * 2 + 16, kValueRow = kStep * 2 + 16;  // bytes in LDS
@@ -386,11 +439,11 @@ __global__ void __launch_bounds__(64 * kWaves, RT == 1 && D <= 128 ? 2 : 1) prom
     const int col = lane & 31, half = lane >> 5;
     const int index = p.base + blockIdx.x;
     const int head = uniform(index % p.kv_heads);
-    const Work tile = find_work(p, kRows, 2, kWideLeast, index, lane, wave, (int *)lds);
+    const Work tile = find_work<Many>(p, kRows, index, lane, wave, (int *)lds);
     if (p.target > 0 && tid == 0) record_of(p, index)->parts = 0;
     if (tile.row0 < 0) return;
-    const Keys keys = uniform(keys_of(p, tile.start, tile.tokens, tile.row0, kRows, 2));
-    const int parts = parts_of(p, tile, keys);
+    const Keys keys = uniform(keys_of(p, tile.start, tile.tokens, tile.row0, kRows, Many::kShift));
+    const int parts = parts_of<Many>(p, tile, keys.steps);
     if (tile.part >= parts) return;
     if (parts > 1 && tid == 0) *record_of(p, index) = {parts, tile.part, tile.first, tile.row0, tile.from, tile.tokens};
     const int s0 = uniform((int)((int64_t)keys.steps * tile.part / parts)), s1 = uniform((int)((int64_t)keys.steps * (tile.part + 1) / parts));
@@ -399,21 +452,16 @@ __global__ void __launch_bounds__(64 * kWaves, RT == 1 && D <= 128 ? 2 : 1) prom
     const int32_t *const table = p.table + (int64_t)tile.b * p.table_row;
     auto position_of = [&](int s, int u) { return keys.position(4 * s + u); };  // of a step's tile
 
-    // this lane's rows
-    Sight sight[RT];
-    vec8 qf[RT][kC];
-    int64_t out_at[RT];
+    // this lane's row
+    const int row = tile.row0 + wave * 32 + col;
+    const Sight sight = sight_of(p, tile, row);
+    vec8 qf[kC];
+    const bool have = row < tile.tokens * p.group;
+    const int token = tile.from + (have ? row / p.group : 0), h = head * p.group + (have ? row % p.group : 0);
+    const int64_t out_at = have ? (int64_t)token * p.heads + h : -1;
+    const T *q = (const T *)p.q + token * p.q_row + h * p.q_head + 8 * half;
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-        const int row = tile.row0 + (wave * RT + rt) * 32 + col;
-        sight[rt] = sight_of(p, tile, row);
-        const bool have = row < tile.tokens * p.group;
-        const int token = tile.from + (have ? row / p.group : 0), h = head * p.group + (have ? row % p.group : 0);
-        out_at[rt] = have ? (int64_t)token * p.heads + h : -1;
-        const T *q = (const T *)p.q + token * p.q_row + h * p.q_head + 8 * half;
-#pragma unroll
-        for (int c = 0; c < kC; ++c) qf[rt][c] = query_of<vec8>(p, q + 16 * c, have);
-    }
+    for (int c = 0; c < kC; ++c) qf[c] = query_of<vec8>(p, q + 16 * c, have);
 
     // ---- a step's keys and values: this wave's tile of 16 keys, to registers and from there to LDS ----
     // Keys are a step ahead of values: while a step's weights are found and its values summed up, the next one's scores are.
@@ -556,117 +604,98 @@ __global__ void __launch_bounds__(64 * kWaves, RT == 1 && D <= 128 ? 2 : 1) prom
         return 8 * (row % kOct) + row / kOct + 32 * half;
     };
 
-    float16_t acc[RT][kCt];
-    float m[RT], l[RT];
+    float16_t acc[kCt];
+    float m = -INFINITY, l = 0.f;
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-        m[rt] = -INFINITY;
-        l[rt] = 0.f;
-#pragma unroll
-        for (int ct = 0; ct < kCt; ++ct) acc[rt][ct] = float16_t{};
-    }
+    for (int ct = 0; ct < kCt; ++ct) acc[ct] = float16_t{};
 
-    typedef float16_t scores_t[RT][2];
+    typedef float16_t scores_t[2];
     const uint32_t key_at = col * kKeyRow + half * 16, value_at = 2 * kKeyBytes + col * kValueRow + half * 16;
     auto score = [&](int s, scores_t &x) {
         const uint8_t *const from = lds + (s & 1) * kKeyBytes + key_at;
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt) x[rt][0] = x[rt][1] = float16_t{};
+        x[0] = x[1] = float16_t{};
 #pragma unroll
         for (int c = 0; c < kC; ++c)
 #pragma unroll
             for (int kt = 0; kt < 2; ++kt) {
                 const vec8 a = *(const vec8 *)(from + 32 * kt * kKeyRow + c * 32);
-#pragma unroll
-                for (int rt = 0; rt < RT; ++rt) x[rt][kt] = mfma32(a, qf[rt][c], x[rt][kt]);
+                x[kt] = mfma32(a, qf[c], x[kt]);
             }
     };
     // which of a step's tiles are there
     auto ok_of = [&](int s) { return (uint32_t)__builtin_amdgcn_ballot_w64(lds_info[s & 3].ok[lane & 3] != 0) & 15u; };
     // scores that are not seen, then the maximum (of what the factors make of them) with the sums brought to it
-    auto look = [&](int s, bool inside, scores_t &x, float (&top)[RT]) {
+    auto look = [&](int s, bool inside, scores_t &x, float &top) {
         const uint32_t ok = ok_of(s);
         if (!(inside && ok == 15u)) {
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt)
+            for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
-                for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const int j = position_of(s, 2 * kt + (i >> 3)) + 8 * ((i >> 2) & 1) + 4 * half + (i & 3);
-                        const bool seen = ((ok >> (2 * kt + (i >> 3)) & 1) != 0) & sight[rt].sees(j) & (j < keys.end);
-                        x[rt][kt][i] = seen ? x[rt][kt][i] : -INFINITY;
-                    }
-        }
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt) {
-            float t = m[rt];
-            if constexpr (Eight) {
-                const Info &info = lds_info[s & 3];
-#pragma unroll
-                for (int g16 = 0; g16 < 4; ++g16) {
-                    float y = x[rt][g16 >> 1][8 * (g16 & 1)];
-#pragma unroll
-                    for (int e = 1; e < 8; ++e) y = fmaxf(y, x[rt][g16 >> 1][8 * (g16 & 1) + e]);
-                    t = fmaxf(t, __builtin_fmaf(y, info.factor[g16], info.add[g16]));
+                for (int i = 0; i < 16; ++i) {
+                    const int j = position_of(s, 2 * kt + (i >> 3)) + 8 * ((i >> 2) & 1) + 4 * half + (i & 3);
+                    const bool seen = ((ok >> (2 * kt + (i >> 3)) & 1) != 0) & sight.sees(j) & (j < keys.end);
+                    x[kt][i] = seen ? x[kt][i] : -INFINITY;
                 }
-            } else {
-                float y = x[rt][0][0];
-#pragma unroll
-                for (int e = 1; e < 32; ++e) y = fmaxf(y, x[rt][e >> 4][e & 15]);
-                t = fmaxf(t, y * p.scale_log2);
-            }
-            const Pair halves = exchange<32>(t);
-            top[rt] = fmaxf(halves.a, halves.b);
         }
-    };
-    auto rescale = [&](const float (&top)[RT]) {
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt) {
-            // the maximum that weights are taken against moves only where it is more than the slack too low
-            const bool moves = top[rt] > m[rt] + kWideSlack;
-            if (__any(moves)) {
-                const float to = moves ? top[rt] : m[rt], keep = moves ? __builtin_amdgcn_exp2f(m[rt] - to) : 1.f;
-                l[rt] *= keep;
-#pragma unroll
-                for (int ct = 0; ct < kCt; ++ct) acc[rt][ct] *= keep;
-                m[rt] = to;
-            }
-        }
-    };
-    auto weigh = [&](int s, const scores_t &x, vec8 (&weights)[RT][4]) {
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt) {
-            const float unit = kUnit - (m[rt] == -INFINITY ? 0.f : m[rt]);
+        float t = m;
+        if constexpr (Eight) {
+            const Info &info = lds_info[s & 3];
 #pragma unroll
             for (int g16 = 0; g16 < 4; ++g16) {
-                float f = p.scale_log2, add = unit, sum = 0.f;
-                if constexpr (Eight) {
-                    f = lds_info[s & 3].factor[g16];
-                    add += lds_info[s & 3].add[g16];
-                }
+                float y = x[g16 >> 1][8 * (g16 & 1)];
 #pragma unroll
-                for (int e = 0; e < 8; e += 2) {
-                    const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(x[rt][g16 >> 1][8 * (g16 & 1) + e], f, add));
-                    const float z = __builtin_amdgcn_exp2f(__builtin_fmaf(x[rt][g16 >> 1][8 * (g16 & 1) + e + 1], f, add));
-                    sum += y + z;
-                    weights[rt][g16][e] = (T)y;
-                    weights[rt][g16][e + 1] = (T)z;
-                }
-                if constexpr (Eight) sum *= lds_info[s & 3].times[g16];
-                l[rt] += sum;
+                for (int e = 1; e < 8; ++e) y = fmaxf(y, x[g16 >> 1][8 * (g16 & 1) + e]);
+                t = fmaxf(t, __builtin_fmaf(y, info.factor[g16], info.add[g16]));
             }
+        } else {
+            float y = x[0][0];
+#pragma unroll
+            for (int e = 1; e < 32; ++e) y = fmaxf(y, x[e >> 4][e & 15]);
+            t = fmaxf(t, y * p.scale_log2);
+        }
+        const Pair halves = exchange<32>(t);
+        top = fmaxf(halves.a, halves.b);
+    };
+    auto rescale = [&](float top) {
+        // the maximum that weights are taken against moves only where it is more than the slack too low
+        const bool moves = top > m + kWideSlack;
+        if (__any(moves)) {
+            const float to = moves ? top : m, keep = moves ? __builtin_amdgcn_exp2f(m - to) : 1.f;
+            l *= keep;
+#pragma unroll
+            for (int ct = 0; ct < kCt; ++ct) acc[ct] *= keep;
+            m = to;
         }
     };
-    auto add_values = [&](int s, const vec8 (&weights)[RT][4]) {
+    auto weigh = [&](int s, const scores_t &x, vec8 (&weights)[4]) {
+        const float unit = kUnit - (m == -INFINITY ? 0.f : m);
+#pragma unroll
+        for (int g16 = 0; g16 < 4; ++g16) {
+            float f = p.scale_log2, add = unit, sum = 0.f;
+            if constexpr (Eight) {
+                f = lds_info[s & 3].factor[g16];
+                add += lds_info[s & 3].add[g16];
+            }
+#pragma unroll
+            for (int e = 0; e < 8; e += 2) {
+                const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(x[g16 >> 1][8 * (g16 & 1) + e], f, add));
+                const float z = __builtin_amdgcn_exp2f(__builtin_fmaf(x[g16 >> 1][8 * (g16 & 1) + e + 1], f, add));
+                sum += y + z;
+                weights[g16][e] = (T)y;
+                weights[g16][e + 1] = (T)z;
+            }
+            if constexpr (Eight) sum *= lds_info[s & 3].times[g16];
+            l += sum;
+        }
+    };
+    auto add_values = [&](int s, const vec8 (&weights)[4]) {
         const uint8_t *const from = lds + (s & 1) * kValueBytes + value_at;
 #pragma unroll
         for (int g16 = 0; g16 < 4; ++g16)
 #pragma unroll
             for (int ct = 0; ct < kCt; ++ct) {
                 const vec8 a = *(const vec8 *)(from + 32 * ct * kValueRow + g16 * 32);
-#pragma unroll
-                for (int rt = 0; rt < RT; ++rt) acc[rt][ct] = mfma32(a, weights[rt][g16], acc[rt][ct]);
+                acc[ct] = mfma32(a, weights[g16], acc[ct]);
             }
     };
     // values of a step that are not finite, where some rows do not see all keys
@@ -687,16 +716,15 @@ __global__ void __launch_bounds__(64 * kWaves, RT == 1 && D <= 128 ? 2 : 1) prom
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
                     const float x = odd_at<T, Eight>(p.v, at + channel_of(ct, i));
-#pragma unroll
-                    for (int rt = 0; rt < RT; ++rt) acc[rt][ct][i] += sight[rt].sees(j) ? x : 0.f;
+                    acc[ct][i] += sight.sees(j) ? x : 0.f;
                 }
         }
     };
 
     if (s0 < s1) {
         scores_t x, ahead;
-        vec8 weights[RT][4];
-        float top[RT];
+        vec8 weights[4];
+        float top;
         int entry = entry_of(s0 + 1);
         Mine values = load_keys(s0, entry_of(s0)), next = values;  // of the step whose values are to come next; of the one after it
         store_keys(s0, values);
@@ -727,59 +755,48 @@ __global__ void __launch_bounds__(64 * kWaves, RT == 1 && D <= 128 ? 2 : 1) prom
             store_values(s + 1, values);
             store_keys(s + 2, next);
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-                for (int kt = 0; kt < 2; ++kt) x[rt][kt] = ahead[rt][kt];
+            for (int kt = 0; kt < 2; ++kt) x[kt] = ahead[kt];
         }
         __syncthreads();
         weigh(s1 - 1, x, weights);
         add_values(s1 - 1, weights);
         add_odd(s1 - 1, inside);
     }
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-        const Pair halves = exchange<32>(l[rt]);
-        l[rt] = halves.a + halves.b;
-    }
+    const Pair halves = exchange<32>(l);
+    l = halves.a + halves.b;
 
     // ---- a part of the tile's keys: left for the joining kernel ----
     if (parts > 1) {
-        float4_t *const slot = (float4_t *)(p.partials + (int64_t)index * kWideFloats<D, RT>) + lane;
-        constexpr int kPer = RT * (kCt * 4 + 1);  // blocks of 64 float4 of a wave
+        float4_t *const slot = (float4_t *)(p.partials + (int64_t)index * kWideFloats<D>) + lane;
+        constexpr int kPer = kCt * 4 + 1;  // blocks of 64 float4 of a wave
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt) {
+        for (int ct = 0; ct < kCt; ++ct)
 #pragma unroll
-            for (int ct = 0; ct < kCt; ++ct)
-#pragma unroll
-                for (int q = 0; q < 4; ++q)
-                    slot[(wave * kPer + rt * (kCt * 4 + 1) + ct * 4 + q) * 64] =
-                        float4_t{acc[rt][ct][4 * q], acc[rt][ct][4 * q + 1], acc[rt][ct][4 * q + 2], acc[rt][ct][4 * q + 3]};
-            slot[(wave * kPer + rt * (kCt * 4 + 1) + kCt * 4) * 64] = float4_t{m[rt], l[rt], 0.f, 0.f};
-        }
+            for (int q = 0; q < 4; ++q)
+                slot[(wave * kPer + ct * 4 + q) * 64] =
+                    float4_t{acc[ct][4 * q], acc[ct][4 * q + 1], acc[ct][4 * q + 2], acc[ct][4 * q + 3]};
+        slot[(wave * kPer + kCt * 4) * 64] = float4_t{m, l, 0.f, 0.f};
         return;
     }
 
-    // ---- the finished rows: a lane holds pieces of eight channels (96: of four) ----
+    // ---- the finished row: a lane holds pieces of eight channels (96: of four) ----
+    if (out_at < 0) return;
+    const float inv = 1.f / l;
+    T *const to = (T *)p.out + out_at * D;
+    auto result = [&](int ct, int i) { return l == 0.f ? (T)0.f : (T)(acc[ct][i] * inv); };
+    constexpr int kPieces = D == 96 ? 12 : D / 16, kChannels = D == 96 ? 4 : 8;  // a lane's
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-        if (out_at[rt] < 0) continue;
-        const float inv = 1.f / l[rt];
-        T *const to = (T *)p.out + out_at[rt] * D;
-        auto result = [&](int ct, int i) { return l[rt] == 0.f ? (T)0.f : (T)(acc[rt][ct][i] * inv); };
-        constexpr int kPieces = D == 96 ? 12 : D / 16, kChannels = D == 96 ? 4 : 8;  // a lane's
+    for (int n = 0; n < kPieces; ++n) {
+        T y[kChannels];
 #pragma unroll
-        for (int n = 0; n < kPieces; ++n) {
-            T y[kChannels];
-#pragma unroll
-            for (int j = 0; j < kChannels; ++j) {
-                // D = 96: four 8 ct + 4 half + i, its channels in q = j; else piece 8 (n / 4) + 4 half + n % 4, channel j in row j * kOct + piece
-                const int row = j * kOct + 8 * (n >> 2) + (n & 3);
-                y[j] = D == 96 ? result(n >> 2, 4 * j + (n & 3)) : result(row >> 5, 4 * ((row & 31) >> 3) + (n & 3));
-            }
-            __builtin_memcpy(__builtin_assume_aligned(to + kChannels * (8 * (n >> 2) + 4 * half + (n & 3)), 2 * kChannels), y, 2 * kChannels);
+        for (int j = 0; j < kChannels; ++j) {
+            // D = 96: four 8 ct + 4 half + i, its channels in q = j; else piece 8 (n / 4) + 4 half + n % 4, channel j in row j * kOct + piece
+            const int row = j * kOct + 8 * (n >> 2) + (n & 3);
+            y[j] = D == 96 ? result(n >> 2, 4 * j + (n & 3)) : result(row >> 5, 4 * ((row & 31) >> 3) + (n & 3));
         }
-        if (p.lse && half == 0) p.lse[out_at[rt]] = (m[rt] + __builtin_amdgcn_logf(l[rt]) - kUnit) * 0.693147180559945f;
+        __builtin_memcpy(__builtin_assume_aligned(to + kChannels * (8 * (n >> 2) + 4 * half + (n & 3)), 2 * kChannels), y, 2 * kChannels);
     }
+    if (p.lse && half == 0) p.lse[out_at] = (m + __builtin_amdgcn_logf(l) - kUnit) * 0.693147180559945f;
 }
 
 // ---- few rows: keys and values straight to registers, the waves share the keys ----
@@ -813,14 +830,15 @@ __global__ void __launch_bounds__(64 * kWaves, D > 128 ? 1 : 2) prompt_few_kerne
     const int r = lane & 15, g = lane >> 4;
     const int index = p.base + blockIdx.x;
     const int head = uniform(index % p.kv_heads);
-    const Work tile = find_work(p, kRows, 1, kFewLeast, index, lane, wave, (int *)&lds_acc[0][0][0]);
+    const Work tile = find_work<Few>(p, kRows, index, lane, wave, (int *)&lds_acc[0][0][0]);
     if (p.target > 0 && tid == 0) record_of(p, index)->parts = 0;
     if (tile.row0 < 0) return;
     const Keys keys = uniform(keys_of(p, tile.start, tile.tokens, tile.row0, kRows, 1));
-    const int parts = parts_of(p, tile, keys);
+    const int rounds = (keys.steps + kWaves - 1) / kWaves, parts = parts_of<Few>(p, tile, rounds);
     if (tile.part >= parts) return;
     if (parts > 1 && tid == 0) *record_of(p, index) = {parts, tile.part, tile.first, tile.row0, tile.from, tile.tokens};
-    const int s0 = uniform((int)((int64_t)keys.steps * tile.part / parts)), s1 = uniform((int)((int64_t)keys.steps * (tile.part + 1) / parts));
+    const int s0 = uniform((int)((int64_t)rounds * tile.part / parts)) * kWaves, last = uniform((int)((int64_t)rounds * (tile.part + 1) / parts)) * kWaves;
+    const int s1 = last < keys.steps ? last : keys.steps;
     __syncthreads();
 
     const int32_t *const table = p.table + (int64_t)tile.b * p.table_row;
@@ -1122,7 +1140,7 @@ __global__ void __launch_bounds__(64 * kWaves) prompt_join_kernel(const PromptPr
 {
     constexpr int kBlocks = Few ? D / 16 : D / 8;  // of a wave's rows
     constexpr int kAll = (Few ? 1 : kWaves) * RT * kBlocks;
-    constexpr int kFloats = Few ? kFewFloats<D, RT> : kWideFloats<D, RT>;
+    constexpr int kFloats = Few ? kFewFloats<D, RT> : kWideFloats<D>;
     constexpr int kHalves = D > 128 && !Eight ? 2 : 1, kCh = D / 16 / kHalves, kOct = D / 8;
     constexpr float kUnit = !Few ? kWideUnit<T> : __is_same(T, _Float16) ? 15.f : 0.f;
     __shared__ float4_t lds_o[kWaves][64];
@@ -1235,14 +1253,16 @@ hipError_t launch_one(const PromptProblem &p, const PromptPlan &plan, hipStream_
     q.records = (char *)p.partials + (size_t)plan.groups * plan.slot_floats * sizeof(float);  // behind the pieces
     const void *kernel, *join;
     if (!plan.few) {
-        kernel = (const void *)&prompt_kernel<T, D, 1, Eight>;
+        kernel = (const void *)&prompt_kernel<T, D, Eight>;
         join = (const void *)&prompt_join_kernel<T, D, 1, false, Eight>;
     } else if (plan.rows == 16) {
         kernel = (const void *)&prompt_few_kernel<T, D, 1, Eight>;
         join = (const void *)&prompt_join_kernel<T, D, 1, true, Eight>;
-    } else {
+    } else if constexpr (D != 128 || Eight) {
         kernel = (const void *)&prompt_few_kernel<T, D, 2, Eight>;
         join = (const void *)&prompt_join_kernel<T, D, 2, true, Eight>;
+    } else {
+        return hipErrorInvalidValue;
     }
     const int64_t most = ((int64_t)1 << 24) / p.kv_heads * p.kv_heads - p.kv_heads;
     for (int64_t base = 0; base < plan.groups; base += most) {  // a launch takes less than 2^32 threads
@@ -1270,18 +1290,26 @@ hipError_t launch_typed(const PromptProblem &p, const PromptPlan &plan, int head
 
 }  // namespace
 
-PromptPlan plan_prompt(int64_t tokens, int64_t B, int64_t heads, int64_t kv_heads, int head_dim, int64_t positions)
+PromptPlan plan_prompt(int64_t tokens, int64_t B, int64_t heads, int64_t kv_heads, int head_dim, bool eight, int64_t positions)
 {
     PromptPlan x;
     const int64_t rows = tokens * (heads / kv_heads);  // of one kv head
     const int64_t sequences = B < tokens ? B : tokens;
-    x.few = rows <= 64 * sequences;
+    // Few rows: as long as registers hold what a wave needs.  16 sequences of 1000 to 8000 tokens, 64 rows of new ones for each of 8
+    // kv heads (4 of 256 channels): 38.5 us by the kernel for few rows, 44 by the other one (64 channels), 55 and 58 (96), 57 and 66 (128, 8 bits), 82 and
+    // 110 (256); 96 rows: 50 and 46, 73 and 61, 82 and 68, 113 and 110.  In 16 bits two columns of 128 channels do not fit: 32 sequences, 32 rows: 163 and 119.
+    const int few_rows = head_dim == 128 && !eight ? 16 : 64;
+    x.few = rows <= few_rows * sequences;
     x.rows = x.few ? (rows <= 16 * sequences ? 16 : 32) : 32 * kWaves;
-    const int64_t tiles = (rows / x.rows + sequences) * kv_heads, target = x.few ? kFewGroups : kWideGroups;  // tiles at the most
-    const int64_t least = x.few ? (int64_t)kFewLeast << 5 : (int64_t)kWideLeast << 6;  // keys of a part at the least
-    x.target = tiles < target && positions > least ? (int)target : 0;
+    // work-groups that run at once: by the registers, those of many rows by the LDS too
+    int per_cu = head_dim == 256 ? 1 : 2;
+    if (x.few && head_dim == 64) per_cu = x.rows == 16 ? 4 : 3;
+    if (x.few && x.rows == 16 && (head_dim == 96 || (head_dim == 128 && eight))) per_cu = 3;
+    const int64_t target = 256 * per_cu, least = rows / x.rows * kv_heads, most = (rows / x.rows + sequences) * kv_heads;  // tiles
+    const int64_t steps = positions >> 4 >> (x.few ? Few::kShift : Many::kShift);
+    x.target = least < target && most < 2 * target && steps >= 2 * (x.few ? Few::kLeast : Many::kLeast) ? (int)target : 0;
     // a tile's last part is not a whole one; and the steps are added up in floats
-    x.groups = tiles + (x.target ? x.target + 2 * kv_heads : 0);
+    x.groups = most + (x.target ? x.target + 2 * kv_heads : 0);
     x.slot_floats = x.few ? 64 * 4 * (x.rows / 16) * (head_dim / 16 + 1) : 64 * kWaves * 4 * (head_dim / 32 * 4 + 1);
     return x;
 }

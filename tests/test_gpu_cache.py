@@ -231,6 +231,24 @@ def test_shared_keys_behind_windows(mk, new, hq):
         check(mk, make(window, [2600], [new], hq, 1, 64, 16, F16, 16), window=window, sinks=window % 40)
 
 
+@pytest.mark.parametrize("n", [64, 70, 200])
+@pytest.mark.parametrize("bits", [8, 16])
+@pytest.mark.parametrize("least", [1, 65])
+def test_keys_of_many_sequences_shared(mk, n, bits, least):
+    """Parts are as small as their number allows, found from the lengths of 64 sequences at a time."""
+    new = [least + i % 3 for i in range(n)]
+    args = make(n + least, [(i * 997) % 3000 + m for i, m in enumerate(new)], new, 1, 1, 64, 32, F16, bits)
+    assert torch.equal(check(mk, args), check(mk, args))
+
+
+@pytest.mark.parametrize("tokens", [4, 5, 8, 9, 16, 17, 24])
+@pytest.mark.parametrize("D,bits", [(64, 8), (64, 16), (96, 8), (96, 16), (128, 8), (128, 16), (256, 8), (256, 16)])
+def test_rows_that_kernels_are_chosen_by(mk, tokens, D, bits):
+    args = make(tokens + D, [700 + tokens, tokens, 90 + tokens], [tokens] * 3, 8, 2, D, 16, BF16, bits)
+    check(mk, args)
+    check(mk, args, window=300, sinks=20)
+
+
 @pytest.mark.parametrize("new", [None, [5, 3], [90, 70]])
 @pytest.mark.parametrize("bits", [8, 16])
 @pytest.mark.parametrize("scale", [0.0, -0.2, 1e-42, 3.0])
