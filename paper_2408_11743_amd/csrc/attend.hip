@@ -32,6 +32,11 @@
 // 6 us where rows are cut between work-groups (77 tokens of 32 heads: 5.4 us,
 // one sequence of 8000 tokens over 8 kv heads, 33 MB: 13.6).  Four waves a work-group,
 // two work-groups a compute unit: 96 us for the 131071 tokens; eight and two: 99.5.
+//
+// A cache of e4m3 codes is read as it is: codes become the queries' type in registers, exactly, and scales, one for 16 slots, are a factor of the
+// tile's scores and a summand in the exponent of its weights.  The 64 sequences, 4.3 GB in 8 bits: 632 us, 6.8 TB/s;
+// 16 of up to 4001 tokens, 32 heads over 8 (57 MB): 17.9, in 16 bits 24.8.  Through a window a row's steps are those of the sinks and of
+// the window: 32 sequences of up to 60001 tokens, 64 heads over 8, the last 4096 and 4 sinks seen (321 MB): 59 us, 5.4 TB/s.
 #include <hip/hip_runtime.h>
 
 #include "device.h"

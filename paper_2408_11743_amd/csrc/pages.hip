@@ -8,8 +8,9 @@
 // A sequence's new pages are all among its new tokens' (each has its first slot there), so
 // whoever finds a token's slot takes the page from the free ones by the sums, without a loop over pages.
 //
-// Latency is all there is: a scan is 1.5 us, a token's slot a search among the sequences and two
-// dependent loads.  Up to kFusedTokens new tokens the same work-group finds the slots, more are a second launch.
+// Latency is all there is: launch, loads, two scans, a token's slot a search among the sequences and two dependent
+// loads (128 sequences of one new token behind windows: 7 us).  Up to kFusedTokens new tokens the same work-group finds the slots, more are a second
+// launch: 700 tokens of 16 sequences 8.9 us, by two launches 11.6; 2200 9.2 and 11.7; 6400 12.5 and 11.8; 240000 of 512 sequences 265 and 14.5.
 #include <hip/hip_runtime.h>
 
 #include "kv.h"
@@ -21,7 +22,7 @@ namespace {
 using namespace dev;
 
 constexpr int kThreads = 1024, kSums = kThreads / 64;
-constexpr int kFusedTokens = 2048;
+constexpr int kFusedTokens = 4096;
 
 // Two sums over the work-group's threads up to and with each, on top of `before`, which becomes the sums of all; saturating.
 struct Two {
