@@ -1,13 +1,15 @@
 """One attention layer of a served model: 4-bit projections, the paged key-value
 cache between them, prompts and then decode steps as a HIP graph.
 
-    python examples/decode_layer.py [--sequences 16] [--steps 32] [--select 64]
+    python examples/decode_layer.py [--sequences 16] [--steps 32] [--select 64 | --bits 8 --window 256 --sinks 4]
 
 The layer's qkv projection is one 4-bit matrix; its output rows are handed to
 ``kv_append`` as they lie (q, k and v are slices), which rotates them and
-fills the pages.  A decode step is projection, append, attention, projection; with
---select the attention reads the most promising pages only.  The graph is
-captured once: the lengths live on the device, so its replays follow the
+fills the pages, which ``assign_pages`` has given to the sequences.  The prompts attend
+by ``cache_attention``; a decode step is pages, projection, append, attention, projection.  With
+--select the attention reads the most promising pages only, with --bits 8 the cache is in 8 bits, and with --window
+a token sees the last ones and --sinks first ones, and pages behind them go to other tokens.  The graph is
+captured once: tables and lengths live on the device, so its replays follow the
 sequences as they grow.  Weights and prompts are random.
 """
 import argparse
@@ -35,50 +37,68 @@ class Attention(torch.nn.Module):
         self.register_buffer("cos_sin", mk.rotation_table(positions, head_dim))
 
     def forward(self, x, cache, starts=None, select=0):
-        """x [tokens, hidden]: one new token per sequence, or with ``starts`` prompts, of which the last
-        token's output is returned."""
-        k_cache, v_cache, bounds = cache["pages"]
+        """x [tokens, hidden]: one new token per sequence, or with ``starts`` each one's prompt."""
+        k_cache, v_cache, extra = cache["pages"]  # scales in 8 bits, else bounds
+        seen = dict(window=cache["window"], sinks=cache["sinks"])
+        table, lengths, eight = cache["table"], cache["lengths"], k_cache.dtype == torch.float8_e4m3fn
         rows = self.qkv(x).view(x.shape[0], -1, self.head_dim)
         q, k, v = rows.split([self.heads, self.kv_heads, self.kv_heads], 1)
-        q = mk.kv_append(q, k, v, k_cache, v_cache, cache["table"], cache["lengths"], self.cos_sin, starts=starts,
-                         bounds=bounds)
-        if starts is not None:
-            q = q[(starts[1:] - 1).long()]
-        table, lengths = cache["table"], cache["lengths"]
-        if select:
-            table, lengths = mk.select_pages(q, bounds, table, lengths, k_cache.shape[2], select)
-        o = mk.paged_attention(q, k_cache, v_cache, table, lengths)
+        if eight:
+            q = mk.kv_append8(q, k, v, k_cache, v_cache, extra, table, lengths, self.cos_sin, starts=starts)
+        else:
+            q = mk.kv_append(q, k, v, k_cache, v_cache, table, lengths, self.cos_sin, starts=starts, bounds=extra)
+        if select and starts is None:
+            table, lengths = mk.select_pages(q, extra, table, lengths, k_cache.shape[2], select)
+            o = mk.paged_attention(q, k_cache, v_cache, table, lengths)
+        else:
+            o = mk.cache_attention(q, k_cache, v_cache, table, lengths, scales=extra if eight else None, starts=starts, **seen)
         return self.out(o.flatten(1))
 
 
-def make_cache(sequences, room, page_size, kv_heads, head_dim):
-    """Pages for `room` tokens of each sequence, dealt out in turn."""
+def make_cache(sequences, room, page_size, kv_heads, head_dim, bits=16, window=None, sinks=0):
+    """Pages for `room` tokens of each sequence, all of them free."""
     width = -(-room // page_size)
-    table = torch.arange(sequences * width, dtype=torch.int32, device="cuda").view(width, sequences).t().contiguous()
-    return {"pages": mk.kv_cache(sequences * width, kv_heads, page_size, head_dim, bounds=True), "table": table,
-            "lengths": torch.zeros(sequences, dtype=torch.int32, device="cuda")}
+    pages = sequences * width
+    made = (mk.kv_cache8(pages, kv_heads, page_size, head_dim) if bits == 8 else
+            mk.kv_cache(pages, kv_heads, page_size, head_dim, bounds=True))
+
+    def ints(*shape, value=0):
+        return torch.full(shape, value, dtype=torch.int32, device="cuda")
+    return {"pages": made, "table": ints(sequences, width, value=-1), "lengths": ints(sequences), "window": window, "sinks": sinks,
+            "free": torch.arange(pages, dtype=torch.int32, device="cuda"), "free_count": ints(1, value=pages)}
+
+
+def give_pages(cache, new, tokens):
+    """To ``new[b]`` tokens of every sequence, ``tokens`` in all; returns the tokens' first rows."""
+    return mk.assign_pages(cache["table"], cache["lengths"], new, cache["free"], cache["free_count"], cache["pages"][0].shape[2], tokens,
+                           cache["window"], cache["sinks"])[0]
 
 
 def main(argv=None):
     ap = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
     for name, value in (("hidden", 4096), ("heads", 32), ("kv-heads", 8), ("head-dim", 128), ("sequences", 16),
-                        ("prompt", 1000), ("steps", 32), ("page-size", 16), ("select", 0)):
+                        ("prompt", 1000), ("steps", 32), ("page-size", 16), ("select", 0), ("bits", 16), ("window", 0), ("sinks", 0)):
         ap.add_argument("--" + name, type=int, default=value)
     a = ap.parse_args(argv)
+    if a.bits not in (8, 16) or (a.select and (a.bits == 8 or a.window)):
+        ap.error("--bits is 8 or 16, and --select goes with neither 8 bits nor a window")
     g = torch.Generator(device="cuda").manual_seed(0)
     room = a.prompt + a.steps + 8
     layer = Attention(a.hidden, a.heads, a.kv_heads, a.head_dim, room, g)
-    cache = make_cache(a.sequences, room, a.page_size, a.kv_heads, a.head_dim)
+    cache = make_cache(a.sequences, room, a.page_size, a.kv_heads, a.head_dim, a.bits, a.window or None, a.sinks)
 
     # prompts of different lengths, one after another in the rows of x
     new = torch.linspace(max(1, a.prompt // 4), a.prompt, a.sequences).int()
-    starts = torch.cat([new.new_zeros(1), new.cumsum(0, dtype=torch.int32)]).cuda()
-    cache["lengths"] += new.cuda()
-    x = layer(torch.randn(int(new.sum()), a.hidden, device="cuda", generator=g).half(), cache, starts)
+    tokens = int(new.sum())
+    starts = give_pages(cache, new.cuda(), tokens)
+    x = layer(torch.randn(tokens, a.hidden, device="cuda", generator=g).half(), cache, starts)
+    x = x[(starts[1:] - 1).long()]  # the last tokens'
 
     # a step adds a token to every sequence; the layer's output is the next step's input
+    one = torch.ones_like(cache["lengths"])
+
     def step():
-        cache["lengths"].add_(1)
+        give_pages(cache, one, a.sequences)
         x.copy_(torch.nn.functional.normalize(layer(x, cache, select=a.select).float(), dim=1).mul_(a.hidden ** 0.5))
 
     side = torch.cuda.Stream()
@@ -91,11 +111,12 @@ def main(argv=None):
         step()
 
     # the first replay against the same step run eagerly
-    before = x.clone(), cache["lengths"].clone()
+    state = [x] + [cache[name] for name in ("table", "lengths", "free", "free_count")]
+    before = [y.clone() for y in state]
     graph.replay()
     replayed = x.clone()
-    x.copy_(before[0])
-    cache["lengths"].copy_(before[1])
+    for y, old in zip(state, before):
+        y.copy_(old)
     step()
     same = torch.equal(x, replayed)
 

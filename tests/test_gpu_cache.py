@@ -578,7 +578,7 @@ def state(seed, B, ps, most, spare, ends=0.2, least=0, width=None, windowed=Fals
 
 
 @pytest.mark.parametrize("B", [1, 2, 63, 64, 65, 200, 1023, 1024, 1025, 2500])
-@pytest.mark.parametrize("tokens", [0, 1, 100, 2048, 2049, 200000])
+@pytest.mark.parametrize("tokens", [0, 1, 100, 2048, 2049, 4096, 4097, 200000])
 def test_pages_of_many_sequences(mk, B, tokens):
     table, lengths, new, free, count = state(B + tokens, B, 16, 200, 3 * B)
     check_pages(mk, table, lengths, new, free, count, 16, tokens)
@@ -825,3 +825,15 @@ def test_refusals(mk):
                          (mk.MarlinError, dict(sinks=-1)), (ValueError, dict(table=t[:1].expand(8, -1))), (TypeError, dict(free=free.cpu())),
                          (mk.MarlinError, dict(free=free[:0])), (TypeError, dict(tokens=2.5))):
         refused(kind, mk.assign_pages, **{**good, **change})
+
+
+@pytest.mark.parametrize("more", [["--bits", "8"], ["--window", "40", "--sinks", "3"], ["--bits", "8", "--window", "64", "--page-size", "32"]])
+def test_example_layer(mk, more):
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "decode_layer.py")
+    spec = importlib.util.spec_from_file_location("decode_layer", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    assert example.main(["--hidden", "512", "--heads", "8", "--kv-heads", "2", "--head-dim", "64", "--sequences", "5",
+                         "--prompt", "90", "--steps", "9", *more])
