@@ -26,7 +26,7 @@
 // cycles, the softmax's vector instructions most of the rest, beside them from the other work-group.  Two columns of rows a wave, one wave a SIMD:
 // 780 us; eight waves a work-group: 2 % less, but 20 % more where tiles are few.  Four prompts, 2270 tokens, 64 heads over 8, through a window of 1024: 100 us;
 // four chunks of 512 tokens behind up to 16384 in 8 bits (535 GFLOP): 622.  Few rows are bound by memory and the latency of two launches: 32 sequences of up to
-// 8000 tokens in 8 bits, four new ones each (160 MB): 42 us.
+// 8000 tokens in 8 bits, four new ones each (160 MB): 39 us.
 #include <hip/hip_runtime.h>
 
 #include "device.h"
@@ -828,6 +828,9 @@ __global__ void __launch_bounds__(64 * kWaves, D > 128 ? 1 : 2) prompt_few_kerne
     constexpr int kAcc = D / 16;
     constexpr float kUnit = __is_same(T, _Float16) ? 15.f : 0.f;
     constexpr int kSlot = kFewFloats<D, RT>;
+    // Values are read past the caches where a sequence is one tile and a row whole lines of 128 bytes (200 sequences of up to 5000 tokens, four new
+    // ones each, 8 bits: 184 us, through the caches 192, 100 of them 74 and 81; two tiles a sequence, 48 rows: 57 and 54; keys too: 190 and 82).
+    constexpr bool kOnce = RT == 1 && D * (Eight ? 1 : 2) % 128 == 0;
 
     __shared__ float4_t lds_acc[kWaves][kAcc][64];
     __shared__ float lds_m[kWaves][kHeadTile], lds_l[kWaves][kHeadTile];
@@ -894,6 +897,12 @@ __global__ void __launch_bounds__(64 * kWaves, D > 128 ? 1 : 2) prompt_few_kerne
         }
     };
     auto load_values = [&](const Places &k, uint32_t named) {
+        auto read = [](uint32_t(&to)[kValueDw], const void *from) {
+            if constexpr (kOnce)
+                load_dwords_once<kValueDw>(to, from);
+            else
+                load_dwords<kValueDw>(to, from);
+        };
 #pragma unroll
         for (int u = 0; u < KT; ++u) {
             if (!(named >> u & 1)) continue;
@@ -902,7 +911,7 @@ __global__ void __launch_bounds__(64 * kWaves, D > 128 ? 1 : 2) prompt_few_kerne
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
 #pragma unroll
-                    for (int hf = 0; hf < kHalves; ++hf) load_dwords<kValueDw>(vr[u][i][hf], v + i * D + 128 * hf);
+                    for (int hf = 0; hf < kHalves; ++hf) read(vr[u][i][hf], v + i * D + 128 * hf);
             } else {
                 const uint8_t *v = (const uint8_t *)p.v + k.at[u] + 4 * g * D;
 #pragma unroll
@@ -911,7 +920,7 @@ __global__ void __launch_bounds__(64 * kWaves, D > 128 ? 1 : 2) prompt_few_kerne
                         vr[u][i][0][0] = *(const uint32_t *)(v + i * D + 4 * r);
                         vr[u][i][0][1] = *(const uint16_t *)(v + i * D + 64 + 2 * r);
                     } else {
-                        load_dwords<kValueDw>(vr[u][i][0], v + i * D + kCh * r);
+                        read(vr[u][i][0], v + i * D + kCh * r);
                     }
                 }
             }
