@@ -471,7 +471,8 @@ __global__ void __launch_bounds__(64 * kWaves, D <= 128 ? 2 : 1) prompt_kernel(c
     for (int c = 0; c < kC; ++c) qf[c] = query_of<vec8>(p, q + 16 * c, have);
 
     // ---- a step's keys and values: this wave's tile of 16 keys, to registers and from there to LDS ----
-    // Keys are a step ahead of values: while a step's weights are found and its values summed up, the next one's scores are.
+    // Keys are a step ahead of values: between a step's weights, which free the scores' registers, and its values' sums come the next one's
+    // scores (four chunks in 8 bits 624 us; scores before the weights, in registers of their own, 637; after the sums 623, but heads of 64 and 96 2 % slower).
     uint32_t kreg[kKeyPasses][kLoad / 4], vreg[kValuePasses][4][kPiece];
     const uint32_t key_from = lane * kLoad, value_from = ((lane / kOct) * 4 * D + (lane % kOct) * 8) * kSize;
     // whether every row sees every key of a step, as far as its position says
@@ -729,7 +730,7 @@ __global__ void __launch_bounds__(64 * kWaves, D <= 128 ? 2 : 1) prompt_kernel(c
     };
 
     if (s0 < s1) {
-        scores_t x, ahead;
+        scores_t x;
         vec8 weights[4];
         float top;
         int entry = entry_of(s0 + 1);
@@ -752,17 +753,15 @@ __global__ void __launch_bounds__(64 * kWaves, D <= 128 ? 2 : 1) prompt_kernel(c
             load_values(values);
             next = load_keys(s + 2, entry);
             entry = entry_of(s + 3);
-            score(s + 1, ahead);
             weigh(s, x, weights);
+            score(s + 1, x);
             add_values(s, weights);
-            look(s + 1, values.within, ahead, top);
+            look(s + 1, values.within, x, top);
             add_odd(s, inside);
             inside = values.within;
             rescale(top);
             store_values(s + 1, values);
             store_keys(s + 2, next);
-#pragma unroll
-            for (int kt = 0; kt < 2; ++kt) x[kt] = ahead[kt];
         }
         __syncthreads();
         weigh(s1 - 1, x, weights);
