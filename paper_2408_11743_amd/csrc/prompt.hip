@@ -24,7 +24,7 @@
 // Many rows are bound by power: a prompt of 8192 tokens, 32 heads over 8 of 128 channels (550 GFLOP), takes 605 to 640 us, 0.86 to 0.91 PFLOP/s, where
 // a matrix product of 8192 cubed takes 1.11; with inputs of zero, a fifth less.  Per score the 32 MFMAs of 64 keys are 45 % of the SIMDs'
 // cycles, the softmax's vector instructions most of the rest, beside them from the other work-group.  Two columns of rows a wave, one wave a SIMD:
-// 780 us; eight waves a work-group: 2 % less, but 20 % more where tiles are few.  Four prompts, 2270 tokens, 64 heads over 8, through a window of 1024: 100 us;
+// 780 us; eight waves a work-group: 2 % less, but 20 % more where tiles are few.  Four prompts, 2270 tokens, 64 heads over 8, through a window of 1024: 98 us;
 // four chunks of 512 tokens behind up to 16384 in 8 bits (535 GFLOP): 622.  Few rows are bound by memory and the latency of two launches: 32 sequences of up to
 // 8000 tokens in 8 bits, four new ones each (160 MB): 39 us.
 #include <hip/hip_runtime.h>
