@@ -1181,11 +1181,13 @@ __global__ void __launch_bounds__(64 * kWaves) prompt_join_kernel(const PromptPr
             float4_t v[kAhead], z[kAhead];
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) {
-                const bool have = k + i * step < parts;  // or the first again, without a weight
+                const bool have = k + i * step < parts;  // or the first again, as nothing: a weight of zero does not take an infinity away
                 const int64_t at = (have ? k + i * step : k) * stride;
                 v[i] = ml[at];
                 z[i] = o[at];
                 v[i][0] = have ? v[i][0] : -INFINITY;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) z[i][e] = have ? z[i][e] : 0.f;
             }
             float top = x.top;
 #pragma unroll
