@@ -563,7 +563,8 @@ size_t marlin_cache_attention_workspace_bytes(int64_t starts, int64_t tokens, in
  *
  * Scores, sums and partial results are fp32.  One token per sequence (starts NULL): the weights are rounded as by
  * marlin_paged_attention (to 21 bits, 15 of bfloat16).  Several: once to dtype (of float16's, those below 2^-36 of the
- * row's maximum are lost).  Bitwise reproducible for a given device and input.
+ * row's maximum are lost).  An infinite value that a token sees gives an infinity in its channel (one token per sequence: where its
+ * weight is not lost; several: where it is 2^-126 of the row's maximum or more).  Bitwise reproducible for a given device and input.
  * Errors: as marlin_paged_attention (the limit of 2^31 without starts only); INVALID_SHAPE also for tokens, for
  * tokens * heads / kv_heads beyond 2^30, for table_head with starts, and for tokens other than B without; INVALID_ARGUMENT
  * also for window and sinks.

@@ -68,6 +68,7 @@ __device__ __forceinline__ float16_t mfma32(Elem<__bf16>::vec8 a, Elem<__bf16>::
 
 // A masked key's value may be anything, and its weight of zero does not take an infinity or NaN away.  In steps in which some rows
 // do not see all keys what is not finite is left out of the second product, and added by itself for the rows that do see it.
+// In the others an infinity becomes NaN where its weight is too small for T: results that are NaN are looked into at the end.
 //
 // A dword of elements, or of codes, without those that are not finite.
 template <typename T, bool Eight>
@@ -92,6 +93,15 @@ __device__ __forceinline__ float odd_at(const void *cache, int64_t at)
     else
         x = (float)((const T *)cache)[at];
     return __builtin_fabsf(x) < INFINITY ? 0.f : x;
+}
+
+// A result that is NaN, and may not be if its row's sum is a number: marked, the first value that is not finite takes its place, others
+// are added.  If there is none it stays a NaN.
+constexpr uint32_t kMarked = 0x7FC0BEEFu;  // no element becomes this one
+__device__ __forceinline__ float marked(float x, bool row) { return row && x != x ? __builtin_bit_cast(float, kMarked) : x; }
+__device__ __forceinline__ float add_to_marked(float x, float odd)
+{
+    return odd == 0.f ? x : __builtin_bit_cast(uint32_t, x) == kMarked ? odd : x + odd;
 }
 
 // The keys that a tile's rows see: those below `sinks` and from a window's lower end on, in tiles of 16 of which the first `sink_tiles`
@@ -770,6 +780,34 @@ __global__ void __launch_bounds__(64 * kWaves, D <= 128 ? 2 : 1) prompt_kernel(c
     }
     const Pair halves = exchange<32>(l);
     l = halves.a + halves.b;
+    if constexpr (!Eight) {  // codes have no infinities
+        float sum = 0.f;
+#pragma unroll
+        for (int ct = 0; ct < kCt; ++ct)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) sum += acc[ct][i];
+        if (__any((sum != sum) & (l == l))) {
+#pragma unroll
+            for (int ct = 0; ct < kCt; ++ct)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) acc[ct][i] = marked(acc[ct][i], l == l);
+#pragma unroll 1
+            for (int n = 4 * kTileKeys * s0; n < 4 * kTileKeys * s1; ++n) {
+                const int j = keys.position(n / kTileKeys) + n % kTileKeys;
+                if (j >= keys.end) continue;
+                const int entry = scalar_load(table + (j >> p.page_shift));
+                if ((uint32_t)entry >= (uint32_t)p.pages) continue;
+                const int64_t at = place_of(p, entry, head, j, D);
+#pragma unroll
+                for (int ct = 0; ct < kCt; ++ct)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const float x = odd_at<T, Eight>(p.v, at + channel_of(ct, i));
+                        acc[ct][i] = add_to_marked(acc[ct][i], sight.sees(j) ? x : 0.f);
+                    }
+            }
+        }
+    }
 
     // ---- a part of the tile's keys: left for the joining kernel ----
     if (parts > 1) {
@@ -1100,6 +1138,44 @@ __global__ void __launch_bounds__(64 * kWaves, D > 128 ? 1 : 2) prompt_few_kerne
             load_values(places, next.named);
             raw = next;
             s += kWaves;
+        }
+    }
+    if constexpr (!Eight) {
+        bool look = false;
+        float of_row[RT];  // the row's sum
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            of_row[rt] = sum_over_groups(l[rt]);
+            float sum = 0.f;
+#pragma unroll
+            for (int j = 0; j < kAcc; ++j) sum += (acc[rt][j][0] + acc[rt][j][1]) + (acc[rt][j][2] + acc[rt][j][3]);
+            look |= (sum != sum) & (of_row[rt] == of_row[rt]);
+        }
+        if (__any(look)) {
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                for (int j = 0; j < kAcc; ++j)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc[rt][j][i] = marked(acc[rt][j][i], of_row[rt] == of_row[rt]);
+#pragma unroll 1
+            for (int at_step = s0 + wave; at_step < s1; at_step += kWaves)
+#pragma unroll 1
+                for (int n = 0; n < kKeys; ++n) {
+                    const int pos = position_of(at_step, n >> 4) + (n & 15);
+                    if (pos >= keys.end) continue;
+                    const int entry = scalar_load(table + (pos >> p.page_shift));
+                    if ((uint32_t)entry >= (uint32_t)p.pages) continue;
+                    const int64_t at = place_of(p, entry, head, pos, D);
+#pragma unroll
+                    for (int c = 0; c < kAcc; ++c)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const float x = odd_at<T, Eight>(p.v, at + channel_of(c, 4 * g + i));
+#pragma unroll
+                            for (int rt = 0; rt < RT; ++rt) acc[rt][c][i] = add_to_marked(acc[rt][c][i], sight[rt].sees(pos) ? x : 0.f);
+                        }
+                }
         }
     }
 
