@@ -561,9 +561,10 @@ size_t marlin_cache_attention_workspace_bytes(int64_t starts, int64_t tokens, in
  * slots hold does not matter, NaN included.  A token that sees nothing gives 0 and -inf.
  * Rows of out and lse that belong to no sequence are left as they are.
  *
- * Scores, sums and partial results are fp32.  One token per sequence (starts NULL): the weights are rounded as by
- * marlin_paged_attention (to 21 bits, 15 of bfloat16).  Several: once to dtype (of float16's, those below 2^-36 of the
- * row's maximum are lost).  An infinite value that a token sees gives an infinity in its channel (one token per sequence: where its
+ * Scores, sums and partial results are fp32.  The weights are rounded as by marlin_paged_attention (to 21 bits, 15 of bfloat16) for one
+ * token per sequence (starts NULL), and for several up to 64 rows (tokens times heads / kv_heads) a sequence on the average; of more rows
+ * once to dtype.  Of float16's, those below 2^-36 of the row's largest (one token: 2^-40) are lost; in an 8-bit cache weights count
+ * times their block's scale of values for that.  An infinite value that a token sees gives an infinity in its channel (one token per sequence: where its
  * weight is not lost; several: where it is 2^-126 of the row's maximum or more).  Bitwise reproducible for a given device and input.
  * Errors: as marlin_paged_attention (the limit of 2^31 without starts only); INVALID_SHAPE also for tokens, for
  * tokens * heads / kv_heads beyond 2^30, for table_head with starts, and for tokens other than B without; INVALID_ARGUMENT

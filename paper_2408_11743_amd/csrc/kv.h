@@ -110,6 +110,7 @@ struct PromptProblem {
 // How a call of these sizes is split: rows of a tile, work-groups to split the keys for (or 0) and at the most, workspace floats of one.
 struct PromptPlan {
     bool few;  // the kernel for few rows a sequence
+    bool two;  // weights in two parts
     int rows, target, slot_floats;
     int64_t groups;
 };

@@ -17,9 +17,14 @@
 // scans, the longest of a sequence first.  Where there are few tiles, their keys are split into parts of one length, a work-group
 // each, which leave partial results in the workspace; a second launch joins those in order.
 //
-// Weights go to the second product rounded once to the cache's type: an error of half a step of each weight, as the output's
-// own, and averaged over the keys.  float16's are times 2^11 (few rows: 2^15), so that they are no subnormals until 2^-25 of the maximum, and lost
-// below 2^-36: 2^20 keys that are lost are less than half a step of the sum.  Scores, maxima, sums and results are fp32.
+// Weights go to the second product in the cache's type.  Up to kTwoRows rows a sequence and kv head (the mean) in two parts, as those of one token
+// per sequence (attend.hip: 21 bits in float16, 15 in bfloat16), so that drafted tokens are weighed as decoding weighs them: 32 sequences'
+// drafts over 8 bits 39.9 us, rounded once 39.4; one of 60000 tokens 41.8 and 38.9.  Of more rows they are rounded once, an error of half a step of each weight, as
+// the output's own, and averaged over the keys; float16's are times 2^11, so that they are no subnormals until 2^-25 of the maximum, and lost
+// below 2^-36: 2^20 keys that are lost are less than half a step of the sum.  Second parts would take half the matrix products again: a prompt of 8192
+// tokens 854 us for 644, windowed ones 126 for 101, chunks over 8 bits 836 for 640, where the errors against 64 bits (2-norm) are 2.03e-4 for 2.05e-4 and
+// in bfloat16 1.65e-3 for 1.69e-3, nearly all of it the output's rounding.  Over 8 bits a weight is times its block's scale of values in all of
+// this.  Scores, maxima, sums and results are fp32.
 //
 // Many rows are bound by power: a prompt of 8192 tokens, 32 heads over 8 of 128 channels (550 GFLOP), takes 605 to 640 us, 0.86 to 0.91 PFLOP/s, where
 // a matrix product of 8192 cubed takes 1.11; with inputs of zero, a fifth less.  Per score the 32 MFMAs of 64 keys are 45 % of the SIMDs'
@@ -410,10 +415,11 @@ __device__ __forceinline__ V query_of(const PromptProblem &p, const T *q, bool h
 constexpr int kStep = 64;
 
 // Weights are taken against a row's maximum as it was when the results were last brought to it: doing so takes a multiplication of
-// every result, and of 32 rows some one's maximum grows by a little in most steps.  float16's weights are times 2^11, 2^15 at the most.
+// every result, and of 32 rows some one's maximum grows by a little in most steps.  float16's weights are times 2^11, 2^15 at the most, those in
+// two parts times 2^-4 before they are taken apart.
 constexpr float kWideSlack = 4.f;  // log2
-template <typename T>
-constexpr float kWideUnit = __is_same(T, _Float16) ? 11.f : 0.f;
+template <typename T, bool Two>
+constexpr float kWideUnit = !__is_same(T, _Float16) ? 0.f : Two ? -kWideSlack : 11.f;
 
 template <int D>
 constexpr int kWideFloats = 64 * kWaves * 4 * ((D / 32) * 4 + 1);
@@ -423,7 +429,8 @@ constexpr int kWideFloats = 64 * kWaves * 4 * ((D / 32) * 4 + 1);
 // apart than they are long, an odd number of 16-byte pieces: reads are of distinct banks, and at constant distances.  V^T's
 // rows are in an order of their own, eight-channel pieces side by side, so that most writes are too (conflicts take 14 % of
 // the LDS's busy cycles, 22 % in an 8-bit cache; an order of the lanes without them took the same time), and a lane's results are whole pieces: row 8 * oct + j of the channels is row j * (D / 8) + oct (96 channels: four-channel pieces, below).
-template <typename T, int D, bool Eight>
+// Two: weights in two parts.
+template <typename T, int D, bool Eight, bool Two>
 __global__ void __launch_bounds__(64 * kWaves, D <= 128 ? 2 : 1) prompt_kernel(const PromptProblem p)
 {
     typedef Elem<T> E;
@@ -439,7 +446,7 @@ __global__ void __launch_bounds__(64 * kWaves, D <= 128 ? 2 : 1) prompt_kernel(c
     constexpr int kValueItems = 4 * kOct, kValuePasses = (kValueItems + 63) / 64;  // four keys, eight channels
     constexpr int kPiece = 2 * kSize;                      // dwords of eight elements in the cache
     constexpr int kCt = D / 32, kC = D / 16;
-    constexpr float kUnit = kWideUnit<T>;  // log2 of what a weight of 1 is, against a maximum that may be kWideSlack too low
+    constexpr float kUnit = kWideUnit<T, Two>;  // log2 of what a weight of 1 is, against a maximum that may be kWideSlack too low
     static_assert(16 * D % (kElems * 64) == 0, "");
 
     __shared__ __attribute__((aligned(16))) uint8_t lds[2 * (kKeyBytes + kValueBytes)];
@@ -685,7 +692,9 @@ __global__ void __launch_bounds__(64 * kWaves, D <= 128 ? 2 : 1) prompt_kernel(c
             m = to;
         }
     };
-    auto weigh = [&](int s, const scores_t &x, vec8 (&weights)[4]) {
+    constexpr int kParts = Two ? 2 : 1;
+    typedef vec8 weights_t[kParts][4];
+    auto weigh = [&](int s, const scores_t &x, weights_t &weights) {
         const float unit = kUnit - (m == -INFINITY ? 0.f : m);
 #pragma unroll
         for (int g16 = 0; g16 < 4; ++g16) {
@@ -699,21 +708,31 @@ __global__ void __launch_bounds__(64 * kWaves, D <= 128 ? 2 : 1) prompt_kernel(c
                 const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(x[g16 >> 1][8 * (g16 & 1) + e], f, add));
                 const float z = __builtin_amdgcn_exp2f(__builtin_fmaf(x[g16 >> 1][8 * (g16 & 1) + e + 1], f, add));
                 sum += y + z;
-                weights[g16][e] = (T)y;
-                weights[g16][e + 1] = (T)z;
+                if constexpr (Two) {
+                    const typename E::Parts both = E::part(y, z);
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        weights[0][g16][e + i] = both.first[i];
+                        weights[kParts - 1][g16][e + i] = both.rest[i];
+                    }
+                } else {
+                    weights[0][g16][e] = (T)y;
+                    weights[0][g16][e + 1] = (T)z;
+                }
             }
             if constexpr (Eight) sum *= lds_info[s & 3].times[g16];
             l += sum;
         }
     };
-    auto add_values = [&](int s, const vec8 (&weights)[4]) {
+    auto add_values = [&](int s, const weights_t &weights) {
         const uint8_t *const from = lds + (s & 1) * kValueBytes + value_at;
 #pragma unroll
         for (int g16 = 0; g16 < 4; ++g16)
 #pragma unroll
             for (int ct = 0; ct < kCt; ++ct) {
                 const vec8 a = *(const vec8 *)(from + 32 * ct * kValueRow + g16 * 32);
-                acc[ct] = mfma32(a, weights[g16], acc[ct]);
+#pragma unroll
+                for (int part = 0; part < kParts; ++part) acc[ct] = mfma32(a, weights[part][g16], acc[ct]);
             }
     };
     // values of a step that are not finite, where some rows do not see all keys
@@ -741,7 +760,7 @@ __global__ void __launch_bounds__(64 * kWaves, D <= 128 ? 2 : 1) prompt_kernel(c
 
     if (s0 < s1) {
         scores_t x;
-        vec8 weights[4];
+        weights_t weights;
         float top;
         int entry = entry_of(s0 + 1);
         Mine values = load_keys(s0, entry_of(s0)), next = values;  // of the step whose values are to come next; of the one after it
@@ -825,7 +844,7 @@ __global__ void __launch_bounds__(64 * kWaves, D <= 128 ? 2 : 1) prompt_kernel(c
 
     // ---- the finished row: a lane holds pieces of eight channels (96: of four) ----
     if (out_at < 0) return;
-    const float inv = 1.f / l;
+    const float inv = 1.f / (Two ? l * E::kWeightUnit : l);
     T *const to = (T *)p.out + out_at * D;
     auto result = [&](int ct, int i) { return l == 0.f ? (T)0.f : (T)(acc[ct][i] * inv); };
     constexpr int kPieces = D == 96 ? 12 : D / 16, kChannels = D == 96 ? 4 : 8;  // a lane's
@@ -863,7 +882,6 @@ __global__ void __launch_bounds__(64 * kWaves, D > 128 ? 1 : 2) prompt_few_kerne
     constexpr bool kBy32 = D % 64 != 0;
     constexpr int kKeyDw = Eight ? D / 16 : kQ * 4;
     constexpr int kAcc = D / 16;
-    constexpr float kUnit = __is_same(T, _Float16) ? 15.f : 0.f;
     constexpr int kSlot = kFewFloats<D, RT>;
     // Values are read past the caches where a sequence is one tile and a row whole lines of 128 bytes (200 sequences of up to 5000 tokens, four new
     // ones each, 8 bits: 184 us, through the caches 192, 100 of them 74 and 81; two tiles a sequence, 48 rows: 57 and 54; keys too: 190 and 82).
@@ -1045,7 +1063,7 @@ __global__ void __launch_bounds__(64 * kWaves, D > 128 ? 1 : 2) prompt_few_kerne
                                 for (int w = 0; w < kValueDw; ++w) vr[u][i][hf][w] = 0;
                         }
             }
-            vec8 weights[RT];
+            vec8 weights[RT], rest[RT];  // in two parts
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) {
 #pragma unroll
@@ -1085,10 +1103,15 @@ __global__ void __launch_bounds__(64 * kWaves, D > 128 ? 1 : 2) prompt_few_kerne
                 for (int u = 0; u < KT; ++u) {
                     float sum = 0.f;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float x = __builtin_amdgcn_exp2f(sc[rt][u][i] - (ref - kUnit));
-                        sum += x;
-                        weights[rt][4 * u + i] = (T)x;
+                    for (int i = 0; i < 4; i += 2) {
+                        const float x = __builtin_amdgcn_exp2f(sc[rt][u][i] - ref), y = __builtin_amdgcn_exp2f(sc[rt][u][i + 1] - ref);
+                        sum += x + y;
+                        const typename E::Parts both = E::part(x, y);
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            weights[rt][4 * u + i + e] = both.first[e];
+                            rest[rt][4 * u + i + e] = both.rest[e];
+                        }
                     }
                     if constexpr (Eight) sum *= cur.times[u];
                     l[rt] += sum;
@@ -1131,7 +1154,10 @@ __global__ void __launch_bounds__(64 * kWaves, D > 128 ? 1 : 2) prompt_few_kerne
                 for (int j = 0; j < kCh; ++j) {
                     const vec8 x = values_of(hf, j);
 #pragma unroll
-                    for (int rt = 0; rt < RT; ++rt) acc[rt][hf * kCh + j] = E::mfma(x, weights[rt], acc[rt][hf * kCh + j]);
+                    for (int rt = 0; rt < RT; ++rt) {
+                        acc[rt][hf * kCh + j] = E::mfma(x, weights[rt], acc[rt][hf * kCh + j]);
+                        acc[rt][hf * kCh + j] = E::mfma(x, rest[rt], acc[rt][hf * kCh + j]);
+                    }
                 }
             issue_order_point();
             if (!more) break;
@@ -1201,7 +1227,7 @@ __global__ void __launch_bounds__(64 * kWaves, D > 128 ? 1 : 2) prompt_few_kerne
             f[w] = __builtin_amdgcn_exp2f(lds_m[w][r] - ref);
             sum += lds_l[w][r] * f[w];
         }
-        const float inv = 1.f / sum;
+        const float inv = 1.f / (sum * E::kWeightUnit);
 #pragma unroll 1
         for (int j = wave; j < kAcc; j += kWaves) {
             float4_t o{0.f, 0.f, 0.f, 0.f};
@@ -1215,7 +1241,7 @@ __global__ void __launch_bounds__(64 * kWaves, D > 128 ? 1 : 2) prompt_few_kerne
             if (out_at[rt] < 0) continue;
 #pragma unroll
             for (int i = 0; i < 4; ++i) ((T *)p.out)[out_at[rt] * D + channel_of(j, 4 * g + i)] = sum == 0.f ? (T)0.f : (T)(o[i] * inv);
-            if (p.lse && g == 0 && j == 0) p.lse[out_at[rt]] = (top + __builtin_amdgcn_logf(sum) - kUnit) * 0.693147180559945f;
+            if (p.lse && g == 0 && j == 0) p.lse[out_at[rt]] = (top + __builtin_amdgcn_logf(sum)) * 0.693147180559945f;
         }
     }
 }
@@ -1226,14 +1252,15 @@ __global__ void __launch_bounds__(64 * kWaves, D > 128 ? 1 : 2) prompt_few_kerne
 // work-groups that made a tile's pieces join a share of its blocks each: few pieces a wave a block, in order; of many
 // the waves take some each, in order, and are added up in LDS.  So the pieces of any number are read side by side, and the
 // same bits come of them every time.
-template <typename T, int D, int RT, bool Few, bool Eight>
+template <typename T, int D, int RT, bool Few, bool Eight, bool Two>
 __global__ void __launch_bounds__(64 * kWaves) prompt_join_kernel(const PromptProblem p)
 {
     constexpr int kBlocks = Few ? D / 16 : D / 8;  // of a wave's rows
     constexpr int kAll = (Few ? 1 : kWaves) * RT * kBlocks;
     constexpr int kFloats = Few ? kFewFloats<D, RT> : kWideFloats<D>;
     constexpr int kHalves = D > 128 && !Eight ? 2 : 1, kCh = D / 16 / kHalves, kOct = D / 8;
-    constexpr float kUnit = !Few ? kWideUnit<T> : __is_same(T, _Float16) ? 15.f : 0.f;
+    // what the sum is times (log2), and results beside it
+    constexpr float kUnit = Few ? 0.f : kWideUnit<T, Two>, kWeight = Two ? Elem<T>::kWeightUnit : 1.f;
     __shared__ float4_t lds_o[kWaves][64];
     __shared__ float lds_top[kWaves][64], lds_sum[kWaves][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -1285,7 +1312,7 @@ __global__ void __launch_bounds__(64 * kWaves) prompt_join_kernel(const PromptPr
         const int row = x.row0 + (Few ? group * 16 + (lane & 15) : group * 32 + (lane & 31));
         if (row >= x.tokens * p.group) return;
         const int64_t at = (int64_t)(x.from + row / p.group) * p.heads + head * p.group + row % p.group;
-        const float inv = 1.f / sum;
+        const float inv = 1.f / (sum * kWeight);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             int ch;
@@ -1337,6 +1364,12 @@ __global__ void __launch_bounds__(64 * kWaves) prompt_join_kernel(const PromptPr
     }
 }
 
+// Rows of a sequence and kv head (the mean) up to which the kernel for few takes them, and up to which weights are in two parts.
+constexpr int few_rows(int head_dim, bool eight) { return head_dim == 128 && !eight ? 16 : 64; }
+template <int D, bool Eight>
+constexpr int kFewRows = few_rows(D, Eight);
+constexpr int kTwoRows = 64;
+
 template <typename T, int D, bool Eight>
 hipError_t launch_one(const PromptProblem &p, const PromptPlan &plan, hipStream_t stream)
 {
@@ -1345,17 +1378,18 @@ hipError_t launch_one(const PromptProblem &p, const PromptPlan &plan, hipStream_
     q.groups = plan.groups;
     q.records = (char *)p.partials + (size_t)plan.groups * plan.slot_floats * sizeof(float);  // behind the pieces
     const void *kernel, *join;
-    if (!plan.few) {
-        kernel = (const void *)&prompt_kernel<T, D, Eight>;
-        join = (const void *)&prompt_join_kernel<T, D, 1, false, Eight>;
+    if (!plan.few && !plan.two) {
+        kernel = (const void *)&prompt_kernel<T, D, Eight, false>;
+        join = (const void *)&prompt_join_kernel<T, D, 1, false, Eight, false>;
     } else if (plan.rows == 16) {
         kernel = (const void *)&prompt_few_kernel<T, D, 1, Eight>;
-        join = (const void *)&prompt_join_kernel<T, D, 1, true, Eight>;
-    } else if constexpr (D != 128 || Eight) {
+        join = (const void *)&prompt_join_kernel<T, D, 1, true, Eight, true>;
+    } else if constexpr (kFewRows<D, Eight> > 16) {
         kernel = (const void *)&prompt_few_kernel<T, D, 2, Eight>;
-        join = (const void *)&prompt_join_kernel<T, D, 2, true, Eight>;
+        join = (const void *)&prompt_join_kernel<T, D, 2, true, Eight, true>;
     } else {
-        return hipErrorInvalidValue;
+        kernel = (const void *)&prompt_kernel<T, D, Eight, true>;
+        join = (const void *)&prompt_join_kernel<T, D, 1, false, Eight, true>;
     }
     const int64_t most = ((int64_t)1 << 24) / p.kv_heads * p.kv_heads - p.kv_heads;
     for (int64_t base = 0; base < plan.groups; base += most) {  // a launch takes less than 2^32 threads
@@ -1391,8 +1425,8 @@ PromptPlan plan_prompt(int64_t tokens, int64_t B, int64_t heads, int64_t kv_head
     // Few rows: as long as registers hold what a wave needs.  16 sequences of 1000 to 8000 tokens, 64 rows of new ones for each of 8
     // kv heads (4 of 256 channels): 38.5 us by the kernel for few rows, 44 by the other one (64 channels), 55 and 58 (96), 57 and 66 (128, 8 bits), 82 and
     // 110 (256); 96 rows: 50 and 46, 73 and 61, 82 and 68, 113 and 110.  In 16 bits two columns of 128 channels do not fit: 32 sequences, 32 rows: 163 and 119.
-    const int few_rows = head_dim == 128 && !eight ? 16 : 64;
-    x.few = rows <= few_rows * sequences;
+    x.few = rows <= few_rows(head_dim, eight) * sequences;
+    x.two = rows <= kTwoRows * sequences;
     x.rows = x.few ? (rows <= 16 * sequences ? 16 : 32) : 32 * kWaves;
     // work-groups that run at once: by the registers, those of many rows by the LDS too
     int per_cu = head_dim == 256 ? 1 : 2;
