@@ -527,20 +527,22 @@ __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendPr
                 cut |= pos < low && pos + kStepKeys > sinks;
             }
             if (cut) {
-                // whatever a masked slot holds (an infinity, not a number) stays out of both products
+                // Whatever a masked slot holds (an infinity, not a number) stays out of both products.  Selects: the compiler (ROCm 7.2) has
+                // dropped assignments to elements of MFMA results in divergent branches, and scores are not far from being those.
 #pragma unroll
                 for (int u = 0; u < KT; ++u) {
                     const int from_tile = pos + kTileKeys * u;
                     const int valid = (uint32_t)cur.e[u] < (uint32_t)p.pages ? end - from_tile : 0;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (4 * g + i >= valid || (Window && from_tile + 4 * g + i < low && from_tile + 4 * g + i >= sinks)) {
-                            sc[u][i] = -INFINITY;
+                    for (int i = 0; i < 4; ++i) {
+                        const int at = 4 * g + i, j = from_tile + at;
+                        const bool off = (at >= valid) | (Window & (j < low) & (j >= sinks));
+                        sc[u][i] = off ? -INFINITY : sc[u][i];
 #pragma unroll
-                            for (int hf = 0; hf < kHalves; ++hf)
+                        for (int hf = 0; hf < kHalves; ++hf)
 #pragma unroll
-                                for (int w = 0; w < kValueDw; ++w) vr[u][i][hf][w] = 0;
-                        }
+                            for (int w = 0; w < kValueDw; ++w) vr[u][i][hf][w] = off ? 0 : vr[u][i][hf][w];
+                    }
                 }
             }
             float top = m;
