@@ -584,6 +584,7 @@ typedef struct {
     void *workspace;             /* as for marlin_gemm (one buffer serves all)              */
     uint64_t workspace_bytes;
     int64_t B, width, pages, page_size, tokens, window, sinks;
+    const int32_t *back;         /* [B]: tokens taken back from the sequence's end first, or NULL */
 } marlin_assign_pages_args;
 
 /* Bytes of workspace marlin_assign_pages needs (0 for a B it does not take). */
@@ -593,6 +594,9 @@ size_t marlin_assign_pages_workspace_bytes(int64_t B);
  * marlin_assign_pages - the tables of a step: pages for its new tokens, pages given back.
  *
  * In the sequences' order, with L = lengths[b] (below 0: 0; past the table: its end) and n = new_tokens[b]:
+ *  0. With back: L and the length fall by back[b] (drafted tokens that were not accepted; 0 .. L, others count as the nearer of those), and the entries of
+ *     the pages that no token is left in, ceil(L / page_size) on, that name pages are appended to the free ones and become -1.
+ *     This comes before step 1 of any sequence.
  *  1. n < 0: the sequence ends.  The entries of its ceil(L / page_size) pages that name pages are appended
  *     to the free ones and become -1, and its length 0.  Otherwise, where window > 0, the same is done to the entries
  *     below position L - window (whole pages) from there back to the first that names
@@ -603,6 +607,8 @@ size_t marlin_assign_pages_workspace_bytes(int64_t B);
  *  starts: where each sequence's new tokens begin (those of a sequence not served: none), as the other entry
  *  points take it.  slots[t]: page * page_size + slot of new token t, -1 where
  *  the sequence's last page so far is no page, or behind the last token.
+ * A page belongs to one sequence: one that two rows name is given back with the first of them.  Entries behind a sequence's last page are not
+ * looked at and may be overwritten, so who lowers a length in another way than by back has to put those pages among the free ones.
  * A free_count outside 0 .. pages is clamped to it, and pages beyond `pages` free ones are not kept.  An entry of free_pages
  * that names no page is handed out as it is, and its tokens count as masked.
  * B 0 .. 2^16 (0: starts[0] and slots are written), tokens 0 .. 2^24; sizes as above.

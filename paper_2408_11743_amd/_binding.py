@@ -226,7 +226,7 @@ KV_APPEND8_FIELDS = ["scales" if f == "bounds" else f for f in KV_APPEND_FIELDS]
 CACHE_ATTENTION_FIELDS = ("q q_row q_head k_cache v_cache scales table table_row table_head lengths starts tokens window sinks "
                           "out lse workspace workspace_bytes B heads kv_heads head_dim pages page_size width scale dtype").split()
 ASSIGN_PAGES_FIELDS = ("table table_row lengths new_tokens free_pages free_count starts slots workspace workspace_bytes B width "
-                       "pages page_size tokens window sinks").split()
+                       "pages page_size tokens window sinks back").split()
 pack_kv_append = struct.Struct("%dq" % len(KV_APPEND_FIELDS)).pack
 pack_paged_attention = struct.Struct("20qdq").pack
 pack_select_pages = struct.Struct("%dq" % len(SELECT_PAGES_FIELDS)).pack
@@ -288,7 +288,7 @@ def marlin_assign_pages_workspace_bytes(B: int) -> int:
     return lib().marlin_assign_pages_workspace_bytes(B)
 
 
-def marlin_assign_pages(stream=None, **args) -> None:
-    """args: the fields of marlin_assign_pages_args by name."""
+def marlin_assign_pages(stream=None, back=None, **args) -> None:
+    """args: the fields of marlin_assign_pages_args by name (back may be left out)."""
     _check("marlin_assign_pages", lib().marlin_assign_pages(
-        pack_assign_pages(*_fields("marlin_assign_pages", ASSIGN_PAGES_FIELDS, args)), _stream(stream)))
+        pack_assign_pages(*_fields("marlin_assign_pages", ASSIGN_PAGES_FIELDS, {**args, "back": back})), _stream(stream)))

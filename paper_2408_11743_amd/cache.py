@@ -220,7 +220,7 @@ def _cache_attention(q, k_cache, v_cache, table, lengths, scales, starts, window
 
 def assign_pages(table: torch.Tensor, lengths: torch.Tensor, new: torch.Tensor, free: torch.Tensor, free_count: torch.Tensor,
                  page_size: int, tokens: int, window: int | None = None, sinks: int = 0,
-                 workspace: "ops.Workspace | None" = None):
+                 workspace: "ops.Workspace | None" = None, back: torch.Tensor | None = None):
     """The tables of a step (``marlin_assign_pages``): sequence b of ``table`` int32 [sequences, width] gets ``new[b]`` tokens, or ends
     where that is below 0.  Takes pages from, and gives them back to, ``free`` int32 [pages], whose
     first ``free_count`` (int32 [1]) entries are the free pages, and brings ``lengths`` up to date, all in place.
@@ -229,20 +229,28 @@ def assign_pages(table: torch.Tensor, lengths: torch.Tensor, new: torch.Tensor, 
 
     Sequences are served in their order while pages, room in the table and ``tokens`` rows last; one that is not gets no tokens in this
     step and keeps its length (its rows in ``starts`` are none).  With ``window`` the pages that a token sees neither through it nor among the
-    first ``sinks`` positions are given back and their entries become -1."""
-    done = (_native or _connect()).assign_pages(table, lengths, new, free, free_count, page_size, tokens, window, sinks, workspace)
+    first ``sinks`` positions are given back and their entries become -1.
+
+    ``back`` int32 [sequences] takes tokens back first: drafted ones that were not accepted.  Lengths fall by it, and the pages that no token is
+    left in are given back; the next tokens take the others' slots.  (What those had widened stays: the scale of an 8-bit block, a page's
+    bounds.  Behind a window take back no more than the last call's tokens, as pages that earlier ones would see may be gone.)  A length that is lowered in another way loses the pages behind it, as entries behind a sequence's last page are overwritten without a
+    look.  A page belongs to one sequence: it is given back with the first that names it."""
+    done = (_native or _connect()).assign_pages(table, lengths, new, free, free_count, page_size, tokens, window, sinks, workspace, back)
     if done is not None:
         return done
-    if _watched(table, lengths, new, free, free_count):
+    if _watched(table, lengths, new, free, free_count, back):
         window, sinks = _visible("assign_pages", window, sinks)
-        return torch.ops.marlin_mi355x.assign_pages(table, lengths, new, free, free_count, page_size, tokens, window, sinks)
-    return _assign_pages(table, lengths, new, free, free_count, page_size, tokens, window, sinks, workspace)
+        return torch.ops.marlin_mi355x.assign_pages(table, lengths, new, free, free_count, page_size, tokens, window, sinks, back)
+    return _assign_pages(table, lengths, new, free, free_count, page_size, tokens, window, sinks, workspace, back)
 
 
-def _assign_pages(table, lengths, new, free, free_count, page_size, tokens, window, sinks, workspace):
+def _assign_pages(table, lengths, new, free, free_count, page_size, tokens, window, sinks, workspace, back):
     f, device = "assign_pages", table.device
     for name, x, dims in (("table", table, 2), ("lengths", lengths, 1), ("new", new, 1), ("free", free, 1), ("free_count", free_count, 1)):
         _check_ints(f, name, x, dims, device)
+    if back is not None:
+        _check_ints(f, "back", back, 1, device)
+        _need(back.shape == lengths.shape, f, "back must have one entry per row of table")
     window, sinks = _visible(f, window, sinks)
     page_size, tokens = operator.index(page_size), operator.index(tokens)
     n, width = table.shape
@@ -261,7 +269,8 @@ def _assign_pages(table, lengths, new, free, free_count, page_size, tokens, wind
         buf = kv._workspace(f, dev, stream, workspace, nbytes)
         with torch.cuda.device(dev):
             status = B.lib().marlin_assign_pages(B.pack_assign_pages(
-                *ptrs, buf.data_ptr(), buf.numel(), n, width, free.shape[0], page_size, tokens, window, sinks), stream)
+                *ptrs, buf.data_ptr(), buf.numel(), n, width, free.shape[0], page_size, tokens, window, sinks,
+                0 if back is None else back.data_ptr()), stream)
         if status != 5:
             break
     if status:

@@ -511,10 +511,10 @@ try {
     return not_here();
 }
 
-// table, lengths, new, free, free_count, page_size, tokens, window, sinks, workspace
+// table, lengths, new, free, free_count, page_size, tokens, window, sinks, workspace, back
 PyObject *assign_pages(PyObject *, PyObject *const *o, Py_ssize_t n)
 try {
-    if (n != 10 || !g_assign || watched()) return not_here();
+    if (n != 11 || !g_assign || watched()) return not_here();
     const at::Tensor *table = plain(o[0]), *lengths = plain(o[1]), *fresh = plain(o[2]), *free = plain(o[3]), *count = plain(o[4]);
     if (!table) return not_here();
     const Place at{at::kInt, table->get_device()};
@@ -523,6 +523,12 @@ try {
         lengths->size(0) != table->size(0) || fresh->size(0) != table->size(0) || count->size(0) != 1 ||
         (table->size(0) > 1 && table->stride(0) < table->size(1)))
         return not_here();
+    a.back = nullptr;
+    if (o[10] != Py_None) {
+        const at::Tensor *t = plain(o[10]);
+        if (!at.ints(t, 1) || t->size(0) != table->size(0)) return not_here();
+        a.back = t->const_data_ptr<int32_t>();
+    }
     a.page_size = PyLong_AsLongLong(o[5]);
     a.tokens = PyLong_AsLongLong(o[6]);
     if (PyErr_Occurred() || a.tokens < 0 || a.tokens > (1 << 24) || !visible_of(o[7], o[8], a.window, a.sinks)) return not_here();

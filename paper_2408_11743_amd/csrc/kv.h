@@ -129,6 +129,7 @@ struct PagesProblem {
     int64_t *slots;
     int32_t *before;  // workspace: [B] pages taken before the sequence, then the free ones' count
     int B, width, pages, page_shift, tokens, window, sinks;
+    const int32_t *back;  // [B] tokens taken back first, or NULL
 };
 
 hipError_t launch_pages(const PagesProblem &p, hipStream_t stream);

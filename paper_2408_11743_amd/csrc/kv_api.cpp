@@ -385,7 +385,8 @@ marlin_status_t marlin_assign_pages(const marlin_assign_pages_args *a, hipStream
         (a->tokens > 0 && !a->slots) || !a->workspace)
         return MARLIN_ERR_NULL_POINTER;
     if (!aligned(a->table, 4) || !aligned(a->lengths, 4) || !aligned(a->new_tokens, 4) || !aligned(a->free_pages, 4) ||
-        !aligned(a->free_count, 4) || !aligned(a->starts, 4) || !aligned(a->slots, 8) || !aligned16(a->workspace))
+        !aligned(a->free_count, 4) || !aligned(a->starts, 4) || !aligned(a->slots, 8) || !aligned16(a->workspace) ||
+        !aligned(a->back, 4))
         return MARLIN_ERR_MISALIGNED;
     if (a->workspace_bytes < marlin_assign_pages_workspace_bytes(a->B)) return MARLIN_ERR_WORKSPACE_TOO_SMALL;
     PagesProblem p;
@@ -397,6 +398,7 @@ marlin_status_t marlin_assign_pages(const marlin_assign_pages_args *a, hipStream
     p.free_count = a->free_count;
     p.starts = a->starts;
     p.slots = a->slots;
+    p.back = a->back;
     p.before = (int32_t *)((char *)a->workspace + kCounterRegionBytes);
     p.B = (int)a->B;
     p.width = (int)a->width;

@@ -1,4 +1,4 @@
-// The page tables of a step: pages that ended sequences and windows leave go back to the free ones,
+// The page tables of a step: pages that ended sequences, windows and tokens taken back leave go back to the free ones,
 // new tokens get pages from there, and each its slot (marlin_assign_pages).
 //
 // All of it follows from sums over the sequences in their order: of pages given back, of pages needed, of new
@@ -79,7 +79,8 @@ __device__ __forceinline__ int64_t slot_of_token(const PagesProblem &p, int b, i
     return (uint32_t)page >= (uint32_t)p.pages ? -1 : ((int64_t)page << p.page_shift) + (pos & ((1 << p.page_shift) - 1));
 }
 
-template <bool Fused>
+// Back: tokens are taken back; a variant, as looking for them took 0.3 us of each call.
+template <bool Fused, bool Back>
 __global__ void __launch_bounds__(kThreads) assign_kernel(const PagesProblem p)
 {
     __shared__ Two lds_sums[kSums], lds_served[kSums];
@@ -91,85 +92,96 @@ __global__ void __launch_bounds__(kThreads) assign_kernel(const PagesProblem p)
     int count = *p.free_count;
     count = count < 0 ? 0 : count < p.pages ? count : p.pages;
 
-    auto length_of = [&](int b) {
+    auto whole_length_of = [&](int b) {
         const int n = p.lengths[b];
         return n < 0 ? 0 : n < cap ? n : cap;
+    };
+    // without the tokens that are taken back
+    auto length_of = [&](int b) {
+        const int n = whole_length_of(b), back = Back ? p.back[b] : 0;
+        return back <= 0 ? n : n > back ? n - back : 0;
     };
 
     // ---- given back ----
     Two returned{0, 0};
     int had0 = 0, new0 = 0;  // of the first 1024 sequences
-    for (int b0 = 0; b0 < p.B; b0 += kThreads) {
-        const int b = b0 + tid;
-        if (tid == 0) lds_works = 0;
-        __syncthreads();
-        // entries first .. last - 1 are looked at, all of them (an ended sequence's) or from the last down to one that names no page
-        int first = 0, last = 0;
-        bool ends = false;
-        if (b < p.B) {
-            const int had = length_of(b), fresh = p.new_tokens[b];
-            if (b0 == 0) {
-                had0 = had;
-                new0 = fresh;
-            }
-            ends = fresh < 0;
-            if (ends) {
-                last = (had + ps - 1) >> p.page_shift;
-            } else if (p.window > 0 && had > p.window) {
-                first = (p.sinks + ps - 1) >> p.page_shift;
-                last = (had - p.window) >> p.page_shift;
-                if (last > first && (uint32_t)p.table[b * p.table_row + last - 1] >= (uint32_t)p.pages) last = 0;
-            }
-        }
-        lds_given[tid] = 0;
-        if (last > first) {
-            const int at = atomicAdd(&lds_works, 1);  // in any order
-            lds_of[at] = tid;
-            lds_first[at] = first;
-            lds_last[at] = ends ? last | 1 << 31 : last;
-        }
-        __syncthreads();
-        const int works = lds_works;
-        if (works == 0) continue;
-        // a sequence is a wave's, 64 entries at a time
-        for (int i = wave; i < works; i += kSums) {
-            const int of = lds_of[i], f = lds_first[i], l = lds_last[i] & 0x7FFFFFFF;
-            const bool whole = lds_last[i] < 0;
-            const int32_t *const row = p.table + (int64_t)(b0 + of) * p.table_row;
-            int n = 0;
-            for (int at = l; at > f; at -= 64) {
-                const int e = at - 1 - lane;
-                const uint64_t named = __builtin_amdgcn_ballot_w64(e >= f && (uint32_t)row[e >= f ? e : f] < (uint32_t)p.pages);
-                if (whole) {
-                    n += __popcll(named);
-                } else {
-                    const int run = ~named ? __builtin_ctzll(~named) : 64;
-                    n += run;
-                    if (run < 64) break;
+    for (int pass = Back ? 0 : 1; pass < 2; ++pass) {  // pages without a token left, then those of ended sequences and behind windows
+        const bool taken_back = Back && pass == 0;
+        for (int b0 = 0; b0 < p.B; b0 += kThreads) {
+            const int b = b0 + tid;
+            if (tid == 0) lds_works = 0;
+            __syncthreads();
+            // entries first .. last - 1 are looked at, all of them (an ended sequence's) or from the last down to one that names no page
+            int first = 0, last = 0;
+            bool ends = false;
+            if (b < p.B) {
+                const int had = length_of(b), fresh = p.new_tokens[b];
+                if (b0 == 0) {
+                    had0 = had;
+                    new0 = fresh;
+                }
+                ends = fresh < 0 || taken_back;
+                if (taken_back) {
+                    first = (had + ps - 1) >> p.page_shift;
+                    last = (whole_length_of(b) + ps - 1) >> p.page_shift;
+                } else if (ends) {
+                    last = (had + ps - 1) >> p.page_shift;
+                } else if (p.window > 0 && had > p.window) {
+                    first = (p.sinks + ps - 1) >> p.page_shift;
+                    last = (had - p.window) >> p.page_shift;
+                    if (last > first && (uint32_t)p.table[b * p.table_row + last - 1] >= (uint32_t)p.pages) last = 0;
                 }
             }
-            if (lane == 0) lds_given[of] = n;
-        }
-        __syncthreads();
-        const Two upto = block_scan({(uint32_t)lds_given[tid], 0}, returned, lds_sums, lane, wave, kSums);
-        lds_upto[tid] = (int)upto.a;
-        __syncthreads();
-        // written in ascending order: the run below a window's end is its last entries
-        for (int i = wave; i < works; i += kSums) {
-            const int of = lds_of[i], l = lds_last[i] & 0x7FFFFFFF, n = lds_given[of], f = lds_last[i] < 0 ? lds_first[i] : l - n;
-            int32_t *const row = p.table + (int64_t)(b0 + of) * p.table_row;
-            int64_t to = (int64_t)count + (uint32_t)lds_upto[of] - n;
-            for (int at = f; at < l; at += 64) {
-                const int e = at + lane;
-                const int page = e < l ? row[e] : -1;
-                const bool named = (uint32_t)page < (uint32_t)p.pages;
-                const uint64_t all = __builtin_amdgcn_ballot_w64(named);
-                const int64_t at_free = to + __popcll(all & (((uint64_t)1 << lane) - 1));
-                if (named) {
-                    if (at_free < p.pages) p.free_pages[at_free] = page;
-                    row[e] = -1;
+            lds_given[tid] = 0;
+            if (last > first) {
+                const int at = atomicAdd(&lds_works, 1);  // in any order
+                lds_of[at] = tid;
+                lds_first[at] = first;
+                lds_last[at] = ends ? last | 1 << 31 : last;
+            }
+            __syncthreads();
+            const int works = lds_works;
+            if (works == 0) continue;
+            // a sequence is a wave's, 64 entries at a time
+            for (int i = wave; i < works; i += kSums) {
+                const int of = lds_of[i], f = lds_first[i], l = lds_last[i] & 0x7FFFFFFF;
+                const bool whole = lds_last[i] < 0;
+                const int32_t *const row = p.table + (int64_t)(b0 + of) * p.table_row;
+                int n = 0;
+                for (int at = l; at > f; at -= 64) {
+                    const int e = at - 1 - lane;
+                    const uint64_t named = __builtin_amdgcn_ballot_w64(e >= f && (uint32_t)row[e >= f ? e : f] < (uint32_t)p.pages);
+                    if (whole) {
+                        n += __popcll(named);
+                    } else {
+                        const int run = ~named ? __builtin_ctzll(~named) : 64;
+                        n += run;
+                        if (run < 64) break;
+                    }
                 }
-                to += __popcll(all);
+                if (lane == 0) lds_given[of] = n;
+            }
+            __syncthreads();
+            const Two upto = block_scan({(uint32_t)lds_given[tid], 0}, returned, lds_sums, lane, wave, kSums);
+            lds_upto[tid] = (int)upto.a;
+            __syncthreads();
+            // written in ascending order: the run below a window's end is its last entries
+            for (int i = wave; i < works; i += kSums) {
+                const int of = lds_of[i], l = lds_last[i] & 0x7FFFFFFF, n = lds_given[of], f = lds_last[i] < 0 ? lds_first[i] : l - n;
+                int32_t *const row = p.table + (int64_t)(b0 + of) * p.table_row;
+                int64_t to = (int64_t)count + (uint32_t)lds_upto[of] - n;
+                for (int at = f; at < l; at += 64) {
+                    const int e = at + lane;
+                    const int page = e < l ? row[e] : -1;
+                    const bool named = (uint32_t)page < (uint32_t)p.pages;
+                    const uint64_t all = __builtin_amdgcn_ballot_w64(named);
+                    const int64_t at_free = to + __popcll(all & (((uint64_t)1 << lane) - 1));
+                    if (named) {
+                        if (at_free < p.pages) p.free_pages[at_free] = page;
+                        row[e] = -1;
+                    }
+                    to += __popcll(all);
+                }
             }
         }
     }
@@ -211,6 +223,8 @@ __global__ void __launch_bounds__(kThreads) assign_kernel(const PagesProblem p)
                 p.lengths[b] = had + n;
             else if (n < 0)
                 p.lengths[b] = 0;
+            else if (Back && p.back[b] > 0)
+                p.lengths[b] = had;
             if (Fused) {
                 if (p.B <= kThreads) {
                     lds_starts[b + 1] = (int)end;
@@ -263,8 +277,9 @@ hipError_t launch_pages(const PagesProblem &p, hipStream_t stream)
     PagesProblem q = p;
     void *args[] = {&q};
     const bool fused = p.tokens <= kFusedTokens;
-    const hipError_t e = hipLaunchKernel(fused ? (const void *)&assign_kernel<true> : (const void *)&assign_kernel<false>, dim3(1),
-                                         dim3(kThreads), args, 0, stream);
+    const void *const kernel = !p.back ? (fused ? (const void *)&assign_kernel<true, false> : (const void *)&assign_kernel<false, false>)
+                                       : (fused ? (const void *)&assign_kernel<true, true> : (const void *)&assign_kernel<false, true>);
+    const hipError_t e = hipLaunchKernel(kernel, dim3(1), dim3(kThreads), args, 0, stream);
     if (e != hipSuccess || fused) return e;
     return hipLaunchKernel((const void *)&slots_kernel, dim3((p.tokens + 255) / 256), dim3(256), args, 0, stream);
 }

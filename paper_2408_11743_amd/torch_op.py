@@ -137,14 +137,14 @@ def _cache_attention_fake(q, k_cache, v_cache, table, lengths, scales=None, star
 
 @torch.library.custom_op(_NS + "::assign_pages", mutates_args=("table", "lengths", "free", "free_count"))
 def assign_pages(table: torch.Tensor, lengths: torch.Tensor, new: torch.Tensor, free: torch.Tensor, free_count: torch.Tensor,
-                 page_size: int, tokens: int, window: int = 0, sinks: int = 0) -> Tuple[torch.Tensor, torch.Tensor]:
-    args = table, lengths, new, free, free_count, page_size, tokens, window or None, sinks, None
+                 page_size: int, tokens: int, window: int = 0, sinks: int = 0, back: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    args = table, lengths, new, free, free_count, page_size, tokens, window or None, sinks, None, back
     done = (cache._native or cache._connect()).assign_pages(*args)
     return cache._assign_pages(*args) if done is None else done
 
 
 @assign_pages.register_fake
-def _assign_pages_fake(table, lengths, new, free, free_count, page_size, tokens, window=0, sinks=0):
+def _assign_pages_fake(table, lengths, new, free, free_count, page_size, tokens, window=0, sinks=0, back=None):
     if table.dim() != 2 or tokens < 0:
         raise ValueError("marlin_mi355x::assign_pages: table must be [sequences, width], tokens at least 0")
     return table.new_empty(table.shape[0] + 1), table.new_empty(tokens, dtype=torch.int64)

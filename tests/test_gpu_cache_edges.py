@@ -1,12 +1,13 @@
-"""Attention of several new tokens where a result can go wrong without a crash: infinite values."""
+"""The 8-bit cache's neighbours where a result can go wrong without a crash: infinite values, softmax weights, pages of tokens taken back."""
 import math
 
 import pytest
 
 torch = pytest.importorskip("torch")
 
+import cache_back  # noqa: E402
 import cache_reference as ref  # noqa: E402
-from test_gpu_cache import check, cuda, make, mk  # noqa: E402, F401
+from test_gpu_cache import check, cuda, expect, gen, make, mk, serve, state  # noqa: E402, F401
 
 pytestmark = pytest.mark.gpu
 
@@ -152,3 +153,102 @@ def test_weights_of_scales_far_apart(mk, new, hq, dtype, apart):
     if dtype == F16:
         args["scales"][:, :, 1] = torch.where(args["scales"][:, :, 1] < 1, 2.0 ** (4 - apart if apart < 30 else 6 - apart), args["scales"][:, :, 1])
     held_to(mk, args)
+
+
+# ---- tokens taken back ----
+
+def check_back(mk, table, lengths, new, free, count, ps, tokens, back, window=None, sinks=0):
+    want = cache_back.assign_pages(table, lengths, new, free, count, ps, tokens, window, sinks, back)
+    on = [x.cuda() for x in (table, lengths, new, free, torch.tensor([count], dtype=torch.int32))]
+    starts, slots = mk.assign_pages(*on, ps, tokens, window=window, sinks=sinks, back=back.cuda())
+    for name, x, y in zip(("table", "lengths", "free", "count", "starts", "slots"), want, (on[0], on[1], on[3], on[4], starts, slots)):
+        x = torch.tensor([x], dtype=torch.int32) if name == "count" else x
+        assert torch.equal(x, y.cpu()), (name, x, y)
+
+
+@pytest.mark.parametrize("B", [1, 2, 64, 200, 1023, 1024, 1025, 2500])
+@pytest.mark.parametrize("tokens", [0, 100, 4096, 4097, 200000])
+@pytest.mark.parametrize("window,sinks", [(None, 0), (40, 5)])
+def test_pages_of_tokens_taken_back(mk, B, tokens, window, sinks):
+    table, lengths, new, free, count = state(B + tokens, B, 16, 200, 2 * B, windowed=window is not None)
+    g = gen(B)
+    back = torch.randint(-3, 40, (B,), generator=g).int()
+    back[torch.rand(B, generator=g) < 0.1] = 1000
+    check_back(mk, table, lengths, new, free, count, 16, tokens, back, window, sinks)
+    check_back(mk, table, lengths, torch.where(new < 0, new, 1), free, count, 16, tokens, back.clamp(max=4), window, sinks)
+
+
+def test_tokens_taken_back_at_the_edges(mk):
+    # lengths past the table and below none, all of a sequence, a full list, the largest numbers
+    table, lengths, new, free, count = state(1, 20, 16, 100, 60, width=7)
+    back = torch.full((20,), 20, dtype=torch.int32)
+    lengths[0], lengths[1], lengths[2] = 112, 5000, -4
+    back[3], back[4], back[5], back[6] = 2 ** 31 - 1, -(2 ** 31), 100, 0
+    new[0], new[1], new[3], new[4] = 1, 30, 5, -1
+    check_back(mk, table, lengths, new, free, count, 16, 500, back)
+    check_back(mk, table, lengths, new, free, len(free) - 2, 16, 500, back)
+    table[7:12] = -1  # nothing of theirs is a page
+    check_back(mk, table, lengths, new, free, count, 16, 500, back)
+    with pytest.raises(ValueError):
+        mk.assign_pages(*[x.cuda() for x in (table, lengths, new, free, torch.tensor([count], dtype=torch.int32))], 16, 500, back=back[:3].cuda())
+    with pytest.raises(TypeError):
+        mk.assign_pages(*[x.cuda() for x in (table, lengths, new, free, torch.tensor([count], dtype=torch.int32))], 16, 500, back=back.long().cuda())
+
+
+@pytest.mark.parametrize("bits,dtype", [(8, F16), (16, BF16)])
+@pytest.mark.parametrize("window,sinks", [(None, 0), (40, 5)])
+def test_steps_of_drafts(mk, bits, dtype, window, sinks):
+    """Drafted tokens of which some are accepted, step after step over page borders: every page is in one place once, and the attention is that of
+    what was kept."""
+    st, _, (hq, hkv, D, B) = serve(mk, bits, dtype, window, sinks)
+    g, ps, pages = gen(4), 16, 200
+    back = torch.zeros(B, dtype=torch.int32)
+    kept = torch.zeros(B, dtype=torch.int32)
+    for i in range(40):
+        new = torch.tensor([20, 3, 17, 1, 40, 16]) if i == 0 else torch.full((B,), 5)
+        if i == 25:
+            new[2] = -1
+        tokens = int(new.clamp(min=0).sum())
+        q, k, v = torch.randn(tokens, hq + 2 * hkv, D, generator=g).to(dtype).cuda().split([hq, hkv, hkv], 1)
+        starts, slots = mk.assign_pages(st["table"], st["lengths"], new.int().cuda(), st["free"], st["count"], ps, tokens, window=window, sinks=sinks,
+                                        back=back.cuda())
+        kept = torch.where(new < 0, 0, kept - back + new.int())
+        assert torch.equal(st["lengths"].cpu(), kept.int()) and int(starts[-1]) == tokens and (slots >= 0).all()
+        if bits == 8:
+            q = mk.kv_append8(q, k, v, st["k"], st["v"], st["s"], st["table"], st["lengths"], st["cs"], starts)
+        else:
+            q = mk.kv_append(q, k, v, st["k"], st["v"], st["table"], st["lengths"], st["cs"], starts)
+        o = mk.cache_attention(q, st["k"], st["v"], st["table"], st["lengths"], st["s"], starts, window, sinks)
+        want, _, tol, _, mine = expect(st, q, starts, window, sinks)
+        assert mine.all() and ((o.cpu().double() - want).abs() <= tol).all()
+        both = torch.cat([st["table"][st["table"] >= 0], st["free"][:int(st["count"])]]).long().cpu()
+        assert len(both) == pages and len(both.unique()) == pages
+        back = torch.randint(0, 5, (B,), generator=g).int().clamp(max=kept)  # one of five drafts is accepted at least
+
+
+def test_tokens_taken_back_in_a_graph_and_by_the_operator(mk):
+    table, lengths, new, free, count = state(5, 100, 16, 300, 400)
+    back = torch.randint(0, 30, (100,), generator=gen(5)).int().cuda()
+    first = [x.cuda() for x in (table, lengths, new, free, torch.tensor([count], dtype=torch.int32))]
+    def fresh():
+        return [x.clone() for x in first]
+    want = fresh()
+    want += mk.assign_pages(*want, 16, 3000, 200, 3, back=back)
+    got = fresh()
+    got += torch.ops.marlin_mi355x.assign_pages(*got, 16, 3000, 200, 3, back)
+    assert all(torch.equal(a, b) for a, b in zip(want, got))
+    on = fresh()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        mk.assign_pages(*on, 16, 3000, 200, 3, back=back)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        out = mk.assign_pages(*on, 16, 3000, 200, 3, back=back)
+    for _ in range(3):
+        for a, b in zip(on, first):
+            a.copy_(b)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(want, [*on, *out]))
