@@ -10,7 +10,7 @@ by ``cache_attention``; a decode step is pages, projection, append, attention, p
 --select the attention reads the most promising pages only, with --bits 8 the cache is in 8 bits, and with --window
 a token sees the last ones and --sinks first ones, and pages behind them go to other tokens.  The graph is
 captured once: tables and lengths live on the device, so its replays follow the
-sequences as they grow.  Weights and prompts are random.
+sequences as they grow, and pass over one that there are no pages for.  Weights and prompts are random.
 """
 import argparse
 import os
@@ -36,11 +36,12 @@ class Attention(torch.nn.Module):
         self.out = linear(hidden, heads * head_dim)
         self.register_buffer("cos_sin", mk.rotation_table(positions, head_dim))
 
-    def forward(self, x, cache, starts=None, select=0):
-        """x [tokens, hidden]: one new token per sequence, or with ``starts`` each one's prompt."""
+    def forward(self, x, cache, starts=None, lengths=None, select=0):
+        """x [tokens, hidden]: with ``starts`` each sequence's new tokens, or one of every sequence, but those with a 0 in ``lengths``."""
         k_cache, v_cache, extra = cache["pages"]  # scales in 8 bits, else bounds
         seen = dict(window=cache["window"], sinks=cache["sinks"])
-        table, lengths, eight = cache["table"], cache["lengths"], k_cache.dtype == torch.float8_e4m3fn
+        table, eight = cache["table"], k_cache.dtype == torch.float8_e4m3fn
+        lengths = cache["lengths"] if lengths is None else lengths
         rows = self.qkv(x).view(x.shape[0], -1, self.head_dim)
         q, k, v = rows.split([self.heads, self.kv_heads, self.kv_heads], 1)
         if eight:
@@ -98,8 +99,9 @@ def main(argv=None):
     one = torch.ones_like(cache["lengths"])
 
     def step():
-        give_pages(cache, one, a.sequences)
-        x.copy_(torch.nn.functional.normalize(layer(x, cache, select=a.select).float(), dim=1).mul_(a.hidden ** 0.5))
+        starts = give_pages(cache, one, a.sequences)
+        lengths = torch.where(starts[1:] > starts[:-1], cache["lengths"], 0)  # of those that got pages
+        x.copy_(torch.nn.functional.normalize(layer(x, cache, lengths=lengths, select=a.select).float(), dim=1).mul_(a.hidden ** 0.5))
 
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())

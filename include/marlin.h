@@ -604,6 +604,7 @@ size_t marlin_assign_pages_workspace_bytes(int64_t B);
  *  2. A sequence with n > 0 is served if L + n fits the table, and if the pages that it and the
  *     fitting sequences before it need are among the free ones, their new tokens among `tokens`.  It takes pages from
  *     the end of the free ones, the last first, and its length becomes L + n.  A sequence that is not served keeps its length and gets nothing.
+ *     (An entry point called without starts would put a token over its last one: there its length has to be 0.)
  *  starts: where each sequence's new tokens begin (those of a sequence not served: none), as the other entry
  *  points take it.  slots[t]: page * page_size + slot of new token t, -1 where
  *  the sequence's last page so far is no page, or behind the last token.

@@ -10,8 +10,16 @@ the device, is
     q = kv_append8(q, k, v, k_cache, v_cache, scales, table, lengths, cos_sin, starts)
     o = cache_attention(q, k_cache, v_cache, table, lengths, scales, starts)
 
-with ``starts`` left out where every sequence has one new token.  ``cache_attention`` takes the 16-bit
-caches of ``kv_cache`` as well (without scales), behind ``kv_append``.
+``cache_attention`` takes the 16-bit caches of ``kv_cache`` as well (without scales), behind ``kv_append``.
+
+Without ``starts`` every row of the table has one new token, row b of q, k and v, at position lengths[b] - 1: a sequence that
+``assign_pages`` gave none (``new[b]`` of 0, or no pages left) keeps its length, and its row would be written over its last token.
+Where that can be, a decode step takes lengths of 0 for those, which the calls without ``starts`` pass over:
+
+    starts, slots = assign_pages(table, lengths, ones, free, free_count, page_size, len(table))
+    now = torch.where(starts[1:] > starts[:-1], lengths, 0)
+    q = kv_append8(q, k, v, k_cache, v_cache, scales, table, now, cos_sin)
+    o = cache_attention(q, k_cache, v_cache, table, now, scales)
 
 What ``kv``'s functions do about arguments, streams, workspaces, graphs, gradients, modes and transforms, these do too.
 """
@@ -228,7 +236,7 @@ def assign_pages(table: torch.Tensor, lengths: torch.Tensor, new: torch.Tensor, 
     token's page * page_size + slot, -1 behind the last.
 
     Sequences are served in their order while pages, room in the table and ``tokens`` rows last; one that is not gets no tokens in this
-    step and keeps its length (its rows in ``starts`` are none).  With ``window`` the pages that a token sees neither through it nor among the
+    step and keeps its length (its rows in ``starts`` are none; calls without ``starts`` have to be told: see the module's docstring).  With ``window`` the pages that a token sees neither through it nor among the
     first ``sinks`` positions are given back and their entries become -1.
 
     ``back`` int32 [sequences] takes tokens back first: drafted ones that were not accepted.  Lengths fall by it, and the pages that no token is

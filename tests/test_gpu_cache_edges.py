@@ -252,3 +252,39 @@ def test_tokens_taken_back_in_a_graph_and_by_the_operator(mk):
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(want, [*on, *out]))
+
+
+# ---- sequences that get nothing ----
+
+@pytest.mark.parametrize("bits,dtype", [(8, F16), (16, F16), (8, BF16)])
+@pytest.mark.parametrize("window,sinks", [(None, 0), (40, 5)])
+def test_decode_where_some_sequences_get_nothing(mk, bits, dtype, window, sinks):
+    """Pages run out and some ask for nothing: the calls for one token, given 0 for their lengths, leave their tokens as they are."""
+    st, step, (hq, hkv, D, B) = serve(mk, bits, dtype, window, sinks)
+    g = gen(6)
+    first = torch.tensor([30, 64, 1, 16, 130, 9], dtype=torch.int32)
+    rows = torch.randn(int(first.sum()), hq + 2 * hkv, D, generator=g).to(dtype).cuda()
+    step(rows, first.cuda(), len(rows))
+    st["count"].fill_(2)  # pages for two sequences more
+    ones, passed_over = torch.tensor([1, 1, 1, 1, 0, 1], dtype=torch.int32).cuda(), 0
+    for _ in range(20):
+        q, k, v = torch.randn(B, hq + 2 * hkv, D, generator=g).to(dtype).cuda().split([hq, hkv, hkv], 1)
+        before = st["lengths"].clone()
+        starts, _ = mk.assign_pages(st["table"], st["lengths"], ones, st["free"], st["count"], 16, B, window=window, sinks=sinks)
+        served = starts[1:] > starts[:-1]
+        assert torch.equal(st["lengths"] - before, served.int())
+        now = torch.where(served, st["lengths"], 0)
+        old = [x.view(torch.uint8).clone() for x in (st["k"], st["v"], st["s"]) if x is not None]
+        if bits == 8:
+            q = mk.kv_append8(q, k, v, st["k"], st["v"], st["s"], st["table"], now, st["cs"])
+        else:
+            q = mk.kv_append(q, k, v, st["k"], st["v"], st["table"], now, st["cs"])
+        o = mk.cache_attention(q, st["k"], st["v"], st["table"], now, st["s"], None, window, sinks)
+        mine = st["table"][~served].flatten()
+        mine = mine[mine >= 0].long()
+        passed_over += int((~served).sum())
+        for x, y in zip([x for x in (st["k"], st["v"], st["s"]) if x is not None], old):
+            assert torch.equal(x.view(torch.uint8)[mine], y[mine])
+        want, _, tol, _, _ = expect({**st, "lengths": now}, q, None, window, sinks)
+        assert ((o.cpu().double() - want).abs() <= tol).all() and (o[~served] == 0).all() and (q[~served] == 0).all()
+    assert passed_over > 20 and int(st["count"]) == 0
