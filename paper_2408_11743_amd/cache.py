@@ -92,7 +92,7 @@ def kv_append8(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_cache: torch
         return done
     if _watched(q, k, v, k_cache, v_cache, scales, table, lengths, cos_sin, starts, out):
         y = torch.ops.marlin_mi355x.kv_append8(q, k, v, k_cache, v_cache, scales, table, lengths, cos_sin, starts, bool(interleaved))
-        return _into("kv_append8", out, y)
+        return _into("kv_append8", out, y, starts)
     return _kv_append8(q, k, v, k_cache, v_cache, scales, table, lengths, cos_sin, starts, interleaved, out)
 
 
@@ -170,7 +170,7 @@ def cache_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tenso
     if _watched(q, k_cache, v_cache, table, lengths, scales, starts, out):
         window, sinks = _visible("cache_attention", window, sinks)
         o, lse = torch.ops.marlin_mi355x.cache_attention(q, k_cache, v_cache, table, lengths, scales, starts, window, sinks, scale)
-        o = _into("cache_attention", out, o)
+        o = _into("cache_attention", out, o, starts)
         return (o, lse) if return_lse else o
     return _cache_attention(q, k_cache, v_cache, table, lengths, scales, starts, window, sinks, scale, return_lse, out, workspace)
 

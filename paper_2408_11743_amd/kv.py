@@ -151,11 +151,15 @@ def _check_out(func: str, out: torch.Tensor, shape, dtype, device) -> None:
           and not out.is_neg(), func, "out must be a contiguous tensor of q's shape, dtype and device")
 
 
-def _into(func: str, out, result: torch.Tensor) -> torch.Tensor:
-    """A registered operator's result, in the caller's tensor if there is one."""
+def _into(func: str, out, result: torch.Tensor, starts: torch.Tensor | None = None) -> torch.Tensor:
+    """A registered operator's result, in the caller's tensor if there is one: with starts, the rows that belong to sequences."""
     if out is None:
         return result
     _check_out(func, out, result.shape, result.dtype, result.device)
+    if starts is not None:
+        row = torch.arange(result.shape[0], dtype=starts.dtype, device=starts.device)
+        mine = (row >= starts[0]) & (row < starts[-1])
+        result = torch.where(mine[:, None, None], result, out)
     return out.copy_(result)
 
 
@@ -194,7 +198,7 @@ def kv_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_cache: torch.
     if _watched(q, k, v, k_cache, v_cache, table, lengths, cos_sin, starts, bounds, out):
         y = torch.ops.marlin_mi355x.kv_append(q, k, v, k_cache, v_cache, bounds, table, lengths, cos_sin, starts,
                                               bool(interleaved))
-        return _into("kv_append", out, y)
+        return _into("kv_append", out, y, starts)
     return _kv_append(q, k, v, k_cache, v_cache, table, lengths, cos_sin, starts, interleaved, bounds, out)
 
 

@@ -288,3 +288,33 @@ def test_decode_where_some_sequences_get_nothing(mk, bits, dtype, window, sinks)
         want, _, tol, _, _ = expect({**st, "lengths": now}, q, None, window, sinks)
         assert ((o.cpu().double() - want).abs() <= tol).all() and (o[~served] == 0).all() and (q[~served] == 0).all()
     assert passed_over > 20 and int(st["count"]) == 0
+
+
+# ---- rows of no sequence ----
+
+@pytest.mark.parametrize("first,new", [(0, [6, 3]), (2, [1, 0]), (0, [40, 25]), (3, [0, 0])])
+def test_rows_of_no_sequence_where_a_mode_sees_the_call(mk, first, new):
+    """What a call writes into out does not go by whether it became the registered operator's."""
+    from torch.utils._python_dispatch import TorchDispatchMode
+
+    class Watch(TorchDispatchMode):
+        def __torch_dispatch__(self, func, types, args=(), kwargs=None):
+            seen.append(str(func))
+            return func(*args, **(kwargs or {}))
+
+    seen, n, rest = [], sum(new), 7
+    a = cuda(make(1, [30 + m for m in new], new, 4, 2, 64, 16, F16, 8, junk=False))
+    a["starts"] += first
+    a["q"] = torch.randn(first + n + rest, 4, 64, generator=gen(7)).half().cuda()
+    kv = torch.randn(2, first + n + rest, 2, 64, generator=gen(8)).half().cuda()
+    k16, v16 = mk.kv_cache(len(a["k_cache"]), 2, 16, 64)
+    where = a["table"], a["lengths"], None, a["starts"]
+    for call in (lambda out: mk.cache_attention(**a, out=out),
+                 lambda out: mk.kv_append8(a["q"], *kv, *[a[x].clone() for x in ("k_cache", "v_cache", "scales")], *where, out=out),
+                 lambda out: mk.kv_append(a["q"], *kv, k16, v16, *where, out=out)):
+        got = [torch.full(a["q"].shape, 123.0, dtype=F16, device="cuda") for _ in range(2)]
+        call(got[0])
+        with Watch():
+            assert call(got[1]) is got[1]
+        assert torch.equal(*got) and (got[0][:first] == 123).all() and (got[0][first + n:] == 123).all()
+    assert any("marlin_mi355x.cache_attention" in x for x in seen)
