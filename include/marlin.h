@@ -612,7 +612,7 @@ size_t marlin_assign_pages_workspace_bytes(int64_t B);
  * looked at and may be overwritten, so who lowers a length in another way than by back has to put those pages among the free ones.
  * A free_count outside 0 .. pages is clamped to it, and pages beyond `pages` free ones are not kept.  An entry of free_pages
  * that names no page is handed out as it is, and its tokens count as masked.
- * B 0 .. 2^16 (0: starts[0] and slots are written), tokens 0 .. 2^24; sizes as above.
+ * B 0 .. 2^16 (0: starts[0] and slots are written), tokens 0 .. 2^24, table_row no less than width where B > 1; sizes as above.
  * Errors: NULL_POINTER, INVALID_SHAPE, MISALIGNED, INVALID_ARGUMENT (window, sinks), WORKSPACE_TOO_SMALL, HIP.
  */
 marlin_status_t marlin_assign_pages(const marlin_assign_pages_args *args, hipStream_t stream);

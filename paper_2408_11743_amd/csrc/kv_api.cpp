@@ -380,6 +380,7 @@ marlin_status_t marlin_assign_pages(const marlin_assign_pages_args *a, hipStream
     if (!a) return MARLIN_ERR_NULL_POINTER;
     if (!shape_ok(a->B, 1, 1, 64, a->pages, a->page_size, a->width) || a->table_row < 0 || a->tokens < 0 || a->tokens > kMaxTokens)
         return MARLIN_ERR_INVALID_SHAPE;
+    if (a->B > 1 && a->table_row < a->width) return MARLIN_ERR_INVALID_SHAPE;  // rows that are written must not overlap
     if (!visible_ok(a->window, a->sinks)) return MARLIN_ERR_INVALID_ARGUMENT;
     if ((a->B > 0 && (!a->table || !a->lengths || !a->new_tokens)) || !a->free_pages || !a->free_count || !a->starts ||
         (a->tokens > 0 && !a->slots) || !a->workspace)

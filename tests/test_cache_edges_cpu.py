@@ -1,4 +1,4 @@
-"""The page tables' tokens taken back without a GPU: refusals, the operator's fake implementation, and the plain form's invariants."""
+"""The page tables without a GPU: tokens taken back (refusals, the operator's fake implementation, the plain form's invariants) and rows that overlap."""
 import random
 
 import pytest
@@ -7,7 +7,7 @@ torch = pytest.importorskip("torch")
 
 import cache_back  # noqa: E402
 import paper_2408_11743_amd as mk  # noqa: E402
-from test_cache_cpu import ALIGN, FAKE, PAGES, WS, invariants, state, status  # noqa: E402
+from test_cache_cpu import ALIGN, FAKE, PAGES, SHAPE, WS, invariants, state, status  # noqa: E402
 
 
 def test_back_is_optional_and_aligned():
@@ -38,3 +38,11 @@ def test_pages_reference_with_tokens_taken_back():
         assert (named == (short[1] + 15) // 16).all()
         invariants((short[0], short[1], short[2], short[3], new), after, 16, tokens)
         assert int(short[3]) + int(named.sum()) == int(count) + int((table >= 0).sum())
+
+
+def test_rows_of_a_table_that_overlap_are_refused():
+    """Both would be written."""
+    for row in (0, 1, PAGES["width"] - 1):
+        assert status("pages", table_row=row, workspace_bytes=8) == SHAPE
+        assert status("pages", table_row=row, B=1, workspace_bytes=8) == WS
+    assert status("pages", table_row=PAGES["width"], workspace_bytes=8) == WS
