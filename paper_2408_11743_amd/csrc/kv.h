@@ -114,8 +114,8 @@ struct PromptPlan {
     int rows, target, slot_floats;
     int64_t groups;
 };
-// positions: of a table's row, at most.
-PromptPlan plan_prompt(int64_t tokens, int64_t B, int64_t heads, int64_t kv_heads, int head_dim, bool eight, int64_t positions);
+// positions: of a table's row, at most.  A plan for more compute units, up to kKvMaxCus, needs no less of the workspace.
+PromptPlan plan_prompt(int64_t tokens, int64_t B, int64_t heads, int64_t kv_heads, int head_dim, bool eight, int64_t positions, int cus);
 size_t prompt_workspace(const PromptPlan &plan);  // bytes behind the counters
 
 hipError_t launch_prompt(const PromptProblem &p, const PromptPlan &plan, int head_dim, marlin_dtype_t dtype, hipStream_t stream);

@@ -274,7 +274,7 @@ size_t marlin_cache_attention_workspace_bytes(int64_t starts, int64_t tokens, in
     if (!starts) return marlin_paged_attention_workspace_bytes(head_dim);
     size_t most = 0;
     for (const bool eight : {false, true}) {
-        const size_t x = prompt_workspace(plan_prompt(tokens, B, heads, kv_heads, (int)head_dim, eight, kMaxPositions));
+        const size_t x = prompt_workspace(plan_prompt(tokens, B, heads, kv_heads, (int)head_dim, eight, kMaxPositions, kKvMaxCus));
         if (x > most) most = x;
     }
     return kCounterRegionBytes + most;
@@ -304,6 +304,10 @@ marlin_status_t marlin_cache_attention(const marlin_cache_attention_args *a, hip
         marlin_cache_attention_workspace_bytes(a->starts != nullptr, a->tokens, a->B, a->heads, a->kv_heads, a->head_dim))
         return MARLIN_ERR_WORKSPACE_TOO_SMALL;
 
+    int device = 0;
+    if (hipGetDevice(&device) != hipSuccess) return MARLIN_ERR_HIP;
+    const int cus = device_cu_count(device);
+    if (cus <= 0) return MARLIN_ERR_HIP;
     if (a->starts) {
         PromptProblem p;
         p.q = a->q;
@@ -334,13 +338,10 @@ marlin_status_t marlin_cache_attention(const marlin_cache_attention_args *a, hip
         p.scale_log2 = std::fabs(scale) > least ? std::fabs(scale) : least;
         p.q_and = std::fabs(scale) > 0 ? 0xFFFFFFFFu : 0u;
         p.q_xor = scale < 0 ? 0x80008000u : 0u;
-        const PromptPlan plan = plan_prompt(a->tokens, a->B, a->heads, a->kv_heads, (int)a->head_dim, a->scales != nullptr, a->width * a->page_size);
+        const PromptPlan plan = plan_prompt(a->tokens, a->B, a->heads, a->kv_heads, (int)a->head_dim, a->scales != nullptr,
+                                            a->width * a->page_size, cus);
         return launch_prompt(p, plan, (int)a->head_dim, (marlin_dtype_t)a->dtype, stream) == hipSuccess ? MARLIN_OK : MARLIN_ERR_HIP;
     }
-    int device = 0;
-    if (hipGetDevice(&device) != hipSuccess) return MARLIN_ERR_HIP;
-    const int cus = device_cu_count(device);
-    if (cus <= 0) return MARLIN_ERR_HIP;
     AttendProblem p;
     p.q = a->q;
     p.q_row = a->q_row;

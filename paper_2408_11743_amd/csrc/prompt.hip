@@ -1417,7 +1417,7 @@ hipError_t launch_typed(const PromptProblem &p, const PromptPlan &plan, int head
 
 }  // namespace
 
-PromptPlan plan_prompt(int64_t tokens, int64_t B, int64_t heads, int64_t kv_heads, int head_dim, bool eight, int64_t positions)
+PromptPlan plan_prompt(int64_t tokens, int64_t B, int64_t heads, int64_t kv_heads, int head_dim, bool eight, int64_t positions, int cus)
 {
     PromptPlan x;
     const int64_t rows = tokens * (heads / kv_heads);  // of one kv head
@@ -1432,7 +1432,7 @@ PromptPlan plan_prompt(int64_t tokens, int64_t B, int64_t heads, int64_t kv_head
     int per_cu = head_dim == 256 ? 1 : 2;
     if (x.few && head_dim == 64) per_cu = x.rows == 16 ? 4 : 3;
     if (x.few && x.rows == 16 && (head_dim == 96 || (head_dim == 128 && eight))) per_cu = 3;
-    const int64_t target = 256 * per_cu, least = rows / x.rows * kv_heads, most = (rows / x.rows + sequences) * kv_heads;  // tiles
+    const int64_t target = (cus < kKvMaxCus ? cus : kKvMaxCus) * per_cu, least = rows / x.rows * kv_heads, most = (rows / x.rows + sequences) * kv_heads;  // tiles
     const int64_t steps = positions >> 4 >> (x.few ? Few::kShift : Many::kShift);
     x.target = least < target && most < 2 * target && steps >= 2 * (x.few ? Few::kLeast : Many::kLeast) ? (int)target : 0;
     // a tile's last part is not a whole one; and the steps are added up in floats
