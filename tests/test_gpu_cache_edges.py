@@ -1,4 +1,6 @@
-"""The 8-bit cache's neighbours where a result can go wrong without a crash: infinite values, softmax weights, pages of tokens taken back."""
+"""The 8-bit cache's neighbours where a result can go wrong without a crash: infinite values, softmax weights, pages of tokens taken back,
+sequences that get nothing, rows of no sequence, any number of kv heads.
+"""
 import math
 
 import pytest
@@ -318,3 +320,18 @@ def test_rows_of_no_sequence_where_a_mode_sees_the_call(mk, first, new):
             assert call(got[1]) is got[1]
         assert torch.equal(*got) and (got[0][:first] == 123).all() and (got[0][first + n:] == 123).all()
     assert any("marlin_mi355x.cache_attention" in x for x in seen)
+
+
+# ---- kv heads that do not divide the work-groups ----
+
+@pytest.mark.parametrize("hq,hkv", [(3, 3), (6, 3), (5, 5), (20, 5), (40, 40), (12, 12)])
+@pytest.mark.parametrize("new,cached", [([4], [5000]), ([3, 5, 1], [3000, 700, 6000]), ([130], [4000]), ([140, 1, 70], [2500, 4000, 100])])
+@pytest.mark.parametrize("bits,D", [(8, 128), (16, 64)])
+def test_shared_keys_of_any_number_of_heads(mk, hq, hkv, new, cached, bits, D):
+    """Every row of out is written, whatever the kv heads: parts, records and pieces go by their number."""
+    args = make(hkv, [c + n for c, n in zip(cached, new)], new, hq, hkv, D, 32, F16, bits)
+    for more in (dict(), dict(window=2000, sinks=70)):
+        out = torch.full(args["q"].shape, math.nan, dtype=F16, device="cuda")
+        got, lse = mk.cache_attention(**cuda(args), out=out, return_lse=True, **more)
+        want, want_lse, tol, tol_lse, mine = ref.attention(**args, **more)
+        assert mine.all() and ((got.cpu().double() - want).abs() <= tol).all() and ((lse.cpu().double() - want_lse).abs() <= tol_lse).all()
