@@ -73,7 +73,8 @@ __device__ __forceinline__ float16_t mfma32(Elem<__bf16>::vec8 a, Elem<__bf16>::
 
 // A masked key's value may be anything, and its weight of zero does not take an infinity or NaN away.  In steps in which some rows
 // do not see all keys what is not finite is left out of the second product, and added by itself for the rows that do see it.
-// In the others an infinity becomes NaN where its weight is too small for T: results that are NaN are looked into at the end.
+// In the others an infinity becomes NaN where its weight is too small for T: results that are NaN are looked into at the end, until all
+// of them are settled (a prompt of 8192 tokens with one NaN among its values 1.4 ms, with nothing else 1.1, without any 0.65 to 0.78).
 //
 // A dword of elements, or of codes, without those that are not finite.
 template <typename T, bool Eight>
@@ -100,6 +101,20 @@ __device__ __forceinline__ float odd_at(const void *cache, int64_t at)
     return __builtin_fabsf(x) < INFINITY ? 0.f : x;
 }
 
+// Whether the values of a tile of keys, whose first is at `values`, are not all finite.
+template <typename T, int D>
+__device__ __forceinline__ bool odd_tile(const T *values, int lane)
+{
+    uint32_t odd = 0;
+#pragma unroll
+    for (int i = 0; i < kTileKeys * D / 512; ++i) {
+        const u32x4_t w = *(const u32x4_t *)(values + (lane + 64 * i) * 8);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) odd |= w[e] ^ finite_of<T, false>(w[e]);
+    }
+    return __any(odd != 0);
+}
+
 // A result that is NaN, and may not be if its row's sum is a number: marked, the first value that is not finite takes its place, others
 // are added.  If there is none it stays a NaN.
 constexpr uint32_t kMarked = 0x7FC0BEEFu;  // no element becomes this one
@@ -108,6 +123,8 @@ __device__ __forceinline__ float add_to_marked(float x, float odd)
 {
     return odd == 0.f ? x : __builtin_bit_cast(uint32_t, x) == kMarked ? odd : x + odd;
 }
+// More values may change it.
+__device__ __forceinline__ bool is_open(float x) { return (x == x) | (__builtin_bit_cast(uint32_t, x) == kMarked); }
 
 // The keys that a tile's rows see: those below `sinks` and from a window's lower end on, in tiles of 16 of which the first `sink_tiles`
 // and those `skip` further on are taken, 2^shift to a step.
@@ -811,19 +828,28 @@ __global__ void __launch_bounds__(64 * kWaves, D <= 128 ? 2 : 1) prompt_kernel(c
 #pragma unroll
                 for (int i = 0; i < 16; ++i) acc[ct][i] = marked(acc[ct][i], l == l);
 #pragma unroll 1
-            for (int n = 4 * kTileKeys * s0; n < 4 * kTileKeys * s1; ++n) {
-                const int j = keys.position(n / kTileKeys) + n % kTileKeys;
-                if (j >= keys.end) continue;
-                const int entry = scalar_load(table + (j >> p.page_shift));
+            for (int t = 4 * s0; t < 4 * s1; ++t) {
+                const int pos = keys.position(t);
+                if (pos >= keys.end) break;
+                const int entry = scalar_load(table + (pos >> p.page_shift));
                 if ((uint32_t)entry >= (uint32_t)p.pages) continue;
-                const int64_t at = place_of(p, entry, head, j, D);
+                const int64_t first = place_of(p, entry, head, pos, D);
+                if (!odd_tile<T, D>((const T *)p.v + first, lane)) continue;
+#pragma unroll 1
+                for (int j = pos; j < pos + kTileKeys && j < keys.end; ++j)
+#pragma unroll
+                    for (int ct = 0; ct < kCt; ++ct)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            const float x = odd_at<T, Eight>(p.v, first + (j - pos) * D + channel_of(ct, i));
+                            acc[ct][i] = add_to_marked(acc[ct][i], sight.sees(j) ? x : 0.f);
+                        }
+                bool open = false;
 #pragma unroll
                 for (int ct = 0; ct < kCt; ++ct)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const float x = odd_at<T, Eight>(p.v, at + channel_of(ct, i));
-                        acc[ct][i] = add_to_marked(acc[ct][i], sight.sees(j) ? x : 0.f);
-                    }
+                    for (int i = 0; i < 16; ++i) open |= is_open(acc[ct][i]);
+                if (!__any(open & have)) break;
             }
         }
     }
@@ -1185,23 +1211,32 @@ __global__ void __launch_bounds__(64 * kWaves, D > 128 ? 1 : 2) prompt_few_kerne
 #pragma unroll
                     for (int i = 0; i < 4; ++i) acc[rt][j][i] = marked(acc[rt][j][i], of_row[rt] == of_row[rt]);
 #pragma unroll 1
-            for (int at_step = s0 + wave; at_step < s1; at_step += kWaves)
+            for (int t = KT * (s0 + wave); t < KT * s1; t += t % KT + 1 < KT ? 1 : KT * (kWaves - 1) + 1) {
+                const int pos = keys.position(t);
+                if (pos >= keys.end) break;
+                const int entry = scalar_load(table + (pos >> p.page_shift));
+                if ((uint32_t)entry >= (uint32_t)p.pages) continue;
+                const int64_t first = place_of(p, entry, head, pos, D);
+                if (!odd_tile<T, D>((const T *)p.v + first, lane)) continue;
 #pragma unroll 1
-                for (int n = 0; n < kKeys; ++n) {
-                    const int pos = position_of(at_step, n >> 4) + (n & 15);
-                    if (pos >= keys.end) continue;
-                    const int entry = scalar_load(table + (pos >> p.page_shift));
-                    if ((uint32_t)entry >= (uint32_t)p.pages) continue;
-                    const int64_t at = place_of(p, entry, head, pos, D);
+                for (int j = pos; j < pos + kTileKeys && j < keys.end; ++j)
 #pragma unroll
                     for (int c = 0; c < kAcc; ++c)
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
-                            const float x = odd_at<T, Eight>(p.v, at + channel_of(c, 4 * g + i));
+                            const float x = odd_at<T, Eight>(p.v, first + (j - pos) * D + channel_of(c, 4 * g + i));
 #pragma unroll
-                            for (int rt = 0; rt < RT; ++rt) acc[rt][c][i] = add_to_marked(acc[rt][c][i], sight[rt].sees(pos) ? x : 0.f);
+                            for (int rt = 0; rt < RT; ++rt) acc[rt][c][i] = add_to_marked(acc[rt][c][i], sight[rt].sees(j) ? x : 0.f);
                         }
-                }
+                bool open = false;
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                    for (int c = 0; c < kAcc; ++c)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) open |= is_open(acc[rt][c][i]) & (out_at[rt] >= 0);
+                if (!__any(open)) break;
+            }
         }
     }
 
