@@ -304,8 +304,10 @@ hipError_t launch_one(const Append8Problem &p, hipStream_t stream)
     // a sequence of n tokens touches at most n / page size + 2 pages
     const int pages = (p.tokens >> p.page_shift) + 2 * (p.B < p.tokens ? p.B : p.tokens);
     const int slabs = (p.heads + kSlab - 1) / kSlab + 2 * ((p.kv_heads + kSlab - 1) / kSlab);
-    // Rows read once, past the caches, where they would fill those: of the prompts above 112 us, through the caches 122; a quarter of
-    // that length 39 either way.
+    // Rows read once, past the caches, where they would fill those and pieces fill whole lines of 128 bytes.  64, 96, 128, 160, 256 and 512 MB
+    // of rows, 64 + 16 heads of 128, so: 33.6, 45.1, 56.0, 66.2, 101 and 206 us, through the caches 27.6, 44.6, 56.1, 73, 111 and 209; 16 + 4 heads
+    // of 256: 37.8, 51.1, 63.2, 72.2, 114 and 230, and 32.0, 51.2, 64.7, 77, 125 and 234.  Heads of 64 and 96 gain nothing at any size
+    // (160 MB of 40 + 80 heads of 64: 96 and 93.5, 512 MB 298 and 289; 32 + 16 heads of 96: 89.1 and 87.9, 273 and 265).
     bool once = D % 128 == 0 && (int64_t)p.tokens * (p.heads + 2 * p.kv_heads) * D * 2 > ((int64_t)128 << 20);
     const int most = (1 << 24) / slabs - 1;  // pages of a launch, which takes less than 2^32 threads
     for (int base = 0; base < pages; base += most) {

@@ -110,8 +110,10 @@ struct Step {
 // An 8-bit cache's codes become elements of T in the registers, exactly, and never meet their scales there.  A tile's keys share
 // one, which joins the scores' factor, and its values' scale s is a part of the weights: p' = exp2(score + log2 s - m'), where m' is
 // the maximum of score + log2 s, is what the second product takes, and the sum of the softmax takes p' / s.  With scales from
-// 2^-40 to 2^40 nothing of either sum is lost that fp32 would keep: a weight below 2^-126 in p' is below 2^-86 in the sum, whose
-// largest term is 2^-40 at the least.
+// 2^-40 to 2^40 nothing of that sum is lost that fp32 would keep: a weight below 2^-126 in p' is below 2^-86 in the sum, whose
+// largest term is 2^-40 at the least.  Of the second product's float16 parts those of a p' below 2^-40 of the largest are lost, which
+// need not be a small weight: beside a block of values whose scale is 2^40 times larger it is the largest one.  What is lost is
+// that part of the row's largest values, but in a channel where those are zero it may be all there is.
 template <typename T, int D, int NW, int KT, bool Eight, bool Window>
 __global__ void __launch_bounds__(64 * NW) paged_attention_kernel(const AttendProblem p)
 {

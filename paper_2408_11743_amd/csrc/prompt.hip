@@ -909,8 +909,10 @@ __global__ void __launch_bounds__(64 * kWaves, D > 128 ? 1 : 2) prompt_few_kerne
     constexpr int kKeyDw = Eight ? D / 16 : kQ * 4;
     constexpr int kAcc = D / 16;
     constexpr int kSlot = kFewFloats<D, RT>;
-    // Values are read past the caches where a sequence is one tile and a row whole lines of 128 bytes (200 sequences of up to 5000 tokens, four new
-    // ones each, 8 bits: 184 us, through the caches 192, 100 of them 74 and 81; two tiles a sequence, 48 rows: 57 and 54; keys too: 190 and 82).
+    // Values are read past the caches where rows are whole lines of 128 bytes and a sequence has 16 rows at the most on the average, which where all are
+    // alike is one tile: 100 sequences of 5000 tokens, four new ones each, 8 bits 212 us, through the caches 230, in 16 bits 359 and 390 (keys too: of
+    // 200 sequences 190 for 184).  A sequence of more rows than that reads its values once for each tile: one and seven new ones in turn 219 and
+    // 214, in 16 bits 385 and 370; one three times, then thirteen 247 and 238, 423 and 392.  Two tiles a sequence, 48 rows: 57 so, 54 through the caches.
     constexpr bool kOnce = RT == 1 && D * (Eight ? 1 : 2) % 128 == 0;
 
     __shared__ float4_t lds_acc[kWaves][kAcc][64];

@@ -137,10 +137,10 @@ def test_weights_of_many_keys_far_below_one(mk, new, hq, n, dtype, gap, bits, D)
     held_to(mk, args)
 
 
-@pytest.mark.parametrize("new,hq", FEW + MANY)
+@pytest.mark.parametrize("new,hq,starts", [(*x, True) for x in FEW + MANY] + [([1], 1, False), ([1], 16, False)])
 @pytest.mark.parametrize("dtype", [F16, BF16])
 @pytest.mark.parametrize("apart", [20, 30, 45])
-def test_weights_of_scales_far_apart(mk, new, hq, dtype, apart):
+def test_weights_of_scales_far_apart(mk, new, hq, starts, dtype, apart):
     """Blocks of values 2^20 to 2^45 larger than the others, but zero in half of the channels: there the others are the output, as far as weights
     times scales go."""
     n, D = 500, 64
@@ -154,6 +154,8 @@ def test_weights_of_scales_far_apart(mk, new, hq, dtype, apart):
         args["v_cache"][page, 0, :16] = v.to(torch.float8_e4m3fn)
     if dtype == F16:
         args["scales"][:, :, 1] = torch.where(args["scales"][:, :, 1] < 1, 2.0 ** (4 - apart if apart < 30 else 6 - apart), args["scales"][:, :, 1])
+    if not starts:
+        args["starts"] = None
     held_to(mk, args)
 
 
