@@ -26,12 +26,12 @@
 // in bfloat16 1.65e-3 for 1.69e-3, nearly all of it the output's rounding.  Over 8 bits a weight is times its block's scale of values in all of
 // this.  Scores, maxima, sums and results are fp32.
 //
-// Many rows are bound by power: a prompt of 8192 tokens, 32 heads over 8 of 128 channels (550 GFLOP), takes 605 to 640 us, 0.86 to 0.91 PFLOP/s, where
+// Many rows are bound by power: a prompt of 8192 tokens, 32 heads over 8 of 128 channels (550 GFLOP), takes 602 to 655 us, 0.84 to 0.91 PFLOP/s, where
 // a matrix product of 8192 cubed takes 1.11; with inputs of zero, a fifth less.  Per score the 32 MFMAs of 64 keys are 45 % of the SIMDs'
 // cycles, the softmax's vector instructions most of the rest, beside them from the other work-group.  Two columns of rows a wave, one wave a SIMD:
-// 780 us; eight waves a work-group: 2 % less, but 20 % more where tiles are few.  Four prompts, 2270 tokens, 64 heads over 8, through a window of 1024: 98 us;
-// four chunks of 512 tokens behind up to 16384 in 8 bits (535 GFLOP): 622.  Few rows are bound by memory and the latency of two launches: 32 sequences of up to
-// 8000 tokens in 8 bits, four new ones each (160 MB): 39 us.
+// 780 us; eight waves a work-group: 2 % less, but 20 % more where tiles are few.  Four prompts, 2270 tokens, 64 heads over 8, through a window of 1024: 97 to 102 us;
+// four chunks of 512 tokens behind up to 16384 in 8 bits (535 GFLOP): 605 to 650.  Few rows are bound by memory and the latency of two launches: 32 sequences of up to
+// 8000 tokens in 8 bits, four new ones each (160 MB): 40 us.
 #include <hip/hip_runtime.h>
 
 #include "device.h"
@@ -54,7 +54,8 @@ constexpr int kSearch = 6;  // tries to find how large parts are
 
 // Parts of a tile's keys, counted in steps of many rows, in rounds of the four waves' steps of few: at most the root of kRoot times
 // as many, as joining takes longer the more there are, and none of less than kLeast.  One sequence, 32 heads over 8 of 128 channels, 16 bits, four
-// new tokens: 2000 long 12.0 us (half the parts: 14.3, parts of four rounds: 14.0), 20000 long 22.7 (half the root's square 24.3, double 27.9); 64 new ones behind 8000: 30.2 (33.5 and 31.3).
+// new tokens: 2000 long 12.7 us (half the root's square 15.0, double 13.0, parts of four rounds 15.0), 20000 long 24.2 (27.0, 30.1 and 24.3); 64 new ones behind
+// 8000: 32.5 (half the square 35.2, double 33.5).
 struct Many {
     static constexpr int kShift = 2, kLeast = 3, kRoot = 2;  // 16-key tiles of a step (log2)
 };
@@ -1460,8 +1461,10 @@ PromptPlan plan_prompt(int64_t tokens, int64_t B, int64_t heads, int64_t kv_head
     const int64_t rows = tokens * (heads / kv_heads);  // of one kv head
     const int64_t sequences = B < tokens ? B : tokens;
     // Few rows: as long as registers hold what a wave needs.  16 sequences of 1000 to 8000 tokens, 64 rows of new ones for each of 8
-    // kv heads (4 of 256 channels): 38.5 us by the kernel for few rows, 44 by the other one (64 channels), 55 and 58 (96), 57 and 66 (128, 8 bits), 82 and
-    // 110 (256); 96 rows: 50 and 46, 73 and 61, 82 and 68, 113 and 110.  In 16 bits two columns of 128 channels do not fit: 32 sequences, 32 rows: 163 and 119.
+    // kv heads (4 of 256 channels): 41 us by the kernel for few rows, 50 by the other one (64 channels), 48 and 60 (96), 58 and 73 (128, 8 bits), 78 and
+    // 98 (256); 96 rows: 52 and 45, 69 and 53, 88 and 66, 101 and 96.  Of 32 sequences of 300 to 8000, whose tiles of 64 rows are as many as run
+    // at once here and not there, 57 and 66, 101 and 77, 126 and 96, 194 and 142.  In 16 bits two columns of 128 channels do not fit: 32 sequences, 32
+    // rows: 163 and 119 (weights rounded once).
     x.few = rows <= few_rows(head_dim, eight) * sequences;
     x.two = rows <= kTwoRows * sequences;
     x.rows = x.few ? (rows <= 16 * sequences ? 16 : 32) : 32 * kWaves;
