@@ -26,7 +26,7 @@ def put_values(args, h, odd):
 # ---- infinite values ----
 
 @pytest.mark.parametrize("new,hq,D,dtype", [([4], 4, 128, F16), ([5], 16, 64, BF16), ([3], 2, 256, F16), ([130], 1, 64, F16), ([200], 1, 128, BF16),
-                                            ([130], 1, 96, BF16)])
+                                            ([130], 1, 96, BF16), ([10], 3, 128, F16), ([12], 4, 128, BF16), ([10], 3, 96, F16)])
 @pytest.mark.parametrize("cached", [700, 1100, 1500, 2100, 3000, 4100, 9000])
 def test_infinite_values_of_shared_keys(mk, new, hq, D, dtype, cached):
     """Keys in any number of parts, an infinity in the first, one in the middle and one in the last."""
@@ -39,7 +39,7 @@ def test_infinite_values_of_shared_keys(mk, new, hq, D, dtype, cached):
 
 @pytest.mark.parametrize("new,hq,hkv,D,dtype", [([4], 4, 1, 128, F16), ([3, 2], 8, 2, 64, F16), ([4], 4, 1, 128, BF16), ([6], 3, 1, 256, F16), ([4], 4, 2, 96, F16),
                                                 ([130], 1, 1, 64, F16), ([140, 90], 4, 2, 128, F16), ([130], 1, 1, 128, BF16), ([130], 1, 1, 96, F16),
-                                                ([130], 2, 1, 256, F16)])
+                                                ([130], 2, 1, 256, F16), ([10], 3, 1, 128, F16), ([12, 9], 8, 2, 128, BF16), ([10], 3, 1, 96, F16)])
 @pytest.mark.parametrize("cached", [200, 3000])
 @pytest.mark.parametrize("far", [26.0, 32.0, 60.0])
 def test_infinite_values_of_small_weights(mk, new, hq, hkv, D, dtype, cached, far):
